@@ -16,6 +16,15 @@
  *   chunk_tree_refine              Sec. 4.2: tree-structured split / merge of chunks
  *                                  around the k most important tokens.
  *
+ * The cache as a serving program keeps it, in pages of a pool (further below):
+ *
+ *   kv_page_append                 new queries, keys and values: rotated by position, stored
+ *                                  into the pages (16 / 32 bits, or 8 bits with a scale for
+ *                                  each page and head), abstracts and boundaries kept up.
+ *   page_attention_decode          Eq. (1) for one token per sequence over all of its
+ *                                  pages, or over the pages chunk_topk_select kept.
+ *   page_attention_prefill         causal attention of a prompt's tokens.
+ *
  * Conventions (all entry points)
  *   - Every pointer except `const leoam_shape*` is a DEVICE pointer owned by the
  *     caller.  The library allocates nothing and keeps no state between calls.
@@ -67,7 +76,13 @@ typedef enum {
     LEOAM_E_HIP = -6             /* a HIP call or launch failed */
 } leoam_status;
 
-typedef enum { LEOAM_F32 = 0, LEOAM_F16 = 1, LEOAM_BF16 = 2, LEOAM_Q8Q4 = 3 } leoam_dtype;
+typedef enum {
+    LEOAM_F32 = 0,
+    LEOAM_F16 = 1,
+    LEOAM_BF16 = 2,
+    LEOAM_Q8Q4 = 3,
+    LEOAM_E4M3 = 4      /* pages of the paged cache only (leoam_pages) */
+} leoam_dtype;
 
 /*
  * Compressed KV store (kv_dtype == LEOAM_Q8Q4; paper Sec. 4.4 "Dynamic KV
@@ -424,6 +439,102 @@ int chunk_compression_tags(const leoam_shape* shape, const int32_t* n_chunks, co
  */
 double leoam_compression_share(double n_bytes, double ratio, double bandwidth, double t_other, double t_compute,
                                double decompress_rate);
+
+/* ------------------------------------------------------------------------
+ * The paged cache.  A layer's keys and values live in pages of page_size tokens that come from a pool; the pages
+ * of a sequence are listed in its row of page_table, in order.  All calls of a step share seq_len, the sequences'
+ * lengths with the step's new tokens counted in, and (prompts) new_off, the rows that each sequence brings.
+ *   k_pages, v_pages  [n_pages, n_kv_heads, page_size, head_dim]  kv_dtype
+ *   page_table        [batch, max_pages] int32, entry i = the pool's page that holds tokens [i * page_size, ...)
+ *   seq_len           [batch] int32, 0 <= seq_len[b] <= max_pages * page_size
+ *   new_off           [batch + 1] int32, 0 = off[0] <= off[1] <= ... <= off[batch] = n_new: sequence b's new tokens are
+ *                     rows off[b] .. off[b + 1] of the call's tensors and positions seq_len[b] - (their number) ..
+ *                     seq_len[b] - 1 of the sequence.  NULL: one row each (n_new == batch); a sequence of length 0 is idle.
+ *   k_scale, v_scale  [n_pages, n_kv_heads] float (LEOAM_E4M3; NULL otherwise)
+ * LEOAM_E4M3 pages hold 8-bit codes (4 exponent bits, 3 fraction bits, largest 448, no infinity), a stored value is
+ * scale * code with one scale per (page, kv head, tensor), a power of two: with a floating-point code that costs
+ * no precision, and scale * code is a number of q_dtype (the exponent stays in [-15, 7] for fp16 and [-100, 118] for
+ * bf16), so every kernel works on exactly what is stored.
+ * Entries of page_table that a call does not need are not read; one that it needs and that lies outside
+ * [0, n_pages) holds no tokens (nothing is stored to it, attention skips it).  Values of tokens at or beyond seq_len, and of
+ * pages that are not listed, may be anything, NaN included.  k_pages, v_pages, q, k, v, rope, abstract and out must be 16-byte
+ * aligned.
+ * ------------------------------------------------------------------------ */
+typedef struct {
+    int32_t batch;            /* B  >= 1, <= 65535 */
+    int32_t n_q_heads;        /* Hq, multiple of n_kv_heads, Hq/Hkv in {1,2,4,8} */
+    int32_t n_kv_heads;       /* Hkv >= 1 */
+    int32_t head_dim;         /* must be 128 */
+    int32_t n_pages;          /* pages in the pool */
+    int32_t page_size;        /* tokens in a page: 16, 32, 64, 128 or 256 */
+    int32_t max_pages;        /* row stride of page_table: the most pages of a sequence, max_pages * page_size < 2^30 */
+    int32_t q_dtype;          /* LEOAM_F32, LEOAM_F16 or LEOAM_BF16: q, the new keys and values, the abstract */
+    int32_t kv_dtype;         /* of the pages: == q_dtype, or LEOAM_E4M3 when q_dtype is LEOAM_F16 / LEOAM_BF16 */
+    int32_t rot_dim;          /* channels [0, rot_dim) of q and k are rotated: 0 (none) or a multiple of 16 up to 128 */
+    int32_t rope_interleaved; /* 0: channel i turns with i + rot_dim/2; 1: channel 2i with 2i + 1 */
+    int32_t rope_len;         /* rows of the rope table (rot_dim > 0) */
+} leoam_pages;
+
+/*
+ * New tokens into the cache.  Row r of q / k / v is [heads, 128] contiguous; the next row begins q_stride / k_stride /
+ * v_stride elements later (so the three may be slices of one projection's output; strides are multiples of 16 bytes).
+ * The row's token has position t (see new_off), and with c_i = rope[t][i], s_i = rope[t][rot_dim/2 + i], i < rot_dim/2,
+ * every pair (x_a, x_b) of rotated channels of q and k becomes
+ *     (x_a c_i - x_b s_i,  x_b c_i + x_a s_i),
+ * products and sums single binary32 operations.  q_out[r] (contiguous [n_new, Hq, 128], may be q itself if q is contiguous)
+ * receives the rotated query, rounded once; q and q_out may both be NULL.  Keys (rotated) and values go to their places in the
+ * pages, rounded once.
+ * LEOAM_E4M3: scale = the smallest power of two s with |x| <= 448 s for all finite x that the page holds so far (0 for
+ * none but zeros; it never falls while a page fills up; a page's first token starts it anew), code = round-half-even(x /
+ * scale); infinities are stored as +-448 scale, NaN as NaN.  When a new token raises a page's scale, its older codes are
+ * encoded again from their stored values (exact but for codes that become subnormal).
+ * Every page that takes a token must belong to one sequence only.  For each of them
+ *   abstract   [batch, n_kv_heads, max_pages, 2, 128] q_dtype (nullable): the page's rows become the maximum / minimum of
+ *              its stored keys (as kv_chunk_abstract_build with the pages as chunks, c_max = max_pages);
+ *   chunk_off  [batch, max_pages + 1], n_chunks [batch] int32 (nullable): brought up to date with the pages as chunks,
+ * so chunk_score and chunk_topk_select run on a leoam_shape with c_max = max_pages and n_ctx = max_pages * page_size.
+ *   status[b] (nullable)  0 done; 1 seq_len[b] negative, beyond the capacity or below the number of new tokens, or new_off not
+ *             ascending; 2 a page to write is not in the pool (its tokens are left out, all others are stored); 3 a position
+ *             beyond the rope table.  With 1 and 3 nothing of the sequence is written.
+ */
+int kv_page_append(const leoam_pages* pages, const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
+                   int64_t v_stride, int32_t n_new, const int32_t* new_off, const int32_t* seq_len,
+                   const int32_t* page_table, const float* rope, void* q_out, void* k_pages, void* v_pages, float* k_scale,
+                   float* v_scale, void* abstract, int32_t* chunk_off, int32_t* n_chunks, int32_t* status, void* stream);
+
+/*
+ * Sec. 2.1 Eq. (1) for the last token of every sequence, q [batch, Hq, 128], over its seq_len[b] tokens:
+ *   z_t = softmax_scale * (q_j . K_t),  out[b,j,:] = sum_t softmax(z)_t V_t  (float),  lse[b,j] = log sum_t exp(z_t).
+ * With sel_idx [batch, n_kv_heads, k_max] and sel_count [batch, n_kv_heads] (both or neither) only over the tokens of
+ * the listed pages (places in the sequence, as chunk_topk_select writes them; ids outside the sequence add nothing; a
+ * page listed twice counts twice).  Nothing to attend to: out = 0, lse = -inf.  lse may be NULL.
+ * Workspace: leoam_page_workspace_bytes(pages, 0) gives the intended launch; less gives fewer splits
+ * (LEOAM_E_WORKSPACE below leoam_page_workspace_min()).  16-byte aligned, contents irrelevant.
+ * Calls that share a workspace must not overlap.
+ */
+int page_attention_decode(const leoam_pages* pages, const void* q, const void* k_pages, const void* v_pages,
+                          const float* k_scale, const float* v_scale, const int32_t* page_table, const int32_t* seq_len,
+                          const int32_t* sel_idx, const int32_t* sel_count, int32_t k_max, float softmax_scale, float* out,
+                          float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Causal attention of the new tokens (already appended): row r of q [n_new, Hq, 128] has position t and attends to
+ * positions 0 .. t of its sequence.  out [n_new, Hq, 128] in q_dtype, rounded once; lse [n_new, Hq] float, nullable.  What
+ * stands at positions beyond t, NaN and infinities included, does not reach the row.  Rows outside every sequence, and rows
+ * of a sequence with seq_len[b] below its number of new tokens whose position is negative, have nothing to attend to: the
+ * former are left as they are, the latter get out = 0, lse = -inf.  Workspace as above, of
+ * leoam_page_workspace_bytes(pages, n_new) bytes.
+ */
+int page_attention_prefill(const leoam_pages* pages, const void* q, int32_t n_new, const int32_t* new_off,
+                           const void* k_pages, const void* v_pages, const float* k_scale, const float* v_scale,
+                           const int32_t* page_table, const int32_t* seq_len, float softmax_scale, void* out, float* lse,
+                           void* workspace, size_t workspace_bytes, void* stream);
+
+/* Bytes of workspace for page_attention_decode (n_new <= 0) or page_attention_prefill over n_new rows.  0 on a bad shape. */
+size_t leoam_page_workspace_bytes(const leoam_pages* pages, int32_t n_new);
+
+/* The smallest workspace either call accepts. */
+size_t leoam_page_workspace_min(const leoam_pages* pages);
 
 const char* leoam_status_string(int status);
 int leoam_version(void);

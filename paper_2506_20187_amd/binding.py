@@ -17,7 +17,7 @@ import torch
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libleoam.so")
 
-F32, F16, BF16, Q8Q4 = 0, 1, 2, 3
+F32, F16, BF16, Q8Q4, E4M3 = 0, 1, 2, 3, 4
 _DTYPE_TAG = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16}
 
 OK = 0
@@ -33,6 +33,13 @@ class LeoamError(RuntimeError):
 class Shape(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("batch", "n_q_heads", "n_kv_heads", "head_dim", "n_ctx", "c_max",
                                                 "k_max", "kv_dtype", "abstract_dtype")]
+
+
+class Pages(ctypes.Structure):
+    """leoam_pages: the paged cache's shape (make_pages)."""
+    _fields_ = [(n, ctypes.c_int32) for n in ("batch", "n_q_heads", "n_kv_heads", "head_dim", "n_pages", "page_size",
+                                                "max_pages", "q_dtype", "kv_dtype", "rot_dim", "rope_interleaved",
+                                                "rope_len")]
 
 
 def _load() -> ctypes.CDLL:
@@ -70,6 +77,14 @@ def _load() -> ctypes.CDLL:
     lib.leoam_fused_workspace_bytes.restype = sz
     lib.leoam_fused_control_bytes.argtypes = [sp]
     lib.leoam_fused_control_bytes.restype = sz
+    pp, i64, f32 = ctypes.POINTER(Pages), ctypes.c_int64, ctypes.c_float
+    lib.kv_page_append.argtypes = [pp, vp, i64, vp, i64, vp, i64, i32] + [vp] * 14
+    lib.page_attention_decode.argtypes = [pp] + [vp] * 9 + [i32, f32, vp, vp, vp, sz, vp]
+    lib.page_attention_prefill.argtypes = [pp, vp, i32] + [vp] * 7 + [f32, vp, vp, vp, sz, vp]
+    lib.leoam_page_workspace_bytes.argtypes = [pp, i32]
+    lib.leoam_page_workspace_bytes.restype = sz
+    lib.leoam_page_workspace_min.argtypes = [pp]
+    lib.leoam_page_workspace_min.restype = sz
     lib.leoam_workspace_init.argtypes = [vp, sz, vp]
     lib.leoam_validate_boundaries.argtypes = [sp, vp, vp, vp]
     lib.leoam_copy_probe.argtypes = [vp, vp, sz, vp]
@@ -80,6 +95,7 @@ def _load() -> ctypes.CDLL:
     for name in ("kv_chunk_abstract_build", "chunk_score", "chunk_score_pin", "chunk_topk_select", "sparse_chunk_attention_decode",
                  "chunk_select_attention_decode", "chunk_select_attention_decode_static", "kv_chunk_abstract_append", "chunk_tree_refine",
                  "kv_chunk_compress", "kv_chunk_recompress", "chunk_compression_tags", "leoam_workspace_init",
+                 "kv_page_append", "page_attention_decode", "page_attention_prefill",
                  "leoam_validate_boundaries", "leoam_copy_probe", "leoam_read_probe"):
         getattr(lib, name).restype = ctypes.c_int
     return lib
@@ -93,6 +109,8 @@ EXPORTS = ("kv_chunk_abstract_build", "chunk_score", "chunk_score_pin", "chunk_t
            "leoam_workspace_init",
            "kv_chunk_abstract_append", "leoam_tree_evaluations", "chunk_tree_refine", "leoam_tree_workspace_bytes",
            "kv_chunk_compress", "kv_chunk_recompress", "chunk_compression_tags", "leoam_compressed_bytes_bound", "leoam_compression_share",
+           "kv_page_append", "page_attention_decode", "page_attention_prefill", "leoam_page_workspace_bytes",
+           "leoam_page_workspace_min",
            "leoam_workspace_bytes", "leoam_validate_boundaries", "leoam_copy_probe", "leoam_read_probe", "leoam_status_string",
            "leoam_version")
 
@@ -133,9 +151,10 @@ def _load_bind():
         raise ImportError(f"{path} is missing: run `python -c 'import __graft_entry__ as g; g.build()'` "
                           "(or python paper_2506_20187_amd/build.py) first")
     from . import _bind
-    _bind.setup(Shape, _p, _stream, *(ctypes.cast(getattr(_lib, n), ctypes.c_void_p).value for n in (
+    _bind.setup(Shape, Pages, _p, _stream, *(ctypes.cast(getattr(_lib, n), ctypes.c_void_p).value for n in (
         "chunk_score", "chunk_score_pin", "kv_chunk_abstract_append", "chunk_topk_select",
-        "sparse_chunk_attention_decode", "chunk_select_attention_decode")))
+        "sparse_chunk_attention_decode", "chunk_select_attention_decode",
+        "kv_page_append", "page_attention_decode", "page_attention_prefill")))
     return _bind
 
 
@@ -280,6 +299,50 @@ def leoam_workspace_bytes(shape: Shape, max_tokens: int) -> int:
 
 def leoam_validate_boundaries(shape: Shape, chunk_off, n_chunks, stream=None) -> int:
     return int(_lib.leoam_validate_boundaries(ctypes.byref(shape), _p(chunk_off), _p(n_chunks), _stream(stream)))
+
+
+def make_pages(batch, n_q_heads, n_kv_heads, head_dim, n_pages, page_size, max_pages, dtype, kv_dtype=None, rot_dim=0,
+               interleaved=False, rope_len=0) -> Pages:
+    """dtype: torch dtype of q and of new keys and values; kv_dtype: of the pages (None: the same; E4M3 or
+    torch.float8_e4m3fn: 8-bit codes with a scale for each page and kv head)."""
+    tag = _DTYPE_TAG[dtype] if isinstance(dtype, torch.dtype) else int(dtype)
+    if kv_dtype is None:
+        kv_tag = tag
+    elif isinstance(kv_dtype, torch.dtype):
+        kv_tag = E4M3 if kv_dtype == torch.float8_e4m3fn else _DTYPE_TAG[kv_dtype]
+    else:
+        kv_tag = int(kv_dtype)
+    return Pages(batch, n_q_heads, n_kv_heads, head_dim, n_pages, page_size, max_pages, tag, kv_tag, int(rot_dim),
+                 int(bool(interleaved)), int(rope_len))
+
+
+def kv_page_append(pages: Pages, q, k, v, new_off, seq_len, page_table, rope, q_out, k_pages, v_pages, k_scale=None,
+                   v_scale=None, abstract=None, chunk_off=None, n_chunks=None, status=None, stream=None) -> None:
+    """q [n, Hq, 128], k, v [n, Hkv, 128]: rows may be strided (slices of one projection's output)."""
+    _check(_bind.kv_page_append(pages, q, k, v, new_off, seq_len, page_table, rope, q_out, k_pages, v_pages, k_scale, v_scale,
+                                abstract, chunk_off, n_chunks, status, stream), "kv_page_append")
+
+
+def page_attention_decode(pages: Pages, q, k_pages, v_pages, k_scale, v_scale, page_table, seq_len, sel_idx, sel_count,
+                          softmax_scale, out, lse, workspace, stream=None) -> None:
+    """One token per sequence over its pages; sel_idx [B, Hkv, k_max], sel_count (or None, None): over the kept ones."""
+    _check(_bind.page_attention_decode(pages, q, k_pages, v_pages, k_scale, v_scale, page_table, seq_len, sel_idx, sel_count,
+                                       softmax_scale, out, lse, workspace, stream), "page_attention_decode")
+
+
+def page_attention_prefill(pages: Pages, q, new_off, k_pages, v_pages, k_scale, v_scale, page_table, seq_len, softmax_scale,
+                           out, lse, workspace, stream=None) -> None:
+    """Causal attention of the new tokens, already appended; out in q's type."""
+    _check(_bind.page_attention_prefill(pages, q, new_off, k_pages, v_pages, k_scale, v_scale, page_table, seq_len,
+                                        softmax_scale, out, lse, workspace, stream), "page_attention_prefill")
+
+
+def leoam_page_workspace_bytes(pages: Pages, n_new: int = 0) -> int:
+    return int(_lib.leoam_page_workspace_bytes(ctypes.byref(pages), int(n_new)))
+
+
+def leoam_page_workspace_min(pages: Pages) -> int:
+    return int(_lib.leoam_page_workspace_min(ctypes.byref(pages)))
 
 
 def leoam_copy_probe(dst, src, nbytes: int, stream=None) -> None:

@@ -37,6 +37,17 @@ hipError_t compress_dispatch(const leoam_shape*, const void*, const void*, const
 hipError_t recompress_dispatch(const leoam_shape*, const void*, const void*, const int32_t*, const int32_t*, const uint8_t*,
                                const uint8_t*, void*, void*, void*, size_t, long long*, long long*, hipStream_t);
 hipError_t abstract_append_dispatch(const leoam_shape*, const void*, int32_t*, int32_t*, int, void*, int32_t*, hipStream_t);
+hipError_t page_append_dispatch(const leoam_pages*, const void*, int64_t, const void*, int64_t, const void*, int64_t, int,
+                                const int32_t*, const int32_t*, const int32_t*, const float*, void*, void*, void*, float*,
+                                float*, void*, int32_t*, int32_t*, int32_t*, hipStream_t);
+hipError_t page_decode_dispatch(const leoam_pages*, const void*, const void*, const void*, const float*, const float*,
+                                const int32_t*, const int32_t*, const int32_t*, const int32_t*, int, float, float*, float*,
+                                void*, size_t, hipStream_t);
+hipError_t page_prefill_dispatch(const leoam_pages*, const void*, int, const int32_t*, const void*, const void*, const float*,
+                                 const float*, const int32_t*, const int32_t*, float, void*, float*, void*, size_t,
+                                 hipStream_t);
+size_t page_workspace_bytes(const leoam_pages*, int);
+size_t page_min_workspace_bytes(const leoam_pages*);
 
 // scores of the first `sink` and the last `tail` chunks of every (b, h) row become FLT_MAX
 __global__ void score_pin_kernel(const int32_t* __restrict__ n_chunks, int sink, int tail, float* __restrict__ score,
@@ -98,6 +109,26 @@ static int check_shape(const leoam_shape* s) {
     if (s->c_max > 16384) return LEOAM_E_UNSUPPORTED;
     if ((long long)s->batch * s->n_kv_heads > 65535 * 8) return LEOAM_E_UNSUPPORTED;
     if (s->n_kv_heads > 65535 || s->batch > 65535) return LEOAM_E_UNSUPPORTED;
+    return LEOAM_OK;
+}
+
+static int check_pages(const leoam_pages* s) {
+    if (!s) return LEOAM_E_INVALID_ARG;
+    if (s->batch < 1 || s->n_q_heads < 1 || s->n_kv_heads < 1 || s->n_pages < 1 || s->max_pages < 1 || s->page_size < 1)
+        return LEOAM_E_INVALID_ARG;
+    if (s->n_q_heads % s->n_kv_heads) return LEOAM_E_INVALID_ARG;
+    if (s->rot_dim < 0 || s->rot_dim > LEOAM_D || s->rot_dim % 16 || (s->rot_dim && s->rope_len < 1))
+        return LEOAM_E_INVALID_ARG;
+    if (s->rope_interleaved != 0 && s->rope_interleaved != 1) return LEOAM_E_INVALID_ARG;
+    if (s->head_dim != LEOAM_D) return LEOAM_E_UNSUPPORTED;
+    const int g = s->n_q_heads / s->n_kv_heads;
+    if (g != 1 && g != 2 && g != 4 && g != 8) return LEOAM_E_UNSUPPORTED;
+    if (s->page_size < 16 || s->page_size > 256 || (s->page_size & (s->page_size - 1))) return LEOAM_E_UNSUPPORTED;
+    if ((long long)s->max_pages * s->page_size >= (1ll << 30)) return LEOAM_E_UNSUPPORTED;
+    if (s->q_dtype != LEOAM_F32 && s->q_dtype != LEOAM_F16 && s->q_dtype != LEOAM_BF16) return LEOAM_E_UNSUPPORTED;
+    if (s->kv_dtype != s->q_dtype && !(s->kv_dtype == LEOAM_E4M3 && s->q_dtype != LEOAM_F32)) return LEOAM_E_UNSUPPORTED;
+    if ((long long)s->batch * s->n_kv_heads > 65535 * 8) return LEOAM_E_UNSUPPORTED;
+    if (s->n_kv_heads > 4096 || s->batch > 65535) return LEOAM_E_UNSUPPORTED;
     return LEOAM_OK;
 }
 
@@ -426,6 +457,89 @@ int leoam_read_probe(const void* src, size_t bytes, void* sink, void* stream) {
     hipLaunchKernelGGL(read_probe_kernel, dim3((unsigned)blocks), dim3(256), 0, (hipStream_t)stream, (const uint4*)src,
                        n16, (uint32_t*)sink);
     return from_hip(hipGetLastError());
+}
+
+// ---- the paged cache --------------------------------------------------------------------------------
+// strides of the new rows: 16-byte loads, so multiples of 16 bytes, and far from overflowing byte offsets
+static bool bad_stride(int64_t stride, int q_dtype, int heads, int rows) {
+    const int64_t e = q_dtype == LEOAM_F32 ? 4 : 2;
+    if (rows < 2) return false;
+    return stride < (int64_t)heads * LEOAM_D || stride > (1ll << 31) || (stride * e) % 16;
+}
+
+int kv_page_append(const leoam_pages* pages, const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
+                   int64_t v_stride, int32_t n_new, const int32_t* new_off, const int32_t* seq_len,
+                   const int32_t* page_table, const float* rope, void* q_out, void* k_pages, void* v_pages, float* k_scale,
+                   float* v_scale, void* abstract, int32_t* chunk_off, int32_t* n_chunks, int32_t* status, void* stream) {
+    int rc = check_pages(pages);
+    if (rc) return rc;
+    if (n_new < 0 || (!new_off && n_new != pages->batch)) return LEOAM_E_INVALID_ARG;
+    if (!seq_len || !page_table || !k_pages || !v_pages || !q != !q_out) return LEOAM_E_INVALID_ARG;
+    if (n_new > 0 && (!k || !v)) return LEOAM_E_INVALID_ARG;
+    if (pages->rot_dim && !rope) return LEOAM_E_INVALID_ARG;
+    if (pages->kv_dtype == LEOAM_E4M3 && (!k_scale || !v_scale)) return LEOAM_E_INVALID_ARG;
+    if (misaligned16(q, k, v, rope, q_out, k_pages, v_pages, abstract)) return LEOAM_E_INVALID_ARG;
+    if ((q && bad_stride(q_stride, pages->q_dtype, pages->n_q_heads, n_new)) ||
+        bad_stride(k_stride, pages->q_dtype, pages->n_kv_heads, n_new) ||
+        bad_stride(v_stride, pages->q_dtype, pages->n_kv_heads, n_new))
+        return LEOAM_E_INVALID_ARG;
+    if (q && q == q_out && n_new > 1 && q_stride != (int64_t)pages->n_q_heads * LEOAM_D) return LEOAM_E_INVALID_ARG;
+    if (n_new == 0) return LEOAM_OK;
+    return from_hip(page_append_dispatch(pages, q, q_stride, k, k_stride, v, v_stride, n_new, new_off, seq_len, page_table, rope,
+                                         q_out, k_pages, v_pages, k_scale, v_scale, abstract, chunk_off, n_chunks, status,
+                                         (hipStream_t)stream));
+}
+
+static int check_page_attention(const leoam_pages* pages, const void* q, const void* k_pages, const void* v_pages,
+                                const float* k_scale, const float* v_scale, const int32_t* page_table,
+                                const int32_t* seq_len, const void* out, const void* workspace, size_t workspace_bytes) {
+    int rc = check_pages(pages);
+    if (rc) return rc;
+    if (!q || !k_pages || !v_pages || !page_table || !seq_len || !out) return LEOAM_E_INVALID_ARG;
+    if (pages->kv_dtype == LEOAM_E4M3 && (!k_scale || !v_scale)) return LEOAM_E_INVALID_ARG;
+    if (misaligned16(q, k_pages, v_pages, out)) return LEOAM_E_INVALID_ARG;
+    if (!workspace || workspace_bytes < page_min_workspace_bytes(pages) || ((uintptr_t)workspace & 15u))
+        return LEOAM_E_WORKSPACE;
+    return LEOAM_OK;
+}
+
+int page_attention_decode(const leoam_pages* pages, const void* q, const void* k_pages, const void* v_pages,
+                          const float* k_scale, const float* v_scale, const int32_t* page_table, const int32_t* seq_len,
+                          const int32_t* sel_idx, const int32_t* sel_count, int32_t k_max, float softmax_scale, float* out,
+                          float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+    int rc = check_page_attention(pages, q, k_pages, v_pages, k_scale, v_scale, page_table, seq_len, out, workspace,
+                                  workspace_bytes);
+    if (rc) return rc;
+    if (!sel_idx != !sel_count) return LEOAM_E_INVALID_ARG;
+    if (sel_idx && k_max < 1) return LEOAM_E_INVALID_ARG;
+    if (sel_idx && (long long)k_max * pages->page_size >= (1ll << 30)) return LEOAM_E_UNSUPPORTED;
+    return from_hip(page_decode_dispatch(pages, q, k_pages, v_pages, k_scale, v_scale, page_table, seq_len, sel_idx, sel_count,
+                                         k_max, softmax_scale, out, lse, workspace, workspace_bytes, (hipStream_t)stream));
+}
+
+int page_attention_prefill(const leoam_pages* pages, const void* q, int32_t n_new, const int32_t* new_off,
+                           const void* k_pages, const void* v_pages, const float* k_scale, const float* v_scale,
+                           const int32_t* page_table, const int32_t* seq_len, float softmax_scale, void* out, float* lse,
+                           void* workspace, size_t workspace_bytes, void* stream) {
+    int rc = check_pages(pages);
+    if (rc) return rc;
+    if (n_new < 0 || (!new_off && n_new != pages->batch)) return LEOAM_E_INVALID_ARG;
+    if (n_new == 0) return LEOAM_OK;
+    rc = check_page_attention(pages, q, k_pages, v_pages, k_scale, v_scale, page_table, seq_len, out, workspace,
+                              workspace_bytes);
+    if (rc) return rc;
+    return from_hip(page_prefill_dispatch(pages, q, n_new, new_off, k_pages, v_pages, k_scale, v_scale, page_table, seq_len,
+                                          softmax_scale, out, lse, workspace, workspace_bytes, (hipStream_t)stream));
+}
+
+size_t leoam_page_workspace_bytes(const leoam_pages* pages, int32_t n_new) {
+    if (check_pages(pages)) return 0;
+    return page_workspace_bytes(pages, n_new);
+}
+
+size_t leoam_page_workspace_min(const leoam_pages* pages) {
+    if (check_pages(pages)) return 0;
+    return page_min_workspace_bytes(pages);
 }
 
 const char* leoam_status_string(int status) {

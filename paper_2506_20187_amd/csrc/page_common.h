@@ -1,0 +1,58 @@
+// Pieces shared by the kernels over the paged cache: 8-bit codes, rounding to the model's type, looking up
+// pages and the sequence that a row of a ragged call belongs to.
+#pragma once
+#include "attention_common.h"
+
+namespace leoam {
+
+// 8-bit pages: e4m3 codes (4 exponent bits, 3 fraction bits, largest 448, no infinity), a lane moves 8 of them
+struct E4M3 { static constexpr int kBytes = 1; };
+
+typedef __attribute__((ext_vector_type(2))) float f32x2_t;
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2_t;
+typedef __attribute__((ext_vector_type(2))) _Float16 f16x2_t;
+
+// four codes of a register to floats (exact)
+__device__ __forceinline__ void unpack_e4m3(uint32_t w, float* x) {
+    const f32x2_t a = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
+    x[0] = a.x; x[1] = a.y; x[2] = b.x; x[3] = b.y;
+}
+
+// Two floats to two codes (round half to even), beyond +-448 to +-448 (the conversion alone would give NaN there),
+// NaN stays NaN.
+__device__ __forceinline__ float clamp_e4m3(float x) { return x > 448.f ? 448.f : x < -448.f ? -448.f : x; }
+__device__ __forceinline__ uint32_t pack_e4m3(const float* x) {
+    int w = __builtin_amdgcn_cvt_pk_fp8_f32(clamp_e4m3(x[0]), clamp_e4m3(x[1]), 0, false);
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(clamp_e4m3(x[2]), clamp_e4m3(x[3]), w, true);
+}
+
+// floats rounded once to the model's type (half to even): the 16 bytes a lane holds of a row
+template <typename T> __device__ __forceinline__ uint4 round_pack(const float* x);
+template <> __device__ __forceinline__ uint4 round_pack<F32>(const float* x) { return pack<F32>(x); }
+template <> __device__ __forceinline__ uint4 round_pack<F16>(const float* x) { return pack<F16>(x); }
+template <> __device__ __forceinline__ uint4 round_pack<BF16>(const float* x) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        bf16x2_t p;
+        p.x = (__bf16)x[2 * i];
+        p.y = (__bf16)x[2 * i + 1];
+        w[i] = __builtin_bit_cast(uint32_t, p);
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// Number of entries i in 1..n of an ascending list with value(i) <= x, found by the whole wave 64 entries at a
+// time: the sequence that owns element x when value(i) is where sequence i begins.
+template <typename F> __device__ __forceinline__ int wave_count_below(int n, int x, F&& value) {
+    int found = 0;
+    for (int i0 = 1; i0 <= n; i0 += LEOAM_WAVE) {
+        const int i = i0 + lane_id();
+        const uint64_t hit = __ballot(i <= n && value(min(i, n)) <= x);
+        found += __popcll(hit);
+        if (hit != ~0ull) break;
+    }
+    return found;
+}
+
+}  // namespace leoam
