@@ -165,8 +165,12 @@ template <bool kPrompt> static hipError_t attention_of(const leoam_pages* s, con
     }
 }
 
-size_t page_workspace_bytes(const leoam_pages*, int) { return 16; }
-size_t page_min_workspace_bytes(const leoam_pages*) { return 0; }
+size_t page_decode_workspace_bytes(const leoam_pages*);
+size_t page_decode_min_workspace_bytes(const leoam_pages*);
+size_t page_workspace_bytes(const leoam_pages* s, int n_new) {
+    return n_new <= 0 ? page_decode_workspace_bytes(s) : page_decode_min_workspace_bytes(s);
+}
+size_t page_min_workspace_bytes(const leoam_pages* s) { return page_decode_min_workspace_bytes(s); }
 
 static PageAttArgs args_of(const leoam_pages* s, const void* q, const void* k_pages, const void* v_pages, const float* k_scale,
                            const float* v_scale, const int32_t* page_table, const int32_t* seq_len, float softmax_scale,
@@ -179,15 +183,6 @@ static PageAttArgs args_of(const leoam_pages* s, const void* q, const void* k_pa
     a.batch = s->batch; a.n_kv_heads = s->n_kv_heads; a.n_pages = s->n_pages; a.page_size = s->page_size;
     a.page_shift = __builtin_ctz((unsigned)s->page_size); a.max_pages = s->max_pages;
     return a;
-}
-
-hipError_t page_decode_dispatch(const leoam_pages* s, const void* q, const void* k_pages, const void* v_pages,
-                                const float* k_scale, const float* v_scale, const int32_t* page_table, const int32_t* seq_len,
-                                const int32_t* sel_idx, const int32_t* sel_count, int k_max, float softmax_scale, float* out,
-                                float* lse, void* workspace, size_t, hipStream_t stream) {
-    PageAttArgs a = args_of(s, q, k_pages, v_pages, k_scale, v_scale, page_table, seq_len, softmax_scale, out, lse, workspace);
-    a.sel_idx = sel_idx; a.sel_count = sel_count; a.k_max = k_max; a.n_rows = s->batch;
-    return attention_of<false>(s, a, stream);
 }
 
 hipError_t page_prefill_dispatch(const leoam_pages* s, const void* q, int n_new, const int32_t* new_off, const void* k_pages,
