@@ -55,4 +55,47 @@ template <typename F> __device__ __forceinline__ int wave_count_below(int n, int
     return found;
 }
 
+// a value that is the same in every lane, held once for the wave
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+
+__device__ __forceinline__ float exp2_raw(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// eight codes to the operand type, times a power of two (exact)
+template <typename T> __device__ __forceinline__ uint4 widen8(uint32_t a, uint32_t b, float scale);
+template <> __device__ __forceinline__ uint4 widen8<BF16>(uint32_t a, uint32_t b, float s) {
+    return make_uint4(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, s, false)),
+                      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, s, true)),
+                      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, s, false)),
+                      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, s, true)));
+}
+template <> __device__ __forceinline__ uint4 widen8<F16>(uint32_t a, uint32_t b, float s) {
+    return make_uint4(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, s, false)),
+                      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, s, true)),
+                      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, s, false)),
+                      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, s, true)));
+}
+
+// p (>= 0) as hi + lo of the 16-bit type
+__device__ __forceinline__ uint32_t pair_of(BF16, float a, float b) {
+    bf16x2_t p;
+    p.x = (__bf16)a;
+    p.y = (__bf16)b;
+    return __builtin_bit_cast(uint32_t, p);
+}
+__device__ __forceinline__ uint32_t pair_of(F16, float a, float b) {
+    f16x2_t p;
+    p.x = (_Float16)a;
+    p.y = (_Float16)b;
+    return __builtin_bit_cast(uint32_t, p);
+}
+__device__ __forceinline__ void pair_back(BF16, uint32_t w, float& a, float& b) {
+    a = bits_to_float(w << 16);
+    b = bits_to_float(w & 0xffff0000u);
+}
+__device__ __forceinline__ void pair_back(F16, uint32_t w, float& a, float& b) {
+    const f16x2_t p = __builtin_bit_cast(f16x2_t, w);
+    a = (float)p.x;
+    b = (float)p.y;
+}
+
 }  // namespace leoam
