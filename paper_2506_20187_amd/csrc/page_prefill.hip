@@ -6,6 +6,10 @@
 // Each of the four waves owns 32 rows.  S^T = K Q^T (32x32 products) leaves lane = row, registers = keys: the row's
 // maximum and sum need no exchange but one with the lane 32 away, and P is already the second operand of O^T = V^T P^T;
 // the first operand, four keys of one channel at a time, comes out of LDS by the transposing read.
+//
+// A unit of work is (128 rows, kv head).  With enough units to fill the chip each takes a workgroup.  With few (a
+// handful of rows behind a long context) the key tiles of all units are laid end to end and shared out equally; a
+// unit cut by the ends of shares leaves its pieces, (acc, m, l) per row, in the workspace, and a second kernel folds them.
 #include "page_common.h"
 
 namespace leoam {
@@ -24,8 +28,24 @@ struct PagePrefillArgs {
     uint32_t flip;         // sign bits of the queries, turned if softmax_scale is negative
     char* out;
     float* lse;
+    struct UnitPieces* pieces;      // shared out: directory of the units, then the pieces
+    float* partial;
     int batch, n_kv_heads, n_pages, page_shift, max_pages;
 };
+
+// pieces of a unit (0: its result is final), where the first lies, its first row of the call, its rows
+struct UnitPieces { int32_t count, first_slot, token0, rows; };
+
+constexpr int kSharers = 512;         // workgroups that share the tiles: two fill a compute unit
+constexpr int kMostUnits = 1024;      // more units than this are not shared out: two rounds of workgroups or more
+constexpr int kMostSlots = 768;       // of as many slots: their tables stay in LDS
+template <typename T> constexpr int kUncutTiles = T::kTag == LEOAM_F32 ? 1 : 8;      // if no unit has more tiles, none is cut
+// a piece: [32 groups of 4 channels][128 rows][4], maxima, sums
+constexpr int kPieceFloats = kRows * (LEOAM_D + 2);
+
+// the rows of slot `slot`: sequence, its first row in the call, its number of rows, which tile of them
+struct Unit { int b, row0, m, local; };
+__device__ __forceinline__ int first_slot_of(int row0, int i, int group) { return (int)((long long)row0 * group / kRows) + i; }
 
 template <typename T> __device__ __forceinline__ f32x16_t mfma_32x32x16(const uint4& a, const uint4& b, f32x16_t c);
 template <> __device__ __forceinline__ f32x16_t mfma_32x32x16<BF16>(const uint4& a, const uint4& b, f32x16_t c) {
@@ -47,7 +67,7 @@ template <typename T> __device__ __forceinline__ uint32_t not_finite(uint32_t w)
     return (w & m) == m || (w & (m << 16)) == (m << 16);
 }
 
-template <typename T, typename S, int G>
+template <typename T, typename S, int G, bool kShared>
 __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))) void page_prefill_kernel(PagePrefillArgs a) {
     constexpr bool k8 = std::is_same<S, E4M3>::value, k32 = T::kTag == LEOAM_F32;
     constexpr int ROWB = LEOAM_D * T::kBytes, SROWB = LEOAM_D * S::kBytes;      // a row in LDS, in the pages
@@ -62,23 +82,11 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
 
     const int tid = threadIdx.x, lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(tid / LEOAM_WAVE);
     const int half = lane >> 5, l32 = lane & 31;
-    const int hkv = a.n_kv_heads, h = blockIdx.x % hkv;
-    // (later rows see more keys: they are started first)
-    const int slot = a.n_slots - 1 - (int)(blockIdx.x / hkv);
-    int b, local = 0, row0 = 0, m = 1;
-    if (a.new_off) {
-        // sequence i's tiles begin at slot new_off[i] G / 128 + i
-        b = uniform(wave_count_below(a.batch, slot, [&](int i) { return (int)((long long)a.new_off[i] * G / kRows) + i; }));
-        if (b >= a.batch) return;
-        row0 = uniform(a.new_off[b]);
-        m = uniform(a.new_off[b + 1]) - row0;
-        local = slot - ((int)((long long)row0 * G / kRows) + b);
-        if (row0 < 0 || m < 0 || m > a.n_new - row0) return;
-    } else {
-        b = slot;
-        row0 = b;
-    }
-    if (local < 0 || (long long)local * kRows >= (long long)m * G) return;
+    const int hkv = a.n_kv_heads;
+
+    // tiles [j0, j1) of a unit; j1 < 0: all.  slot: where to leave a piece, < 0: the result is final
+    auto run = [&](const Unit& unit, int h, int j0, int j1, int piece_slot) {
+    const int b = unit.b, row0 = unit.row0, m = unit.m, local = unit.local;
     const int len = min(max(uniform(a.seq_len[b]), 0), a.max_pages << a.page_shift);
     const int first = len - m;                                   // position of the sequence's first new token (may be negative)
     const int tok0 = local * (kRows / G), n_tok = min(m - tok0, kRows / G);
@@ -87,6 +95,7 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
     const int row = 32 * wave + l32, tok = min(tok0 + row / G, m - 1);
     const int my_pos = first + tok;
     const bool stored = row / G < n_tok;
+    const bool idle = (32 * wave) / G >= n_tok;                   // none of the wave's rows is one
     const size_t q_row = ((size_t)(row0 + tok) * hkv + h) * G + row % G;
     const int wave_lo = first + tok0 + 32 * wave / G;             // the wave's rows see at least / at most
     const int wave_hi = min(first + tok0 + (32 * wave + 31) / G, first + m - 1);
@@ -289,21 +298,22 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
         }
     };
 
-    if (n_tiles > 0) {
+    const int j_end = j1 < 0 ? n_tiles : min(j1, n_tiles);
+    if (j0 < j_end) {
         int id[GROUPS];
-        pages_of(0, id);
-        fetch(0, id);
-        pages_of(min(1, n_tiles - 1), id);
-        stage(0, 0);
+        pages_of(j0, id);
+        fetch(j0, id);
+        pages_of(min(j0 + 1, n_tiles - 1), id);
+        stage(j0, j0 & 1);
         uint32_t ok = ok_next;
         __syncthreads();
-        for (int j = 0; j < n_tiles; ++j) {
-            const bool more = j + 1 < n_tiles;
+        for (int j = j0; j < j_end; ++j) {
+            const bool more = j + 1 < j_end;
             if (more) {
                 fetch(j + 1, id);
                 pages_of(min(j + 2, n_tiles - 1), id);
             }
-            if (j * KEYS <= wave_hi) work(j, j & 1, ok);
+            if (!idle && j * KEYS <= wave_hi) work(j, j & 1, ok);
             if (more) stage(j + 1, (j + 1) & 1);
             ok = ok_next;
             __syncthreads();
@@ -313,6 +323,22 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
     // ---- the rows' results -------------------------------------------------------------------------------
     const float l = l_run + shfl_xor_f(l_run, 32), inv = l == 0.f ? 0.f : 1.f / l;      // (NaN stays)
     if (!stored) return;
+    if (kShared && piece_slot >= 0) {
+        float* piece = a.partial + (size_t)piece_slot * kPieceFloats;
+#pragma unroll
+        for (int db = 0; db < 4; ++db)
+#pragma unroll
+            for (int r = 0; r < 16; r += 4) {
+                const int d4 = 8 * db + r / 2 + half;
+                store16(piece, ((size_t)d4 * kRows + row) * 16, make_uint4(float_to_bits(acc[db][r]), float_to_bits(acc[db][r + 1]),
+                                                                           float_to_bits(acc[db][r + 2]), float_to_bits(acc[db][r + 3])));
+            }
+        if (half == 0) {
+            piece[kRows * LEOAM_D + row] = ref;
+            piece[kRows * (LEOAM_D + 1) + row] = l;
+        }
+        return;
+    }
     if (a.lse && half == 0) a.lse[q_row] = l == 0.f ? -INFINITY : (ref + log2f(l)) * kLn2;
     char* out = a.out + q_row * ROWB;
 #pragma unroll
@@ -326,48 +352,250 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
             if constexpr (k32) store16(out, 4 * d, pack<F32>(x));
             else *reinterpret_cast<uint2*>(out + 2 * d) = make_uint2(pair_of(T{}, x[0], x[1]), pair_of(T{}, x[2], x[3]));
         }
+    };      // run
+
+    if constexpr (!kShared) {
+        const int h = blockIdx.x % hkv;
+        // (later rows see more keys: they are started first)
+        const int slot = a.n_slots - 1 - (int)(blockIdx.x / hkv);
+        Unit u = {slot, slot, 1, 0};
+        if (a.new_off) {
+            u.b = uniform(wave_count_below(a.batch, slot, [&](int i) { return first_slot_of(a.new_off[i], i, G); }));
+            if (u.b >= a.batch) return;
+            u.row0 = uniform(a.new_off[u.b]);
+            u.m = uniform(a.new_off[u.b + 1]) - u.row0;
+            u.local = slot - first_slot_of(u.row0, u.b, G);
+            if (u.row0 < 0 || u.m < 0 || u.m > a.n_new - u.row0) return;
+        }
+        if (u.local < 0 || (long long)u.local * kRows >= (long long)u.m * G) return;
+        run(u, h, 0, -1, -1);
+    } else {
+        // ---- this workgroup's share (at most kMostSlots slots, and no more sequences than slots) -------------
+        __shared__ int sh_off[kMostSlots + 1], sh_len[kMostSlots], sh_tiles[kMostSlots], sh_before[kMostSlots + 1];
+        __shared__ int sh_most;
+        for (int i = tid; i <= a.batch; i += kAttThreads) {
+            sh_off[i] = a.new_off ? a.new_off[i] : i;
+            if (i < a.batch) sh_len[i] = a.seq_len[i];
+        }
+        if (tid == 0) sh_most = 0;
+        __syncthreads();
+        auto unit_of = [&](int slot) {
+            Unit u;
+            if (!a.new_off) return Unit{slot, slot, 1, 0};
+            int lo = 0, hi = a.batch;      // the last sequence whose slots begin at or before this one
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) >> 1;
+                if (first_slot_of(sh_off[mid], mid, G) <= slot) lo = mid;
+                else hi = mid;
+            }
+            u.b = lo;
+            u.row0 = sh_off[lo];
+            u.m = sh_off[lo + 1] - u.row0;
+            u.local = slot - first_slot_of(u.row0, lo, G);
+            if (u.row0 < 0 || u.m < 0 || u.m > a.n_new - u.row0 || u.local < 0 || (long long)u.local * kRows >= (long long)u.m * G) u.m = 0;
+            return u;
+        };
+        for (int slot = tid; slot < a.n_slots; slot += kAttThreads) {
+            const Unit u = unit_of(slot);
+            int tiles = 0;
+            if (u.m > 0) {
+                const int first = min(max(sh_len[u.b], 0), a.max_pages << a.page_shift) - u.m, tok0 = u.local * (kRows / G);
+                tiles = max(1, (max(first + tok0 + min(u.m - tok0, kRows / G), 0) + KEYS - 1) / KEYS);
+                atomicMax(&sh_most, tiles);
+            } else if (blockIdx.x == 0) {
+                for (int h = 0; h < hkv; ++h) a.pieces[slot * hkv + h] = UnitPieces{0, 0, 0, 0};
+            }
+            sh_tiles[slot] = tiles;
+        }
+        __syncthreads();
+        if (wave == 0) {      // tiles before each slot (every slot has hkv units)
+            int run_sum = 0;
+            for (int s0 = 0; s0 < a.n_slots; s0 += LEOAM_WAVE) {
+                const int slot = s0 + lane;
+                const uint32_t mine = slot < a.n_slots ? (uint32_t)sh_tiles[slot] * hkv : 0u, incl = wave_incl_scan_u32(mine);
+                if (slot < a.n_slots) sh_before[slot] = run_sum + (int)(incl - mine);
+                run_sum += __builtin_amdgcn_readlane((int)incl, LEOAM_WAVE - 1);
+            }
+            if (lane == 0) sh_before[a.n_slots] = run_sum;
+        }
+        __syncthreads();
+        const int total = uniform(sh_before[a.n_slots]), W = gridDim.x;
+        const bool uncut = uniform(sh_most) <= kUncutTiles<T>;      // then workgroup w takes units w, w + W, ...
+        const int share = uncut ? 0 : (total + W - 1) / W;
+        int slot = 0, h = 0, off = 0, pos = 0, end = 0;
+        int next = blockIdx.x;
+        auto whole_unit = [&] {
+            while (next < a.n_slots * hkv) {
+                slot = next / hkv;
+                h = next % hkv;
+                next += W;
+                pos = 0;
+                end = uniform(sh_tiles[slot]);
+                if (end > 0) return;
+            }
+            pos = end = 0;
+        };
+        if (uncut) {
+            whole_unit();
+        } else {
+            pos = share * blockIdx.x;
+            end = min(total, pos + share);
+            if (pos >= end) return;
+            int lo = 0, hi = a.n_slots;
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) >> 1;
+                if (sh_before[mid] <= pos) lo = mid;
+                else hi = mid;
+            }
+            slot = uniform(lo);      // (of equal ones the last: the one that has tiles)
+            const int n = uniform(sh_tiles[slot]), in = pos - uniform(sh_before[slot]);
+            h = in / n;
+            off = in - h * n;
+        }
+        bool first_piece = true;
+        while (pos < end) {
+            const int n = uniform(sh_tiles[slot]), take = min(n - off, end - pos);
+            Unit u = unit_of(slot);
+            u = Unit{uniform(u.b), uniform(u.row0), uniform(u.m), uniform(u.local)};
+            const int id = slot * hkv + h;
+            const bool whole = take == n;
+            const int piece_slot = 2 * (int)blockIdx.x + (first_piece ? 0 : 1);      // opens the share, or closes it
+            first_piece = false;
+            if (off == 0 && tid == 0) {
+                UnitPieces up = {0, 0, 0, 0};
+                if (!whole) {
+                    const int tok0 = u.local * (kRows / G);
+                    up.count = (pos + n - 1) / share - (int)blockIdx.x + 1;
+                    up.first_slot = piece_slot;
+                    up.token0 = u.row0 + tok0;
+                    up.rows = min(u.m - tok0, kRows / G) * G;
+                }
+                a.pieces[id] = up;
+            }
+            run(u, h, off, off + take, whole ? -1 : piece_slot);
+            __syncthreads();
+            if (uncut) {
+                whole_unit();
+                continue;
+            }
+            pos += take;
+            off = 0;
+            if (++h == hkv) {
+                h = 0;
+                do ++slot;
+                while (slot < a.n_slots && sh_tiles[slot] == 0);
+            }
+        }
+    }
+}
+
+// 128 rows and 8 channels of a unit: its pieces, in order
+template <typename T>
+__global__ __launch_bounds__(256) void page_prefill_merge_kernel(PagePrefillArgs a, int group) {
+    const UnitPieces up = a.pieces[blockIdx.x];
+    const int row = threadIdx.x % kRows, d4 = 2 * blockIdx.y + threadIdx.x / kRows;
+    if (up.count == 0 || row >= up.rows) return;
+    float m = -INFINITY, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < up.count; ++i) {
+        // (each further one opens the next workgroup's share)
+        const int slot = i == 0 ? up.first_slot : 2 * (up.first_slot / 2 + i);
+        const float* piece = a.partial + (size_t)slot * kPieceFloats;
+        const float ms = piece[kRows * LEOAM_D + row], ls = piece[kRows * (LEOAM_D + 1) + row];
+        float x[4];
+        unpack<F32>(load16(piece, ((size_t)d4 * kRows + row) * 16), x);
+        const float mm = fmaxf(m, ms), c = exp2_or_zero(m, mm), w = exp2_or_zero(ms, mm);
+        m = mm;
+        l = l * c + w * ls;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] = o[e] * c + w * x[e];
+    }
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    const int h = blockIdx.x % a.n_kv_heads;
+    const size_t q_row = ((size_t)(up.token0 + row / group) * a.n_kv_heads + h) * group + row % group;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] *= inv;
+    char* out = a.out + q_row * LEOAM_D * T::kBytes;
+    if constexpr (T::kTag == LEOAM_F32) store16(out, 16 * d4, pack<F32>(o));
+    else *reinterpret_cast<uint2*>(out + 8 * d4) = make_uint2(pair_of(T{}, o[0], o[1]), pair_of(T{}, o[2], o[3]));
+    if (a.lse && d4 == 0) a.lse[q_row] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
 }
 
 size_t page_decode_workspace_bytes(const leoam_pages*);
 size_t page_decode_min_workspace_bytes(const leoam_pages*);
-size_t page_workspace_bytes(const leoam_pages* s, int n_new) {
-    return n_new <= 0 ? page_decode_workspace_bytes(s) : page_decode_min_workspace_bytes(s);
-}
-size_t page_min_workspace_bytes(const leoam_pages* s) { return page_decode_min_workspace_bytes(s); }
 
-template <typename T, typename S> static hipError_t launch_prefill(const PagePrefillArgs& a, int group, hipStream_t stream) {
+static long long prefill_slots(const leoam_pages* s, long long n_new) {
+    return n_new * (s->n_q_heads / s->n_kv_heads) / kRows + s->batch;
+}
+static size_t prefill_directory_bytes(long long units) { return (size_t)(units * sizeof(UnitPieces) + 255) / 256 * 256; }
+
+size_t page_min_workspace_bytes(const leoam_pages* s) { return page_decode_min_workspace_bytes(s); }
+size_t page_workspace_bytes(const leoam_pages* s, int n_new) {
+    if (n_new <= 0) return page_decode_workspace_bytes(s);
+    const long long units = prefill_slots(s, n_new) * s->n_kv_heads;
+    size_t bytes = 16;
+    if (units <= kMostUnits && prefill_slots(s, n_new) <= kMostSlots)
+        bytes = prefill_directory_bytes(units) + 2 * (size_t)kSharers * kPieceFloats * sizeof(float);
+    const size_t least = page_min_workspace_bytes(s);
+    return bytes > least ? bytes : least;
+}
+
+template <typename T, typename S, int G> static hipError_t launch_prefill(const PagePrefillArgs& a, int sharers, hipStream_t stream) {
     const long long units = (long long)a.n_slots * a.n_kv_heads;
     if (units > 0x7fffffffll) return hipErrorInvalidValue;
-    const dim3 grid((unsigned)units), block(kAttThreads);
-    switch (group) {
-    case 1: hipLaunchKernelGGL((page_prefill_kernel<T, S, 1>), grid, block, 0, stream, a); break;
-    case 2: hipLaunchKernelGGL((page_prefill_kernel<T, S, 2>), grid, block, 0, stream, a); break;
-    case 4: hipLaunchKernelGGL((page_prefill_kernel<T, S, 4>), grid, block, 0, stream, a); break;
-    default: hipLaunchKernelGGL((page_prefill_kernel<T, S, 8>), grid, block, 0, stream, a); break;
+    const dim3 block(kAttThreads);
+    if (sharers == 0) {
+        hipLaunchKernelGGL((page_prefill_kernel<T, S, G, false>), dim3((unsigned)units), block, 0, stream, a);
+        return hipGetLastError();
     }
+    hipLaunchKernelGGL((page_prefill_kernel<T, S, G, true>), dim3(sharers), block, 0, stream, a);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((page_prefill_merge_kernel<T>), dim3((unsigned)units, LEOAM_D / 8), dim3(256), 0, stream, a, G);
     return hipGetLastError();
+}
+template <typename T, typename S> static hipError_t prefill_of(const PagePrefillArgs& a, int group, int sharers, hipStream_t stream) {
+    switch (group) {
+    case 1: return launch_prefill<T, S, 1>(a, sharers, stream);
+    case 2: return launch_prefill<T, S, 2>(a, sharers, stream);
+    case 4: return launch_prefill<T, S, 4>(a, sharers, stream);
+    default: return launch_prefill<T, S, 8>(a, sharers, stream);
+    }
 }
 
 hipError_t page_prefill_dispatch(const leoam_pages* s, const void* q, int n_new, const int32_t* new_off, const void* k_pages,
                                  const void* v_pages, const float* k_scale, const float* v_scale, const int32_t* page_table,
-                                 const int32_t* seq_len, float softmax_scale, void* out, float* lse, void*, size_t,
-                                 hipStream_t stream) {
+                                 const int32_t* seq_len, float softmax_scale, void* out, float* lse, void* workspace,
+                                 size_t workspace_bytes, hipStream_t stream) {
     PagePrefillArgs a;
     const int group = s->n_q_heads / s->n_kv_heads;
+    const long long slots = new_off ? prefill_slots(s, n_new) : s->batch, units = slots * s->n_kv_heads;
+    if (units > 0x7fffffffll) return hipErrorInvalidValue;
     a.q = (const char*)q; a.k_pages = (const char*)k_pages; a.v_pages = (const char*)v_pages;
     a.k_scale = k_scale; a.v_scale = v_scale; a.page_table = page_table; a.seq_len = seq_len; a.new_off = new_off;
     a.n_new = n_new;
-    a.n_slots = new_off ? (int)((long long)n_new * group / kRows) + s->batch : s->batch;
+    a.n_slots = (int)slots;
     a.scale_log2 = fabsf(softmax_scale) * kLog2e;
     a.flip = softmax_scale < 0.f ? (s->q_dtype == LEOAM_F32 ? 0x80000000u : 0x80008000u) : 0u;
     a.out = (char*)out; a.lse = lse;
     a.batch = s->batch; a.n_kv_heads = s->n_kv_heads; a.n_pages = s->n_pages;
     a.page_shift = __builtin_ctz((unsigned)s->page_size); a.max_pages = s->max_pages;
+    // shared out if the units make less than two rounds of workgroups and the workspace holds two pieces for each of at least
+    // as many sharers as there are units (or as fill half the chip)
+    int sharers = 0;
+    a.pieces = (UnitPieces*)workspace;
+    a.partial = nullptr;
+    const long long most_tiles = (((long long)s->max_pages * s->page_size + 31) / 32) * units;      // 32-bit sums
+    if (units <= kMostUnits && slots <= kMostSlots && most_tiles < (1ll << 30)) {
+        const size_t dir = prefill_directory_bytes(units), piece = kPieceFloats * sizeof(float);
+        const long long fit = workspace_bytes > dir ? (long long)((workspace_bytes - dir) / (2 * piece)) : 0;
+        if (fit >= (units < kSharers / 2 ? units : kSharers / 2)) sharers = (int)(fit < kSharers ? fit : kSharers);
+        a.partial = (float*)((char*)workspace + dir);
+    }
     const bool k8 = s->kv_dtype == LEOAM_E4M3;
     switch (s->q_dtype) {
-    case LEOAM_F32: return launch_prefill<F32, F32>(a, group, stream);
-    case LEOAM_F16: return k8 ? launch_prefill<F16, E4M3>(a, group, stream) : launch_prefill<F16, F16>(a, group, stream);
-    default: return k8 ? launch_prefill<BF16, E4M3>(a, group, stream) : launch_prefill<BF16, BF16>(a, group, stream);
+    case LEOAM_F32: return prefill_of<F32, F32>(a, group, sharers, stream);
+    case LEOAM_F16: return k8 ? prefill_of<F16, E4M3>(a, group, sharers, stream) : prefill_of<F16, F16>(a, group, sharers, stream);
+    default: return k8 ? prefill_of<BF16, E4M3>(a, group, sharers, stream) : prefill_of<BF16, BF16>(a, group, sharers, stream);
     }
 }
 

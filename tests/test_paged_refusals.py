@@ -103,7 +103,7 @@ def test_workspace_sizes(L):
     for s in (pages(L), pages(L, kv=4), pages(L, dtype=0, kv=0), pages(L, hq=64, hkv=8, batch=300)):
         assert 0 <= L.leoam_page_workspace_min(s) <= L.leoam_page_workspace_bytes(s) <= 64 << 20
         for n in (1, 100, 1 << 20):
-            assert L.leoam_page_workspace_min(s) <= L.leoam_page_workspace_bytes(s, n) <= 64 << 20
+            assert L.leoam_page_workspace_min(s) <= L.leoam_page_workspace_bytes(s, n) <= 72 << 20
 
 
 def test_binding_looks_at_its_tensors(L):
