@@ -399,31 +399,45 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
     }
 }
 
-// A row's pieces: the first at first_slot, each further one opens the next workgroup's share.
-__global__ __launch_bounds__(256) void page_decode_merge_kernel(const float* __restrict__ partial, const RowPieces* __restrict__ pieces,
-                                                                int group, float* __restrict__ out, float* __restrict__ lse) {
+// A row's pieces: the first at first_slot, each further one opens the next workgroup's share.  128 threads take eight pieces
+// of a head at a time, all on their way together; PARTS groups of threads share a head's pieces, folded in order.  Four where
+// rows are few and pieces many (32 heads of 32 pieces: 4.0 us against 5.9 with two), one where it is the other way round
+// (2560 heads of 2 or 3: 5.2 against 7.9).
+constexpr int kMergeGroups = 4;
+constexpr int kManyRows = 64;
+template <int PARTS>
+__global__ __launch_bounds__(kMergeGroups * LEOAM_D) void page_decode_merge_kernel(const float* __restrict__ partial,
+                                                                                   const RowPieces* __restrict__ pieces, int group,
+                                                                                   int n_heads, float* __restrict__ out,
+                                                                                   float* __restrict__ lse) {
+    constexpr int HEADS = kMergeGroups / PARTS;
     constexpr int kBatch = 8;
-    __shared__ float sm[2], sl[2], so[LEOAM_D];
-    const size_t j = blockIdx.x;
+    __shared__ float sm[PARTS], sl[PARTS], so[PARTS][LEOAM_D];
+    const int d = threadIdx.x % LEOAM_D, tg = threadIdx.x / LEOAM_D, part = PARTS == 1 ? 0 : tg;
+    const int j = blockIdx.x * HEADS + (PARTS == 1 ? tg : 0);
+    if (j >= n_heads) return;
     const RowPieces rp = pieces[j / group];
     if (rp.count == 0) return;
-    const int g = (int)(j % group), d = threadIdx.x % LEOAM_D, part = threadIdx.x / LEOAM_D;
+    const int g = j % group;
     const size_t wg0 = rp.first_slot / 2;
     float m = -INFINITY, l = 0.f, o = 0.f;
-    for (int i0 = part * kBatch; i0 < rp.count; i0 += 2 * kBatch) {
+    for (int i0 = part * kBatch; i0 < rp.count; i0 += PARTS * kBatch) {
         float ms[kBatch], ls[kBatch], os[kBatch];
 #pragma unroll
         for (int u = 0; u < kBatch; ++u) {
             const int i = min(i0 + u, rp.count - 1);
             const size_t slot = i == 0 ? (size_t)rp.first_slot : 2 * (wg0 + i);
             const float* p = partial + (slot * group + g) * kPartStride;
-            ms[u] = i0 + u < rp.count ? p[LEOAM_D] : -INFINITY;
+            ms[u] = p[LEOAM_D];
             ls[u] = p[LEOAM_D + 1];
             os[u] = p[d];
         }
         float mb = m;
 #pragma unroll
-        for (int u = 0; u < kBatch; ++u) mb = fmaxf(mb, ms[u]);
+        for (int u = 0; u < kBatch; ++u) {
+            if (i0 + u >= rp.count) ms[u] = -INFINITY;
+            mb = fmaxf(mb, ms[u]);
+        }
         const float c = exp2_or_zero(m, mb);
         m = mb;
         l *= c;
@@ -436,20 +450,31 @@ __global__ __launch_bounds__(256) void page_decode_merge_kernel(const float* __r
             o += w * os[u];
         }
     }
-    if (d == 0) {
-        sm[part] = m;
-        sl[part] = l;
+    if constexpr (PARTS > 1) {      // (one head to a workgroup: all its threads are here)
+        if (d == 0) {
+            sm[part] = m;
+            sl[part] = l;
+        }
+        so[part][d] = o;
+        __syncthreads();
+        if (part) return;
+        m = sm[0];
+        l = o = 0.f;
+#pragma unroll
+        for (int p = 1; p < PARTS; ++p) m = fmaxf(m, sm[p]);
+#pragma unroll
+        for (int p = 0; p < PARTS; ++p) {
+            const float w = exp2_or_zero(sm[p], m);
+            l += w * sl[p];
+            o += w * so[p][d];
+        }
     }
-    if (part == 1) so[d] = o;
-    __syncthreads();
-    if (part == 1) return;
-    const float mm = fmaxf(sm[0], sm[1]), w0 = exp2_or_zero(sm[0], mm), w1 = exp2_or_zero(sm[1], mm);
-    const float ll = sl[0] * w0 + sl[1] * w1, oo = o * w0 + so[d] * w1;
-    out[j * LEOAM_D + d] = ll == 0.f ? 0.f : oo / ll;
-    if (lse && d == 0) lse[j] = ll == 0.f ? -INFINITY : (mm + log2f(ll)) * kLn2;
+    out[(size_t)j * LEOAM_D + d] = l == 0.f ? 0.f : o / l;      // (NaN stays)
+    if (lse && d == 0) lse[j] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
 }
 
-// Workgroups of the attention kernel: two fill a compute unit's registers.
+// Workgroups of the attention kernel: two fill a compute unit's registers (three, with fewer registers each, measured 101 against
+// 84 us for 40 sequences of up to 9000 tokens in 8 bits; one 111; twice as many shares 84.5 and more pieces).
 constexpr int kDecodeGroups = 512;
 
 static size_t piece_bytes(const leoam_pages* s) { return 2 * (size_t)(s->n_q_heads / s->n_kv_heads) * kPartStride * sizeof(float); }
@@ -469,8 +494,13 @@ template <typename T, typename S> static hipError_t launch_decode(const PageDeco
     }
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(page_decode_merge_kernel, dim3(a.batch * a.n_kv_heads * group), dim3(256), 0, stream, a.partial, a.pieces, group,
-                       a.out, a.lse);
+    const int n_heads = a.batch * a.n_kv_heads * group;
+    if (a.batch * a.n_kv_heads >= kManyRows)
+        hipLaunchKernelGGL(page_decode_merge_kernel<1>, dim3((n_heads + kMergeGroups - 1) / kMergeGroups), dim3(kMergeGroups * LEOAM_D), 0,
+                           stream, a.partial, a.pieces, group, n_heads, a.out, a.lse);
+    else
+        hipLaunchKernelGGL(page_decode_merge_kernel<kMergeGroups>, dim3(n_heads), dim3(kMergeGroups * LEOAM_D), 0, stream, a.partial,
+                           a.pieces, group, n_heads, a.out, a.lse);
     return hipGetLastError();
 }
 

@@ -495,19 +495,41 @@ __global__ __launch_bounds__(256) void page_prefill_merge_kernel(PagePrefillArgs
     const UnitPieces up = a.pieces[blockIdx.x];
     const int row = threadIdx.x % kRows, d4 = 2 * blockIdx.y + threadIdx.x / kRows;
     if (up.count == 0 || row >= up.rows) return;
+    constexpr int kBatch = 8;      // pieces that are on their way together
     float m = -INFINITY, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int i = 0; i < up.count; ++i) {
-        // (each further one opens the next workgroup's share)
-        const int slot = i == 0 ? up.first_slot : 2 * (up.first_slot / 2 + i);
-        const float* piece = a.partial + (size_t)slot * kPieceFloats;
-        const float ms = piece[kRows * LEOAM_D + row], ls = piece[kRows * (LEOAM_D + 1) + row];
-        float x[4];
-        unpack<F32>(load16(piece, ((size_t)d4 * kRows + row) * 16), x);
-        const float mm = fmaxf(m, ms), c = exp2_or_zero(m, mm), w = exp2_or_zero(ms, mm);
-        m = mm;
-        l = l * c + w * ls;
+    for (int i0 = 0; i0 < up.count; i0 += kBatch) {
+        float ms[kBatch], ls[kBatch];
+        uint4 x4[kBatch];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) o[e] = o[e] * c + w * x[e];
+        for (int u = 0; u < kBatch; ++u) {
+            const int i = min(i0 + u, up.count - 1);
+            // (each further piece opens the next workgroup's share)
+            const float* piece = a.partial + (size_t)(i == 0 ? up.first_slot : 2 * (up.first_slot / 2 + i)) * kPieceFloats;
+            ms[u] = piece[kRows * LEOAM_D + row];
+            ls[u] = piece[kRows * (LEOAM_D + 1) + row];
+            x4[u] = load16(piece, ((size_t)d4 * kRows + row) * 16);
+        }
+        float now = m;
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+            if (i0 + u >= up.count) ms[u] = -INFINITY;
+            now = fmaxf(now, ms[u]);
+        }
+        const float c = exp2_or_zero(m, now);
+        m = now;
+        l *= c;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] *= c;
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+            if (i0 + u >= up.count) continue;
+            const float w = exp2_or_zero(ms[u], m);
+            float x[4];
+            unpack<F32>(x4[u], x);
+            l += w * ls[u];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] += w * x[e];
+        }
     }
     const float inv = l == 0.f ? 0.f : 1.f / l;
     const int h = blockIdx.x % a.n_kv_heads;

@@ -338,6 +338,16 @@ def test_decode_long_and_few(L, dtype, q8):
     run_decode(L, Made(dtype, q8, [9001, 1, 40], 2, 16, seed=4, k_gain=4.0), 2)
 
 
+@pytest.mark.parametrize("dtype,q8", [(F32, False), (BF16, False), (F16, True)], ids=["f32", "bf16", "f16-e4m3"])
+@pytest.mark.parametrize("hkv,lengths", [(8, [9000]), (8, [3000, 1, 0, 700]), (9, [40, 2500, 33]), (16, [64] * 5)])
+def test_decode_rows_in_pieces(L, dtype, q8, hkv, lengths):
+    made = Made(dtype, q8, lengths, hkv, 64, seed=hkv)
+    first = run_decode(L, made, hkv * (2 if hkv == 8 else 1))
+    for _ in range(3):
+        again = run_decode(L, made, hkv * (2 if hkv == 8 else 1))
+        assert torch.equal(first[1], again[1]) and torch.equal(first[2], again[2])
+
+
 @pytest.mark.parametrize("dtype,q8", [(F32, False), (F16, True), (BF16, False)], ids=["f32", "f16-e4m3", "bf16"])
 def test_decode_small_workspaces(L, dtype, q8):
     made = Made(dtype, q8, [900, 0, 3, 1500], 2, 32, seed=5)
