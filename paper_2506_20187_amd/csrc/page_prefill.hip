@@ -38,10 +38,15 @@ struct UnitPieces { int32_t count, first_slot, token0, rows; };
 
 constexpr int kSharers = 512;         // workgroups that share the tiles: two fill a compute unit
 constexpr int kMostUnits = 1024;      // more units than this are not shared out: two rounds of workgroups or more
-constexpr int kMostSlots = 768;       // of as many slots: their tables stay in LDS
+constexpr int kMostSlots = 256;       // of as many slots: their tables stay in LDS
 template <typename T> constexpr int kUncutTiles = T::kTag == LEOAM_F32 ? 1 : 8;      // if no unit has more tiles, none is cut
 // a piece: [32 groups of 4 channels][128 rows][4], maxima, sums
 constexpr int kPieceFloats = kRows * (LEOAM_D + 2);
+
+// four keys of one channel: lane l of 16 gives the address of channels 4 (l % 4) .. + 3 of key l / 4 and gets channel l
+__device__ __forceinline__ uint2 transposed(const char* at) {
+    return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)at));
+}
 
 // the rows of slot `slot`: sequence, its first row in the call, its number of rows, which tile of them
 struct Unit { int b, row0, m, local; };
@@ -55,29 +60,42 @@ template <> __device__ __forceinline__ f32x16_t mfma_32x32x16<F16>(const uint4& 
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8_t, a), __builtin_bit_cast(f16x8_t, b), c, 0, 0, 0);
 }
 
-// Where 16-byte piece `piece` of row `row` lies in a tile: the pieces of a row are permuted by the row so that neither
-// eight rows at one piece (keys) nor four rows at four neighbouring pieces (values) meet in the banks.
-__device__ __forceinline__ uint32_t tile_at(int row, int piece, int row_bytes) {
-    return (uint32_t)(row * row_bytes + ((piece ^ (((row & 3) << 2) | ((row >> 2) & 3))) << 4));
-}
+// Bytes from one row to the next of a tile in LDS.  Keys are read 16 bytes of eight rows at a time: a row further is
+// four banks further.  Values are read, by half a wave, as 64 bytes of four rows (fp32: 128 bytes of two rows four apart): 16 banks
+// further (fp32: eight).  All offsets within a tile are constants that way.
+template <typename T> constexpr int kKeyStride = LEOAM_D * T::kBytes + 16;
+template <typename T> constexpr int kValueStride = LEOAM_D * T::kBytes + (T::kTag == LEOAM_F32 ? 32 : 64);
 
-template <typename T> __device__ __forceinline__ uint32_t not_finite(uint32_t w) {      // of a value in the register
-    if (T::kTag == LEOAM_F32) return (w & 0x7f800000u) == 0x7f800000u;
-    const uint32_t m = T::kTag == LEOAM_F16 ? 0x7c00u : 0x7f80u;
-    return (w & m) == m || (w & (m << 16)) == (m << 16);
+// the values of a register that are not finite become zero; whether there were any
+template <typename T> __device__ __forceinline__ bool silence(uint32_t& w) {
+    if constexpr (T::kTag == LEOAM_F32) {
+        const bool bad = (w & 0x7f800000u) == 0x7f800000u;
+        if (bad) w = 0;
+        return bad;
+    } else {
+        constexpr uint32_t m = T::kTag == LEOAM_F16 ? 0x7c00u : 0x7f80u;
+        const bool lo = (w & m) == m, hi = (w & (m << 16)) == (m << 16);
+        if (lo) w &= 0xffff0000u;
+        if (hi) w &= 0x0000ffffu;
+        return lo || hi;
+    }
+}
+template <typename T> __device__ __forceinline__ bool silence(uint4& w) {
+    const bool a = silence<T>(w.x), b = silence<T>(w.y), c = silence<T>(w.z), d = silence<T>(w.w);
+    return a || b || c || d;
 }
 
 template <typename T, typename S, int G, bool kShared>
 __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))) void page_prefill_kernel(PagePrefillArgs a) {
     constexpr bool k8 = std::is_same<S, E4M3>::value, k32 = T::kTag == LEOAM_F32;
     constexpr int ROWB = LEOAM_D * T::kBytes, SROWB = LEOAM_D * S::kBytes;      // a row in LDS, in the pages
-    constexpr int KEYS = k32 ? 32 : 64, KB = KEYS / 32, TILE_BYTES = KEYS * ROWB, NQ = k32 ? 16 : 8;
+    constexpr int KEYS = k32 ? 32 : 64, KB = KEYS / 32, KSTR = kKeyStride<T>, VSTR = kValueStride<T>, NQ = k32 ? 16 : 8;
     constexpr int LOADS = KEYS * SROWB / (kAttThreads * 16), PIECES = SROWB / 16, ROWS_PER_LOAD = kAttThreads / PIECES;
     constexpr int GROUPS = KEYS / 16;      // 16 keys never straddle a page
     // fp16: small weights stay clear of fp16's subnormals; the reference may lag the maximum by 2^kLag
     constexpr float kLag = 8.f, kBias = T::kTag == LEOAM_F16 ? 7.f : 0.f;
-    __shared__ __align__(16) char sh_k[2][TILE_BYTES];
-    __shared__ __align__(16) char sh_v[2][TILE_BYTES];
+    __shared__ __align__(16) char sh_k[2][KEYS * KSTR];
+    __shared__ __align__(16) char sh_v[2][KEYS * VSTR];
     __shared__ int sh_bad;
 
     const int tid = threadIdx.x, lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(tid / LEOAM_WAVE);
@@ -112,60 +130,73 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
     const int n_tiles = (keys + KEYS - 1) / KEYS, last = keys - 1;
     const int first_masked = max(first + tok0 + 1, 0) / KEYS;     // tiles from here on hide keys from some row
     const int32_t* table = a.page_table + (size_t)b * a.max_pages;
-    auto pages_of = [&](int j, int* id) {      // physical page of each 16-key group of tile j
+    // A tile's 16-key groups: the page of each (its number times the bytes of a page is where its rows begin in both pools), and
+    // which of them have one.
+    const uint32_t head_bytes = (uint32_t)SROWB << a.page_shift, page_bytes = head_bytes * (uint32_t)hkv;
+    const char *kh = a.k_pages + (size_t)h * head_bytes, *vh = a.v_pages + (size_t)h * head_bytes;
+    struct Pages { int id[GROUPS]; };
+    auto pages_of = [&](int j) {
+        Pages p;
 #pragma unroll
-        for (int g = 0; g < GROUPS; ++g) id[g] = uniform(table[min(j * KEYS + 16 * g, last) >> a.page_shift]);
+        for (int g = 0; g < GROUPS; ++g) p.id[g] = uniform(table[min(j * KEYS + 16 * g, last) >> a.page_shift]);
+        return p;
     };
     uint4 kr[LOADS], vr[LOADS];
     float ks[LOADS], vs[LOADS];
     uint32_t ok_next = 0;      // bit g: group g of the tile in registers has a page
-    auto fetch = [&](int j, const int* id) {
+    constexpr uint32_t kAllOk = (1u << GROUPS) - 1;
+    auto fetch = [&](int j, Pages p) {
         ok_next = 0;
 #pragma unroll
-        for (int g = 0; g < GROUPS; ++g) ok_next |= (id[g] >= 0 && id[g] < a.n_pages ? 1u : 0u) << g;
+        for (int g = 0; g < GROUPS; ++g) {
+            const bool ok = (uint32_t)p.id[g] < (uint32_t)a.n_pages;
+            ok_next |= ok ? 1u << g : 0u;
+            p.id[g] = ok ? p.id[g] : 0;
+        }
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
-            const int r = i * ROWS_PER_LOAD + tid / PIECES;      // (a load's 16-key group is the same for the wave)
-            const int g = uniform(r / 16);
-            int page = id[0];
+            // (a load's 16-key group is the same for the wave)
+            constexpr int kPerLoad = ROWS_PER_LOAD > 16 ? ROWS_PER_LOAD / 16 : 1;      // groups of one load: waves differ
+            const int r = i * ROWS_PER_LOAD + tid / PIECES, g0 = i * ROWS_PER_LOAD / 16;
+            const int wg = kPerLoad > 1 ? (wave * (LEOAM_WAVE / PIECES)) / 16 : 0;
+            int page = p.id[g0];
 #pragma unroll
-            for (int u = 1; u < GROUPS; ++u) page = g == u ? id[u] : page;
-            if (!(ok_next >> g & 1)) page = 0;
-            const size_t base = ((size_t)page * hkv + h);
-            const int e = min(j * KEYS + 16 * g, last) >> a.page_shift;
+            for (int u = 1; u < kPerLoad; ++u) page = wg == u ? p.id[g0 + u] : page;
+            const int e = min(j * KEYS + 16 * (g0 + wg), last) >> a.page_shift;
             const uint32_t at = (uint32_t)(min(j * KEYS + r, last) - (e << a.page_shift)) * SROWB + 16 * (tid % PIECES);
-            kr[i] = load16(a.k_pages + (base << a.page_shift) * SROWB, at);
-            vr[i] = load16(a.v_pages + (base << a.page_shift) * SROWB, at);
+            const uint64_t base = (uint64_t)(uint32_t)page * page_bytes;
+            kr[i] = load16(kh + base, at);
+            vr[i] = load16(vh + base, at);
             if (k8) {
-                ks[i] = a.k_scale[base];
-                vs[i] = a.v_scale[base];
+                const uint32_t row = (uint32_t)page * (uint32_t)hkv + (uint32_t)h;      // (pages * heads fit: their scales are addressed)
+                ks[i] = a.k_scale[(size_t)row];
+                vs[i] = a.v_scale[(size_t)row];
             }
         }
     };
     auto stage = [&](int j, int buf) {
-        uint32_t bad = 0;
+        // A value that is not finite must not reach rows that its key is hidden from, which a weight of zero does not
+        // prevent: from the first tile that hides keys on such values are left out here and added at the end.
+        const bool look = j >= first_masked;
+        bool bad = false;
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
             const int r = i * ROWS_PER_LOAD + tid / PIECES, piece = tid % PIECES;
-            if (!(ok_next >> (r / 16) & 1)) {      // nothing there: no value may matter
+            if (ok_next != kAllOk && !(ok_next >> (r / 16) & 1)) {      // nothing there: no value may matter
                 vr[i] = make_uint4(0, 0, 0, 0);
                 vs[i] = 1.f;
             }
             if constexpr (k8) {
-                const uint4 k0 = widen8<T>(kr[i].x, kr[i].y, ks[i]), k1 = widen8<T>(kr[i].z, kr[i].w, ks[i]);
                 uint4 v0 = widen8<T>(vr[i].x, vr[i].y, vs[i]), v1 = widen8<T>(vr[i].z, vr[i].w, vs[i]);
-                store16(sh_k[buf], tile_at(r, 2 * piece, ROWB), k0);
-                store16(sh_k[buf], tile_at(r, 2 * piece + 1, ROWB), k1);
-                store16(sh_v[buf], tile_at(r, 2 * piece, ROWB), v0);
-                store16(sh_v[buf], tile_at(r, 2 * piece + 1, ROWB), v1);
-                if (j >= first_masked)
-                    bad |= not_finite<T>(v0.x) | not_finite<T>(v0.y) | not_finite<T>(v0.z) | not_finite<T>(v0.w) |
-                           not_finite<T>(v1.x) | not_finite<T>(v1.y) | not_finite<T>(v1.z) | not_finite<T>(v1.w);
+                if (look) bad |= silence<T>(v0) | silence<T>(v1);
+                store16(sh_k[buf], r * KSTR + 32 * piece, widen8<T>(kr[i].x, kr[i].y, ks[i]));
+                store16(sh_k[buf], r * KSTR + 32 * piece + 16, widen8<T>(kr[i].z, kr[i].w, ks[i]));
+                store16(sh_v[buf], r * VSTR + 32 * piece, v0);
+                store16(sh_v[buf], r * VSTR + 32 * piece + 16, v1);
             } else {
-                store16(sh_k[buf], tile_at(r, piece, ROWB), kr[i]);
-                store16(sh_v[buf], tile_at(r, piece, ROWB), vr[i]);
-                if (j >= first_masked)
-                    bad |= not_finite<T>(vr[i].x) | not_finite<T>(vr[i].y) | not_finite<T>(vr[i].z) | not_finite<T>(vr[i].w);
+                if (look) bad |= silence<T>(vr[i]);
+                store16(sh_k[buf], r * KSTR + 16 * piece, kr[i]);
+                store16(sh_v[buf], r * VSTR + 16 * piece, vr[i]);
             }
         }
         if (bad) sh_bad = 1;
@@ -181,7 +212,11 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
     // key of register r of key block kb in this lane
     auto key_of = [&](int kb, int r) { return 32 * kb + 8 * (r / 4) + 4 * half + r % 4; };
 
+    const uint32_t k_lane = l32 * KSTR + 16 * half;
+    const uint32_t v_lane = k32 ? 4 * half * VSTR + 4 * l32
+                                : (4 * half + (lane & 15) / 4) * VSTR + 32 * ((lane >> 4) & 1) + 8 * (lane & 3);
     auto work = [&](int j, int buf, uint32_t ok) {
+        const char *kt = sh_k[buf] + k_lane, *vt = sh_v[buf] + v_lane;
         f32x16_t s[KB];
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb) {
@@ -189,7 +224,7 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
             for (int r = 0; r < 16; ++r) s[kb][r] = 0.f;
 #pragma unroll
             for (int i = 0; i < NQ; ++i) {
-                const uint4 ka = load16(sh_k[buf], tile_at(32 * kb + l32, 2 * i + half, ROWB));
+                const uint4 ka = load16(kt, 32 * kb * KSTR + 32 * i);
                 if constexpr (k32) {
                     float kx[4], qx[4];
                     unpack<F32>(ka, kx);
@@ -201,7 +236,7 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
                 }
             }
         }
-        const bool masked = j * KEYS + KEYS - 1 > wave_lo || ok != (1u << GROUPS) - 1;
+        const bool masked = j * KEYS + KEYS - 1 > wave_lo || ok != kAllOk;
         if (masked) {
 #pragma unroll
             for (int kb = 0; kb < KB; ++kb)
@@ -220,7 +255,7 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
             mt = fmaxf(x, y) * a.scale_log2 - kBias;
         }
         // The reference is the maximum of some earlier tile; it moves only when the maximum has left it behind by 2^kLag.
-        if (__ballot(mt > ref + kLag || (ref == -INFINITY && mt > ref))) {
+        if (__ballot(mt > ref + kLag)) {
             const float now = fmaxf(ref, mt), c = exp2_or_zero(ref, now);
             ref = now;
             l_run *= c;
@@ -237,16 +272,14 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
                 s[kb][r] = exp2_raw(fmaf(s[kb][r], a.scale_log2, -base));
                 l_run += s[kb][r];
             }
-        const bool careful = masked && sh_bad;      // a hidden key may have a value that is not finite
         if constexpr (k32) {
 #pragma unroll
             for (int r = 0; r < 16; ++r)
 #pragma unroll
                 for (int db = 0; db < 4; ++db) {
-                    const int key = key_of(0, r), d = 32 * db + l32;
-                    uint32_t v = *reinterpret_cast<const uint32_t*>(sh_v[buf] + tile_at(key, d / 4, ROWB) + 4 * (d % 4));
-                    if (careful && not_finite<T>(v)) v = 0;
-                    acc[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(bits_to_float(v), s[0][r], acc[db], 0, 0, 0);
+                    // key_of(0, r), channel 32 db + l32
+                    const float v = *reinterpret_cast<const float*>(vt + (8 * (r / 4) + r % 4) * VSTR + 128 * db);
+                    acc[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, s[0][r], acc[db], 0, 0, 0);
                 }
         } else {
 #pragma unroll
@@ -256,67 +289,55 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
                                            pair_of(T{}, s[kb][r0 + 4], s[kb][r0 + 5]), pair_of(T{}, s[kb][r0 + 6], s[kb][r0 + 7]));
 #pragma unroll
                 for (int db = 0; db < 4; ++db) {
-                    uint2 w[2];
-#pragma unroll
-                    for (int u = 0; u < 2; ++u) {
-                        const int key = 16 * t + 8 * u + 4 * half + (lane & 15) / 4, d = 32 * db + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
-                        char* at = sh_v[buf] + tile_at(key, d / 8, ROWB) + 2 * (d % 8);
-                        w[u] = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                                                             (__attribute__((address_space(3))) s16x4_t*)at));
-                    }
-                    uint4 v = make_uint4(w[0].x, w[0].y, w[1].x, w[1].y);
-                    if (careful) {
-                        const uint32_t mk = T::kTag == LEOAM_F16 ? 0x7c00u : 0x7f80u;
-                        auto clean = [&](uint32_t x) {
-                            if ((x & mk) == mk) x &= 0xffff0000u;
-                            if ((x & (mk << 16)) == (mk << 16)) x &= 0xffffu;
-                            return x;
-                        };
-                        v = make_uint4(clean(v.x), clean(v.y), clean(v.z), clean(v.w));
-                    }
-                    acc[db] = mfma_32x32x16<T>(v, p, acc[db]);
+                    // the lane's address is that of 4 channels of one key; what it gets is one channel of 4 keys
+                    const uint2 w0 = transposed(vt + 16 * t * VSTR + 64 * db), w1 = transposed(vt + (16 * t + 8) * VSTR + 64 * db);
+                    acc[db] = mfma_32x32x16<T>(make_uint4(w0.x, w0.y, w1.x, w1.y), p, acc[db]);
                 }
-            }
-        }
-        if (careful) {
-            // values that are not finite were left out: they reach the rows that see their key
-            for (int key = 0; key < KEYS; ++key) {
-                const bool sees = j * KEYS + key <= my_pos && (ok >> (key / 16) & 1);
-#pragma unroll
-                for (int db = 0; db < 4; ++db)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        const int d = 32 * db + 8 * (r / 4) + 4 * half + r % 4;
-                        const char* at = sh_v[buf] + tile_at(key, d * T::kBytes / 16, ROWB) + (d * T::kBytes) % 16;
-                        float v;
-                        if constexpr (k32) v = *reinterpret_cast<const float*>(at);
-                        else if constexpr (T::kTag == LEOAM_F16) v = (float)*reinterpret_cast<const _Float16*>(at);
-                        else v = bits_to_float((uint32_t) * reinterpret_cast<const uint16_t*>(at) << 16);
-                        if (sees && not_finite<F32>(float_to_bits(v))) acc[db][r] += v;
-                    }
             }
         }
     };
 
     const int j_end = j1 < 0 ? n_tiles : min(j1, n_tiles);
     if (j0 < j_end) {
-        int id[GROUPS];
-        pages_of(j0, id);
-        fetch(j0, id);
-        pages_of(min(j0 + 1, n_tiles - 1), id);
+        fetch(j0, pages_of(j0));
+        Pages next = pages_of(min(j0 + 1, n_tiles - 1));
         stage(j0, j0 & 1);
         uint32_t ok = ok_next;
         __syncthreads();
         for (int j = j0; j < j_end; ++j) {
             const bool more = j + 1 < j_end;
             if (more) {
-                fetch(j + 1, id);
-                pages_of(min(j + 2, n_tiles - 1), id);
+                fetch(j + 1, next);
+                next = pages_of(min(j + 2, n_tiles - 1));
             }
             if (!idle && j * KEYS <= wave_hi) work(j, j & 1, ok);
             if (more) stage(j + 1, (j + 1) & 1);
             ok = ok_next;
             __syncthreads();
+        }
+    }
+
+    if (sh_bad) {      // values that were left out reach the rows that see their keys
+        for (int t = max(j0, first_masked) * KEYS; t < min(j_end * KEYS, keys); ++t) {
+            const int id = uniform(table[t >> a.page_shift]);
+            if ((uint32_t)id >= (uint32_t)a.n_pages || t > my_pos) continue;
+            const char* v = vh + (uint64_t)(uint32_t)id * page_bytes + (size_t)(t & ((1 << a.page_shift) - 1)) * SROWB;
+#pragma unroll
+            for (int db = 0; db < 4; ++db)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int d = 32 * db + 8 * (r / 4) + 4 * half + r % 4;
+                    uint32_t w;
+                    if constexpr (k32) w = *reinterpret_cast<const uint32_t*>(v + 4 * d);
+                    else if constexpr (k8) w = (*reinterpret_cast<const uint8_t*>(v + d) & 0x7fu) == 0x7fu ? 0x7fc00000u : 0u;
+                    else {
+                        w = *reinterpret_cast<const uint16_t*>(v + 2 * d);
+                        // (the sign, the exponent's ones and whether there is a fraction, as a float has them)
+                        constexpr uint32_t m = T::kTag == LEOAM_F16 ? 0x7c00u : 0x7f80u;
+                        w = (w & m) != m ? 0u : (w & 0x8000u) << 16 | 0x7f800000u | (w & 0x7fffu & ~m ? 0x400000u : 0u);
+                    }
+                    if ((w & 0x7f800000u) == 0x7f800000u) acc[db][r] += bits_to_float(w);
+                }
         }
     }
 
