@@ -48,6 +48,10 @@ __device__ __forceinline__ uint2 transposed(const char* at) {
     return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)at));
 }
 
+// how the scheduler is to interleave what stands before it: n instructions of a kind
+enum : int { kMfma = 0x8, kValu = 0x2, kTrans = 0x400, kLdsRead = 0x100 };
+template <int KIND, int N> __device__ __forceinline__ void then() { __builtin_amdgcn_sched_group_barrier(KIND, N, 0); }
+
 // the rows of slot `slot`: sequence, its first row in the call, its number of rows, which tile of them
 struct Unit { int b, row0, m, local; };
 __device__ __forceinline__ int first_slot_of(int row0, int i, int group) { return (int)((long long)row0 * group / kRows) + i; }
@@ -82,6 +86,18 @@ template <typename T> __device__ __forceinline__ bool silence(uint32_t& w) {
 }
 template <typename T> __device__ __forceinline__ bool silence(uint4& w) {
     const bool a = silence<T>(w.x), b = silence<T>(w.y), c = silence<T>(w.z), d = silence<T>(w.w);
+    return a || b || c || d;
+}
+
+// the same for 8-bit codes: 0x7f and 0xff are not finite
+__device__ __forceinline__ bool silence_codes(uint32_t& w) {
+    // (a byte of `full` is 0x80 where the code's lower seven bits are all ones)
+    const uint32_t full = ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+    w &= ~((full >> 7) * 0xffu);
+    return full != 0;
+}
+__device__ __forceinline__ bool silence_codes(uint4& w) {
+    const bool a = silence_codes(w.x), b = silence_codes(w.y), c = silence_codes(w.z), d = silence_codes(w.w);
     return a || b || c || d;
 }
 
@@ -130,47 +146,34 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
     const int n_tiles = (keys + KEYS - 1) / KEYS, last = keys - 1;
     const int first_masked = max(first + tok0 + 1, 0) / KEYS;     // tiles from here on hide keys from some row
     const int32_t* table = a.page_table + (size_t)b * a.max_pages;
-    // A tile's 16-key groups: the page of each (its number times the bytes of a page is where its rows begin in both pools), and
-    // which of them have one.
-    const uint32_t head_bytes = (uint32_t)SROWB << a.page_shift, page_bytes = head_bytes * (uint32_t)hkv;
+    // Rows of head h of page p begin p * page_bytes behind kh and vh.  Lane l looks after 16-key group l % GROUPS of a tile.
+    const uint32_t head_bytes = (uint32_t)SROWB << a.page_shift, page_bytes = head_bytes * (uint32_t)hkv, in_page = (1u << a.page_shift) - 1;
     const char *kh = a.k_pages + (size_t)h * head_bytes, *vh = a.v_pages + (size_t)h * head_bytes;
-    struct Pages { int id[GROUPS]; };
-    auto pages_of = [&](int j) {
-        Pages p;
-#pragma unroll
-        for (int g = 0; g < GROUPS; ++g) p.id[g] = uniform(table[min(j * KEYS + 16 * g, last) >> a.page_shift]);
-        return p;
-    };
+    auto pages_of = [&](int j) { return table[min(j * KEYS + 16 * (lane % GROUPS), last) >> a.page_shift]; };
     uint4 kr[LOADS], vr[LOADS];
     float ks[LOADS], vs[LOADS];
     uint32_t ok_next = 0;      // bit g: group g of the tile in registers has a page
     constexpr uint32_t kAllOk = (1u << GROUPS) - 1;
-    auto fetch = [&](int j, Pages p) {
-        ok_next = 0;
-#pragma unroll
-        for (int g = 0; g < GROUPS; ++g) {
-            const bool ok = (uint32_t)p.id[g] < (uint32_t)a.n_pages;
-            ok_next |= ok ? 1u << g : 0u;
-            p.id[g] = ok ? p.id[g] : 0;
-        }
+    auto fetch = [&](int j, int id) {
+        const bool ok = (uint32_t)id < (uint32_t)a.n_pages;
+        ok_next = (uint32_t)__ballot(ok) & kAllOk;
+        const uint32_t page = ok ? (uint32_t)id : 0u;
+        const uint64_t begin = (uint64_t)page * page_bytes;
+        const int lo = (int)(uint32_t)begin, hi = (int)(uint32_t)(begin >> 32);
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
-            // (a load's 16-key group is the same for the wave)
+            // a load's 16-key group is the same for the wave
             constexpr int kPerLoad = ROWS_PER_LOAD > 16 ? ROWS_PER_LOAD / 16 : 1;      // groups of one load: waves differ
-            const int r = i * ROWS_PER_LOAD + tid / PIECES, g0 = i * ROWS_PER_LOAD / 16;
-            const int wg = kPerLoad > 1 ? (wave * (LEOAM_WAVE / PIECES)) / 16 : 0;
-            int page = p.id[g0];
-#pragma unroll
-            for (int u = 1; u < kPerLoad; ++u) page = wg == u ? p.id[g0 + u] : page;
-            const int e = min(j * KEYS + 16 * (g0 + wg), last) >> a.page_shift;
-            const uint32_t at = (uint32_t)(min(j * KEYS + r, last) - (e << a.page_shift)) * SROWB + 16 * (tid % PIECES);
-            const uint64_t base = (uint64_t)(uint32_t)page * page_bytes;
+            const int r = i * ROWS_PER_LOAD + tid / PIECES;
+            const int g = i * ROWS_PER_LOAD / 16 + (kPerLoad > 1 ? wave * (LEOAM_WAVE / PIECES) / 16 : 0);
+            const uint32_t at = ((uint32_t)min(j * KEYS + r, last) & in_page) * SROWB + 16 * (tid % PIECES);
+            const uint64_t base = (uint64_t)(uint32_t)__builtin_amdgcn_readlane(hi, g) << 32 | (uint32_t)__builtin_amdgcn_readlane(lo, g);
             kr[i] = load16(kh + base, at);
             vr[i] = load16(vh + base, at);
             if (k8) {
-                const uint32_t row = (uint32_t)page * (uint32_t)hkv + (uint32_t)h;      // (pages * heads fit: their scales are addressed)
-                ks[i] = a.k_scale[(size_t)row];
-                vs[i] = a.v_scale[(size_t)row];
+                const size_t row = (size_t)(uint32_t)__builtin_amdgcn_readlane((int)page, g) * hkv + h;
+                ks[i] = a.k_scale[row];
+                vs[i] = a.v_scale[row];
             }
         }
     };
@@ -179,22 +182,31 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
         // prevent: from the first tile that hides keys on such values are left out here and added at the end.
         const bool look = j >= first_masked;
         bool bad = false;
+        if (ok_next != kAllOk) {
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) {
+                if (ok_next >> ((i * ROWS_PER_LOAD + tid / PIECES) / 16) & 1) continue;
+                vr[i] = make_uint4(0, 0, 0, 0);      // nothing there: no value may matter
+                vs[i] = 1.f;
+            }
+        }
+        if (look) {
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) {
+                if constexpr (k8) bad |= silence_codes(vr[i]);
+                else bad |= silence<T>(vr[i]);
+            }
+        }
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
             const int r = i * ROWS_PER_LOAD + tid / PIECES, piece = tid % PIECES;
-            if (ok_next != kAllOk && !(ok_next >> (r / 16) & 1)) {      // nothing there: no value may matter
-                vr[i] = make_uint4(0, 0, 0, 0);
-                vs[i] = 1.f;
-            }
             if constexpr (k8) {
-                uint4 v0 = widen8<T>(vr[i].x, vr[i].y, vs[i]), v1 = widen8<T>(vr[i].z, vr[i].w, vs[i]);
-                if (look) bad |= silence<T>(v0) | silence<T>(v1);
+                const uint4 v0 = widen8<T>(vr[i].x, vr[i].y, vs[i]), v1 = widen8<T>(vr[i].z, vr[i].w, vs[i]);
                 store16(sh_k[buf], r * KSTR + 32 * piece, widen8<T>(kr[i].x, kr[i].y, ks[i]));
                 store16(sh_k[buf], r * KSTR + 32 * piece + 16, widen8<T>(kr[i].z, kr[i].w, ks[i]));
                 store16(sh_v[buf], r * VSTR + 32 * piece, v0);
                 store16(sh_v[buf], r * VSTR + 32 * piece + 16, v1);
             } else {
-                if (look) bad |= silence<T>(vr[i]);
                 store16(sh_k[buf], r * KSTR + 16 * piece, kr[i]);
                 store16(sh_v[buf], r * VSTR + 16 * piece, vr[i]);
             }
@@ -236,6 +248,14 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
                 }
             }
         }
+        if constexpr (!k32) {      // six reads ahead of the products
+            then<kLdsRead, 6>();
+            static_for<0, 10>([](auto) {
+                then<kMfma, 1>();
+                then<kLdsRead, 1>();
+            });
+            then<kMfma, 6>();
+        }
         const bool masked = j * KEYS + KEYS - 1 > wave_lo || ok != kAllOk;
         if (masked) {
 #pragma unroll
@@ -265,26 +285,27 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
                 for (int r = 0; r < 16; ++r) acc[i][r] *= c;
         }
         const float base = ref == -INFINITY ? 0.f : ref;
-#pragma unroll
-        for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                s[kb][r] = exp2_raw(fmaf(s[kb][r], a.scale_log2, -base));
-                l_run += s[kb][r];
-            }
+        auto weigh = [&](int kb, int r) {
+            s[kb][r] = exp2_raw(fmaf(s[kb][r], a.scale_log2, -base));
+            l_run += s[kb][r];
+        };
         if constexpr (k32) {
 #pragma unroll
-            for (int r = 0; r < 16; ++r)
+            for (int r = 0; r < 16; ++r) {
+                weigh(0, r);
 #pragma unroll
                 for (int db = 0; db < 4; ++db) {
                     // key_of(0, r), channel 32 db + l32
                     const float v = *reinterpret_cast<const float*>(vt + (8 * (r / 4) + r % 4) * VSTR + 128 * db);
                     acc[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, s[0][r], acc[db], 0, 0, 0);
                 }
+            }
         } else {
 #pragma unroll
             for (int t = 0; t < 2 * KB; ++t) {      // 16 keys
                 const int kb = t / 2, r0 = 8 * (t % 2);
+#pragma unroll
+                for (int r = r0; r < r0 + 8; ++r) weigh(kb, r);
                 const uint4 p = make_uint4(pair_of(T{}, s[kb][r0], s[kb][r0 + 1]), pair_of(T{}, s[kb][r0 + 2], s[kb][r0 + 3]),
                                            pair_of(T{}, s[kb][r0 + 4], s[kb][r0 + 5]), pair_of(T{}, s[kb][r0 + 6], s[kb][r0 + 7]));
 #pragma unroll
@@ -294,13 +315,26 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
                     acc[db] = mfma_32x32x16<T>(make_uint4(w0.x, w0.y, w1.x, w1.y), p, acc[db]);
                 }
             }
+            // the products of 16 keys run while the weights of the next 16 are computed and their values read
+            then<kLdsRead, 8>();
+            static_for<0, 8>([](auto) {
+                then<kValu, 3>();
+                then<kTrans, 1>();
+            });
+            static_for<0, 12>([](auto) {
+                then<kMfma, 1>();
+                then<kLdsRead, 2>();
+                then<kValu, 5>();
+                then<kTrans, 2>();
+            });
+            then<kMfma, 4>();
         }
     };
 
     const int j_end = j1 < 0 ? n_tiles : min(j1, n_tiles);
     if (j0 < j_end) {
         fetch(j0, pages_of(j0));
-        Pages next = pages_of(min(j0 + 1, n_tiles - 1));
+        int next = pages_of(min(j0 + 1, n_tiles - 1));
         stage(j0, j0 & 1);
         uint32_t ok = ok_next;
         __syncthreads();
