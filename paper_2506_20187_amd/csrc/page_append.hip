@@ -6,10 +6,9 @@
 // rounding to the page's type: what a plain evaluation gives, bit for bit.
 //
 // Bytes-bound (a row is read once and written once) for prompts, a chain of dependent round trips
-// (length -> page -> old scale) for single tokens.  A workgroup owns one (touched page, kv head): the scale of
-// an 8-bit page needs the largest magnitude over all that enters it, and the page's abstract row the maximum and
-// minimum, so nobody else may touch them.  Further workgroups rotate the queries.  A prompt's page takes 256
-// threads, a single token 64.
+// (length -> page -> old scale) for single tokens.  One workgroup owns a (touched page, kv head, tensor): the scale
+// of an 8-bit page needs the largest magnitude over all that enters it, and the page's abstract row the maximum and
+// minimum, so nobody else may touch them.
 #include "page_common.h"
 
 namespace leoam {
@@ -31,19 +30,10 @@ struct AppendArgs {
 struct Taken { int row0, m, n, status; };
 
 __device__ __forceinline__ Taken taken_by(const AppendArgs& a, int b) {
-    Taken t;
-    t.n = a.seq_len[b];
-    if (a.new_off) {
-        t.row0 = a.new_off[b];
-        t.m = a.new_off[b + 1] - t.row0;
-    } else {
-        t.row0 = b;
-        t.m = t.n > 0 ? 1 : 0;
-    }
-    t.status = 0;
-    if (t.m < 0 || t.row0 < 0 || t.m > a.n_new - t.row0 || t.n < t.m || t.n > a.max_pages * a.page_size) t.status = 1;
-    else if (a.rot_dim && t.m && t.n > a.rope_len) t.status = 3;
-    return t;
+    const bool ragged = a.new_off != nullptr;
+    const int n = a.seq_len[b], row0 = ragged ? a.new_off[b] : b, m = ragged ? a.new_off[b + 1] - row0 : n > 0 ? 1 : 0;
+    const bool misfit = m < 0 || row0 < 0 || m > a.n_new - row0 || n < m || n > a.max_pages * a.page_size;
+    return Taken{row0, m, n, misfit ? 1 : a.rot_dim && m && n > a.rope_len ? 3 : 0};
 }
 
 // The cosines and sines that the EPL channels from `col` need, 0-channel pairs beyond rot_dim left alone.
@@ -51,22 +41,28 @@ template <int EPL> struct Turn {
     float c[EPL], s[EPL];
     __device__ __forceinline__ void load(const AppendArgs& a, int pos, int col) {
         if (col >= a.rot_dim) return;
-        const int half = a.rot_dim >> 1;
-        const float* row = a.rope + (size_t)pos * a.rot_dim;
-        if (a.interleaved) {      // pairs (2i, 2i+1)
+        // pairs (2i, 2i+1): EPL / 2 angles from col / 2; pairs (i, i + half): EPL from col or col - half (half is a multiple of EPL)
+        constexpr int N = EPL / 2;
+        const int half = a.rot_dim >> 1, at = a.interleaved ? col >> 1 : col < half ? col : col - half, more = a.interleaved ? 0 : N;
+        const float* row = a.rope + (size_t)pos * a.rot_dim + at;
+        float c0[N], c1[N], s0[N], s1[N];
+        angles(row, c0);
+        angles(row + more, c1);
+        angles(row + half, s0);
+        angles(row + half + more, s1);
 #pragma unroll
-            for (int e = 0; e < EPL; e += 2) {
-                c[e] = c[e + 1] = row[(col + e) >> 1];
-                s[e] = s[e + 1] = row[half + ((col + e) >> 1)];
-            }
-        } else {                  // pairs (i, i + half); half is a multiple of EPL
-            const float* p = row + (col < half ? col : col - half);
-#pragma unroll
-            for (int e = 0; e < EPL; e += 4) {
-                const uint4 cc = load16(p, 4 * e), ss = load16(p + half, 4 * e);
-                unpack<F32>(cc, c + e);
-                unpack<F32>(ss, s + e);
-            }
+        for (int e = 0; e < EPL; ++e) {
+            c[e] = a.interleaved ? c0[e / 2] : e < N ? c0[e % N] : c1[e % N];
+            s[e] = a.interleaved ? s0[e / 2] : e < N ? s0[e % N] : s1[e % N];
+        }
+    }
+    static __device__ __forceinline__ void angles(const float* p, float* x) {
+        if constexpr (EPL == 8) {
+            unpack<F32>(load16(p, 0), x);
+        } else {
+            const float2 v = *reinterpret_cast<const float2*>(p);
+            x[0] = v.x;
+            x[1] = v.y;
         }
     }
 };
@@ -120,245 +116,365 @@ template <int THREADS> __device__ __forceinline__ float group_max(float v, float
     return m;
 }
 
-// ROWS passes of THREADS / lanes-per-row tokens each
-template <typename T, bool kStore8, int THREADS, int PASSES>
-__global__ __launch_bounds__(THREADS) void page_append_kernel(AppendArgs a) {
-    constexpr int EPL = T::kEpl, LPR = Row<T>::kLanesPerRow, RPP = THREADS / LPR, WAVES = THREADS / LEOAM_WAVE;
-    constexpr int ROWB = Row<T>::kRowBytes, STOREB = kStore8 ? LEOAM_D : ROWB;
-    __shared__ float sh_max[WAVES];
-    __shared__ float sh_abs[WAVES][2][LEOAM_D];
-    const int tid = threadIdx.x, lane = lane_id(), wave = tid / LEOAM_WAVE;
-    const int col = (tid % LPR) * EPL, rg = tid / LPR;
-    const int B = a.batch, ps = a.page_size;
-
-    const int n_kv_units = a.n_slots * a.n_kv_heads;
-    if ((int)blockIdx.x >= n_kv_units) {
-        // ---- queries: a token and 2 * RPP of its heads --------------------------------------------------
-        const int per_token = (a.n_q_heads + 2 * RPP - 1) / (2 * RPP);
-        const int u = blockIdx.x - n_kv_units, row = u / per_token, h0 = (u % per_token) * 2 * RPP;
-        int b = row;
-        if (a.new_off) b = wave_count_below(B, row, [&](int i) { return a.new_off[i]; });
-        if (b >= B) return;
-        const Taken t = taken_by(a, b);
-        if (t.status || row < t.row0 || row >= t.row0 + t.m) return;
-        Turn<EPL> turn;
-        turn.load(a, t.n - t.m + (row - t.row0), col);
+// Query rows: a token and 2 * (rows of a pass) of its heads.
+template <typename T, int THREADS> __device__ __forceinline__ void append_queries(const AppendArgs& a, int unit) {
+    constexpr int EPL = T::kEpl, LPR = Row<T>::kLanesPerRow, RPP = THREADS / LPR, ROWB = Row<T>::kRowBytes;
+    const int tid = threadIdx.x, col = (tid % LPR) * EPL, rg = tid / LPR;
+    const int per_token = (a.n_q_heads + 2 * RPP - 1) / (2 * RPP);
+    const int row = unit / per_token, h0 = (unit % per_token) * 2 * RPP;
+    int b = row;
+    if (a.new_off) b = wave_count_below(a.batch, row, [&](int i) { return a.new_off[i]; });
+    if (b >= a.batch) return;
+    const Taken t = taken_by(a, b);
+    if (t.status || row < t.row0 || row >= t.row0 + t.m) return;
+    Turn<EPL> turn;
+    turn.load(a, t.n - t.m + (row - t.row0), col);
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int h = h0 + i * RPP + rg, hc = min(h, a.n_q_heads - 1);
-            float x[EPL];
-            unpack<T>(load16(a.q, row * a.q_stride + (size_t)hc * ROWB + col * T::kBytes), x);
-            rotate<EPL, LPR>(a, turn, col, x);
-            if (h < a.n_q_heads) store16(a.q_out, ((size_t)row * a.n_q_heads + h) * ROWB + col * T::kBytes, round_pack<T>(x));
-        }
-        return;
+    for (int i = 0; i < 2; ++i) {
+        const int h = h0 + i * RPP + rg, hc = min(h, a.n_q_heads - 1);
+        float x[EPL];
+        unpack<T>(load16(a.q, row * a.q_stride + (size_t)hc * ROWB + col * T::kBytes), x);
+        rotate<EPL, LPR>(a, turn, col, x);
+        if (h < a.n_q_heads) store16(a.q_out, ((size_t)row * a.n_q_heads + h) * ROWB + col * T::kBytes, round_pack<T>(x));
     }
+}
 
-    // ---- a touched page of a sequence, one kv head ------------------------------------------------------------
-    const int h = blockIdx.x % a.n_kv_heads, slot = blockIdx.x / a.n_kv_heads;
-    int b = slot, local = 0;
+template <typename T, int THREADS> __global__ __launch_bounds__(THREADS) void page_append_queries_kernel(AppendArgs a) {
+    append_queries<T, THREADS>(a, blockIdx.x);
+}
+
+// A touched page of a sequence: logical page, the positions [p0, p1) that enter it, the row of the call that p0 is, how many
+// tokens the page held, its number in the pool; count = 0: nothing to do.
+struct TouchedPage { int b, p, p0, row0, held, count, id; };
+
+// `slot` of the call's touched pages, by the whole workgroup; the first of a sequence's reports (if `reports`).
+template <int THREADS> __device__ __forceinline__ TouchedPage touched_page(const AppendArgs& a, int slot, bool reports, float* sh_max) {
+    const int tid = threadIdx.x, ps = a.page_size;
+    TouchedPage x = {slot, 0, 0, 0, 0, 0, 0};
+    int local = 0;
     if (a.new_off) {
         // sequence i's pages begin at slot new_off[i] / ps + 2 i: it touches at most m / ps + 2
-        b = wave_count_below(B, slot, [&](int i) { return a.new_off[i] / ps + 2 * i; });
-        if (b >= B) return;
-        local = slot - (a.new_off[b] / ps + 2 * b);
+        x.b = wave_count_below(a.batch, slot, [&](int i) { return a.new_off[i] / ps + 2 * i; });
+        if (x.b >= a.batch) return x;
+        local = slot - (a.new_off[x.b] / ps + 2 * x.b);
     }
-    const Taken t = taken_by(a, b);
-    const int first = t.status || t.m == 0 ? 0 : (t.n - t.m) / ps, last = t.status || t.m == 0 ? -1 : (t.n - 1) / ps;
-    if (local == 0 && h == 0) {
+    const Taken t = taken_by(a, x.b);
+    const bool none = t.status || t.m == 0;
+    const int first = none ? 0 : (t.n - t.m) / ps, last = none ? -1 : (t.n - 1) / ps;
+    if (local == 0 && reports) {
         int bad = 0;
         for (int p = first + tid; p <= last; p += THREADS) {
-            const int id = a.page_table[(size_t)b * a.max_pages + p];
+            const int id = a.page_table[(size_t)x.b * a.max_pages + p];
             bad |= id < 0 || id >= a.n_pages;
         }
         bad = (int)(group_max<THREADS>((float)bad, sh_max));
         if (tid == 0) {
-            if (a.status) a.status[b] = t.status ? t.status : bad ? 2 : 0;
-            if (a.n_chunks && !t.status && t.m) a.n_chunks[b] = (t.n + ps - 1) / ps;
+            if (a.status) a.status[x.b] = t.status ? t.status : bad ? 2 : 0;
+            if (a.n_chunks && !none) a.n_chunks[x.b] = (t.n + ps - 1) / ps;
         }
     }
-    const int p = first + local;
-    if (local < 0 || p > last) return;
-    const int p0 = max(t.n - t.m, p * ps), p1 = min(t.n, (p + 1) * ps);      // positions that enter this page
-    if (h == 0 && tid == 0 && a.chunk_off) {
-        int32_t* off = a.chunk_off + (size_t)b * (a.max_pages + 1);
-        off[p + 1] = p1;
-        if (p == 0) off[0] = 0;
+    x.p = first + local;
+    if (local < 0 || x.p > last) return x;
+    x.p0 = max(t.n - t.m, x.p * ps);
+    const int p1 = min(t.n, (x.p + 1) * ps);
+    if (reports && tid == 0 && a.chunk_off) {
+        int32_t* off = a.chunk_off + (size_t)x.b * (a.max_pages + 1);
+        off[x.p + 1] = p1;
+        if (x.p == 0) off[0] = 0;
     }
-    const int id = a.page_table[(size_t)b * a.max_pages + p];
-    if (id < 0 || id >= a.n_pages) return;
-    const int held = p0 - p * ps, count = p1 - p0;
-    const int row0 = t.row0 + p0 - (t.n - t.m);
-    const size_t at = ((size_t)id * a.n_kv_heads + h), base = at * ps * STOREB;
-    char* abs_row = a.abstract ? a.abstract + (((size_t)b * a.n_kv_heads + h) * a.max_pages + p) * 2 * ROWB : nullptr;
-    // (model type: a lane stores 16 bytes of a row; 8 bits: the 8 codes of its channels)
+    x.id = a.page_table[(size_t)x.b * a.max_pages + x.p];
+    if (x.id < 0 || x.id >= a.n_pages) return x;
+    x.held = x.p0 - x.p * ps;
+    x.count = p1 - x.p0;
+    x.row0 = t.row0 + x.p0 - (t.n - t.m);
+    return x;
+}
 
+// The codes of a page whose scale grows by 1 / f, again; mx, mn (if wanted) take in the values that this thread's channels
+// (col, of 16 threads to a row) then stand for.
+template <int THREADS>
+__device__ __forceinline__ void encode_again(char* page, int held, float f, float now, bool want, float* mx, float* mn) {
+    for (int i = threadIdx.x; i < held * (LEOAM_D / 8); i += THREADS) {      // (THREADS is a multiple of a row's 16: same columns)
+        uint2 w = *reinterpret_cast<uint2*>(page + 8 * (size_t)i);
+        float y[8];
+        unpack_e4m3(w.x, y);
+        unpack_e4m3(w.y, y + 4);
 #pragma unroll
-    for (int which = 0; which < 2; ++which) {
-        const char* src = which ? a.v + (size_t)h * ROWB : a.k + (size_t)h * ROWB;
+        for (int e = 0; e < 8; ++e) y[e] *= f;
+        w = make_uint2(pack_e4m3(y), pack_e4m3(y + 4));
+        *reinterpret_cast<uint2*>(page + 8 * (size_t)i) = w;
+        if (!want) continue;
+        unpack_e4m3(w.x, y);
+        unpack_e4m3(w.y, y + 4);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            mx[e] = fmaxf(mx[e], y[e] * now);
+            mn[e] = fminf(mn[e], y[e] * now);
+        }
+    }
+}
+
+// One token's channels of this lane into its page; mx, mn take in what is stored.  inv: 1 / scale (8 bits).
+template <typename T, bool kStore8>
+__device__ __forceinline__ void store_token(char* page, int slot, int col, const float* x, float scale, float inv, bool valid, float* mx,
+                                            float* mn) {
+    constexpr int EPL = T::kEpl;
+    float y[EPL];
+    if constexpr (kStore8) {
+#pragma unroll
+        for (int e = 0; e < EPL; ++e) y[e] = x[e] * inv;
+        const uint2 w = make_uint2(pack_e4m3(y), pack_e4m3(y + 4));
+        if (valid) *reinterpret_cast<uint2*>(page + (size_t)slot * LEOAM_D + col) = w;
+        unpack_e4m3(w.x, y);
+        unpack_e4m3(w.y, y + 4);
+#pragma unroll
+        for (int e = 0; e < EPL; ++e) y[e] *= scale;
+    } else {
+        const uint4 w = round_pack<T>(x);
+        if (valid) store16(page, (size_t)slot * Row<T>::kRowBytes + col * T::kBytes, w);
+        unpack<T>(w, y);
+    }
+#pragma unroll
+    for (int e = 0; e < EPL; ++e) {      // (a token that does not count repeats one that does)
+        mx[e] = fmaxf(mx[e], y[e]);
+        mn[e] = fminf(mn[e], y[e]);
+    }
+}
+
+// The page's maximum and minimum key, from the lanes' (lanes LPR apart hold the same channels), the waves' and - if the page was
+// begun with another token and keeps its scale - what the row held.
+template <typename T, int THREADS>
+__device__ __forceinline__ void write_abstract(char* abs_row, bool begun, int col, float* mx, float* mn, float (*sh)[2][LEOAM_D]) {
+    constexpr int EPL = T::kEpl, LPR = Row<T>::kLanesPerRow, WAVES = THREADS / LEOAM_WAVE, ROWB = Row<T>::kRowBytes;
+    const int tid = threadIdx.x, lane = lane_id(), wave = tid / LEOAM_WAVE;
+#pragma unroll
+    for (int e = 0; e < EPL; ++e) {
+#pragma unroll
+        for (int msk = LPR; msk < LEOAM_WAVE; msk <<= 1) {
+            mx[e] = fmaxf(mx[e], shfl_xor_f(mx[e], msk));
+            mn[e] = fminf(mn[e], shfl_xor_f(mn[e], msk));
+        }
+    }
+    if constexpr (WAVES > 1) {
+        __syncthreads();
+        if (lane < LPR) {
+#pragma unroll
+            for (int e = 0; e < EPL; ++e) {
+                sh[wave][0][col + e] = mx[e];
+                sh[wave][1][col + e] = mn[e];
+            }
+        }
+        __syncthreads();
+        if (tid < LPR) {
+#pragma unroll
+            for (int w = 1; w < WAVES; ++w)
+#pragma unroll
+                for (int e = 0; e < EPL; ++e) {
+                    mx[e] = fmaxf(mx[e], sh[w][0][col + e]);
+                    mn[e] = fminf(mn[e], sh[w][1][col + e]);
+                }
+        }
+    }
+    if (tid >= LPR) return;
+    if (begun) {
+        float y[EPL];
+        unpack<T>(load16(abs_row, col * T::kBytes), y);
+#pragma unroll
+        for (int e = 0; e < EPL; ++e) mx[e] = fmaxf(mx[e], y[e]);
+        unpack<T>(load16(abs_row, ROWB + col * T::kBytes), y);
+#pragma unroll
+        for (int e = 0; e < EPL; ++e) mn[e] = fminf(mn[e], y[e]);
+    }
+    store16(abs_row, col * T::kBytes, round_pack<T>(mx));
+    store16(abs_row, ROWB + col * T::kBytes, round_pack<T>(mn));
+}
+
+__device__ __forceinline__ char* abstract_row(const AppendArgs& a, const TouchedPage& x, int h, int row_bytes) {
+    return a.abstract + (((size_t)x.b * a.n_kv_heads + h) * a.max_pages + x.p) * 2 * row_bytes;
+}
+
+// Prompts: a touched page and a kv head to a workgroup.
+//   16 / 32 bits (PASSES = 0): keys, then values, a pass of THREADS / lanes-per-row rows at a time; further workgroups take the
+//     queries.  9K tokens of 32 + 64 heads in fp16: 96 us, 4.6 TB/s (a large copy: 4.7).
+//   8 bits: the scale comes before the codes, so the page's new rows stay in registers, PASSES passes of them; keys and
+//     values are workgroups of their own, and so are the queries in a launch of their own.  16K tokens of 32 + 16 heads: 94 us
+//     against 134 with the former's shape (the queries at a quarter of the occupancy).
+// Workgroups of four heads, which would load the angles of a token once for them, were slower (144 against 93 us for the
+// keys and values of the former, 78 against 58 for the latter): a page then takes longer than there are pages to overlap.
+template <typename T, bool kStore8, int THREADS, int PASSES>
+__global__ __launch_bounds__(THREADS) void page_append_prompt_kernel(AppendArgs a) {
+    constexpr int EPL = T::kEpl, LPR = Row<T>::kLanesPerRow, RPP = THREADS / LPR, WAVES = THREADS / LEOAM_WAVE;
+    constexpr int ROWB = Row<T>::kRowBytes, STOREB = kStore8 ? LEOAM_D : ROWB;
+    __shared__ float sh_max[WAVES];
+    __shared__ float sh_abs[WAVES][2][LEOAM_D];
+    const int tid = threadIdx.x, col = (tid % LPR) * EPL, rg = tid / LPR, ps = a.page_size, hkv = a.n_kv_heads;
+    int unit = blockIdx.x, first = 0, last = 1;      // tensors
+    if constexpr (kStore8) {
+        first = last = unit & 1;
+        unit >>= 1;
+    } else if (unit >= a.n_slots * hkv) {
+        append_queries<T, THREADS>(a, unit - a.n_slots * hkv);
+        return;
+    }
+    const int h = unit % hkv;
+    const TouchedPage x = touched_page<THREADS>(a, unit / hkv, h == 0 && first == 0, sh_max);
+    if (x.count == 0) return;
+    const size_t at = (size_t)x.id * hkv + h;
+#pragma unroll kStore8 ? 1 : 2
+    for (int which = first; which <= last; ++which) {
+        const char* src = (which ? a.v : a.k) + (size_t)h * ROWB + col * T::kBytes;
         const long long stride = which ? a.v_stride : a.k_stride;
-        char* page = (which ? a.v_pages : a.k_pages) + base;
+        char* page = (which ? a.v_pages : a.k_pages) + at * ps * STOREB;
+        const bool turned = which == 0 && a.rot_dim > 0, bounded = which == 0 && a.abstract;
+        bool begun = x.held > 0;      // the abstract row counts
         float mx[EPL], mn[EPL];
 #pragma unroll
         for (int e = 0; e < EPL; ++e) {
             mx[e] = -INFINITY;
             mn[e] = INFINITY;
         }
-        bool begun = held > 0;      // the abstract row counts
-        auto fetch = [&](int r, float* x) {
-            const int rc = min(r, count - 1);
-            unpack<T>(load16(src, (row0 + rc) * stride + col * T::kBytes), x);
-            if (which == 0 && a.rot_dim) {
-                Turn<EPL> turn;
-                turn.load(a, p0 + rc, col);
-                rotate<EPL, LPR>(a, turn, col, x);
-            }
+        // (rows past the last repeat it: rotation exchanges lanes, so all of them are here)
+        auto row_of = [&](int r) { return load16(src, (x.row0 + min(r, x.count - 1)) * stride); };
+        auto turn_row = [&](int r, float* y) {
+            if (!turned) return;
+            Turn<EPL> turn;
+            turn.load(a, x.p0 + min(r, x.count - 1), col);
+            rotate<EPL, LPR>(a, turn, col, y);
         };
         if constexpr (!kStore8) {
-            for (int r = rg; r < count + rg; r += RPP) {      // (uniform trip count: rotation exchanges lanes)
-                float x[EPL];
-                fetch(r, x);
-                const uint4 w = round_pack<T>(x);
-                unpack<T>(w, x);
-#pragma unroll
-                for (int e = 0; e < EPL; ++e) {
-                    mx[e] = fmaxf(mx[e], x[e]);
-                    mn[e] = fminf(mn[e], x[e]);
-                }
-                if (r < count) store16(page, (size_t)(held + r) * ROWB + col * T::kBytes, w);
+            for (int r = rg; r < x.count + rg; r += RPP) {      // (uniform trip count)
+                float y[EPL];
+                unpack<T>(row_of(r), y);
+                turn_row(r, y);
+                store_token<T, false>(page, x.held + min(r, x.count - 1), col, y, 1.f, 1.f, r < x.count, mx, mn);
             }
         } else {
-            float x[PASSES][EPL], top = 0.f;
+            uint4 raw[PASSES];
+            float y[PASSES][EPL], top = 0.f;
+#pragma unroll
+            for (int i = 0; i < PASSES; ++i) raw[i] = row_of(i * RPP + rg);
+            float* scales = which ? a.v_scale : a.k_scale;
+            const float old = x.held > 0 ? scales[at] : 0.f;
 #pragma unroll
             for (int i = 0; i < PASSES; ++i) {
-                fetch(i * RPP + rg, x[i]);
+                unpack<T>(raw[i], y[i]);
+                turn_row(i * RPP + rg, y[i]);
 #pragma unroll
                 for (int e = 0; e < EPL; ++e) {
-                    const float m = fabsf(x[i][e]);
+                    const float m = fabsf(y[i][e]);
                     top = fmaxf(top, m < INFINITY ? m : 0.f);
                 }
             }
-            top = group_max<THREADS>(top, sh_max);
-            float* scales = which ? a.v_scale : a.k_scale;
-            const float old = held > 0 ? scales[at] : 0.f;
-            const float now = fmaxf(old, scale_of<T>(top));
-            const float inv = now > 0.f ? 1.f / now : 0.f;      // a power of two: exact
-            if (held > 0 && now > old) {
-                // the page's scale grew: its codes again, in the new scale
-                const float f = old * inv;
-                for (int i = tid; i < held * (LEOAM_D / 8); i += THREADS) {
-                    uint2 w = *reinterpret_cast<uint2*>(page + 8 * (size_t)i);
-                    float y[8];
-                    unpack_e4m3(w.x, y);
-                    unpack_e4m3(w.y, y + 4);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        y[e] *= f;
-                    }
-                    w = make_uint2(pack_e4m3(y), pack_e4m3(y + 4));
-                    *reinterpret_cast<uint2*>(page + 8 * (size_t)i) = w;
-                    if (which == 0 && abs_row) {      // (THREADS is a multiple of a row's 16 lanes: same columns)
-                        unpack_e4m3(w.x, y);
-                        unpack_e4m3(w.y, y + 4);
-#pragma unroll
-                        for (int e = 0; e < EPL; ++e) {
-                            mx[e] = fmaxf(mx[e], y[e] * now);
-                            mn[e] = fminf(mn[e], y[e] * now);
-                        }
-                    }
-                }
+            const float now = fmaxf(old, scale_of<T>(group_max<THREADS>(top, sh_max)));      // (everybody has the old scale)
+            const float inv = now > 0.f ? 1.f / now : 0.f;                                   // a power of two: exact
+            if (x.held > 0 && now > old) {
+                encode_again<THREADS>(page, x.held, old * inv, now, bounded, mx, mn);
                 begun = false;
             }
-            __syncthreads();      // everybody has the old scale
             if (tid == 0) scales[at] = now;
 #pragma unroll
             for (int i = 0; i < PASSES; ++i) {
                 const int r = i * RPP + rg;
-                if (r >= count) continue;
-                float y[EPL];
-#pragma unroll
-                for (int e = 0; e < EPL; ++e) y[e] = x[i][e] * inv;
-                const uint2 w = make_uint2(pack_e4m3(y), pack_e4m3(y + 4));
-                *reinterpret_cast<uint2*>(page + (size_t)(held + r) * LEOAM_D + col) = w;
-                unpack_e4m3(w.x, y);
-                unpack_e4m3(w.y, y + 4);
-#pragma unroll
-                for (int e = 0; e < EPL; ++e) {
-                    mx[e] = fmaxf(mx[e], y[e] * now);
-                    mn[e] = fminf(mn[e], y[e] * now);
-                }
+                store_token<T, true>(page, x.held + min(r, x.count - 1), col, y[i], now, inv, r < x.count, mx, mn);
             }
         }
-        if (which == 1 || !abs_row) continue;
-        // the page's maximum and minimum key: row groups of the wave, then the waves, then what the row held
-#pragma unroll
-        for (int e = 0; e < EPL; ++e) {
-#pragma unroll
-            for (int msk = LPR; msk < LEOAM_WAVE; msk <<= 1) {
-                mx[e] = fmaxf(mx[e], shfl_xor_f(mx[e], msk));
-                mn[e] = fminf(mn[e], shfl_xor_f(mn[e], msk));
-            }
-        }
-        if constexpr (WAVES > 1) {
-            __syncthreads();
-            if (lane < LPR) {
-#pragma unroll
-                for (int e = 0; e < EPL; ++e) {
-                    sh_abs[wave][0][col + e] = mx[e];
-                    sh_abs[wave][1][col + e] = mn[e];
-                }
-            }
-            __syncthreads();
-            if (tid < LPR) {
-#pragma unroll
-                for (int w = 1; w < WAVES; ++w)
-#pragma unroll
-                    for (int e = 0; e < EPL; ++e) {
-                        mx[e] = fmaxf(mx[e], sh_abs[w][0][col + e]);
-                        mn[e] = fminf(mn[e], sh_abs[w][1][col + e]);
-                    }
-            }
-        }
-        if (tid < LPR) {
-            if (begun) {
-                float y[EPL];
-                unpack<T>(load16(abs_row, col * T::kBytes), y);
-#pragma unroll
-                for (int e = 0; e < EPL; ++e) mx[e] = fmaxf(mx[e], y[e]);
-                unpack<T>(load16(abs_row, ROWB + col * T::kBytes), y);
-#pragma unroll
-                for (int e = 0; e < EPL; ++e) mn[e] = fminf(mn[e], y[e]);
-            }
-            store16(abs_row, col * T::kBytes, round_pack<T>(mx));
-            store16(abs_row, ROWB + col * T::kBytes, round_pack<T>(mn));
-        }
+        if (bounded) write_abstract<T, THREADS>(abstract_row(a, x, h, ROWB), begun, col, mx, mn, sh_abs);
     }
 }
 
-template <typename T, bool kStore8, int THREADS, int PASSES>
-static hipError_t launch_append(const AppendArgs& a, hipStream_t stream) {
-    constexpr int RPP = THREADS / Row<T>::kLanesPerRow;
-    const long long q_units = a.q ? (long long)a.n_new * ((a.n_q_heads + 2 * RPP - 1) / (2 * RPP)) : 0;
+// One token for each sequence: a wave to a (sequence, kv head), lanes of the first row's width hold the key and the value; further
+// waves take the queries.
+template <typename T, bool kStore8> __global__ __launch_bounds__(LEOAM_WAVE) void page_append_token_kernel(AppendArgs a) {
+    constexpr int EPL = T::kEpl, LPR = Row<T>::kLanesPerRow, ROWB = Row<T>::kRowBytes, STOREB = kStore8 ? LEOAM_D : ROWB, THREADS = LEOAM_WAVE;
+    const int hkv = a.n_kv_heads, ps = a.page_size, tid = threadIdx.x, col = (tid % LPR) * EPL;
+    if ((int)blockIdx.x >= a.n_slots * hkv) {
+        append_queries<T, THREADS>(a, blockIdx.x - a.n_slots * hkv);
+        return;
+    }
+    const int h = blockIdx.x % hkv;
+    const TouchedPage x = touched_page<THREADS>(a, blockIdx.x / hkv, h == 0, nullptr);
+    if (x.count == 0) return;
+    const uint4 raw[2] = {load16(a.k, x.row0 * a.k_stride + (size_t)h * ROWB + col * T::kBytes),
+                          load16(a.v, x.row0 * a.v_stride + (size_t)h * ROWB + col * T::kBytes)};
+    Turn<EPL> turn;
+    if (a.rot_dim) turn.load(a, x.p0, col);
+    const size_t at = (size_t)x.id * hkv + h;
+    float old[2] = {0.f, 0.f};
+    if (kStore8 && x.held > 0) {
+        old[0] = a.k_scale[at];
+        old[1] = a.v_scale[at];
+    }
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+        char* page = (which ? a.v_pages : a.k_pages) + at * ps * STOREB;
+        const bool bounded = which == 0 && a.abstract;
+        float y[EPL], mx[EPL], mn[EPL], scale = 1.f, inv = 1.f;
+        bool begun = x.held > 0;
+        unpack<T>(raw[which], y);
+        if (which == 0 && a.rot_dim) rotate<EPL, LPR>(a, turn, col, y);
+#pragma unroll
+        for (int e = 0; e < EPL; ++e) {
+            mx[e] = -INFINITY;
+            mn[e] = INFINITY;
+        }
+        if constexpr (kStore8) {
+            float top = 0.f;
+#pragma unroll
+            for (int e = 0; e < EPL; ++e) {
+                const float m = fabsf(y[e]);
+                top = fmaxf(top, m < INFINITY ? m : 0.f);
+            }
+            scale = fmaxf(old[which], scale_of<T>(group_max<THREADS>(top, nullptr)));
+            inv = scale > 0.f ? 1.f / scale : 0.f;
+            if (x.held > 0 && scale > old[which]) {
+                encode_again<THREADS>(page, x.held, old[which] * inv, scale, bounded, mx, mn);
+                begun = false;
+            }
+            if (tid == 0) (which ? a.v_scale : a.k_scale)[at] = scale;
+        }
+        store_token<T, kStore8>(page, x.held, col, y, scale, inv, tid < LPR, mx, mn);
+        if (bounded) write_abstract<T, THREADS>(abstract_row(a, x, h, ROWB), begun, col, mx, mn, nullptr);
+    }
+}
+
+template <typename T> constexpr int queries_per_unit(int threads) { return 2 * (threads / Row<T>::kLanesPerRow); }
+
+template <typename T, bool kStore8> static hipError_t launch_tokens(const AppendArgs& a, hipStream_t stream) {
+    const int per = queries_per_unit<T>(LEOAM_WAVE);
+    const long long q_units = a.q ? (long long)a.n_new * ((a.n_q_heads + per - 1) / per) : 0;
     const long long units = (long long)a.n_slots * a.n_kv_heads + q_units;
     if (units > 0x7fffffffll) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((page_append_kernel<T, kStore8, THREADS, PASSES>), dim3((unsigned)units), dim3(THREADS), 0, stream, a);
+    hipLaunchKernelGGL((page_append_token_kernel<T, kStore8>), dim3((unsigned)units), dim3(LEOAM_WAVE), 0, stream, a);
+    return hipGetLastError();
+}
+
+constexpr int kPromptThreads = 256;
+template <typename T, bool kStore8, int PASSES> static hipError_t launch_prompt(const AppendArgs& a, hipStream_t stream) {
+    const int per = queries_per_unit<T>(kPromptThreads);
+    const long long q_units = a.q ? (long long)a.n_new * ((a.n_q_heads + per - 1) / per) : 0, kv_units = (long long)a.n_slots * a.n_kv_heads;
+    const long long units = kStore8 ? 2 * kv_units : kv_units + q_units;
+    if (units > 0x7fffffffll || q_units > 0x7fffffffll) return hipErrorInvalidValue;
+    hipLaunchKernelGGL((page_append_prompt_kernel<T, kStore8, kPromptThreads, PASSES>), dim3((unsigned)units), dim3(kPromptThreads), 0, stream, a);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || !kStore8 || q_units == 0) return e;
+    hipLaunchKernelGGL((page_append_queries_kernel<T, kPromptThreads>), dim3((unsigned)q_units), dim3(kPromptThreads), 0, stream, a);
     return hipGetLastError();
 }
 
 template <typename T> static hipError_t append_of(const AppendArgs& a, bool store8, bool single, hipStream_t stream) {
     if constexpr (T::kTag != LEOAM_F32) {
         if (store8) {
-            if (single) return launch_append<T, true, LEOAM_WAVE, 1>(a, stream);
+            if (single) return launch_tokens<T, true>(a, stream);
             switch (a.page_size) {
-            case 16: return launch_append<T, true, 256, 1>(a, stream);
-            case 32: return launch_append<T, true, 256, 2>(a, stream);
-            case 64: return launch_append<T, true, 256, 4>(a, stream);
-            case 128: return launch_append<T, true, 256, 8>(a, stream);
-            default: return launch_append<T, true, 256, 16>(a, stream);
+            case 16: return launch_prompt<T, true, 1>(a, stream);
+            case 32: return launch_prompt<T, true, 2>(a, stream);
+            case 64: return launch_prompt<T, true, 4>(a, stream);
+            case 128: return launch_prompt<T, true, 8>(a, stream);
+            default: return launch_prompt<T, true, 16>(a, stream);
             }
         }
     }
-    return single ? launch_append<T, false, LEOAM_WAVE, 1>(a, stream) : launch_append<T, false, 256, 1>(a, stream);
+    return single ? launch_tokens<T, false>(a, stream) : launch_prompt<T, false, 0>(a, stream);
 }
 
 hipError_t page_append_dispatch(const leoam_pages* s, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
