@@ -41,7 +41,7 @@ template <> struct StepOf<F32, F32> {                 // 16 tokens: K 8 loads, V
 struct TileAt {
     uint32_t page;      // physical page, 0 if there is none
     int row0, valid;    // its first token's row in the page; how many of its tokens count
-    float ks, vs;
+    float ks, vs;       // (loaded with the tile: only its weights and products wait for them)
 };
 
 struct PageDecodeArgs {
@@ -72,7 +72,7 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
     __shared__ float xw[kAttWaves][G][kPartStride];
     __shared__ long long sh_sum[kAttWaves];
     __shared__ long long sh_at;
-    __shared__ int sh_entry;
+    __shared__ int sh_entry, sh_tokens;
 
     const int tid = threadIdx.x, lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(tid / LEOAM_WAVE), grp = lane >> 4, l16 = lane & 15;
     const int hkv = a.n_kv_heads;
@@ -107,7 +107,9 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
     if (pos >= before && pos < before + mine) {
         int e = e0;
         for (;;) {
-            const long long n = entry_tiles(e);
+            const int tokens = a.sel_idx ? walk_of(a, e / hkv, e % hkv) : walk_of(a, e, 0);
+            const long long n = (long long)weight * tiles_of(tokens);
+            sh_tokens = tokens;
             if (pos < before + n) break;
             before += n;
             ++e;
@@ -125,7 +127,7 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
             h = e % hkv;
             off = uniform((int)at);
         } else {
-            const int n = tiles_of(walk_of(a, e, 0));
+            const int n = tiles_of(uniform(sh_tokens));
             b = e;
             h = uniform((int)(at / n));
             off = uniform((int)(at - (long long)h * n));
@@ -133,10 +135,15 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
     }
 
     bool first_piece = true;
+    int next_tokens = sh_tokens;
     while (pos < end) {
-        const int tokens = uniform(walk_of(a, b, h)), n_tiles = tiles_of(tokens);
+        const int tokens = uniform(next_tokens), n_tiles = tiles_of(tokens);
         const int take = uniform((int)min((long long)(n_tiles - off), end - pos));
         const size_t bh = (size_t)b * hkv + h;
+        {
+            const int nh = h + 1 < hkv ? h + 1 : 0, nb = h + 1 < hkv ? b : b + 1;
+            if (pos + take < end) next_tokens = walk_of(a, nb, nh);      // (there is a further row)
+        }
         const int len = a.sel_idx ? min(max(a.seq_len[b], 0), a.max_pages << a.page_shift) : tokens;
         const int32_t* sel = a.sel_idx ? a.sel_idx + bh * (size_t)a.k_max : nullptr;
 
@@ -157,7 +164,6 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
 
         // lane i holds entry held0 + i of the walk: its physical page (0 and no tokens if it has none)
         int held0 = -(1 << 30), held_page = 0, held_valid = 0;
-        float held_ks = 0.f, held_vs = 0.f;
         auto hold = [&](int e) {
             held0 = e;
             const int i = e + lane, most = sel ? tokens >> a.page_shift : (tokens + (1 << a.page_shift) - 1) >> a.page_shift;
@@ -170,10 +176,6 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
             const bool ok = id >= 0 && id < a.n_pages;
             held_page = ok ? id : 0;
             held_valid = ok ? valid : 0;
-            if (k8) {
-                held_ks = ok ? a.k_scale[(size_t)held_page * hkv + h] : 0.f;
-                held_vs = ok ? a.v_scale[(size_t)held_page * hkv + h] : 0.f;
-            }
         };
         auto tile_at = [&](int t) {      // the tile that begins at token t (a multiple of 16) of the walk
             TileAt at;
@@ -183,8 +185,12 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
             at.page = (uint32_t)__builtin_amdgcn_readlane(held_page, i);
             at.row0 = t & ((1 << a.page_shift) - 1);
             at.valid = min(max(__builtin_amdgcn_readlane(held_valid, i) - at.row0, 0), 16);
-            at.ks = k8 ? bits_to_float((uint32_t)__builtin_amdgcn_readlane(__builtin_bit_cast(int, held_ks), i)) : 1.f;
-            at.vs = k8 ? bits_to_float((uint32_t)__builtin_amdgcn_readlane(__builtin_bit_cast(int, held_vs), i)) : 1.f;
+            at.ks = at.vs = 1.f;
+            if (k8) {
+                const size_t row = (size_t)at.page * hkv + h;
+                at.ks = a.k_scale[row];
+                at.vs = a.v_scale[row];
+            }
             return at;
         };
         // Loads are unconditional; a token that does not count re-reads the tile's last one that does (what
@@ -221,7 +227,7 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
 #pragma unroll
         for (int i = 0; i < 8; ++i) acc[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 
-        auto consume = [&](StepOf<T, S>& st, const TileAt* at) {
+        auto consume = [&](StepOf<T, S>& st, TileAt* at) {
             float z[4 * NT];
 #pragma unroll
             for (int j = 0; j < NT; ++j) {
@@ -253,6 +259,7 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
                     for (int r = 0; r < 4; ++r)
                         if (4 * grp + r >= at[j].valid) z[4 * j + r] = -INFINITY;
                     if (at[j].valid == 0) {      // nothing was read that counts: values must not matter either
+                        at[j].vs = 1.f;
 #pragma unroll
                         for (int r = 0; r < 4; ++r) {
                             if constexpr (k32) st.v[2 * r] = st.v[2 * r + 1] = make_uint4(0, 0, 0, 0);
