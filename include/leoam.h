@@ -482,7 +482,7 @@ typedef struct {
  * every pair (x_a, x_b) of rotated channels of q and k becomes
  *     (x_a c_i - x_b s_i,  x_b c_i + x_a s_i),
  * products and sums single binary32 operations.  q_out[r] (contiguous [n_new, Hq, 128], may be q itself if q is contiguous)
- * receives the rotated query, rounded once; q and q_out may both be NULL.  Keys (rotated) and values go to their places in the
+ * receives the rotated query, rounded once; q and q_out may both be NULL.  n_new == 0: nothing is done.  Keys (rotated) and values go to their places in the
  * pages, rounded once.
  * LEOAM_E4M3: scale = the smallest power of two s with |x| <= 448 s for all finite x that the page holds so far (0 for
  * none but zeros; it never falls while a page fills up; a page's first token starts it anew), code = round-half-even(x /

@@ -474,8 +474,9 @@ int kv_page_append(const leoam_pages* pages, const void* q, int64_t q_stride, co
     int rc = check_pages(pages);
     if (rc) return rc;
     if (n_new < 0 || (!new_off && n_new != pages->batch)) return LEOAM_E_INVALID_ARG;
+    if (n_new == 0) return LEOAM_OK;
     if (!seq_len || !page_table || !k_pages || !v_pages || !q != !q_out) return LEOAM_E_INVALID_ARG;
-    if (n_new > 0 && (!k || !v)) return LEOAM_E_INVALID_ARG;
+    if (!k || !v) return LEOAM_E_INVALID_ARG;
     if (pages->rot_dim && !rope) return LEOAM_E_INVALID_ARG;
     if (pages->kv_dtype == LEOAM_E4M3 && (!k_scale || !v_scale)) return LEOAM_E_INVALID_ARG;
     if (misaligned16(q, k, v, rope, q_out, k_pages, v_pages, abstract)) return LEOAM_E_INVALID_ARG;
@@ -484,7 +485,6 @@ int kv_page_append(const leoam_pages* pages, const void* q, int64_t q_stride, co
         bad_stride(v_stride, pages->q_dtype, pages->n_kv_heads, n_new))
         return LEOAM_E_INVALID_ARG;
     if (q && q == q_out && n_new > 1 && q_stride != (int64_t)pages->n_q_heads * LEOAM_D) return LEOAM_E_INVALID_ARG;
-    if (n_new == 0) return LEOAM_OK;
     return from_hip(page_append_dispatch(pages, q, q_stride, k, k_stride, v, v_stride, n_new, new_off, seq_len, page_table, rope,
                                          q_out, k_pages, v_pages, k_scale, v_scale, abstract, chunk_off, n_chunks, status,
                                          (hipStream_t)stream));

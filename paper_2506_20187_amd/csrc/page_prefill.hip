@@ -10,6 +10,8 @@
 // A unit of work is (128 rows, kv head).  With enough units to fill the chip each takes a workgroup.  With few (a
 // handful of rows behind a long context) the key tiles of all units are laid end to end and shared out equally; a
 // unit cut by the ends of shares leaves its pieces, (acc, m, l) per row, in the workspace, and a second kernel folds them.
+#include <cfloat>
+
 #include "page_common.h"
 
 namespace leoam {
@@ -651,7 +653,9 @@ hipError_t page_prefill_dispatch(const leoam_pages* s, const void* q, int n_new,
     a.k_scale = k_scale; a.v_scale = v_scale; a.page_table = page_table; a.seq_len = seq_len; a.new_off = new_off;
     a.n_new = n_new;
     a.n_slots = (int)slots;
+    // (hidden logits are -inf before they are scaled: a scale of zero is the smallest there is instead)
     a.scale_log2 = fabsf(softmax_scale) * kLog2e;
+    if (a.scale_log2 < FLT_MIN) a.scale_log2 = FLT_MIN;
     a.flip = softmax_scale < 0.f ? (s->q_dtype == LEOAM_F32 ? 0x80000000u : 0x80008000u) : 0u;
     a.out = (char*)out; a.lse = lse;
     a.batch = s->batch; a.n_kv_heads = s->n_kv_heads; a.n_pages = s->n_pages;

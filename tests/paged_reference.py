@@ -91,7 +91,7 @@ def attend(q, K, V, scale):
         return out, lse, reach
     for h in range(hkv):
         z = (q[h * g: (h + 1) * g] @ K[h].T) * scale
-        reach = max(reach, float((q[h * g: (h + 1) * g].abs() @ K[h].abs().T).max()) * scale)
+        reach = max(reach, float((q[h * g: (h + 1) * g].abs() @ K[h].abs().T).max()) * abs(scale))
         m = z.amax(1, keepdim=True)
         p = torch.exp(z - m)
         out[h * g: (h + 1) * g] = (p @ V[h]) / p.sum(1, keepdim=True)

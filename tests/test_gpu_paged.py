@@ -76,6 +76,11 @@ class Made:
         return v[self.table[b, pos // self.page].long(), :, pos % self.page].transpose(0, 1)
 
 
+def scratch(nbytes):
+    """A workspace: anything may stand in it."""
+    return torch.full((max(16, nbytes),), 0xAA, dtype=torch.uint8, device="cuda")
+
+
 def check(name, got, want, tol):
     got = got.double().cpu()
     assert torch.isfinite(got).all(), f"{name}: not finite"
@@ -83,10 +88,10 @@ def check(name, got, want, tol):
     assert (off <= tol).all(), f"{name}: off by {float((off - tol).max() + 0):.3g} more than allowed (largest {float(off.max()):.3g})"
 
 
-def check_rows(L, made, out, lse, rows, weight_half, out_half):
+def check_rows(L, made, out, lse, rows, weight_half, out_half, scale=SCALE):
     """rows: (index into out, q [Hq,128], per-head K, V lists)."""
     for i, q, K, V in rows:
-        want, want_lse, reach = R.attend(q.double(), K, V, SCALE)
+        want, want_lse, reach = R.attend(q.double(), K, V, scale)
         n = K.shape[1]
         if n == 0:
             assert (out[i] == 0).all() and (lse[i] == -math.inf).all()
@@ -271,7 +276,7 @@ KINDS = [(F32, False), (F16, False), (BF16, False), (F16, True), (BF16, True)]
 KIND_IDS = ["f32", "f16", "bf16", "f16-e4m3", "bf16-e4m3"]
 
 
-def run_decode(L, made, hq, seed=0, keep=None, workspace_bytes=None):
+def run_decode(L, made, hq, seed=0, keep=None, workspace_bytes=None, scale=SCALE):
     B, hkv = len(made.lengths), made.hkv
     g = torch.Generator().manual_seed(seed + 77)
     q = torch.randn(B, hq, 128, generator=g).to(made.dtype)
@@ -279,19 +284,19 @@ def run_decode(L, made, hq, seed=0, keep=None, workspace_bytes=None):
     out = torch.full((B, hq, 128), math.nan, device="cuda")
     lse = torch.full((B, hq), math.nan, device="cuda")
     nbytes = L.leoam_page_workspace_bytes(pages) if workspace_bytes is None else workspace_bytes
-    ws = torch.full((max(16, nbytes),), 0xAA, dtype=torch.uint8, device="cuda")
+    ws = scratch(nbytes)
     idx = count = None
     if keep is not None:
         idx, count = keep
     L.page_attention_decode(pages, q.cuda(), made.k_pages, made.v_pages, made.k_scale, made.v_scale, made.table.cuda(), made.seq_len,
-                            idx.cuda() if keep else None, count.cuda() if keep else None, SCALE, out, lse, ws)
+                            idx.cuda() if keep else None, count.cuda() if keep else None, scale, out, lse, ws)
     torch.cuda.synchronize()
     G = hq // hkv
     half = 0.0 if made.dtype == F32 else 2.0 ** -16
     for b, n in enumerate(made.lengths):
         if not keep:
             rows = [(b, q[b], made.tokens(0, b, range(n)), made.tokens(1, b, range(n)))]
-            check_rows(L, made, out, lse, rows, half, 2.0 ** -23)
+            check_rows(L, made, out, lse, rows, half, 2.0 ** -23, scale)
             continue
         for h in range(hkv):
             pos = []
@@ -365,16 +370,81 @@ def test_decode_bad_page_ids_hold_no_tokens(L):
     q = torch.randn(2, 4, 128, generator=g).to(BF16)
     out, lse = torch.empty(2, 4, 128, device="cuda"), torch.empty(2, 4, device="cuda")
     pages = made.pages(L, 4)
-    ws = torch.empty(max(16, L.leoam_page_workspace_bytes(pages)), dtype=torch.uint8, device="cuda")
+    ws = scratch(L.leoam_page_workspace_bytes(pages))
     L.page_attention_decode(pages, q.cuda(), made.k_pages, made.v_pages, None, None, made.table.cuda(), made.seq_len, None, None,
                             SCALE, out, lse, ws)
     for b, pos in ((0, [t for t in range(100) if t // 16 != 2]), (1, list(range(16, 64)))):
         check_rows(L, made, out, lse, [(b, q[b], made.tokens(0, b, pos), made.tokens(1, b, pos))], 2.0 ** -16, 2.0 ** -23)
 
 
+@pytest.mark.parametrize("dtype,q8", KINDS, ids=KIND_IDS)
+@pytest.mark.parametrize("scale", [-0.07, 0.0, 1.0])
+def test_scales_of_any_sign(L, dtype, q8, scale):
+    made = Made(dtype, q8, [70, 33], 2, 16, seed=21)
+    run_decode(L, made, 4, scale=scale)
+    run_prefill(L, made, 4, [20, 33], scale=scale)
+
+
+@pytest.mark.parametrize("dtype,q8", KINDS, ids=KIND_IDS)
+def test_one_heavy_token_among_many_light_ones(L, dtype, q8):
+    # weights down to 2^-26 of the largest, thousands of them: together they count
+    made = Made(dtype, q8, [6000], 1, 64, seed=22, k_gain=2.0)
+    run_decode(L, made, 2, scale=0.25)
+    run_prefill(L, made, 2, [3], scale=0.25)
+    run_prefill(L, made, 2, [6000], scale=0.25, rows={0, 64, 3000, 5999})
+
+
+@pytest.mark.parametrize("dtype,q8", [(BF16, False), (F16, True)], ids=["bf16", "f16-e4m3"])
+def test_a_page_listed_twice_counts_twice(L, dtype, q8):
+    made = Made(dtype, q8, [50], 1, 16, seed=23)
+    idx, count = torch.tensor([[[1, 1, 3, 3]]], dtype=torch.int32), torch.tensor([[4]], dtype=torch.int32)
+    run_decode(L, made, 4, keep=(idx, count))
+
+
+@pytest.mark.parametrize("dtype,q8", [(F32, False), (BF16, False), (BF16, True)], ids=["f32", "bf16", "bf16-e4m3"])
+def test_sequences_that_share_pages(L, dtype, q8):
+    made = Made(dtype, q8, [96, 40, 96], 2, 16, seed=24)
+    made.table[2, :4] = made.table[0, :4]                  # the first 64 tokens of the third are those of the first
+    run_decode(L, made, 8)
+    run_prefill(L, made, 8, [30, 40, 50])
+
+
+@pytest.mark.parametrize("dtype,q8", KINDS, ids=KIND_IDS)
+def test_pages_behind_4_gib(L, dtype, q8):
+    page, hkv = 256, 1
+    size = page * hkv * 128 * (1 if q8 else 4 if dtype == F32 else 2)
+    n_pages = (1 << 32) // size + 300
+    store = torch.float8_e4m3fn if q8 else dtype
+    g = torch.Generator().manual_seed(25)
+    k_pages = torch.empty(n_pages, hkv, page, 128, dtype=store, device="cuda")
+    v_pages = torch.empty_like(k_pages)
+    ks = torch.zeros(n_pages, hkv, device="cuda") if q8 else None
+    vs = torch.zeros(n_pages, hkv, device="cuda") if q8 else None
+    n, hq = 300, 2
+    table = torch.tensor([[n_pages - 1, n_pages - 7]], dtype=torch.int32)
+    pages = L.make_pages(1, hq, hkv, 128, n_pages, page, 2, dtype, L.E4M3 if q8 else None)
+    x = torch.randn(n, hq + 2 * hkv, 128, generator=g).to(dtype)
+    xg = x.cuda()
+    q, out, lse = torch.empty(n, hq, 128, dtype=dtype, device="cuda"), torch.empty(n, hq, 128, dtype=dtype, device="cuda"), torch.empty(n, hq, device="cuda")
+    off, seq_len = torch.tensor([0, n], dtype=torch.int32).cuda(), torch.tensor([n], dtype=torch.int32).cuda()
+    L.kv_page_append(pages, xg[:, :hq], xg[:, hq: hq + hkv], xg[:, hq + hkv:], off, seq_len, table.cuda(), None, q, k_pages, v_pages, ks, vs)
+    ws = scratch(max(L.leoam_page_workspace_bytes(pages, n), L.leoam_page_workspace_bytes(pages)))
+    L.page_attention_prefill(pages, q, off, k_pages, v_pages, ks, vs, table.cuda(), seq_len, SCALE, out, lse, ws)
+    dout, dlse = torch.empty(1, hq, 128, device="cuda"), torch.empty(1, hq, device="cuda")
+    L.page_attention_decode(pages, q[-1:].contiguous(), k_pages, v_pages, ks, vs, table.cuda(), seq_len, None, None, SCALE, dout, dlse, ws)
+    used = table[0].long()
+    small = lambda t: t[used].cpu() if t is not None else None  # noqa: E731
+    cache = R.Cache(small(k_pages), small(v_pages), small(ks), small(vs), dtype)
+    K, V = (cache.values(w).transpose(0, 1).reshape(hkv, -1, 128)[:, :n] for w in (0, 1))
+    assert torch.isfinite(K).all() and float(K.abs().max()) > 1
+    weight = 0.0 if dtype == F32 else HALF[dtype]
+    check_rows(L, None, out, lse, [(i, x[i, :hq], K[:, : i + 1], V[:, : i + 1]) for i in (0, 255, 256, n - 1)], weight, HALF[dtype])
+    check_rows(L, None, dout, dlse, [(0, x[n - 1, :hq], K, V)], 0.0 if dtype == F32 else 2.0 ** -16, 2.0 ** -23)
+
+
 # ---- prefill -------------------------------------------------------------------------------------------------
 
-def run_prefill(L, made, hq, new, seed=0, rows=None, workspace_bytes=None):
+def run_prefill(L, made, hq, new, seed=0, rows=None, workspace_bytes=None, scale=SCALE):
     """new: tokens of each sequence that attend; rows: which of the call's rows are compared (None: all)."""
     g = torch.Generator().manual_seed(seed + 5)
     n = sum(new)
@@ -384,9 +454,9 @@ def run_prefill(L, made, hq, new, seed=0, rows=None, workspace_bytes=None):
     out = torch.full((n, hq, 128), math.nan, dtype=made.dtype, device="cuda")
     lse = torch.full((n, hq), math.nan, device="cuda")
     nbytes = L.leoam_page_workspace_bytes(pages, n) if workspace_bytes is None else workspace_bytes
-    ws = torch.full((max(16, nbytes),), 0xAA, dtype=torch.uint8, device="cuda")
+    ws = scratch(nbytes)
     L.page_attention_prefill(pages, q.cuda(), torch.tensor(off, dtype=torch.int32).cuda(), made.k_pages, made.v_pages, made.k_scale,
-                             made.v_scale, made.table.cuda(), made.seq_len, SCALE, out, lse, ws)
+                             made.v_scale, made.table.cuda(), made.seq_len, scale, out, lse, ws)
     torch.cuda.synchronize()
     weight = 0.0 if made.dtype == F32 else HALF[made.dtype]
     for b, m in enumerate(new):
@@ -396,7 +466,7 @@ def run_prefill(L, made, hq, new, seed=0, rows=None, workspace_bytes=None):
             if rows is not None and off[b] + i not in rows:
                 continue
             t = length - m + i
-            check_rows(L, made, out, lse, [(off[b] + i, q[off[b] + i], K[:, : t + 1], V[:, : t + 1])], weight, HALF[made.dtype])
+            check_rows(L, made, out, lse, [(off[b] + i, q[off[b] + i], K[:, : t + 1], V[:, : t + 1])], weight, HALF[made.dtype], scale)
     return q, out, lse
 
 
@@ -429,13 +499,58 @@ def test_prefill_long_prompt(L, dtype, q8):
     run_prefill(L, made, 2, [1500, 1023], rows=some)
 
 
+@pytest.mark.parametrize("dtype,q8", KINDS, ids=KIND_IDS)
+def test_prefill_bad_page_ids_hold_no_tokens(L, dtype, q8):
+    made = Made(dtype, q8, [150, 64], 1, 16, seed=26)
+    made.table[0, 2], made.table[0, 7], made.table[1, 0] = 10 ** 6, -3, -5
+    g = torch.Generator().manual_seed(6)
+    q = torch.randn(70, 4, 128, generator=g).to(dtype)
+    out, lse = torch.empty(70, 4, 128, dtype=dtype, device="cuda"), torch.empty(70, 4, device="cuda")
+    pages = made.pages(L, 4)
+    ws = scratch(L.leoam_page_workspace_bytes(pages, 70))
+    L.page_attention_prefill(pages, q.cuda(), torch.tensor([0, 50, 70], dtype=torch.int32).cuda(), made.k_pages, made.v_pages, made.k_scale,
+                             made.v_scale, made.table.cuda(), made.seq_len, SCALE, out, lse, ws)
+    rows = []
+    for b, (r0, r1, n) in enumerate(((0, 50, 150), (50, 70, 64))):
+        for r in range(r0, r1):
+            pos = [t for t in range(n - (r1 - r) + 1) if not (b == 0 and t // 16 in (2, 7)) and not (b == 1 and t < 16)]
+            rows.append((r, q[r], made.tokens(0, b, pos), made.tokens(1, b, pos)))
+    check_rows(L, made, out, lse, rows, 0.0 if dtype == F32 else HALF[dtype], HALF[dtype])
+
+
+@pytest.mark.parametrize("dtype,q8", [(F32, False), (BF16, False), (F16, True)], ids=["f32", "bf16", "f16-e4m3"])
+def test_prefill_rows_of_no_sequence_and_of_negative_positions(L, dtype, q8):
+    made = Made(dtype, q8, [3, 40], 1, 16, seed=27)
+    q = torch.randn(30, 4, 128, generator=torch.Generator().manual_seed(7)).to(dtype)
+    out, lse = torch.full((30, 4, 128), 7.0, dtype=dtype, device="cuda"), torch.full((30, 4), 7.0, device="cuda")
+    pages = made.pages(L, 4)
+    ws = scratch(L.leoam_page_workspace_bytes(pages, 30))
+    # the first sequence claims 8 new tokens and holds 3; rows 20 .. 29 belong to nobody
+    L.page_attention_prefill(pages, q.cuda(), torch.tensor([0, 8, 20], dtype=torch.int32).cuda(), made.k_pages, made.v_pages, made.k_scale,
+                             made.v_scale, made.table.cuda(), made.seq_len, SCALE, out, lse, ws)
+    assert (out[20:] == 7).all() and (lse[20:] == 7).all()
+    assert (out[:5] == 0).all() and (lse[:5] == -math.inf).all()
+    rows = [(5 + i, q[5 + i], made.tokens(0, 0, range(i + 1)), made.tokens(1, 0, range(i + 1))) for i in range(3)]
+    rows += [(8 + i, q[8 + i], made.tokens(0, 1, range(29 + i)), made.tokens(1, 1, range(29 + i))) for i in range(12)]
+    check_rows(L, made, out, lse, rows, 0.0 if dtype == F32 else HALF[dtype], HALF[dtype])
+
+
+@pytest.mark.parametrize("dtype,q8", [(F32, False), (BF16, False), (F16, True)], ids=["f32", "bf16", "f16-e4m3"])
+def test_prefill_many_units(L, dtype, q8):
+    # more units than are shared out, and - with one sequence less - just as many as are
+    lengths = [130, 129, 128, 1, 300, 17] * 3
+    for n in (18, 3):
+        made = Made(dtype, q8, lengths[:n], 32, 16, seed=28)
+        run_prefill(L, made, 64, lengths[:n], rows=set(range(0, sum(lengths[:n]), 61)))
+
+
 def test_prefill_one_row_each(L):
     made = Made(BF16, True, [1, 300, 0, 17], 2, 16, seed=9)
     g = torch.Generator().manual_seed(2)
     q = torch.randn(4, 8, 128, generator=g).to(BF16)
     out, lse = torch.full((4, 8, 128), math.nan, dtype=BF16, device="cuda"), torch.full((4, 8), math.nan, device="cuda")
     pages = made.pages(L, 8)
-    ws = torch.empty(max(16, L.leoam_page_workspace_bytes(pages, 4)), dtype=torch.uint8, device="cuda")
+    ws = scratch(L.leoam_page_workspace_bytes(pages, 4))
     L.page_attention_prefill(pages, q.cuda(), None, made.k_pages, made.v_pages, made.k_scale, made.v_scale, made.table.cuda(),
                              made.seq_len, SCALE, out, lse, ws)
     check_rows(L, made, out, lse, [(b, q[b], made.tokens(0, b, range(n)), made.tokens(1, b, range(n))) for b, n in enumerate(made.lengths)],
@@ -455,7 +570,7 @@ def test_prefill_later_tokens_that_are_not_finite(L, dtype, q8, bad):
     q = torch.randn(90, 4, 128, generator=g).to(dtype)
     out, lse = torch.empty(90, 4, 128, dtype=dtype, device="cuda"), torch.empty(90, 4, device="cuda")
     pages = made.pages(L, 4)
-    ws = torch.empty(max(16, L.leoam_page_workspace_bytes(pages, 90)), dtype=torch.uint8, device="cuda")
+    ws = scratch(L.leoam_page_workspace_bytes(pages, 90))
     off = torch.tensor([0, 90], dtype=torch.int32).cuda()
     L.page_attention_prefill(pages, q.cuda(), off, made.k_pages, made.v_pages, made.k_scale, made.v_scale, made.table.cuda(), made.seq_len,
                              SCALE, out, lse, ws)
@@ -596,6 +711,92 @@ def test_same_call_twice_gives_the_same_bits(L):
     assert torch.equal(a[1], b[1]) and torch.equal(a[2], b[2])
 
 
+def test_two_calls_at_once(L):
+    """Two streams, each with a workspace of its own, against the calls one after the other."""
+    made = Made(BF16, True, [5000, 900, 70], 8, 32, seed=29)
+    pages = made.pages(L, 16)
+    g = torch.Generator().manual_seed(8)
+    q = torch.randn(3, 16, 128, generator=g).to(BF16).cuda()
+    table = made.table.cuda()
+    off = torch.tensor([0, 1, 2, 3], dtype=torch.int32).cuda()
+
+    def both(streams):
+        torch.cuda.synchronize()
+        res = []
+        for st in streams:
+            out, lse, p = torch.empty(3, 16, 128, device="cuda"), torch.empty(3, 16, device="cuda"), torch.empty(3, 16, 128, dtype=BF16, device="cuda")
+            res.append((out, lse, p, scratch(L.leoam_page_workspace_bytes(pages, 3))))
+        torch.cuda.synchronize()
+        for _ in range(5):
+            for st, (out, lse, p, ws) in zip(streams, res):
+                L.page_attention_decode(pages, q, made.k_pages, made.v_pages, made.k_scale, made.v_scale, table, made.seq_len, None, None, SCALE, out, lse, ws, st)
+                L.page_attention_prefill(pages, q, off, made.k_pages, made.v_pages, made.k_scale, made.v_scale, table, made.seq_len, SCALE, p, None, ws, st)
+        torch.cuda.synchronize()
+        return res
+    want = both([torch.cuda.current_stream()])[0]
+    for got in both([torch.cuda.Stream(), torch.cuda.Stream()]):
+        for a, b in zip(got[:3], want[:3]):
+            assert torch.equal(a, b)
+
+
+def test_prompt_replays_from_a_graph(L):
+    made = Made(BF16, False, [700, 90], 2, 64, seed=30)
+    pages = made.pages(L, 8)
+    g = torch.Generator().manual_seed(9)
+    new = [300, 50]
+    qs = [torch.randn(350, 8, 128, generator=g).to(BF16).cuda() for _ in range(3)]
+    q, out, lse = qs[0].clone(), torch.empty(350, 8, 128, dtype=BF16, device="cuda"), torch.empty(350, 8, device="cuda")
+    off, table = torch.tensor([0, 300, 350], dtype=torch.int32).cuda(), made.table.cuda()
+    ws = scratch(L.leoam_page_workspace_bytes(pages, sum(new)))
+
+    def call():
+        L.page_attention_prefill(pages, q, off, made.k_pages, made.v_pages, None, None, table, made.seq_len, SCALE, out, lse, ws)
+    want = []
+    for x in qs:
+        q.copy_(x)
+        call()
+        torch.cuda.synchronize()
+        want.append((out.clone(), lse.clone()))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for i in (2, 0, 1, 1):
+        q.copy_(qs[i])
+        out.fill_(7)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want[i][0]) and torch.equal(lse, want[i][1])
+
+
+def test_refused_tensors(L):
+    """What a tensor's type, size and layout must be is looked at before anything is launched."""
+    made = Made(BF16, False, [50], 2, 16, seed=31)
+    pages = made.pages(L, 8)
+    q, out, lse = torch.zeros(1, 8, 128, dtype=BF16, device="cuda"), torch.full((1, 8, 128), 7.0, device="cuda"), torch.empty(1, 8, device="cuda")
+    table, ws = made.table.cuda(), scratch(L.leoam_page_workspace_bytes(pages))
+    good = [pages, q, made.k_pages, made.v_pages, None, None, table, made.seq_len, None, None, SCALE, out, lse, ws]
+    bad = {1: [q.half(), q[:, :4].contiguous(), q.cpu(), None], 2: [made.k_pages[:-1], made.k_pages.transpose(2, 3), made.k_pages.half()],
+           6: [table.long(), table[:, :-1].contiguous()], 7: [made.seq_len.long(), made.seq_len[:0]], 11: [out.bfloat16(), out[:, 1:]],
+           12: [lse[:, 1:], lse.double()], 4: [torch.zeros(3, device="cuda", dtype=torch.int32)]}
+    for i, values in bad.items():
+        for v in values:
+            with pytest.raises(ValueError):
+                L.page_attention_decode(*good[:i], v, *good[i + 1:])
+    with pytest.raises(L.LeoamError) as e:
+        L.page_attention_decode(*good[:13], ws[:16])
+    assert e.value.status == -4
+    torch.cuda.synchronize()
+    assert (out == 7).all()
+    L.page_attention_decode(*good)
+    kv = torch.zeros(3, 2, 128, dtype=BF16, device="cuda")
+    off = torch.tensor([0, 3], dtype=torch.int32).cuda()
+    call = [pages, None, kv, kv, off, made.seq_len, table, None, None, made.k_pages, made.v_pages]
+    for i, values in {2: [kv[:2], kv[:, :1], kv.float(), kv[..., ::2], kv.transpose(0, 1)], 4: [off[:1], off.long()], 1: [kv]}.items():
+        for v in values:
+            with pytest.raises(ValueError):
+                L.kv_page_append(*call[:i], v, *call[i + 1:])
+
+
 def test_another_stream(L):
     made = Made(F16, False, [500, 70], 2, 64, seed=15)
     pages = made.pages(L, 4)
@@ -603,7 +804,7 @@ def test_another_stream(L):
     outs = []
     for stream in (None, torch.cuda.Stream()):
         out, lse = torch.empty(2, 4, 128, device="cuda"), torch.empty(2, 4, device="cuda")
-        ws = torch.empty(max(16, L.leoam_page_workspace_bytes(pages)), dtype=torch.uint8, device="cuda")
+        ws = scratch(L.leoam_page_workspace_bytes(pages))
         table = made.table.cuda()
         torch.cuda.synchronize()
         L.page_attention_decode(pages, q, made.k_pages, made.v_pages, None, None, table, made.seq_len, None, None, SCALE, out, lse, ws, stream)

@@ -60,18 +60,17 @@ def test_shapes(L, fields, status):
 
 
 def test_append(L):
+    # (two rows: a call that is refused launches nothing; no rows: a call that is not has nothing to do)
     s, rot, e4 = pages(L), pages(L, rot=64, rope=10), pages(L, kv=4)
     assert append(L, None) == INVALID
-    assert append(L, s) == OK                                         # no rows: nothing to do
-    for name in ("len", "table", "kp", "vp", "q", "q_out"):           # q and q_out only together
-        assert append(L, s, **{name: None}) == INVALID, name
-    assert append(L, s, q=None, q_out=None) == OK
+    assert append(L, s, n=0) == OK and append(L, s, n=0, q=None, k=None, v=None) == OK
+    for name in ("len", "table", "kp", "vp", "q", "q_out", "k", "v"):           # q and q_out only together
+        assert append(L, s, n=2, **{name: None}) == INVALID, name
     for name in ("q", "k", "v", "q_out", "kp", "vp", "abstract"):
-        assert append(L, s, **{name: ODD}) == INVALID, name
-    assert append(L, s, n=-1) == INVALID and append(L, s, n=3, off=None) == INVALID
-    assert append(L, s, n=3, k=None) == INVALID and append(L, s, n=3, v=None) == INVALID
-    assert append(L, rot) == INVALID and append(L, rot, rope=ODD) == INVALID and append(L, rot, rope=P) == OK
-    assert append(L, e4) == INVALID and append(L, e4, k_scale=P) == INVALID and append(L, e4, k_scale=P, v_scale=P) == OK
+        assert append(L, s, n=2, **{name: ODD}) == INVALID, name
+    assert append(L, s, n=-1) == INVALID and append(L, s, n=3, off=None) == INVALID and append(L, s, n=0, off=None) == INVALID
+    assert append(L, rot, n=2) == INVALID and append(L, rot, n=2, rope=ODD) == INVALID
+    assert append(L, e4, n=2) == INVALID and append(L, e4, n=2, k_scale=P) == INVALID
     for name, heads in (("qs", 8), ("ks", 2), ("vs", 2)):
         for stride in (0, -128, heads * 128 - 8, heads * 128 + 4, 1 << 40):
             assert append(L, s, n=3, **{name: stride}) == INVALID, (name, stride)
