@@ -75,7 +75,7 @@ template <> __device__ __forceinline__ uint4 widen8<F16>(uint32_t a, uint32_t b,
                       __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, s, true)));
 }
 
-// p (>= 0) as hi + lo of the 16-bit type
+// two floats rounded to the 16-bit type, and back
 __device__ __forceinline__ uint32_t pair_of(BF16, float a, float b) {
     bf16x2_t p;
     p.x = (__bf16)a;

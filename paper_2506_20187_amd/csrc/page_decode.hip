@@ -11,8 +11,8 @@
 // product O^T = V^T P^T wants of P; and because the order of the tokens in a contraction and of the channels
 // among the rows of a product is free, lane l of a 16-lane group loads channels 8l..8l+7 of the four tokens 4g..4g+3 whose
 // weights its group holds, and the operand (eight tokens of one channel) is put together from them by byte permutes.
-// P goes in as two 16-bit numbers, p = hi + lo (16 or more bits of it), so the float output keeps its precision;
-// the matrix cores are idle otherwise.
+// P goes in as two fp16 or three bf16 numbers that add up to it (22 or 24 bits), so the float output keeps its precision;
+// the matrix cores are idle otherwise.  fp32 keys are contracted in four chains, whose sums are rounded less often.
 #include "page_common.h"
 
 namespace leoam {
@@ -69,6 +69,7 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
     constexpr int STEP = 16 * NT, NV = 4 * NT;
     // fp16 weights: the row's maximum is taken 2^15 lower, so that small weights stay clear of fp16's subnormals
     constexpr float kBias = T::kTag == LEOAM_F16 ? 15.f : 0.f;
+    constexpr int kParts = T::kTag == LEOAM_F16 ? 2 : 3;      // of a weight
     __shared__ float xw[kAttWaves][G][kPartStride];
     __shared__ long long sh_sum[kAttWaves];
     __shared__ long long sh_at;
@@ -228,19 +229,24 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
         for (int i = 0; i < 8; ++i) acc[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 
         auto consume = [&](StepOf<T, S>& st, TileAt* at) {
-            float z[4 * NT];
+            float x[4 * NT], z[4 * NT];      // products, logits (log2 domain)
+            bool partial = false;            // some tile has tokens that do not count
 #pragma unroll
             for (int j = 0; j < NT; ++j) {
                 f32x4_t s = {0.f, 0.f, 0.f, 0.f};
                 if constexpr (k32) {
+                    f32x4_t chain[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) chain[e] = s;
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
                         float kx[4], qx[4];
                         unpack<F32>(st.k[i], kx);
                         unpack<F32>(qb[i], qx);
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_16x16x4f32(kx[e], qx[e], s, 0, 0, 0);
+                        for (int e = 0; e < 4; ++e) chain[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(kx[e], qx[e], chain[e], 0, 0, 0);
                     }
+                    s = (chain[0] + chain[1]) + (chain[2] + chain[3]);
                 } else if constexpr (k8) {
 #pragma unroll
                     for (int c = 0; c < 2; ++c) {
@@ -253,7 +259,11 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
                     for (int i = 0; i < 4; ++i) s = mfma_16x16x32<T>(st.k[4 * j + i], qb[i], s);
                 }
 #pragma unroll
-                for (int r = 0; r < 4; ++r) z[4 * j + r] = s[r] * a.scale_log2;
+                for (int r = 0; r < 4; ++r) {
+                    x[4 * j + r] = s[r];
+                    z[4 * j + r] = s[r] * a.scale_log2;
+                }
+                partial |= at[j].valid < 16;
                 if (at[j].valid < 16) {
 #pragma unroll
                     for (int r = 0; r < 4; ++r)
@@ -286,7 +296,8 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
             float p[4 * NT];
 #pragma unroll
             for (int i = 0; i < 4 * NT; ++i) {
-                p[i] = exp2_raw(z[i] - ref);
+                p[i] = exp2_raw(fmaf(x[i], a.scale_log2, -ref));
+                if (partial && z[i] == -INFINITY) p[i] = 0.f;
                 l_run += p[i];
             }
             if constexpr (k32) {
@@ -301,15 +312,20 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
                             acc[4 * c + e] = __builtin_amdgcn_mfma_f32_16x16x4f32(vx[e], p[r], acc[4 * c + e], 0, 0, 0);
                     }
             } else {
-                uint32_t hi[4], lo[4];
+                uint4 parts[kParts];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    float x, y;
-                    hi[i] = pair_of(T{}, p[2 * i], p[2 * i + 1]);
-                    pair_back(T{}, hi[i], x, y);
-                    lo[i] = pair_of(T{}, p[2 * i] - x, p[2 * i + 1] - y);
+                for (int n = 0; n < kParts; ++n) {
+                    uint32_t w[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        float u, v;
+                        w[i] = pair_of(T{}, p[2 * i], p[2 * i + 1]);
+                        pair_back(T{}, w[i], u, v);
+                        p[2 * i] -= u;      // (exact: what is left has fewer bits)
+                        p[2 * i + 1] -= v;
+                    }
+                    parts[n] = make_uint4(w[0], w[1], w[2], w[3]);
                 }
-                const uint4 ph = make_uint4(hi[0], hi[1], hi[2], hi[3]), pl = make_uint4(lo[0], lo[1], lo[2], lo[3]);
                 uint32_t v[8][4];      // [token slot][two channels each]
 #pragma unroll
                 for (int t = 0; t < 8; ++t) {
@@ -326,8 +342,8 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
                     col.y = __builtin_amdgcn_perm(v[3][e / 2], v[2][e / 2], pick);
                     col.z = __builtin_amdgcn_perm(v[5][e / 2], v[4][e / 2], pick);
                     col.w = __builtin_amdgcn_perm(v[7][e / 2], v[6][e / 2], pick);
-                    acc[e] = mfma_16x16x32<T>(col, ph, acc[e]);
-                    acc[e] = mfma_16x16x32<T>(col, pl, acc[e]);
+#pragma unroll
+                    for (int n = 0; n < kParts; ++n) acc[e] = mfma_16x16x32<T>(col, parts[n], acc[e]);
                 }
             }
         };
