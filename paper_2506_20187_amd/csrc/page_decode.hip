@@ -6,6 +6,8 @@
 // whose results are final, and at most two pieces of rows, which leave (acc[128], m, l) per head in the
 // workspace; a second small kernel folds a row's pieces in order, so results do not depend on scheduling.
 //
+// Where rows are short (uncut_tiles) a workgroup takes a row instead, and nothing is cut.
+//
 // Everything runs on the matrix cores without passing through LDS.  S^T = K Q^T: lane = token takes the 16-byte
 // loads of its key row as they are.  The result has lane = query head, registers = tokens, which is what the second
 // product O^T = V^T P^T wants of P; and because the order of the tokens in a contraction and of the channels
@@ -44,6 +46,13 @@ struct TileAt {
     float ks, vs;       // (loaded with the tile: only its weights and products wait for them)
 };
 
+// A row to a workgroup, or shares?  Cutting costs a second start (5 us: length, page, keys, one after the other), a fold and
+// a piece per cut, not cutting lets the longest row decide.  Rows of at most this many tiles are not cut.  (us, shares against rows,
+// lengths spread from 1 to the given, 8 bits / bf16: 160 rows to 1900 tokens 24 / 29 : 22 / 23, to 4000 33 / 43 : 39 / 51; 512 rows
+// to 900 34 / 40 : 20 / 28, to 4000 75 / 118 : 70 / 117, to 9000 121 / 216 : 148 / 260; 8 rows to 900 10.9 : 13.3.  fp32 takes
+// longer per tile: 64 rows to 400 13.4 : 14.9.)
+__host__ __device__ __forceinline__ int uncut_tiles(int rows, bool k32) { return k32 ? min(max(rows / 32, 1), 32) : min(max(rows / 8, 4), 32); }
+
 struct PageDecodeArgs {
     const char *q, *k_pages, *v_pages;
     const float *k_scale, *v_scale;
@@ -51,7 +60,8 @@ struct PageDecodeArgs {
     int k_max;
     float scale_log2;
     float *out, *lse, *partial;
-    RowPieces* pieces;
+    RowPieces* pieces;       // nullptr: a row to a workgroup, none is cut
+    int sharers;             // workgroups that share the tiles if rows are cut
     int batch, n_kv_heads, n_pages, page_shift, max_pages;
 };
 
@@ -73,77 +83,99 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
     __shared__ float xw[kAttWaves][G][kPartStride];
     __shared__ long long sh_sum[kAttWaves];
     __shared__ long long sh_at;
-    __shared__ int sh_entry, sh_tokens;
+    __shared__ int sh_entry, sh_tokens, sh_most[kAttWaves];
 
     const int tid = threadIdx.x, lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(tid / LEOAM_WAVE), grp = lane >> 4, l16 = lane & 15;
     const int hkv = a.n_kv_heads;
 
-    // ---- this workgroup's share of the tiles -------------------------------------------------------------
-    // entries: sequences (each hkv rows of the same length), or rows if a selection gives each its own
-    const int n_entries = a.sel_idx ? a.batch * hkv : a.batch, weight = a.sel_idx ? 1 : hkv;
-    const int per = (n_entries + kAttThreads - 1) / kAttThreads, e0 = min(tid * per, n_entries), e1 = min(e0 + per, n_entries);
-    auto entry_tiles = [&](int e) {
-        return (long long)weight * tiles_of(a.sel_idx ? walk_of(a, e / hkv, e % hkv) : walk_of(a, e, 0));
-    };
-    long long mine = 0;
-    for (int e = e0; e < e1; ++e) mine += entry_tiles(e);
-    long long incl = mine;
-#pragma unroll
-    for (int d = 1; d < LEOAM_WAVE; d <<= 1) {
-        const long long o = __shfl_up(incl, d, LEOAM_WAVE);
-        if (lane >= d) incl += o;
-    }
-    if (lane == LEOAM_WAVE - 1) sh_sum[wave] = incl;
-    __syncthreads();
-    long long total = 0, before = incl - mine;
-#pragma unroll
-    for (int w = 0; w < kAttWaves; ++w) {
-        if (w < wave) before += sh_sum[w];
-        total += sh_sum[w];
-    }
-    const long long share = (total + gridDim.x - 1) / gridDim.x;
-    long long pos = share * blockIdx.x;
-    const long long end = min(total, pos + share);
-    if (pos >= end) return;
-    if (pos >= before && pos < before + mine) {
-        int e = e0;
-        for (;;) {
-            const int tokens = a.sel_idx ? walk_of(a, e / hkv, e % hkv) : walk_of(a, e, 0);
-            const long long n = (long long)weight * tiles_of(tokens);
-            sh_tokens = tokens;
-            if (pos < before + n) break;
-            before += n;
-            ++e;
+    // ---- this workgroup's share of the tiles, or its rows -------------------------------------------------
+    const int rows = a.batch * hkv;
+    bool whole_rows = a.pieces == nullptr;      // (no row can be long)
+    int b = 0, h = 0, off = 0;                   // the row, and the tile in it
+    long long share = 1, pos = 0, end = 0;
+    int next_tokens = 0;
+    if (!whole_rows) {
+        // entries: sequences (each hkv rows of the same length), or rows if a selection gives each its own
+        const int n_entries = a.sel_idx ? rows : a.batch, weight = a.sel_idx ? 1 : hkv;
+        const int per = (n_entries + kAttThreads - 1) / kAttThreads, e0 = min(tid * per, n_entries), e1 = min(e0 + per, n_entries);
+        auto entry_tokens = [&](int e) { return a.sel_idx ? walk_of(a, e / hkv, e % hkv) : walk_of(a, e, 0); };
+        long long mine = 0;
+        int most = 0;
+        for (int e = e0; e < e1; ++e) {
+            const int n = tiles_of(entry_tokens(e));
+            mine += (long long)weight * n;
+            most = max(most, n);
         }
-        sh_entry = e;
-        sh_at = pos - before;
-    }
-    __syncthreads();
-    int b, h, off;      // the row, and the tile in it
-    {
-        const int e = uniform(sh_entry);
-        const long long at = sh_at;
-        if (a.sel_idx) {
-            b = e / hkv;
-            h = e % hkv;
-            off = uniform((int)at);
-        } else {
-            const int n = tiles_of(uniform(sh_tokens));
-            b = e;
-            h = uniform((int)(at / n));
-            off = uniform((int)(at - (long long)h * n));
+        long long incl = mine;
+#pragma unroll
+        for (int d = 1; d < LEOAM_WAVE; d <<= 1) {
+            const long long o = __shfl_up(incl, d, LEOAM_WAVE);
+            if (lane >= d) incl += o;
         }
+        most = (int)wave_max_u32((uint32_t)most);
+        if (lane == LEOAM_WAVE - 1) {
+            sh_sum[wave] = incl;
+            sh_most[wave] = most;
+        }
+        __syncthreads();
+        long long total = 0, before = incl - mine;
+#pragma unroll
+        for (int w = 0; w < kAttWaves; ++w) {
+            if (w < wave) before += sh_sum[w];
+            total += sh_sum[w];
+            most = max(most, sh_most[w]);
+        }
+        whole_rows = uniform(most) <= uncut_tiles(rows, k32);
+        if (!whole_rows) {
+            share = (total + a.sharers - 1) / a.sharers;
+            pos = share * blockIdx.x;
+            end = min(total, pos + share);
+            if ((int)blockIdx.x >= a.sharers || pos >= end) return;
+            if (pos >= before && pos < before + mine) {
+                int e = e0;
+                for (;;) {
+                    const int tokens = entry_tokens(e);
+                    const long long n = (long long)weight * tiles_of(tokens);
+                    sh_tokens = tokens;
+                    if (pos < before + n) break;
+                    before += n;
+                    ++e;
+                }
+                sh_entry = e;
+                sh_at = pos - before;
+            }
+            __syncthreads();
+            const int e = uniform(sh_entry);
+            const long long at = sh_at;
+            next_tokens = sh_tokens;
+            if (a.sel_idx) {
+                b = e / hkv;
+                h = e % hkv;
+                off = uniform((int)at);
+            } else {
+                const int n = tiles_of(uniform(next_tokens));
+                b = e;
+                h = uniform((int)(at / n));
+                off = uniform((int)(at - (long long)h * n));
+            }
+        }
+    }
+    if (whole_rows) {
+        if ((int)blockIdx.x >= rows) return;
+        b = blockIdx.x / hkv;
+        h = blockIdx.x % hkv;
+        next_tokens = walk_of(a, b, h);
+        end = tiles_of(next_tokens);
     }
 
     bool first_piece = true;
-    int next_tokens = sh_tokens;
     while (pos < end) {
         const int tokens = uniform(next_tokens), n_tiles = tiles_of(tokens);
         const int take = uniform((int)min((long long)(n_tiles - off), end - pos));
         const size_t bh = (size_t)b * hkv + h;
         {
             const int nh = h + 1 < hkv ? h + 1 : 0, nb = h + 1 < hkv ? b : b + 1;
-            if (pos + take < end) next_tokens = walk_of(a, nb, nh);      // (there is a further row)
+            if (pos + take < end) next_tokens = walk_of(a, nb, nh);      // (the share has a further row)
         }
         const int len = a.sel_idx ? min(max(a.seq_len[b], 0), a.max_pages << a.page_shift) : tokens;
         const int32_t* sel = a.sel_idx ? a.sel_idx + bh * (size_t)a.k_max : nullptr;
@@ -404,7 +436,7 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
                 a.partial[(slot * G + g) * kPartStride + d] = d < LEOAM_D ? v : d == LEOAM_D ? m : l;
             }
         }
-        if (off == 0 && tid == 0) {
+        if (a.pieces && off == 0 && tid == 0) {
             RowPieces rp = {0, 0};
             if (!whole) {
                 rp.count = (int)((pos + n_tiles - 1) / share - blockIdx.x) + 1;
@@ -412,6 +444,7 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
             }
             a.pieces[bh] = rp;
         }
+        if (whole_rows) break;
         first_piece = false;
         pos += take;
         off = 0;
@@ -516,7 +549,7 @@ template <typename T, typename S> static hipError_t launch_decode(const PageDeco
     default: hipLaunchKernelGGL((page_decode_kernel<T, S, 8>), grid, block, 0, stream, a); break;
     }
     hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
+    if (e != hipSuccess || !a.pieces) return e;
     const int n_heads = a.batch * a.n_kv_heads * group;
     if (a.batch * a.n_kv_heads >= kManyRows)
         hipLaunchKernelGGL(page_decode_merge_kernel<1>, dim3((n_heads + kMergeGroups - 1) / kMergeGroups), dim3(kMergeGroups * LEOAM_D), 0,
@@ -542,8 +575,16 @@ hipError_t page_decode_dispatch(const leoam_pages* s, const void* q, const void*
     a.batch = s->batch; a.n_kv_heads = s->n_kv_heads; a.n_pages = s->n_pages;
     a.page_shift = __builtin_ctz((unsigned)s->page_size); a.max_pages = s->max_pages;
     const int group = s->n_q_heads / s->n_kv_heads;
+    const int rows = s->batch * s->n_kv_heads;
     const size_t fit = (workspace_bytes - directory_bytes(s)) / piece_bytes(s);
-    const int n_groups = (int)(fit < (size_t)kDecodeGroups ? fit : (size_t)kDecodeGroups);
+    a.sharers = (int)(fit < (size_t)kDecodeGroups ? fit : (size_t)kDecodeGroups);
+    int n_groups = rows > a.sharers ? rows : a.sharers;      // the kernel may take a row to a workgroup, or leave the rest idle
+    // Where even a full table's row is not long, neither the search for shares nor the second kernel are needed.
+    const long long most = (long long)(sel_idx ? k_max : s->max_pages) * s->page_size;
+    if (most <= (long long)uncut_tiles(rows, s->q_dtype == LEOAM_F32) * kTileTokens) {
+        a.pieces = nullptr;
+        n_groups = rows;
+    }
     const bool k8 = s->kv_dtype == LEOAM_E4M3;
     switch (s->q_dtype) {
     case LEOAM_F32: return launch_decode<F32, F32>(a, group, n_groups, stream);

@@ -54,8 +54,8 @@ __device__ __forceinline__ uint2 transposed(const char* at) {
 enum : int { kMfma = 0x8, kValu = 0x2, kTrans = 0x400, kLdsRead = 0x100 };
 template <int KIND, int N> __device__ __forceinline__ void then() { __builtin_amdgcn_sched_group_barrier(KIND, N, 0); }
 
-// the rows of slot `slot`: sequence, its first row in the call, its number of rows, which tile of them
-struct Unit { int b, row0, m, local; };
+// the rows of a slot: sequence, its first row in the call, its number of rows, which tile of them, the sequence's length
+struct Unit { int b, row0, m, local, len; };
 __device__ __forceinline__ int first_slot_of(int row0, int i, int group) { return (int)((long long)row0 * group / kRows) + i; }
 
 template <typename T> __device__ __forceinline__ f32x16_t mfma_32x32x16(const uint4& a, const uint4& b, f32x16_t c);
@@ -123,8 +123,7 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
     // tiles [j0, j1) of a unit; j1 < 0: all.  slot: where to leave a piece, < 0: the result is final
     auto run = [&](const Unit& unit, int h, int j0, int j1, int piece_slot) {
     const int b = unit.b, row0 = unit.row0, m = unit.m, local = unit.local;
-    const int len = min(max(uniform(a.seq_len[b]), 0), a.max_pages << a.page_shift);
-    const int first = len - m;                                   // position of the sequence's first new token (may be negative)
+    const int first = unit.len - m;                                   // position of the sequence's first new token (may be negative)
     const int tok0 = local * (kRows / G), n_tok = min(m - tok0, kRows / G);
     const int keys = max(first + tok0 + n_tok, 0);               // keys that some row of the workgroup sees
     // this lane's row
@@ -136,15 +135,6 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
     const int wave_lo = first + tok0 + 32 * wave / G;             // the wave's rows see at least / at most
     const int wave_hi = min(first + tok0 + (32 * wave + 31) / G, first + m - 1);
 
-    uint4 qb[NQ];
-#pragma unroll
-    for (int s = 0; s < NQ; ++s) {
-        qb[s] = load16(a.q, q_row * ROWB + 32 * s + 16 * half);
-        qb[s].x ^= a.flip; qb[s].y ^= a.flip; qb[s].z ^= a.flip; qb[s].w ^= a.flip;
-    }
-    if (tid == 0) sh_bad = 0;
-    __syncthreads();
-
     const int n_tiles = (keys + KEYS - 1) / KEYS, last = keys - 1;
     const int first_masked = max(first + tok0 + 1, 0) / KEYS;     // tiles from here on hide keys from some row
     const int32_t* table = a.page_table + (size_t)b * a.max_pages;
@@ -152,6 +142,19 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
     const uint32_t head_bytes = (uint32_t)SROWB << a.page_shift, page_bytes = head_bytes * (uint32_t)hkv, in_page = (1u << a.page_shift) - 1;
     const char *kh = a.k_pages + (size_t)h * head_bytes, *vh = a.v_pages + (size_t)h * head_bytes;
     auto pages_of = [&](int j) { return table[min(j * KEYS + 16 * (lane % GROUPS), last) >> a.page_shift]; };
+    const int id0 = n_tiles > 0 ? pages_of(min(j0, n_tiles - 1)) : 0;
+    uint4 qb[NQ];
+#pragma unroll
+    for (int s = 0; s < NQ; ++s) qb[s] = load16(a.q, q_row * ROWB + 32 * s + 16 * half);
+    if (a.flip) {
+#pragma unroll
+        for (int s = 0; s < NQ; ++s) {
+            qb[s].x ^= a.flip; qb[s].y ^= a.flip; qb[s].z ^= a.flip; qb[s].w ^= a.flip;
+        }
+    }
+    if (tid == 0) sh_bad = 0;
+    __syncthreads();
+
     uint4 kr[LOADS], vr[LOADS];
     float ks[LOADS], vs[LOADS];
     uint32_t ok_next = 0;      // bit g: group g of the tile in registers has a page
@@ -335,7 +338,7 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
 
     const int j_end = j1 < 0 ? n_tiles : min(j1, n_tiles);
     if (j0 < j_end) {
-        fetch(j0, pages_of(j0));
+        fetch(j0, id0);
         int next = pages_of(min(j0 + 1, n_tiles - 1));
         stage(j0, j0 & 1);
         uint32_t ok = ok_next;
@@ -415,7 +418,7 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
         const int h = blockIdx.x % hkv;
         // (later rows see more keys: they are started first)
         const int slot = a.n_slots - 1 - (int)(blockIdx.x / hkv);
-        Unit u = {slot, slot, 1, 0};
+        Unit u = {slot, slot, 1, 0, 0};
         if (a.new_off) {
             u.b = uniform(wave_count_below(a.batch, slot, [&](int i) { return first_slot_of(a.new_off[i], i, G); }));
             if (u.b >= a.batch) return;
@@ -425,6 +428,7 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
             if (u.row0 < 0 || u.m < 0 || u.m > a.n_new - u.row0) return;
         }
         if (u.local < 0 || (long long)u.local * kRows >= (long long)u.m * G) return;
+        u.len = min(max(uniform(a.seq_len[u.b]), 0), a.max_pages << a.page_shift);
         run(u, h, 0, -1, -1);
     } else {
         // ---- this workgroup's share (at most kMostSlots slots, and no more sequences than slots) -------------
@@ -432,13 +436,13 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
         __shared__ int sh_most;
         for (int i = tid; i <= a.batch; i += kAttThreads) {
             sh_off[i] = a.new_off ? a.new_off[i] : i;
-            if (i < a.batch) sh_len[i] = a.seq_len[i];
+            if (i < a.batch) sh_len[i] = min(max(a.seq_len[i], 0), a.max_pages << a.page_shift);
         }
         if (tid == 0) sh_most = 0;
         __syncthreads();
         auto unit_of = [&](int slot) {
             Unit u;
-            if (!a.new_off) return Unit{slot, slot, 1, 0};
+            if (!a.new_off) return Unit{slot, slot, 1, 0, sh_len[slot]};
             int lo = 0, hi = a.batch;      // the last sequence whose slots begin at or before this one
             while (hi - lo > 1) {
                 const int mid = (lo + hi) >> 1;
@@ -447,6 +451,7 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
             }
             u.b = lo;
             u.row0 = sh_off[lo];
+            u.len = sh_len[lo];
             u.m = sh_off[lo + 1] - u.row0;
             u.local = slot - first_slot_of(u.row0, lo, G);
             if (u.row0 < 0 || u.m < 0 || u.m > a.n_new - u.row0 || u.local < 0 || (long long)u.local * kRows >= (long long)u.m * G) u.m = 0;
@@ -456,7 +461,7 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
             const Unit u = unit_of(slot);
             int tiles = 0;
             if (u.m > 0) {
-                const int first = min(max(sh_len[u.b], 0), a.max_pages << a.page_shift) - u.m, tok0 = u.local * (kRows / G);
+                const int first = u.len - u.m, tok0 = u.local * (kRows / G);
                 tiles = max(1, (max(first + tok0 + min(u.m - tok0, kRows / G), 0) + KEYS - 1) / KEYS);
                 atomicMax(&sh_most, tiles);
             } else if (blockIdx.x == 0) {
@@ -513,7 +518,7 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
         while (pos < end) {
             const int n = uniform(sh_tiles[slot]), take = min(n - off, end - pos);
             Unit u = unit_of(slot);
-            u = Unit{uniform(u.b), uniform(u.row0), uniform(u.m), uniform(u.local)};
+            u = Unit{uniform(u.b), uniform(u.row0), uniform(u.m), uniform(u.local), uniform(u.len)};
             const int id = slot * hkv + h;
             const bool whole = take == n;
             const int piece_slot = 2 * (int)blockIdx.x + (first_piece ? 0 : 1);      // opens the share, or closes it
@@ -546,15 +551,18 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
     }
 }
 
-// 128 rows and 8 channels of a unit: its pieces, in order
+// 8 channels of a unit's rows: its pieces, in order.  Where rows are few, two or four groups of threads share the pieces.
 template <typename T>
 __global__ __launch_bounds__(256) void page_prefill_merge_kernel(PagePrefillArgs a, int group) {
+    __shared__ float sh[6][2 * kRows];      // states: m, l, 4 sums
     const UnitPieces up = a.pieces[blockIdx.x];
-    const int row = threadIdx.x % kRows, d4 = 2 * blockIdx.y + threadIdx.x / kRows;
-    if (up.count == 0 || row >= up.rows) return;
+    if (up.count == 0) return;
+    const int parts = up.rows <= kRows / 4 ? 4 : up.rows <= kRows / 2 ? 2 : 1, n_rows = kRows / parts;
+    const int t = threadIdx.x % kRows, row = t % n_rows, part = t / n_rows, d4 = 2 * blockIdx.y + threadIdx.x / kRows;
+    const int rc = min(row, up.rows - 1);
     constexpr int kBatch = 8;      // pieces that are on their way together
     float m = -INFINITY, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int i0 = 0; i0 < up.count; i0 += kBatch) {
+    for (int i0 = part * kBatch; i0 < up.count; i0 += parts * kBatch) {
         float ms[kBatch], ls[kBatch];
         uint4 x4[kBatch];
 #pragma unroll
@@ -562,9 +570,9 @@ __global__ __launch_bounds__(256) void page_prefill_merge_kernel(PagePrefillArgs
             const int i = min(i0 + u, up.count - 1);
             // (each further piece opens the next workgroup's share)
             const float* piece = a.partial + (size_t)(i == 0 ? up.first_slot : 2 * (up.first_slot / 2 + i)) * kPieceFloats;
-            ms[u] = piece[kRows * LEOAM_D + row];
-            ls[u] = piece[kRows * (LEOAM_D + 1) + row];
-            x4[u] = load16(piece, ((size_t)d4 * kRows + row) * 16);
+            ms[u] = piece[kRows * LEOAM_D + rc];
+            ls[u] = piece[kRows * (LEOAM_D + 1) + rc];
+            x4[u] = load16(piece, ((size_t)d4 * kRows + rc) * 16);
         }
         float now = m;
 #pragma unroll
@@ -588,6 +596,26 @@ __global__ __launch_bounds__(256) void page_prefill_merge_kernel(PagePrefillArgs
             for (int e = 0; e < 4; ++e) o[e] += w * x[e];
         }
     }
+    if (parts > 1) {
+        sh[0][threadIdx.x] = m;
+        sh[1][threadIdx.x] = l;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sh[2 + e][threadIdx.x] = o[e];
+        __syncthreads();
+        if (part) return;
+        for (int p = 1; p < parts; ++p) m = fmaxf(m, sh[0][threadIdx.x + p * n_rows]);
+        l = 0.f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] = 0.f;
+        for (int p = 0; p < parts; ++p) {
+            const int i = threadIdx.x + p * n_rows;
+            const float w = exp2_or_zero(sh[0][i], m);
+            l += w * sh[1][i];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] += w * sh[2 + e][i];
+        }
+    }
+    if (row >= up.rows) return;
     const float inv = l == 0.f ? 0.f : 1.f / l;
     const int h = blockIdx.x % a.n_kv_heads;
     const size_t q_row = ((size_t)(up.token0 + row / group) * a.n_kv_heads + h) * group + row % group;
@@ -666,7 +694,10 @@ hipError_t page_prefill_dispatch(const leoam_pages* s, const void* q, int n_new,
     a.pieces = (UnitPieces*)workspace;
     a.partial = nullptr;
     const long long most_tiles = (((long long)s->max_pages * s->page_size + 31) / 32) * units;      // 32-bit sums
-    if (units <= kMostUnits && slots <= kMostSlots && most_tiles < (1ll << 30)) {
+    // (nor if no sequence can have so many tiles that it would be cut)
+    const int tile_keys = s->q_dtype == LEOAM_F32 ? 32 : 64, uncut = s->q_dtype == LEOAM_F32 ? kUncutTiles<F32> : kUncutTiles<BF16>;
+    const bool cut = (long long)s->max_pages * s->page_size > (long long)uncut * tile_keys;
+    if (cut && units <= kMostUnits && slots <= kMostSlots && most_tiles < (1ll << 30)) {
         const size_t dir = prefill_directory_bytes(units), piece = kPieceFloats * sizeof(float);
         const long long fit = workspace_bytes > dir ? (long long)((workspace_bytes - dir) / (2 * piece)) : 0;
         if (fit >= (units < kSharers / 2 ? units : kSharers / 2)) sharers = (int)(fit < kSharers ? fit : kSharers);

@@ -353,6 +353,28 @@ def test_decode_rows_in_pieces(L, dtype, q8, hkv, lengths):
         assert torch.equal(first[1], again[1]) and torch.equal(first[2], again[2])
 
 
+def widened(made, columns):
+    """The same pages behind a table with room for more."""
+    table = torch.full((made.table.shape[0], columns), -1, dtype=torch.int32)
+    table[:, : made.table.shape[1]] = made.table
+    made.table = table
+    return made
+
+
+@pytest.mark.parametrize("dtype,q8", KINDS, ids=KIND_IDS)
+def test_decode_short_rows_behind_a_wide_table(L, dtype, q8):
+    # short rows are not cut; whether they are short shows only on the device
+    run_decode(L, widened(Made(dtype, q8, [100, 0, 500, 128, 1, 129], 2, 16, seed=41), 700), 8)
+    run_decode(L, widened(Made(dtype, q8, [2000, 33] + [100] * 6, 16, 64, seed=42), 300), 32)
+
+
+@pytest.mark.parametrize("dtype,q8", [(F32, False), (BF16, False), (F16, True)], ids=["f32", "bf16", "f16-e4m3"])
+@pytest.mark.parametrize("longest", [120, 6000])
+def test_decode_more_rows_than_shares(L, dtype, q8, longest):
+    lengths = [longest] + [0, 1, 17, 40] * 16
+    run_decode(L, widened(Made(dtype, q8, lengths, 8, 16, seed=43), 400), 8)
+
+
 @pytest.mark.parametrize("dtype,q8", [(F32, False), (F16, True), (BF16, False)], ids=["f32", "f16-e4m3", "bf16"])
 def test_decode_small_workspaces(L, dtype, q8):
     made = Made(dtype, q8, [900, 0, 3, 1500], 2, 32, seed=5)
