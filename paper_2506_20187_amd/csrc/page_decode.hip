@@ -6,7 +6,7 @@
 // whose results are final, and at most two pieces of rows, which leave (acc[128], m, l) per head in the
 // workspace; a second small kernel folds a row's pieces in order, so results do not depend on scheduling.
 //
-// Where rows are short (uncut_tiles) a workgroup takes a row instead, and nothing is cut.
+// Where rows are short (uncut_row_tiles) a workgroup takes a row instead, and nothing is cut.
 //
 // Everything runs on the matrix cores without passing through LDS.  S^T = K Q^T: lane = token takes the 16-byte
 // loads of its key row as they are.  The result has lane = query head, registers = tokens, which is what the second
@@ -51,7 +51,7 @@ struct TileAt {
 // lengths spread from 1 to the given, 8 bits / bf16: 160 rows to 1900 tokens 24 / 29 : 22 / 23, to 4000 33 / 43 : 39 / 51; 512 rows
 // to 900 34 / 40 : 20 / 28, to 4000 75 / 118 : 70 / 117, to 9000 121 / 216 : 148 / 260; 8 rows to 900 10.9 : 13.3.  fp32 takes
 // longer per tile: 64 rows to 400 13.4 : 14.9.)
-__host__ __device__ __forceinline__ int uncut_tiles(int rows, bool k32) { return k32 ? min(max(rows / 32, 1), 32) : min(max(rows / 8, 4), 32); }
+__host__ __device__ __forceinline__ int uncut_row_tiles(int rows, bool k32) { return k32 ? min(max(rows / 32, 1), 32) : min(max(rows / 8, 4), 32); }
 
 struct PageDecodeArgs {
     const char *q, *k_pages, *v_pages;
@@ -125,7 +125,7 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
             total += sh_sum[w];
             most = max(most, sh_most[w]);
         }
-        whole_rows = uniform(most) <= uncut_tiles(rows, k32);
+        whole_rows = uniform(most) <= uncut_row_tiles(rows, k32);
         if (!whole_rows) {
             share = (total + a.sharers - 1) / a.sharers;
             pos = share * blockIdx.x;
@@ -581,7 +581,7 @@ hipError_t page_decode_dispatch(const leoam_pages* s, const void* q, const void*
     int n_groups = rows > a.sharers ? rows : a.sharers;      // the kernel may take a row to a workgroup, or leave the rest idle
     // Where even a full table's row is not long, neither the search for shares nor the second kernel are needed.
     const long long most = (long long)(sel_idx ? k_max : s->max_pages) * s->page_size;
-    if (most <= (long long)uncut_tiles(rows, s->q_dtype == LEOAM_F32) * kTileTokens) {
+    if (most <= (long long)uncut_row_tiles(rows, s->q_dtype == LEOAM_F32) * kTileTokens) {
         a.pieces = nullptr;
         n_groups = rows;
     }

@@ -41,7 +41,10 @@ struct UnitPieces { int32_t count, first_slot, token0, rows; };
 constexpr int kSharers = 512;         // workgroups that share the tiles: two fill a compute unit
 constexpr int kMostUnits = 1024;      // more units than this are not shared out: two rounds of workgroups or more
 constexpr int kMostSlots = 256;       // of as many slots: their tables stay in LDS
-template <typename T> constexpr int kUncutTiles = T::kTag == LEOAM_F32 ? 1 : 8;      // if no unit has more tiles, none is cut
+// If no unit has more tiles than this, none is cut: a cut costs a second start, a piece and a fold.  (32 rows behind a context in
+// bf16, us, shares against whole units: 8 units of 11 tiles 15 : 22; 64 of 11 20 : 22, of 24 26 : 41; 256 of 11 40 : 28, of 24 62 : 47,
+// of 46 72 : 92; 512 of 11 70 : 36, of 46 129 : 110, of 94 214 : 217.  A tile of fp32 takes four times as long.)
+__host__ __device__ __forceinline__ int uncut_unit_tiles(int units, bool k32) { return k32 ? min(max(units / 40, 1), 16) : min(max(units / 10, 6), 64); }
 // a piece: [32 groups of 4 channels][128 rows][4], maxima, sums
 constexpr int kPieceFloats = kRows * (LEOAM_D + 2);
 
@@ -482,7 +485,7 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
         }
         __syncthreads();
         const int total = uniform(sh_before[a.n_slots]), W = gridDim.x;
-        const bool uncut = uniform(sh_most) <= kUncutTiles<T>;      // then workgroup w takes units w, w + W, ...
+        const bool uncut = uniform(sh_most) <= uncut_unit_tiles(a.n_slots * hkv, k32);      // then workgroup w takes units w, w + W, ...
         const int share = uncut ? 0 : (total + W - 1) / W;
         int slot = 0, h = 0, off = 0, pos = 0, end = 0;
         int next = blockIdx.x;
@@ -695,9 +698,10 @@ hipError_t page_prefill_dispatch(const leoam_pages* s, const void* q, int n_new,
     a.partial = nullptr;
     const long long most_tiles = (((long long)s->max_pages * s->page_size + 31) / 32) * units;      // 32-bit sums
     // (nor if no sequence can have so many tiles that it would be cut)
-    const int tile_keys = s->q_dtype == LEOAM_F32 ? 32 : 64, uncut = s->q_dtype == LEOAM_F32 ? kUncutTiles<F32> : kUncutTiles<BF16>;
-    const bool cut = (long long)s->max_pages * s->page_size > (long long)uncut * tile_keys;
-    if (cut && units <= kMostUnits && slots <= kMostSlots && most_tiles < (1ll << 30)) {
+    const bool k32 = s->q_dtype == LEOAM_F32;
+    const long long capacity = (long long)s->max_pages * s->page_size;
+    const bool cut = units <= kMostUnits && capacity > (long long)uncut_unit_tiles((int)units, k32) * (k32 ? 32 : 64);
+    if (cut && slots <= kMostSlots && most_tiles < (1ll << 30)) {
         const size_t dir = prefill_directory_bytes(units), piece = kPieceFloats * sizeof(float);
         const long long fit = workspace_bytes > dir ? (long long)((workspace_bytes - dir) / (2 * piece)) : 0;
         if (fit >= (units < kSharers / 2 ? units : kSharers / 2)) sharers = (int)(fit < kSharers ? fit : kSharers);
