@@ -482,11 +482,12 @@ typedef struct {
  * every pair (x_a, x_b) of rotated channels of q and k becomes
  *     (x_a c_i - x_b s_i,  x_b c_i + x_a s_i),
  * products and sums single binary32 operations.  q_out[r] (contiguous [n_new, Hq, 128], may be q itself if q is contiguous)
- * receives the rotated query, rounded once; q and q_out may both be NULL.  n_new == 0: nothing is done.  Keys (rotated) and values go to their places in the
- * pages, rounded once.
+ * receives the rotated query, rounded once; q and q_out may both be NULL.  Keys (rotated) and values go to their places
+ * in the pages, rounded once.  n_new == 0: nothing is done.
  * LEOAM_E4M3: scale = the smallest power of two s with |x| <= 448 s for all finite x that the page holds so far (0 for
  * none but zeros; it never falls while a page fills up; a page's first token starts it anew), code = round-half-even(x /
- * scale); infinities are stored as +-448 scale, NaN as NaN.  When a new token raises a page's scale, its older codes are
+ * scale); infinities are stored as +-448 scale, NaN as NaN (and under fp16, where the scale ends at 2^7, what lies beyond
+ * 57344 as 57344).  When a new token raises a page's scale, its older codes are
  * encoded again from their stored values (exact but for codes that become subnormal).
  * Every page that takes a token must belong to one sequence only.  For each of them
  *   abstract   [batch, n_kv_heads, max_pages, 2, 128] q_dtype (nullable): the page's rows become the maximum / minimum of
