@@ -64,9 +64,17 @@ class PagedLayer:
         return torch.empty(max(16, B.leoam_page_workspace_bytes(self.pages, n_new)), dtype=torch.uint8,
                            device=self.page_table.device)
 
+    @staticmethod
+    def _new(like, stream) -> torch.Tensor:
+        """Contiguous, of the stream's own memory: freed before its kernels have run, it is given to later ones of that stream only."""
+        if stream is not None and not isinstance(stream, torch.cuda.Stream):
+            stream = torch.cuda.ExternalStream(int(getattr(stream, "cuda_stream", stream)), device=like.device)
+        with torch.cuda.stream(stream):      # (None: as it is)
+            return torch.empty(like.shape, dtype=like.dtype, device=like.device)
+
     def append(self, q, k, v, new_off=None, q_out=None, stream=None) -> torch.Tensor:
         if q_out is None:
-            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            q_out = self._new(q, stream)
         B.kv_page_append(self.pages, q, k, v, new_off, self.seq_len, self.page_table, self.rope, q_out, self.k_pages,
                          self.v_pages, self.k_scale, self.v_scale, self.abstract, self.chunk_off, self.n_chunks, self.status,
                          stream)
@@ -91,7 +99,7 @@ class PagedLayer:
     def prompt(self, q, k, v, new_off, out=None, lse=None, q_out=None, stream=None) -> torch.Tensor:
         """Sequence b's new tokens are rows new_off[b] .. new_off[b + 1]; out [n, Hq, 128] in q's type."""
         q_out = self.append(q, k, v, new_off, q_out, stream)
-        out = torch.empty_like(q_out) if out is None else out
+        out = self._new(q_out, stream) if out is None else out
         need = B.leoam_page_workspace_bytes(self.pages, q_out.shape[0])
         if not self.prompt_workspaces or self.prompt_workspaces[-1].numel() < need:
             self.prompt_workspaces.append(self._scratch(q_out.shape[0]))

@@ -833,3 +833,39 @@ def test_another_stream(L):
         torch.cuda.synchronize()
         outs.append(out)
     assert torch.equal(*outs)
+
+
+@pytest.mark.parametrize("as_handle", [False, True], ids=["stream", "handle"])
+def test_layer_on_another_stream_keeps_its_temporaries(L, as_handle):
+    """The rotated queries of a step are freed while its kernels wait: whoever allocates next must not get them."""
+    g = torch.Generator().manual_seed(61)
+    B, hq, hkv, page = 4, 32, 8, 64
+    table, n_pages = spread([200] * B, page, g)
+    seq_len = torch.tensor([100, 7, 64, 130], dtype=torch.int32).cuda()
+    off = torch.tensor([0, 100, 107, 171, 301], dtype=torch.int32).cuda()
+    prompt = torch.randn(301, hq + 2 * hkv, 128, generator=g).to(BF16).cuda()
+    token = torch.randn(B, hq + 2 * hkv, 128, generator=g).to(BF16).cuda()
+    parts = lambda x: (x[:, :hq], x[:, hq: hq + hkv], x[:, hq + hkv:])
+    want = got = None
+    for other in (False, True):
+        layer = L.PagedLayer(table.cuda(), seq_len.clone(), hq, hkv, n_pages, page, BF16)
+        stream = torch.cuda.Stream() if other else None
+        torch.cuda.synchronize()
+        if other:
+            with torch.cuda.stream(stream):
+                torch.cuda._sleep(20_000_000)      # (some 10 ms)
+        handle = stream.cuda_stream if other and as_handle else stream
+        a = layer.prompt(*parts(prompt), off, stream=handle)
+        fill = [torch.full((301, hq, 128), math.nan, dtype=BF16, device="cuda") for _ in range(4)] if other else []
+        torch.cuda.synchronize()
+        layer.seq_len.add_(1)
+        torch.cuda.synchronize()
+        if other:
+            with torch.cuda.stream(stream):
+                torch.cuda._sleep(20_000_000)
+        b = layer.step(*parts(token), stream=handle)
+        fill += [torch.full((B, hq, 128), math.nan, dtype=BF16, device="cuda") for _ in range(4)] if other else []
+        torch.cuda.synchronize()
+        want, got = got, (a, b.clone())
+        assert all(torch.isnan(f).all() for f in fill)      # (nor may the step's kernels write to what others were given)
+    assert torch.equal(want[0], got[0]) and torch.equal(want[1], got[1])
