@@ -56,25 +56,21 @@ class PagedLayer:
             self.score = torch.empty(batch, n_kv_heads, max_pages, dtype=torch.float32, device=dev)
             self.sel_idx = torch.empty(batch, n_kv_heads, k_max, dtype=torch.int32, device=dev)
             self.sel_count = torch.empty(batch, n_kv_heads, dtype=torch.int32, device=dev)
-        self.workspace = self._scratch(0)
+        self.workspace = self._new(B.leoam_page_workspace_bytes(self.pages, 0), torch.uint8, None)
         self.prompt_workspaces = []      # the last is the largest; earlier ones stay, a captured graph may use them
         self.scale = B.default_scale(head_dim)
 
-    def _scratch(self, n_new: int) -> torch.Tensor:
-        return torch.empty(max(16, B.leoam_page_workspace_bytes(self.pages, n_new)), dtype=torch.uint8,
-                           device=self.page_table.device)
-
-    @staticmethod
-    def _new(like, stream) -> torch.Tensor:
-        """Contiguous, of the stream's own memory: freed before its kernels have run, it is given to later ones of that stream only."""
+    def _new(self, shape, dtype, stream) -> torch.Tensor:
+        """Of the stream's own memory: freed before its kernels have run, it is given to later ones of that stream only."""
+        device = self.page_table.device
         if stream is not None and not isinstance(stream, torch.cuda.Stream):
-            stream = torch.cuda.ExternalStream(int(getattr(stream, "cuda_stream", stream)), device=like.device)
+            stream = torch.cuda.ExternalStream(int(getattr(stream, "cuda_stream", stream)), device=device)
         with torch.cuda.stream(stream):      # (None: as it is)
-            return torch.empty(like.shape, dtype=like.dtype, device=like.device)
+            return torch.empty(shape, dtype=dtype, device=device)
 
     def append(self, q, k, v, new_off=None, q_out=None, stream=None) -> torch.Tensor:
         if q_out is None:
-            q_out = self._new(q, stream)
+            q_out = self._new(q.shape, q.dtype, stream)
         B.kv_page_append(self.pages, q, k, v, new_off, self.seq_len, self.page_table, self.rope, q_out, self.k_pages,
                          self.v_pages, self.k_scale, self.v_scale, self.abstract, self.chunk_off, self.n_chunks, self.status,
                          stream)
@@ -99,10 +95,11 @@ class PagedLayer:
     def prompt(self, q, k, v, new_off, out=None, lse=None, q_out=None, stream=None) -> torch.Tensor:
         """Sequence b's new tokens are rows new_off[b] .. new_off[b + 1]; out [n, Hq, 128] in q's type."""
         q_out = self.append(q, k, v, new_off, q_out, stream)
-        out = self._new(q_out, stream) if out is None else out
+        out = self._new(q_out.shape, q_out.dtype, stream) if out is None else out
         need = B.leoam_page_workspace_bytes(self.pages, q_out.shape[0])
         if not self.prompt_workspaces or self.prompt_workspaces[-1].numel() < need:
-            self.prompt_workspaces.append(self._scratch(q_out.shape[0]))
+            # (a longer prompt needs a few bytes more: whole MiB, so that such steps do not pile up)
+            self.prompt_workspaces.append(self._new(-(-need >> 20) << 20, torch.uint8, stream))
         B.page_attention_prefill(self.pages, q_out, new_off, self.k_pages, self.v_pages, self.k_scale, self.v_scale,
                                  self.page_table, self.seq_len, self.scale, out, lse, self.prompt_workspaces[-1], stream)
         return out

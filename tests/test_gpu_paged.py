@@ -7,7 +7,7 @@ Tolerances.  Appending is compared bit for bit (its definition is in binary32 op
 A = max_t scale * sum_d |q_d K_td|:  a logit is a sum of 128 products in 32 bits and is scaled twice, each step off by at
 most 2^-24 relative to the magnitudes summed, so it is within 140 * 2^-24 A < 2^-16 A =: dz (running sums in other
 orders included), which moves a weight by a factor e^dz, numerator and denominator alike: 2 dz together.  Weights enter
-P V in two 16-bit pieces (decode: off by at most 2^-16) or one (prefill: 2^-8 for bf16, 2^-11 for fp16, 0 for fp32).
+P V in 16-bit pieces (decode, two or three: off by at most 2^-16) or one (prefill: 2^-8 for bf16, 2^-11 for fp16, 0 for fp32).
 A sum of n terms in 32 bits is off by at most n 2^-24 of the magnitudes; exp2 and log2 by a few 2^-23.  The output is
 within max|V| times all that; prefill rounds it once more."""
 import math
@@ -566,6 +566,21 @@ def test_prefill_many_units(L, dtype, q8):
         run_prefill(L, made, 64, lengths[:n], rows=set(range(0, sum(lengths[:n]), 61)))
 
 
+@pytest.mark.parametrize("dtype,q8", [(F32, False), (BF16, False), (F16, True)], ids=["f32", "bf16", "f16-e4m3"])
+def test_prefill_small_workspaces(L, dtype, q8):
+    # too small to share the tiles, for about as many workgroups as there are units, for more
+    some = set(range(0, 345, 23)) | {299, 300, 344}
+    made = Made(dtype, q8, [900, 40, 300], 8, 32, seed=63)
+    most = L.leoam_page_workspace_bytes(made.pages(L, 32), 345)
+    for eighths in (1, 2, 5):
+        run_prefill(L, made, 32, [300, 40, 5], rows=some, workspace_bytes=most * eighths // 8 // 16 * 16)
+    # units of few tiles, more than the workgroups that a part of the workspace is enough for
+    made = widened(Made(dtype, q8, [320, 200, 60], 32, 16, seed=64), 200)
+    most = L.leoam_page_workspace_bytes(made.pages(L, 128), 345)
+    for eighths in (5, 8):
+        run_prefill(L, made, 128, [300, 40, 5], rows=some, workspace_bytes=most * eighths // 8 // 16 * 16)
+
+
 def test_prefill_one_row_each(L):
     made = Made(BF16, True, [1, 300, 0, 17], 2, 16, seed=9)
     g = torch.Generator().manual_seed(2)
@@ -869,3 +884,17 @@ def test_layer_on_another_stream_keeps_its_temporaries(L, as_handle):
         want, got = got, (a, b.clone())
         assert all(torch.isnan(f).all() for f in fill)      # (nor may the step's kernels write to what others were given)
     assert torch.equal(want[0], got[0]) and torch.equal(want[1], got[1])
+
+
+def test_layer_prompts_that_grow_share_a_workspace(L):
+    g = torch.Generator().manual_seed(62)
+    hq, hkv, page, lengths = 32, 8, 64, list(range(8, 2400, 230))
+    table, n_pages = spread([lengths[-1]], page, g)
+    seq_len = torch.zeros(1, dtype=torch.int32).cuda()
+    layer = L.PagedLayer(table.cuda(), seq_len, hq, hkv, n_pages, page, BF16)
+    x = torch.randn(lengths[-1], hq + 2 * hkv, 128, generator=g).to(BF16).cuda()
+    parts = lambda n: (x[:n, :hq], x[:n, hq: hq + hkv], x[:n, hq + hkv:])
+    for n in lengths:
+        seq_len.fill_(n)
+        layer.prompt(*parts(n), torch.tensor([0, n], dtype=torch.int32).cuda())
+    assert sum(w.numel() for w in layer.prompt_workspaces) <= 2 * 72 << 20
