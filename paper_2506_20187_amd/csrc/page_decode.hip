@@ -1,8 +1,8 @@
 // page_attention_decode: softmax(scale q K^T) V of one token per sequence over its pages, all of them or the kept ones.
 //
 // HBM-bound: every stored key and value is read once.  The work of a call is the tokens of all (sequence, kv head)
-// rows laid end to end in tiles; every workgroup takes an equal, contiguous share of the tiles, whatever the lengths
-// are (the host does not know them), and its four waves take a quarter of each stretch.  A share covers whole rows,
+// rows laid end to end in tiles; every workgroup takes an equal, contiguous share of the tiles (and of the rows' beginnings,
+// kRowStart), whatever the lengths are (the host does not know them), and its four waves take a quarter of each stretch.  A share covers whole rows,
 // whose results are final, and at most two pieces of rows, which leave (acc[128], m, l) per head in the
 // workspace; a second small kernel folds a row's pieces in order, so results do not depend on scheduling.
 //
@@ -46,12 +46,17 @@ struct TileAt {
     float ks, vs;       // (loaded with the tile: only its weights and products wait for them)
 };
 
-// A row to a workgroup, or shares?  Cutting costs a second start (5 us: length, page, keys, one after the other), a fold and
-// a piece per cut, not cutting lets the longest row decide.  Rows of at most this many tiles are not cut.  (us, shares against rows,
-// lengths spread from 1 to the given, 8 bits / bf16: 160 rows to 1900 tokens 24 / 29 : 22 / 23, to 4000 33 / 43 : 39 / 51; 512 rows
-// to 900 34 / 40 : 20 / 28, to 4000 75 / 118 : 70 / 117, to 9000 121 / 216 : 148 / 260; 8 rows to 900 10.9 : 13.3.  fp32 takes
-// longer per tile: 64 rows to 400 13.4 : 14.9.)
-__host__ __device__ __forceinline__ int uncut_row_tiles(int rows, bool k32) { return k32 ? min(max(rows / 32, 1), 32) : min(max(rows / 8, 4), 32); }
+// A row to a workgroup, or shares?  Cutting costs a second start, a fold and a piece per cut, not cutting lets the longest row
+// decide.  Rows of at most this many tiles are not cut.  (us, shares against rows, lengths spread from 1 to the given, 8 bits / bf16:
+// 160 rows to 900 tokens 15 / 18 : 14 / 14, to 1900 20 / 26 : 22 / 23, to 4000 25 / 38 : 39 / 50; 512 rows to 900 25 / 32 : 20 / 28, to
+// 1900 34 / 60 : 32 / 57, to 4000 65 / 110 : 70 / 116; 8 rows to 900 10.6 : 13.5.  fp32: 64 rows to 400 13.5 : 15.0.)
+__host__ __device__ __forceinline__ int uncut_row_tiles(int rows, bool k32) { return k32 ? min(max(rows / 32, 1), 32) : min(max(rows / 8, 4), 16); }
+
+// What a row's beginning costs a workgroup, in tiles: its page, query, first keys and the fold.  A share is measured in tiles and
+// beginnings, or the workgroup that short rows fall to ends last.  (us with 0, 1, 2, 4: 40 sequences of 1 to 9001 tokens, 8 heads,
+// 8 bits 90, 84, 80, 80, bf16 144, 137, 135, 137; 1280 rows to 9000 tokens 308, 302, 286, 288; rows of one length the same.  fp32, whose
+// tiles take four times as long, 0: 8 rows of 32 tiles 15.0, with 1 18.6.)
+constexpr int kRowStart = 2;
 
 struct PageDecodeArgs {
     const char *q, *k_pages, *v_pages;
@@ -77,6 +82,7 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
     constexpr bool k8 = std::is_same<S, E4M3>::value, k32 = T::kTag == LEOAM_F32;
     constexpr int ROWB = LEOAM_D * S::kBytes, QROWB = Row<T>::kRowBytes, NT = StepOf<T, S>::kTiles;
     constexpr int STEP = 16 * NT, NV = 4 * NT;
+    constexpr int kStart = k32 ? 0 : kRowStart;
     // fp16 weights: the row's maximum is taken 2^15 lower, so that small weights stay clear of fp16's subnormals
     constexpr float kBias = T::kTag == LEOAM_F16 ? 15.f : 0.f;
     constexpr int kParts = T::kTag == LEOAM_F16 ? 2 : 3;      // of a weight
@@ -103,7 +109,7 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
         int most = 0;
         for (int e = e0; e < e1; ++e) {
             const int n = tiles_of(entry_tokens(e));
-            mine += (long long)weight * n;
+            mine += (long long)weight * (n + kStart);
             most = max(most, n);
         }
         long long incl = mine;
@@ -135,7 +141,7 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
                 int e = e0;
                 for (;;) {
                     const int tokens = entry_tokens(e);
-                    const long long n = (long long)weight * tiles_of(tokens);
+                    const long long n = (long long)weight * (tiles_of(tokens) + kStart);
                     sh_tokens = tokens;
                     if (pos < before + n) break;
                     before += n;
@@ -153,7 +159,7 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
                 h = e % hkv;
                 off = uniform((int)at);
             } else {
-                const int n = tiles_of(uniform(next_tokens));
+                const int n = tiles_of(uniform(next_tokens)) + kStart;
                 b = e;
                 h = uniform((int)(at / n));
                 off = uniform((int)(at - (long long)h * n));
@@ -168,14 +174,28 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
         end = tiles_of(next_tokens);
     }
 
+    const int start = whole_rows ? 0 : kStart;
     bool first_piece = true;
+    auto advance = [&](int taken) {
+        pos += taken;
+        off = 0;
+        if (++h == hkv) {
+            h = 0;
+            ++b;
+        }
+    };
     while (pos < end) {
         const int tokens = uniform(next_tokens), n_tiles = tiles_of(tokens);
-        const int take = uniform((int)min((long long)(n_tiles - off), end - pos));
+        const int take = uniform((int)min((long long)(start + n_tiles - off), end - pos));
+        const int tile0 = max(off - start, 0), n_here = off + take - start - tile0;
         const size_t bh = (size_t)b * hkv + h;
         {
             const int nh = h + 1 < hkv ? h + 1 : 0, nb = h + 1 < hkv ? b : b + 1;
             if (pos + take < end) next_tokens = walk_of(a, nb, nh);      // (the share has a further row)
+        }
+        if (n_here <= 0) {      // (the share ends before the row's first tile)
+            advance(take);
+            continue;
         }
         const int len = a.sel_idx ? min(max(a.seq_len[b], 0), a.max_pages << a.page_shift) : tokens;
         const int32_t* sel = a.sel_idx ? a.sel_idx + bh * (size_t)a.k_max : nullptr;
@@ -191,7 +211,7 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
         }
 
         // ---- this wave's part of the stretch, in steps ------------------------------------------------------
-        const int t_begin = off * kTileTokens, t_end = min(tokens, (off + take) * kTileTokens);
+        const int t_begin = tile0 * kTileTokens, t_end = min(tokens, (tile0 + n_here) * kTileTokens);
         const int n_steps = (t_end - t_begin + STEP - 1) / STEP, per_wave = (n_steps + kAttWaves - 1) / kAttWaves;
         const int s0 = min(n_steps, wave * per_wave), s1 = min(n_steps, s0 + per_wave);
 
@@ -413,7 +433,7 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
             }
         }
         __syncthreads();
-        const bool whole = take == n_tiles;
+        const bool whole = n_here == n_tiles;
         // a piece that opens the workgroup's share, or closes it
         const size_t slot = 2 * (size_t)blockIdx.x + (first_piece ? 0 : 1);
         for (int i = tid; i < G * kPartStride; i += kAttThreads) {
@@ -436,22 +456,17 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
                 a.partial[(slot * G + g) * kPartStride + d] = d < LEOAM_D ? v : d == LEOAM_D ? m : l;
             }
         }
-        if (a.pieces && off == 0 && tid == 0) {
+        if (a.pieces && tile0 == 0 && tid == 0) {
             RowPieces rp = {0, 0};
             if (!whole) {
-                rp.count = (int)((pos + n_tiles - 1) / share - blockIdx.x) + 1;
+                rp.count = (int)((pos - off + start + n_tiles - 1) / share - blockIdx.x) + 1;
                 rp.first_slot = (int)slot;
             }
             a.pieces[bh] = rp;
         }
         if (whole_rows) break;
         first_piece = false;
-        pos += take;
-        off = 0;
-        if (++h == hkv) {
-            h = 0;
-            ++b;
-        }
+        advance(take);
     }
 }
 

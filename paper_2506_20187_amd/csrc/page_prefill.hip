@@ -2,13 +2,14 @@
 //
 // Bound by the matrix cores.  A workgroup takes 128 query rows of one kv head - a row is a (token, head of the
 // group) pair, so the heads of a group share every key and value that is fetched - and walks the keys 64 at a time (fp32:
-// 32): the tile after the current one is on its way to registers while the current one is worked on in LDS.
+// 32): the next tile (8 bits: the next two) is on its way to registers while the current one is worked on in LDS.
 // Each of the four waves owns 32 rows.  S^T = K Q^T (32x32 products) leaves lane = row, registers = keys: the row's
 // maximum and sum need no exchange but one with the lane 32 away, and P is already the second operand of O^T = V^T P^T;
 // the first operand, four keys of one channel at a time, comes out of LDS by the transposing read.
 //
 // A unit of work is (128 rows, kv head).  With enough units to fill the chip each takes a workgroup.  With few (a
-// handful of rows behind a long context) the key tiles of all units are laid end to end and shared out equally; a
+// handful of rows behind a long context) the key tiles of all units are laid end to end, each unit's beginning counted as
+// some more (kUnitStart), and shared out equally; a
 // unit cut by the ends of shares leaves its pieces, (acc, m, l) per row, in the workspace, and a second kernel folds them.
 #include <cfloat>
 
@@ -42,10 +43,15 @@ constexpr int kSharers = 512;         // workgroups that share the tiles: two fi
 constexpr int kMostUnits = 1024;      // more units than this are not shared out: two rounds of workgroups or more
 constexpr int kMostSlots = 256;       // of as many slots: their tables stay in LDS
 // If no unit has more tiles than this, none is cut: a cut costs a second start, a piece and a fold.  (32 rows behind a context in
-// bf16, us, shares against whole units: 8 units of 11 tiles 15 : 22; 64 of 11 20 : 22, of 24 26 : 41; 256 of 11 40 : 28, of 24 62 : 47,
-// of 46 72 : 92; 512 of 11 70 : 36, of 46 129 : 110, of 94 214 : 217.  A tile of fp32 takes four times as long.)
-__host__ __device__ __forceinline__ int uncut_unit_tiles(int units, bool k32) { return k32 ? min(max(units / 40, 1), 16) : min(max(units / 10, 6), 64); }
-// `total` tiles among the workgroups, in order: the first `more` take each + 1, the others each.  (The first ones land on compute
+// bf16, us, shares against whole units: 8 units of 11 tiles 15 : 22; 64 of 11 20 : 22, of 24 24 : 42; 256 of 11 32 : 27, of 24 42 : 47,
+// of 46 65 : 92; 512 of 11 50 : 34, of 24 70 : 63, of 46 114 : 111, of 94 183 : 217.  A tile of fp32 takes four times as long.)
+__host__ __device__ __forceinline__ int uncut_unit_tiles(int units, bool k32) {
+    return k32 ? min(max(units / 40, 1), 16) : min(max(units / (units < kSharers ? 20 : 10), 6), 64);
+}
+// What a unit's beginning costs a workgroup, in tiles (fp32: 1): shares are measured in tiles and beginnings.  (us with 0, 1, 2, 4: 81
+// rows of ten sequences behind 89 to 22116 tokens, 16 heads, 8 bits 148, 109, 96, 97; 32 sequences to 6000 in bf16 110, 102, 95, 94.)
+constexpr int kUnitStart = 2;
+// `total` of them among the workgroups, in order: the first `more` take each + 1, the others each.  (The first ones land on compute
 // units of their own, so the units' loads differ by a tile at most; fp32, 1656 tiles of 8 us for 504: 55 -> 51 us against
 // shares of equal size and a last one of what is left.)
 struct Shares {
@@ -124,6 +130,8 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
     constexpr int ROWB = LEOAM_D * T::kBytes, SROWB = LEOAM_D * S::kBytes;      // a row in LDS, in the pages
     constexpr int KEYS = k32 ? 32 : 64, KB = KEYS / 32, KSTR = kKeyStride<T>, VSTR = kValueStride<T>, NQ = k32 ? 16 : 8;
     constexpr int LOADS = KEYS * SROWB / (kAttThreads * 16), PIECES = SROWB / 16, ROWS_PER_LOAD = kAttThreads / PIECES;
+    constexpr int kStart = k32 ? 1 : kUnitStart;
+    constexpr int AHEAD = k8 ? 2 : 1;      // tiles on their way to registers (8 bits, one: 363 us against 357 behind histories of 4K)
     constexpr int GROUPS = KEYS / 16;      // 16 keys never straddle a page
     // fp16: small weights stay clear of fp16's subnormals; the reference may lag the maximum by 2^kLag
     constexpr float kLag = 8.f, kBias = T::kTag == LEOAM_F16 ? 7.f : 0.f;
@@ -170,16 +178,20 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
     if (tid == 0) sh_bad = 0;
     __syncthreads();
 
-    uint4 kr[LOADS], vr[LOADS];
-    float ks[LOADS], vs[LOADS];
-    uint32_t ok_next = 0;      // bit g: group g of the tile in registers has a page
+    struct Tile {
+        uint4 k[LOADS], v[LOADS];
+        float ks[LOADS], vs[LOADS];
+        uint32_t ok;      // bit g: group g has a page
+    };
     constexpr uint32_t kAllOk = (1u << GROUPS) - 1;
-    auto fetch = [&](int j, int id) {
+    // id: the lane's page in tile j; afterwards - on its way ahead of the rows - in the tile behind it
+    auto fetch = [&](int j, int& id, Tile& t) {
         const bool ok = (uint32_t)id < (uint32_t)a.n_pages;
-        ok_next = (uint32_t)__ballot(ok) & kAllOk;
+        t.ok = (uint32_t)__ballot(ok) & kAllOk;
         const uint32_t page = ok ? (uint32_t)id : 0u;
         const uint64_t begin = (uint64_t)page * page_bytes;
         const int lo = (int)(uint32_t)begin, hi = (int)(uint32_t)(begin >> 32);
+        id = pages_of(min(j + 1, n_tiles - 1));
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
             // a load's 16-key group is the same for the wave
@@ -188,47 +200,47 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
             const int g = i * ROWS_PER_LOAD / 16 + (kPerLoad > 1 ? wave * (LEOAM_WAVE / PIECES) / 16 : 0);
             const uint32_t at = ((uint32_t)min(j * KEYS + r, last) & in_page) * SROWB + 16 * (tid % PIECES);
             const uint64_t base = (uint64_t)(uint32_t)__builtin_amdgcn_readlane(hi, g) << 32 | (uint32_t)__builtin_amdgcn_readlane(lo, g);
-            kr[i] = load16(kh + base, at);
-            vr[i] = load16(vh + base, at);
+            t.k[i] = load16(kh + base, at);
+            t.v[i] = load16(vh + base, at);
             if (k8) {
                 const size_t row = (size_t)(uint32_t)__builtin_amdgcn_readlane((int)page, g) * hkv + h;
-                ks[i] = a.k_scale[row];
-                vs[i] = a.v_scale[row];
+                t.ks[i] = a.k_scale[row];
+                t.vs[i] = a.v_scale[row];
             }
         }
     };
-    auto stage = [&](int j, int buf) {
+    auto stage = [&](int j, int buf, Tile& t) {
         // A value that is not finite must not reach rows that its key is hidden from, which a weight of zero does not
         // prevent: from the first tile that hides keys on such values are left out here and added at the end.
         const bool look = j >= first_masked;
         bool bad = false;
-        if (ok_next != kAllOk) {
+        if (t.ok != kAllOk) {
 #pragma unroll
             for (int i = 0; i < LOADS; ++i) {
-                if (ok_next >> ((i * ROWS_PER_LOAD + tid / PIECES) / 16) & 1) continue;
-                vr[i] = make_uint4(0, 0, 0, 0);      // nothing there: no value may matter
-                vs[i] = 1.f;
+                if (t.ok >> ((i * ROWS_PER_LOAD + tid / PIECES) / 16) & 1) continue;
+                t.v[i] = make_uint4(0, 0, 0, 0);      // nothing there: no value may matter
+                t.vs[i] = 1.f;
             }
         }
         if (look) {
 #pragma unroll
             for (int i = 0; i < LOADS; ++i) {
-                if constexpr (k8) bad |= silence_codes(vr[i]);
-                else bad |= silence<T>(vr[i]);
+                if constexpr (k8) bad |= silence_codes(t.v[i]);
+                else bad |= silence<T>(t.v[i]);
             }
         }
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
             const int r = i * ROWS_PER_LOAD + tid / PIECES, piece = tid % PIECES;
             if constexpr (k8) {
-                const uint4 v0 = widen8<T>(vr[i].x, vr[i].y, vs[i]), v1 = widen8<T>(vr[i].z, vr[i].w, vs[i]);
-                store16(sh_k[buf], r * KSTR + 32 * piece, widen8<T>(kr[i].x, kr[i].y, ks[i]));
-                store16(sh_k[buf], r * KSTR + 32 * piece + 16, widen8<T>(kr[i].z, kr[i].w, ks[i]));
+                const uint4 v0 = widen8<T>(t.v[i].x, t.v[i].y, t.vs[i]), v1 = widen8<T>(t.v[i].z, t.v[i].w, t.vs[i]);
+                store16(sh_k[buf], r * KSTR + 32 * piece, widen8<T>(t.k[i].x, t.k[i].y, t.ks[i]));
+                store16(sh_k[buf], r * KSTR + 32 * piece + 16, widen8<T>(t.k[i].z, t.k[i].w, t.ks[i]));
                 store16(sh_v[buf], r * VSTR + 32 * piece, v0);
                 store16(sh_v[buf], r * VSTR + 32 * piece + 16, v1);
             } else {
-                store16(sh_k[buf], r * KSTR + 16 * piece, kr[i]);
-                store16(sh_v[buf], r * VSTR + 16 * piece, vr[i]);
+                store16(sh_k[buf], r * KSTR + 16 * piece, t.k[i]);
+                store16(sh_v[buf], r * VSTR + 16 * piece, t.v[i]);
             }
         }
         if (bad) sh_bad = 1;
@@ -353,21 +365,29 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
 
     const int j_end = j1 < 0 ? n_tiles : min(j1, n_tiles);
     if (j0 < j_end) {
-        fetch(j0, id0);
-        int next = pages_of(min(j0 + 1, n_tiles - 1));
-        stage(j0, j0 & 1);
-        uint32_t ok = ok_next;
+        Tile even, odd;      // (of the tiles from j0 on)
+        int id = id0;
+        fetch(j0, id, even);
+        if constexpr (AHEAD == 2) fetch(min(j0 + 1, j_end - 1), id, odd);
+        stage(j0, j0 & 1, even);
+        uint32_t ok = even.ok;
         __syncthreads();
-        for (int j = j0; j < j_end; ++j) {
-            const bool more = j + 1 < j_end;
-            if (more) {
-                fetch(j + 1, next);
-                next = pages_of(min(j + 2, n_tiles - 1));
-            }
+        // Tile j is worked on, then `in` is staged; `to` takes in tile j + AHEAD.  (Two tiles on their way: no branch around the
+        // loads and none that leads back, or the compiler has everybody wait for the second tile too.)
+        int j = j0;
+        auto step = [&](Tile& in, Tile& to) {
+            if (AHEAD == 2 || j + 1 < j_end) fetch(min(j + AHEAD, j_end - 1), id, to);
             if (!idle && j * KEYS <= wave_hi) work(j, j & 1, ok);
-            if (more) stage(j + 1, (j + 1) & 1);
-            ok = ok_next;
+            if (++j == j_end) return false;
+            stage(j, j & 1, in);
+            ok = in.ok;
             __syncthreads();
+            return true;
+        };
+        if constexpr (AHEAD == 1) {
+            while (step(even, even)) {}
+        } else {
+            while (step(odd, even) && step(even, odd)) {}
         }
     }
 
@@ -489,7 +509,7 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
             int run_sum = 0;
             for (int s0 = 0; s0 < a.n_slots; s0 += LEOAM_WAVE) {
                 const int slot = s0 + lane;
-                const uint32_t mine = slot < a.n_slots ? (uint32_t)sh_tiles[slot] * hkv : 0u, incl = wave_incl_scan_u32(mine);
+                const uint32_t mine = slot < a.n_slots && sh_tiles[slot] ? (uint32_t)(sh_tiles[slot] + kStart) * hkv : 0u, incl = wave_incl_scan_u32(mine);
                 if (slot < a.n_slots) sh_before[slot] = run_sum + (int)(incl - mine);
                 run_sum += __builtin_amdgcn_readlane((int)incl, LEOAM_WAVE - 1);
             }
@@ -507,8 +527,8 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
                 h = next % hkv;
                 next += W;
                 pos = 0;
-                end = uniform(sh_tiles[slot]);
-                if (end > 0) return;
+                end = uniform(sh_tiles[slot]) + kStart;
+                if (end > kStart) return;
             }
             pos = end = 0;
         };
@@ -525,32 +545,35 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
                 else hi = mid;
             }
             slot = uniform(lo);      // (of equal ones the last: the one that has tiles)
-            const int n = uniform(sh_tiles[slot]), in = pos - uniform(sh_before[slot]);
+            const int n = uniform(sh_tiles[slot]) + kStart, in = pos - uniform(sh_before[slot]);
             h = in / n;
             off = in - h * n;
         }
         bool first_piece = true;
         while (pos < end) {
-            const int n = uniform(sh_tiles[slot]), take = min(n - off, end - pos);
-            Unit u = unit_of(slot);
-            u = Unit{uniform(u.b), uniform(u.row0), uniform(u.m), uniform(u.local), uniform(u.len)};
-            const int id = slot * hkv + h;
-            const bool whole = take == n;
-            const int piece_slot = 2 * (int)blockIdx.x + (first_piece ? 0 : 1);      // opens the share, or closes it
-            first_piece = false;
-            if (off == 0 && tid == 0) {
-                UnitPieces up = {0, 0, 0, 0};
-                if (!whole) {
-                    const int tok0 = u.local * (kRows / G);
-                    up.count = shares.owner(pos + n - 1) - (int)blockIdx.x + 1;
-                    up.first_slot = piece_slot;
-                    up.token0 = u.row0 + tok0;
-                    up.rows = min(u.m - tok0, kRows / G) * G;
+            const int n = uniform(sh_tiles[slot]), take = min(kStart + n - off, end - pos);
+            const int tile0 = max(off - kStart, 0), tile1 = off + take - kStart;
+            if (tile0 < tile1) {      // (a share may end before the unit's first tile)
+                Unit u = unit_of(slot);
+                u = Unit{uniform(u.b), uniform(u.row0), uniform(u.m), uniform(u.local), uniform(u.len)};
+                const int id = slot * hkv + h;
+                const bool whole = tile1 - tile0 == n;
+                const int piece_slot = 2 * (int)blockIdx.x + (first_piece ? 0 : 1);      // opens the share, or closes it
+                first_piece = false;
+                if (tile0 == 0 && tid == 0) {
+                    UnitPieces up = {0, 0, 0, 0};
+                    if (!whole) {
+                        const int tok0 = u.local * (kRows / G);
+                        up.count = shares.owner(pos - off + kStart + n - 1) - (int)blockIdx.x + 1;
+                        up.first_slot = piece_slot;
+                        up.token0 = u.row0 + tok0;
+                        up.rows = min(u.m - tok0, kRows / G) * G;
+                    }
+                    a.pieces[id] = up;
                 }
-                a.pieces[id] = up;
+                run(u, h, tile0, tile1, whole ? -1 : piece_slot);
+                __syncthreads();
             }
-            run(u, h, off, off + take, whole ? -1 : piece_slot);
-            __syncthreads();
             if (uncut) {
                 whole_unit();
                 continue;

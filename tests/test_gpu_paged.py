@@ -375,6 +375,14 @@ def test_decode_more_rows_than_shares(L, dtype, q8, longest):
     run_decode(L, widened(Made(dtype, q8, lengths, 8, 16, seed=43), 400), 8)
 
 
+@pytest.mark.parametrize("dtype,q8", [(F32, False), (BF16, False), (F16, True)], ids=["f32", "bf16", "f16-e4m3"])
+def test_decode_short_rows_beside_long_ones(L, dtype, q8):
+    made = Made(dtype, q8, [70, 3] * 7 + [5000] + [0, 3, 170, 1, 129] * 5, 4, 32, seed=66)
+    most, least = L.leoam_page_workspace_bytes(made.pages(L, 8)), L.leoam_page_workspace_min(made.pages(L, 8))
+    for nbytes in (most, most * 7 // 8, most // 3, least):
+        run_decode(L, made, 8, workspace_bytes=max(nbytes // 16 * 16, least))
+
+
 @pytest.mark.parametrize("dtype,q8", [(F32, False), (F16, True), (BF16, False)], ids=["f32", "f16-e4m3", "bf16"])
 def test_decode_small_workspaces(L, dtype, q8):
     made = Made(dtype, q8, [900, 0, 3, 1500], 2, 32, seed=5)
@@ -579,6 +587,17 @@ def test_prefill_small_workspaces(L, dtype, q8):
     most = L.leoam_page_workspace_bytes(made.pages(L, 128), 345)
     for eighths in (5, 8):
         run_prefill(L, made, 128, [300, 40, 5], rows=some, workspace_bytes=most * eighths // 8 // 16 * 16)
+
+
+@pytest.mark.parametrize("dtype,q8", [(F32, False), (BF16, False), (F16, True)], ids=["f32", "bf16", "f16-e4m3"])
+def test_prefill_short_units_beside_long_ones(L, dtype, q8):
+    # shares begin and end before a unit's first tile, within it, behind it
+    lengths = [70, 3] * 7 + [5000] + [0, 3, 70, 1, 129] * 5
+    new = [min(n, 1 + i % 4) for i, n in enumerate(lengths)]
+    made = Made(dtype, q8, lengths, 8, 32, seed=65)
+    most = L.leoam_page_workspace_bytes(made.pages(L, 16), sum(new))
+    for eighths in (8, 7, 5):
+        run_prefill(L, made, 16, new, workspace_bytes=most * eighths // 8 // 16 * 16)
 
 
 def test_prefill_one_row_each(L):
