@@ -98,4 +98,10 @@ __device__ __forceinline__ void pair_back(F16, uint32_t w, float& a, float& b) {
     b = (float)p.y;
 }
 
+// ln(2^m l).  Where the reference m was taken `bias` below the largest logit both are brought back first: the logarithm of
+// a sum near 2^bias would cost the result bits.
+__device__ __forceinline__ float log_sum_exp(float m, float l, int bias) {
+    return l == 0.f ? -INFINITY : ((m + (float)bias) + log2f(ldexpf(l, -bias))) * kLn2;
+}
+
 }  // namespace leoam

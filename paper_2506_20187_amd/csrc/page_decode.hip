@@ -58,6 +58,9 @@ __host__ __device__ __forceinline__ int uncut_row_tiles(int rows, bool k32) { re
 // tiles take four times as long, 0: 8 rows of 32 tiles 15.0, with 1 18.6.)
 constexpr int kRowStart = 2;
 
+// fp16 weights: the row's maximum is taken 2^15 lower, so that small weights stay clear of fp16's subnormals
+template <typename T> constexpr int decode_bias() { return T::kTag == LEOAM_F16 ? 15 : 0; }
+
 struct PageDecodeArgs {
     const char *q, *k_pages, *v_pages;
     const float *k_scale, *v_scale;
@@ -83,8 +86,7 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
     constexpr int ROWB = LEOAM_D * S::kBytes, QROWB = Row<T>::kRowBytes, NT = StepOf<T, S>::kTiles;
     constexpr int STEP = 16 * NT, NV = 4 * NT;
     constexpr int kStart = k32 ? 0 : kRowStart;
-    // fp16 weights: the row's maximum is taken 2^15 lower, so that small weights stay clear of fp16's subnormals
-    constexpr float kBias = T::kTag == LEOAM_F16 ? 15.f : 0.f;
+    constexpr float kBias = decode_bias<T>();
     constexpr int kParts = T::kTag == LEOAM_F16 ? 2 : 3;      // of a weight
     __shared__ float xw[kAttWaves][G][kPartStride];
     __shared__ long long sh_sum[kAttWaves];
@@ -451,7 +453,7 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
             if (whole) {
                 const size_t j = bh * G + g;
                 if (d < LEOAM_D) a.out[j * LEOAM_D + d] = l == 0.f ? 0.f : v / l;      // (NaN stays)
-                else if (d == LEOAM_D && a.lse) a.lse[j] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+                else if (d == LEOAM_D && a.lse) a.lse[j] = log_sum_exp(m, l, decode_bias<T>());
             } else {
                 a.partial[(slot * G + g) * kPartStride + d] = d < LEOAM_D ? v : d == LEOAM_D ? m : l;
             }
@@ -479,7 +481,7 @@ constexpr int kManyRows = 64;
 template <int PARTS>
 __global__ __launch_bounds__(kMergeGroups * LEOAM_D) void page_decode_merge_kernel(const float* __restrict__ partial,
                                                                                    const RowPieces* __restrict__ pieces, int group,
-                                                                                   int n_heads, float* __restrict__ out,
+                                                                                   int n_heads, int bias, float* __restrict__ out,
                                                                                    float* __restrict__ lse) {
     constexpr int HEADS = kMergeGroups / PARTS;
     constexpr int kBatch = 8;
@@ -541,7 +543,7 @@ __global__ __launch_bounds__(kMergeGroups * LEOAM_D) void page_decode_merge_kern
         }
     }
     out[(size_t)j * LEOAM_D + d] = l == 0.f ? 0.f : o / l;      // (NaN stays)
-    if (lse && d == 0) lse[j] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+    if (lse && d == 0) lse[j] = log_sum_exp(m, l, bias);
 }
 
 // Workgroups of the attention kernel: two fill a compute unit's registers (three, with fewer registers each, measured 101 against
@@ -568,10 +570,10 @@ template <typename T, typename S> static hipError_t launch_decode(const PageDeco
     const int n_heads = a.batch * a.n_kv_heads * group;
     if (a.batch * a.n_kv_heads >= kManyRows)
         hipLaunchKernelGGL(page_decode_merge_kernel<1>, dim3((n_heads + kMergeGroups - 1) / kMergeGroups), dim3(kMergeGroups * LEOAM_D), 0,
-                           stream, a.partial, a.pieces, group, n_heads, a.out, a.lse);
+                           stream, a.partial, a.pieces, group, n_heads, decode_bias<T>(), a.out, a.lse);
     else
         hipLaunchKernelGGL(page_decode_merge_kernel<kMergeGroups>, dim3(n_heads), dim3(kMergeGroups * LEOAM_D), 0, stream, a.partial,
-                           a.pieces, group, n_heads, a.out, a.lse);
+                           a.pieces, group, n_heads, decode_bias<T>(), a.out, a.lse);
     return hipGetLastError();
 }
 

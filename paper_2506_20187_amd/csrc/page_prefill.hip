@@ -22,6 +22,9 @@ typedef __attribute__((ext_vector_type(4))) short s16x4_t;
 
 constexpr int kRows = 128;            // query rows of a workgroup, 32 a wave
 
+// fp16 weights: the reference is taken 2^7 lower, so that small weights stay clear of fp16's subnormals
+template <typename T> constexpr int prefill_bias() { return T::kTag == LEOAM_F16 ? 7 : 0; }
+
 struct PagePrefillArgs {
     const char *q, *k_pages, *v_pages;
     const float *k_scale, *v_scale;
@@ -133,8 +136,7 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
     constexpr int kStart = k32 ? 1 : kUnitStart;
     constexpr int AHEAD = k8 ? 2 : 1;      // tiles on their way to registers (8 bits, one: 363 us against 357 behind histories of 4K)
     constexpr int GROUPS = KEYS / 16;      // 16 keys never straddle a page
-    // fp16: small weights stay clear of fp16's subnormals; the reference may lag the maximum by 2^kLag
-    constexpr float kLag = 8.f, kBias = T::kTag == LEOAM_F16 ? 7.f : 0.f;
+    constexpr float kLag = 8.f, kBias = prefill_bias<T>();      // the reference may lag the maximum by 2^kLag
     __shared__ __align__(16) char sh_k[2][KEYS * KSTR];
     __shared__ __align__(16) char sh_v[2][KEYS * VSTR];
     __shared__ int sh_bad;
@@ -434,7 +436,7 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
         }
         return;
     }
-    if (a.lse && half == 0) a.lse[q_row] = l == 0.f ? -INFINITY : (ref + log2f(l)) * kLn2;
+    if (a.lse && half == 0) a.lse[q_row] = log_sum_exp(ref, l, prefill_bias<T>());
     char* out = a.out + q_row * ROWB;
 #pragma unroll
     for (int db = 0; db < 4; ++db)
@@ -662,7 +664,7 @@ __global__ __launch_bounds__(256) void page_prefill_merge_kernel(PagePrefillArgs
     char* out = a.out + q_row * LEOAM_D * T::kBytes;
     if constexpr (T::kTag == LEOAM_F32) store16(out, 16 * d4, pack<F32>(o));
     else *reinterpret_cast<uint2*>(out + 8 * d4) = make_uint2(pair_of(T{}, o[0], o[1]), pair_of(T{}, o[2], o[3]));
-    if (a.lse && d4 == 0) a.lse[q_row] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+    if (a.lse && d4 == 0) a.lse[q_row] = log_sum_exp(m, l, prefill_bias<T>());
 }
 
 size_t page_decode_workspace_bytes(const leoam_pages*);
