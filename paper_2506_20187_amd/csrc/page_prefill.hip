@@ -134,6 +134,9 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
     constexpr int KEYS = k32 ? 32 : 64, KB = KEYS / 32, KSTR = kKeyStride<T>, VSTR = kValueStride<T>, NQ = k32 ? 16 : 8;
     constexpr int LOADS = KEYS * SROWB / (kAttThreads * 16), PIECES = SROWB / 16, ROWS_PER_LOAD = kAttThreads / PIECES;
     constexpr int kStart = k32 ? 1 : kUnitStart;
+    // (few rows are usual where tiles are shared.  8 bits, ten sequences of 22K, 64 heads, us without : with, 2 tokens each 225 : 181, 8 226 : 190,
+    // 16 251 : 223; 16 bits wait for memory with 8 already, 319 : 319)
+    constexpr bool kHalves = kShared && k8;
     constexpr int AHEAD = k8 ? 2 : 1;      // tiles on their way to registers (8 bits, one: 363 us against 357 behind histories of 4K)
     constexpr int GROUPS = KEYS / 16;      // 16 keys never straddle a page
     constexpr float kLag = 8.f, kBias = prefill_bias<T>();      // the reference may lag the maximum by 2^kLag
@@ -151,14 +154,17 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
     const int first = unit.len - m;                                   // position of the sequence's first new token (may be negative)
     const int tok0 = local * (kRows / G), n_tok = min(m - tok0, kRows / G);
     const int keys = max(first + tok0 + n_tok, 0);               // keys that some row of the workgroup sees
+    // Half the rows or fewer: waves 2 and 3 take the same rows as 0 and 1 and the second half of every tile's keys.
+    const bool halves = kHalves && n_tok * G <= kRows / 2;
+    const int rows_of = halves ? wave & 1 : wave;
     // this lane's row
-    const int row = 32 * wave + l32, tok = min(tok0 + row / G, m - 1);
+    const int row = 32 * rows_of + l32, tok = min(tok0 + row / G, m - 1);
     const int my_pos = first + tok;
     const bool stored = row / G < n_tok;
-    const bool idle = (32 * wave) / G >= n_tok;                   // none of the wave's rows is one
+    const bool idle = (32 * rows_of) / G >= n_tok;                   // none of the wave's rows is one
     const size_t q_row = ((size_t)(row0 + tok) * hkv + h) * G + row % G;
-    const int wave_lo = first + tok0 + 32 * wave / G;             // the wave's rows see at least / at most
-    const int wave_hi = min(first + tok0 + (32 * wave + 31) / G, first + m - 1);
+    const int wave_lo = first + tok0 + 32 * rows_of / G;             // the wave's rows see at least / at most
+    const int wave_hi = min(first + tok0 + (32 * rows_of + 31) / G, first + m - 1);
 
     const int n_tiles = (keys + KEYS - 1) / KEYS, last = keys - 1;
     const int first_masked = max(first + tok0 + 1, 0) / KEYS;     // tiles from here on hide keys from some row
@@ -261,11 +267,13 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
     const uint32_t k_lane = l32 * KSTR + 16 * half;
     const uint32_t v_lane = k32 ? 4 * half * VSTR + 4 * l32
                                 : (4 * half + (lane & 15) / 4) * VSTR + 32 * ((lane >> 4) & 1) + 8 * (lane & 3);
-    auto work = [&](int j, int buf, uint32_t ok) {
-        const char *kt = sh_k[buf] + k_lane, *vt = sh_v[buf] + v_lane;
-        f32x16_t s[KB];
+    auto work = [&](auto half_tile, int j, int buf, uint32_t ok) {
+        constexpr int NB = decltype(half_tile)::value ? KB / 2 : KB;      // key blocks, from block b0 on
+        const int b0 = decltype(half_tile)::value ? (wave >> 1) * NB : 0;
+        const char *kt = sh_k[buf] + k_lane + b0 * 32 * KSTR, *vt = sh_v[buf] + v_lane + b0 * 32 * VSTR;
+        f32x16_t s[NB];
 #pragma unroll
-        for (int kb = 0; kb < KB; ++kb) {
+        for (int kb = 0; kb < NB; ++kb) {
 #pragma unroll
             for (int r = 0; r < 16; ++r) s[kb][r] = 0.f;
 #pragma unroll
@@ -284,7 +292,7 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
         }
         if constexpr (!k32) {      // six reads ahead of the products
             then<kLdsRead, 6>();
-            static_for<0, 10>([](auto) {
+            static_for<0, 8 * NB - 6>([](auto) {
                 then<kMfma, 1>();
                 then<kLdsRead, 1>();
             });
@@ -293,14 +301,14 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
         const bool masked = j * KEYS + KEYS - 1 > wave_lo || ok != kAllOk;
         if (masked) {
 #pragma unroll
-            for (int kb = 0; kb < KB; ++kb)
+            for (int kb = 0; kb < NB; ++kb)
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
-                    if (j * KEYS + key_of(kb, r) > my_pos || !(ok >> (2 * kb + r / 8) & 1)) s[kb][r] = -INFINITY;
+                    if (j * KEYS + 32 * b0 + key_of(kb, r) > my_pos || !(ok >> (2 * (b0 + kb) + r / 8) & 1)) s[kb][r] = -INFINITY;
         }
         float mt = s[0][0];
 #pragma unroll
-        for (int kb = 0; kb < KB; ++kb)
+        for (int kb = 0; kb < NB; ++kb)
 #pragma unroll
             for (int r = 0; r < 16; ++r) mt = fmaxf(mt, s[kb][r]);
         {
@@ -336,7 +344,7 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
             }
         } else {
 #pragma unroll
-            for (int t = 0; t < 2 * KB; ++t) {      // 16 keys
+            for (int t = 0; t < 2 * NB; ++t) {      // 16 keys
                 const int kb = t / 2, r0 = 8 * (t % 2);
 #pragma unroll
                 for (int r = r0; r < r0 + 8; ++r) weigh(kb, r);
@@ -355,7 +363,7 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
                 then<kValu, 3>();
                 then<kTrans, 1>();
             });
-            static_for<0, 12>([](auto) {
+            static_for<0, 8 * NB - 4>([](auto) {
                 then<kMfma, 1>();
                 then<kLdsRead, 2>();
                 then<kValu, 5>();
@@ -376,23 +384,47 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
         __syncthreads();
         // Tile j is worked on, then `in` is staged; `to` takes in tile j + AHEAD.  (Two tiles on their way: no branch around the
         // loads and none that leads back, or the compiler has everybody wait for the second tile too.)
-        int j = j0;
-        auto step = [&](Tile& in, Tile& to) {
-            if (AHEAD == 2 || j + 1 < j_end) fetch(min(j + AHEAD, j_end - 1), id, to);
-            if (!idle && j * KEYS <= wave_hi) work(j, j & 1, ok);
-            if (++j == j_end) return false;
-            stage(j, j & 1, in);
-            ok = in.ok;
-            __syncthreads();
-            return true;
+        auto walk = [&](auto half_tile) {
+            int j = j0;
+            auto step = [&](Tile& in, Tile& to) {
+                if (AHEAD == 2 || j + 1 < j_end) fetch(min(j + AHEAD, j_end - 1), id, to);
+                if (!idle && j * KEYS <= wave_hi) work(half_tile, j, j & 1, ok);
+                if (++j == j_end) return false;
+                stage(j, j & 1, in);
+                ok = in.ok;
+                __syncthreads();
+                return true;
+            };
+            if constexpr (AHEAD == 1) {
+                while (step(even, even)) {}
+            } else {
+                while (step(odd, even) && step(even, odd)) {}
+            }
         };
-        if constexpr (AHEAD == 1) {
-            while (step(even, even)) {}
-        } else {
-            while (step(odd, even) && step(even, odd)) {}
-        }
+        if (kHalves && halves) walk(std::integral_constant<bool, kHalves>{});
+        else walk(std::false_type{});
     }
 
+    if (kHalves && halves) {      // the rows' two states become one
+        float* x = reinterpret_cast<float*>(sh_k) + (wave & 1) * 66 * LEOAM_WAVE + lane;
+        __syncthreads();
+        if (wave >= 2) {
+#pragma unroll
+            for (int i = 0; i < 64; ++i) x[i * LEOAM_WAVE] = acc[i / 16][i % 16];
+            x[64 * LEOAM_WAVE] = ref;
+            x[65 * LEOAM_WAVE] = l_run;
+        }
+        __syncthreads();
+        if (wave >= 2) return;
+        const float other = x[64 * LEOAM_WAVE], now = fmaxf(ref, other), c = exp2_or_zero(ref, now), d = exp2_or_zero(other, now);
+        ref = now;
+        l_run = c * l_run + d * x[65 * LEOAM_WAVE];
+#pragma unroll
+        for (int i = 0; i < 64; ++i) {
+            acc[i / 16][i % 16] = c * acc[i / 16][i % 16] + d * x[i * LEOAM_WAVE];
+            if (i % 8 == 7) __builtin_amdgcn_sched_barrier(0);      // (no more registers than that for what is read)
+        }
+    }
     if (sh_bad) {      // values that were left out reach the rows that see their keys
         for (int t = max(j0, first_masked) * KEYS; t < min(j_end * KEYS, keys); ++t) {
             const int id = uniform(table[t >> a.page_shift]);

@@ -639,6 +639,30 @@ def test_prefill_later_tokens_that_are_not_finite(L, dtype, q8, bad):
         assert torch.isnan(out[70:]).all()
 
 
+@pytest.mark.parametrize("dtype,q8", KINDS, ids=KIND_IDS)
+def test_prefill_few_rows_and_values_that_are_not_finite(L, dtype, q8):
+    # the same where a few rows share a tile's keys out among the waves and their tiles among workgroups
+    n, m = 2000, 12
+    made = Made(dtype, q8, [n], 1, 32, seed=67)
+    for pool, pos in ((made.v_pages, n - 8), (made.k_pages, n - 4)):
+        page = int(made.table[0, pos // 32])
+        pool.view(torch.uint8 if q8 else pool.dtype)[page, 0, pos % 32, 9] = 0x7F if q8 else math.nan
+    g = torch.Generator().manual_seed(3)
+    q = torch.randn(m, 4, 128, generator=g).to(dtype)
+    out, lse = torch.empty(m, 4, 128, dtype=dtype, device="cuda"), torch.empty(m, 4, device="cuda")
+    pages = made.pages(L, 4)
+    ws = scratch(L.leoam_page_workspace_bytes(pages, m))
+    off = torch.tensor([0, m], dtype=torch.int32).cuda()
+    L.page_attention_prefill(pages, q.cuda(), off, made.k_pages, made.v_pages, made.k_scale, made.v_scale, made.table.cuda(), made.seq_len,
+                             SCALE, out, lse, ws)
+    K, V = made.tokens(0, 0, range(n)), made.tokens(1, 0, range(n))
+    weight = 0.0 if dtype == F32 else HALF[dtype]
+    check_rows(L, made, out, lse, [(i, q[i], K[:, : n - m + i + 1], V[:, : n - m + i + 1]) for i in range(m - 8)], weight, HALF[dtype])
+    assert not torch.isfinite(out[m - 8: m - 4, :, 9]).any()
+    assert torch.isfinite(out[m - 8: m - 4, :, :9]).all() and torch.isfinite(out[m - 8: m - 4, :, 10:]).all()
+    assert torch.isnan(out[m - 4:]).all()
+
+
 # ---- together ------------------------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("dtype,q8", [(BF16, False), (F16, True), (F32, False)], ids=["bf16", "f16-e4m3", "f32"])
