@@ -383,6 +383,16 @@ def test_decode_short_rows_beside_long_ones(L, dtype, q8):
         run_decode(L, made, 8, workspace_bytes=max(nbytes // 16 * 16, least))
 
 
+@pytest.mark.parametrize("dtype,q8", [(F32, False), (BF16, True)], ids=["f32", "bf16-e4m3"])
+def test_many_sequences(L, dtype, q8):
+    # more sequences than a workgroup has threads: long ones first, in the middle and last
+    lengths = [4000] + [0, 1, 17, 40, 16, 130] * 50 + [3001] + [5, 33, 2] * 100 + [2500]
+    made = Made(dtype, q8, lengths, 1, 16, seed=68)
+    run_decode(L, made, 4)
+    new = [min(n, b % 3) for b, n in enumerate(lengths)]
+    run_prefill(L, made, 4, new)
+
+
 @pytest.mark.parametrize("dtype,q8", [(F32, False), (F16, True), (BF16, False)], ids=["f32", "f16-e4m3", "bf16"])
 def test_decode_small_workspaces(L, dtype, q8):
     made = Made(dtype, q8, [900, 0, 3, 1500], 2, 32, seed=5)
