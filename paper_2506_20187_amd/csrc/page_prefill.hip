@@ -9,8 +9,8 @@
 //
 // A unit of work is (128 rows, kv head).  With enough units to fill the chip each takes a workgroup.  With few (a
 // handful of rows behind a long context) the key tiles of all units are laid end to end, each unit's beginning counted as
-// some more (kUnitStart), and shared out equally; a
-// unit cut by the ends of shares leaves its pieces, (acc, m, l) per row, in the workspace, and a second kernel folds them.
+// some more (kUnitStart), and shared out equally; a unit cut by the ends of shares leaves its pieces, (acc, m, l) per row, in
+// the workspace, and a second kernel folds them.
 #include <cfloat>
 
 #include "page_common.h"
