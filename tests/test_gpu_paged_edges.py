@@ -1,0 +1,83 @@
+"""kv_page_append where sequences do not simply grow: infinities beside zeros, steps back, batch rows that change hands, pages of
+other sequences, lists that descend.  What is expected is read from the definition in include/leoam.h."""
+import math
+
+import pytest
+import torch
+
+from tests.test_gpu_paged import BF16, F16, F32, KIND_IDS, KINDS, L, scratch, spread  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+i32 = lambda x: torch.tensor(x, dtype=torch.int32).cuda()  # noqa: E731
+
+
+class Pool:
+    """An empty cache (NaN wherever no token is) with the buffers of a selection."""
+
+    def __init__(self, L, dtype, q8, batch, hkv, page, max_pages, n_pages, hq=None):
+        self.L, self.dtype, self.q8, self.hkv, self.page = L, dtype, q8, hkv, page
+        store = torch.float8_e4m3fn if q8 else dtype
+        self.hq = hq or hkv
+        self.pages = L.make_pages(batch, self.hq, hkv, 128, n_pages, page, max_pages, dtype, L.E4M3 if q8 else None)
+        self.k = torch.full((n_pages, hkv, page, 128), math.nan).to(store).cuda()
+        self.v = self.k.clone()
+        self.ks, self.vs = (torch.full((n_pages, hkv), math.nan).cuda() for _ in "kv") if q8 else (None, None)
+        self.abstract = torch.full((batch, hkv, max_pages, 2, 128), 77.0, dtype=dtype).cuda()
+        self.off = torch.full((batch, max_pages + 1), -7, dtype=torch.int32).cuda()
+        self.n_chunks = torch.zeros(batch, dtype=torch.int32).cuda()
+        self.status = torch.full((batch,), -7, dtype=torch.int32).cuda()
+
+    def append(self, k, v, new_off, seq_len, table, abstract=True, n_chunks=True):
+        self.L.kv_page_append(self.pages, None, k, v, new_off, i32(seq_len), table.cuda(), None, None, self.k, self.v, self.ks, self.vs,
+                              self.abstract if abstract else None, self.off if abstract else None,
+                              self.n_chunks if abstract and n_chunks else None, self.status)
+        torch.cuda.synchronize()
+
+    def values(self, which, ids, n):
+        """[Hkv, n, 128] float64: the first n tokens of the pages `ids`."""
+        pool, scale = (self.k, self.ks) if which == 0 else (self.v, self.vs)
+        x = pool.float().double()[ids]
+        if self.q8:
+            x = x * scale.double()[ids][..., None, None]
+        return x.transpose(0, 1).reshape(self.hkv, -1, 128)[:, :n]
+
+    def check_rows(self, b, table, n):
+        """Row b's abstract and boundaries are those of its n stored tokens."""
+        ids = table[b, : -(-n // self.page)].long().cuda()
+        K = self.values(0, ids, n)
+        assert torch.isfinite(K).all()
+        for p in range(len(ids)):
+            kept = K[:, p * self.page: (p + 1) * self.page]
+            assert torch.equal(self.abstract[b, :, p, 0].double(), kept.amax(1)), f"maximum, sequence {b}, page {p}"
+            assert torch.equal(self.abstract[b, :, p, 1].double(), kept.amin(1)), f"minimum, sequence {b}, page {p}"
+        assert int(self.n_chunks[b]) == len(ids)
+        assert self.off[b, : len(ids) + 1].tolist() == [min(p * self.page, n) for p in range(len(ids) + 1)]
+
+
+# ---- 8 bits: a page of zeros and infinities -------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", [F16, BF16], ids=["f16", "bf16"])
+@pytest.mark.parametrize("single", [True, False], ids=["tokens", "prompt"])
+def test_infinities_beside_zeros_are_zero(L, dtype, single):
+    # scale 0, so +-448 scale is 0; NaN stays NaN; and nothing changes when the scale grows
+    c = Pool(L, dtype, True, 1, 2, 16, 2, 3)
+    table = torch.tensor([[2, 0]], dtype=torch.int32)
+    k = torch.zeros(3, 2, 128)
+    v = torch.zeros(3, 2, 128)
+    k[0, 0, 5], k[1, 0, 6], k[2, 1, 100] = math.inf, -math.inf, math.nan
+    v[0, 1, 0], v[2, 0, 127] = -math.inf, math.nan
+    k, v = k.to(dtype).cuda(), v.to(dtype).cuda()
+    if single:
+        for i in range(3):
+            c.append(k[i: i + 1], v[i: i + 1], None, [i + 1], table)
+    else:
+        c.append(k, v, i32([0, 3]), [3], table)
+    for grown in (False, True):
+        if grown:
+            one = torch.ones(1, 2, 128, dtype=dtype, device="cuda")
+            c.append(one, one, None, [4], table)
+        for which, x in ((0, k), (1, v)):
+            got, gone = c.values(which, [2], 3).transpose(0, 1), torch.isnan(x)
+            assert torch.equal(torch.isnan(got), gone)
+            assert (got[~gone] == 0).all()
+        assert (c.ks[2] == (2.0 ** -8 if grown else 0)).all() and (c.vs[2] == (2.0 ** -8 if grown else 0)).all()
