@@ -200,7 +200,7 @@ __device__ __forceinline__ void encode_again(char* page, int held, float f, floa
         unpack_e4m3(w.x, y);
         unpack_e4m3(w.y, y + 4);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] *= f;
+        for (int e = 0; e < 8; ++e) y[e] *= f;      // (f < 1)
         w = make_uint2(pack_e4m3(y), pack_e4m3(y + 4));
         *reinterpret_cast<uint2*>(page + 8 * (size_t)i) = w;
         if (!want) continue;
@@ -214,8 +214,8 @@ __device__ __forceinline__ void encode_again(char* page, int held, float f, floa
     }
 }
 
-// One token's channels of this lane into its page; mx, mn take in what is stored.  inv: 1 / scale, or 0 for a scale of 0 (8 bits):
-// only zeros and values that are not finite are stored then, and 0 stands for the infinities too (infinity times 0 would be NaN).
+// One token's channels of this lane into its page; mx, mn take in what is stored.  inv: 1 / scale, or 0 for a scale of 0 (8 bits).
+// 448 * scale bounds what is stored before it is scaled, so that beside nothing but zeros infinities become 0 (infinity * 0 is NaN).
 template <typename T, bool kStore8>
 __device__ __forceinline__ void store_token(char* page, int slot, int col, const float* x, float scale, float inv, bool valid, float* mx,
                                             float* mn) {
@@ -223,7 +223,7 @@ __device__ __forceinline__ void store_token(char* page, int slot, int col, const
     float y[EPL];
     if constexpr (kStore8) {
 #pragma unroll
-        for (int e = 0; e < EPL; ++e) y[e] = inv == 0.f && fabsf(x[e]) == INFINITY ? 0.f : x[e] * inv;
+        for (int e = 0; e < EPL; ++e) y[e] = clamp_nan(x[e], 448.f * scale) * inv;
         const uint2 w = make_uint2(pack_e4m3(y), pack_e4m3(y + 4));
         if (valid) *reinterpret_cast<uint2*>(page + (size_t)slot * LEOAM_D + col) = w;
         unpack_e4m3(w.x, y);

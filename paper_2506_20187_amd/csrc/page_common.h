@@ -18,13 +18,13 @@ __device__ __forceinline__ void unpack_e4m3(uint32_t w, float* x) {
     x[0] = a.x; x[1] = a.y; x[2] = b.x; x[3] = b.y;
 }
 
-// Two floats to two codes (round half to even), beyond +-448 to +-448 (the conversion alone would give NaN there),
-// NaN stays NaN.
-__device__ __forceinline__ float clamp_e4m3(float x) { return x > 448.f ? 448.f : x < -448.f ? -448.f : x; }
+// Four floats of at most 448 (the conversion gives NaN beyond) to four codes, round half to even; NaN stays NaN.
 __device__ __forceinline__ uint32_t pack_e4m3(const float* x) {
-    int w = __builtin_amdgcn_cvt_pk_fp8_f32(clamp_e4m3(x[0]), clamp_e4m3(x[1]), 0, false);
-    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(clamp_e4m3(x[2]), clamp_e4m3(x[3]), w, true);
+    int w = __builtin_amdgcn_cvt_pk_fp8_f32(x[0], x[1], 0, false);
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x[2], x[3], w, true);
 }
+// x within +-most, NaN stays NaN
+__device__ __forceinline__ float clamp_nan(float x, float most) { return x > most ? most : x < -most ? -most : x; }
 
 // floats rounded once to the model's type (half to even): the 16 bytes a lane holds of a row
 template <typename T> __device__ __forceinline__ uint4 round_pack(const float* x);
