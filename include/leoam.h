@@ -492,7 +492,8 @@ typedef struct {
  * become subnormal).
  * Every page that takes a token must belong to one sequence only.  For each of them
  *   abstract   [batch, n_kv_heads, max_pages, 2, 128] q_dtype (nullable): the page's rows become the maximum / minimum of
- *              its stored keys (as kv_chunk_abstract_build with the pages as chunks, c_max = max_pages);
+ *              all keys it then holds up to seq_len (as kv_chunk_abstract_build with the pages as chunks, c_max = max_pages),
+ *              whatever the rows held: tokens may be taken back (seq_len lowered) and others appended in their places;
  *   chunk_off  [batch, max_pages + 1], n_chunks [batch] int32 (nullable): brought up to date with the pages as chunks,
  * so chunk_score and chunk_topk_select run on a leoam_shape with c_max = max_pages and n_ctx = max_pages * page_size.
  *   status[b] (nullable)  0 done; 1 seq_len[b] negative, beyond the capacity or below the number of new tokens, or new_off not

@@ -190,6 +190,14 @@ template <int THREADS> __device__ __forceinline__ TouchedPage touched_page(const
     return x;
 }
 
+template <int N> __device__ __forceinline__ void no_extremes(float* mx, float* mn) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+        mx[e] = -INFINITY;
+        mn[e] = INFINITY;
+    }
+}
+
 // The codes of a page whose scale grows by 1 / f, again; mx, mn (if wanted) take in the values that this thread's channels
 // (col, of 16 threads to a row) then stand for.
 template <int THREADS>
@@ -242,10 +250,49 @@ __device__ __forceinline__ void store_token(char* page, int slot, int col, const
     }
 }
 
-// The page's maximum and minimum key, from the lanes' (lanes LPR apart hold the same channels), the waves' and - if the page was
-// begun with another token and keeps its scale - what the row held.
+// mx, mn take in the keys that a page holds already, read from the page: what its abstract row says may be of tokens that were taken
+// back since, or of whoever had this place in the batch before.  (us for a token each, row folded in : page read; one sequence, 8
+// heads, pages of 64 in bf16 3.5 : 4.2; 96 sequences, pages of 32 in 8 bits 5.4 : 5.5, of 64 5.4 : 5.8, in bf16 4.0 : 4.7, and of 256, 25 MB,
+// 4.0 : 9.4.  Sixteen loads on their way instead of eight: 8.8 for the last, 6.2 against 5.8 for pages of 32.)
+template <typename T, bool kStore8, int THREADS>
+__device__ __forceinline__ void take_in_held(const char* page, int held, float scale, int col, float* mx, float* mn) {
+    constexpr int EPL = T::kEpl, LPR = Row<T>::kLanesPerRow, RPP = THREADS / LPR, BATCH = THREADS == LEOAM_WAVE ? 8 : 4;
+    constexpr int STOREB = kStore8 ? LEOAM_D : Row<T>::kRowBytes;
+    const int rg = threadIdx.x / LPR;
+    for (int r0 = 0; r0 < held; r0 += RPP * BATCH) {
+        uint4 raw[BATCH];
+#pragma unroll
+        for (int u = 0; u < BATCH; ++u) {      // (rows past the last repeat it)
+            const char* at = page + (size_t)min(r0 + u * RPP + rg, held - 1) * STOREB;
+            if constexpr (kStore8) {
+                const uint2 w = *reinterpret_cast<const uint2*>(at + col);
+                raw[u] = make_uint4(w.x, w.y, 0, 0);
+            } else {
+                raw[u] = load16(at, col * T::kBytes);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < BATCH; ++u) {
+            float y[EPL];
+            if constexpr (kStore8) {
+                unpack_e4m3(raw[u].x, y);
+                unpack_e4m3(raw[u].y, y + 4);
+            } else {
+                unpack<T>(raw[u], y);
+            }
+#pragma unroll
+            for (int e = 0; e < EPL; ++e) {
+                const float v = kStore8 ? y[e] * scale : y[e];
+                mx[e] = fmaxf(mx[e], v);
+                mn[e] = fminf(mn[e], v);
+            }
+        }
+    }
+}
+
+// The page's maximum and minimum key, from the lanes' (lanes LPR apart hold the same channels) and the waves'.
 template <typename T, int THREADS>
-__device__ __forceinline__ void write_abstract(char* abs_row, bool begun, int col, float* mx, float* mn, float (*sh)[2][LEOAM_D]) {
+__device__ __forceinline__ void write_abstract(char* abs_row, int col, float* mx, float* mn, float (*sh)[2][LEOAM_D]) {
     constexpr int EPL = T::kEpl, LPR = Row<T>::kLanesPerRow, WAVES = THREADS / LEOAM_WAVE, ROWB = Row<T>::kRowBytes;
     const int tid = threadIdx.x, lane = lane_id(), wave = tid / LEOAM_WAVE;
 #pragma unroll
@@ -277,15 +324,6 @@ __device__ __forceinline__ void write_abstract(char* abs_row, bool begun, int co
         }
     }
     if (tid >= LPR) return;
-    if (begun) {
-        float y[EPL];
-        unpack<T>(load16(abs_row, col * T::kBytes), y);
-#pragma unroll
-        for (int e = 0; e < EPL; ++e) mx[e] = fmaxf(mx[e], y[e]);
-        unpack<T>(load16(abs_row, ROWB + col * T::kBytes), y);
-#pragma unroll
-        for (int e = 0; e < EPL; ++e) mn[e] = fminf(mn[e], y[e]);
-    }
     store16(abs_row, col * T::kBytes, round_pack<T>(mx));
     store16(abs_row, ROWB + col * T::kBytes, round_pack<T>(mn));
 }
@@ -327,13 +365,8 @@ __global__ __launch_bounds__(THREADS) void page_append_prompt_kernel(AppendArgs 
         const long long stride = which ? a.v_stride : a.k_stride;
         char* page = (which ? a.v_pages : a.k_pages) + at * ps * STOREB;
         const bool turned = which == 0 && a.rot_dim > 0, bounded = which == 0 && a.abstract;
-        bool begun = x.held > 0;      // the abstract row counts
         float mx[EPL], mn[EPL];
-#pragma unroll
-        for (int e = 0; e < EPL; ++e) {
-            mx[e] = -INFINITY;
-            mn[e] = INFINITY;
-        }
+        no_extremes<EPL>(mx, mn);
         // (rows past the last repeat it: rotation exchanges lanes, so all of them are here)
         auto row_of = [&](int r) { return load16(src, (x.row0 + min(r, x.count - 1)) * stride); };
         auto turn_row = [&](int r, float* y) {
@@ -343,6 +376,7 @@ __global__ __launch_bounds__(THREADS) void page_append_prompt_kernel(AppendArgs 
             rotate<EPL, LPR>(a, turn, col, y);
         };
         if constexpr (!kStore8) {
+            if (bounded) take_in_held<T, false, THREADS>(page, x.held, 1.f, col, mx, mn);
             for (int r = rg; r < x.count + rg; r += RPP) {      // (uniform trip count)
                 float y[EPL];
                 unpack<T>(row_of(r), y);
@@ -368,18 +402,17 @@ __global__ __launch_bounds__(THREADS) void page_append_prompt_kernel(AppendArgs 
             }
             const float now = fmaxf(old, scale_of<T>(group_max<THREADS>(top, sh_max)));      // (everybody has the old scale)
             const float inv = now > 0.f ? 1.f / now : 0.f;                                   // a power of two: exact
-            if (x.held > 0 && now > old) {
-                encode_again<THREADS>(page, x.held, old * inv, now, bounded, mx, mn);
-                begun = false;
-            }
+            const bool grows = x.held > 0 && now > old;
+            if (grows) encode_again<THREADS>(page, x.held, old * inv, now, bounded, mx, mn);
             if (tid == 0) scales[at] = now;
 #pragma unroll
             for (int i = 0; i < PASSES; ++i) {
                 const int r = i * RPP + rg;
                 store_token<T, true>(page, x.held + min(r, x.count - 1), col, y[i], now, inv, r < x.count, mx, mn);
             }
+            if (bounded && !grows) take_in_held<T, true, THREADS>(page, x.held, now, col, mx, mn);      // (the rows' registers are free)
         }
-        if (bounded) write_abstract<T, THREADS>(abstract_row(a, x, h, ROWB), begun, col, mx, mn, sh_abs);
+        if (bounded) write_abstract<T, THREADS>(abstract_row(a, x, h, ROWB), col, mx, mn, sh_abs);
     }
 }
 
@@ -405,18 +438,20 @@ template <typename T, bool kStore8> __global__ __launch_bounds__(LEOAM_WAVE) voi
         old[0] = a.k_scale[at];
         old[1] = a.v_scale[at];
     }
+    float held_mx[EPL], held_mn[EPL];      // (read before anybody knows whether the scale grows: one round trip less)
+    no_extremes<EPL>(held_mx, held_mn);
+    if (a.abstract) take_in_held<T, kStore8, THREADS>(a.k_pages + at * ps * STOREB, x.held, old[0], col, held_mx, held_mn);
 #pragma unroll
     for (int which = 0; which < 2; ++which) {
         char* page = (which ? a.v_pages : a.k_pages) + at * ps * STOREB;
         const bool bounded = which == 0 && a.abstract;
         float y[EPL], mx[EPL], mn[EPL], scale = 1.f, inv = 1.f;
-        bool begun = x.held > 0;
         unpack<T>(raw[which], y);
         if (which == 0 && a.rot_dim) rotate<EPL, LPR>(a, turn, col, y);
 #pragma unroll
         for (int e = 0; e < EPL; ++e) {
-            mx[e] = -INFINITY;
-            mn[e] = INFINITY;
+            mx[e] = held_mx[e];
+            mn[e] = held_mn[e];
         }
         if constexpr (kStore8) {
             float top = 0.f;
@@ -428,13 +463,13 @@ template <typename T, bool kStore8> __global__ __launch_bounds__(LEOAM_WAVE) voi
             scale = fmaxf(old[which], scale_of<T>(group_max<THREADS>(top, nullptr)));
             inv = scale > 0.f ? 1.f / scale : 0.f;
             if (x.held > 0 && scale > old[which]) {
+                no_extremes<EPL>(mx, mn);
                 encode_again<THREADS>(page, x.held, old[which] * inv, scale, bounded, mx, mn);
-                begun = false;
             }
             if (tid == 0) (which ? a.v_scale : a.k_scale)[at] = scale;
         }
         store_token<T, kStore8>(page, x.held, col, y, scale, inv, tid < LPR, mx, mn);
-        if (bounded) write_abstract<T, THREADS>(abstract_row(a, x, h, ROWB), begun, col, mx, mn, nullptr);
+        if (bounded) write_abstract<T, THREADS>(abstract_row(a, x, h, ROWB), col, mx, mn, nullptr);
     }
 }
 

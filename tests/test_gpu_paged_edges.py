@@ -81,3 +81,47 @@ def test_infinities_beside_zeros_are_zero(L, dtype, single):
             assert torch.equal(torch.isnan(got), gone)
             assert (got[~gone] == 0).all()
         assert (c.ks[2] == (2.0 ** -8 if grown else 0)).all() and (c.vs[2] == (2.0 ** -8 if grown else 0)).all()
+
+
+# ---- the abstract is that of the stored keys ------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype,q8", KINDS, ids=KIND_IDS)
+@pytest.mark.parametrize("page", [16, 64, 256])
+@pytest.mark.parametrize("single", [True, False], ids=["tokens", "prompt"])
+def test_rejected_tokens_leave_the_abstract(L, dtype, q8, page, single):
+    # some tokens are taken back and others stored in their places
+    g = torch.Generator().manual_seed(page)
+    c = Pool(L, dtype, q8, 2, 3, page, 4, 9)
+    table = torch.tensor([[5, 2, 7, 1], [0, 8, 3, 4]], dtype=torch.int32)
+    make = lambda n, gain: (torch.randn(n, 3, 128, generator=g) * gain).to(dtype).cuda()  # noqa: E731
+    first = [page + 11, 9]
+    off = [0, first[0], sum(first)]
+    c.append(make(off[2], 1.0), make(off[2], 1.0), i32(off), first, table)
+    rejected = [n + 4 for n in first]
+    c.append(make(8, 30.0), make(8, 1.0), i32([0, 4, 8]), rejected, table)      # far beyond the others
+    for b in (0, 1):
+        c.check_rows(b, table, rejected[b])
+    now = [rejected[0] - 3, rejected[1] - 4]      # one of them stays, or none
+    for _ in range(2):
+        if single:
+            now = [n + 1 for n in now]
+            c.append(make(2, 0.5), make(2, 1.0), None, now, table)
+        else:
+            now = [now[0] + 2, now[1] + 1]
+            c.append(make(3, 0.5), make(3, 1.0), i32([0, 2, 3]), now, table)
+        for b in (0, 1):
+            c.check_rows(b, table, now[b])
+
+
+@pytest.mark.parametrize("dtype,q8", KINDS, ids=KIND_IDS)
+@pytest.mark.parametrize("single", [True, False], ids=["tokens", "prompt"])
+def test_abstract_of_a_page_begun_without_one(L, dtype, q8, single):
+    # (the rows held something else: of whoever had this place in the batch before)
+    g = torch.Generator().manual_seed(3)
+    c = Pool(L, dtype, q8, 1, 2, 32, 2, 3)
+    table = torch.tensor([[1, 2]], dtype=torch.int32)
+    make = lambda n: torch.randn(n, 2, 128, generator=g).to(dtype).cuda()  # noqa: E731
+    c.append(make(13), make(13), i32([0, 13]), [13], table, abstract=False)
+    n = 14 if single else 17
+    c.append(make(n - 13), make(n - 13), None if single else i32([0, n - 13]), [n], table)
+    c.check_rows(0, table, n)
