@@ -497,8 +497,9 @@ typedef struct {
  *   chunk_off  [batch, max_pages + 1], n_chunks [batch] int32 (nullable): brought up to date with the pages as chunks,
  * so chunk_score and chunk_topk_select run on a leoam_shape with c_max = max_pages and n_ctx = max_pages * page_size.
  *   status[b] (nullable)  0 done; 1 seq_len[b] negative, beyond the capacity or below the number of new tokens, or new_off not
- *             ascending; 2 a page to write is not in the pool (its tokens are left out, all others are stored); 3 a position
- *             beyond the rope table.  With 1 and 3 nothing of the sequence is written.
+ *             ascending (where it descends, 1 is reported of every sequence that it costs tokens or queries; some of them may
+ *             have been stored); 2 a page to write is not in the pool (its tokens are left out, all others are stored); 3 a position
+ *             beyond the rope table.  With 1 (but for lists that descend) and 3 nothing of the sequence is written.
  */
 int kv_page_append(const leoam_pages* pages, const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
                    int64_t v_stride, int32_t n_new, const int32_t* new_off, const int32_t* seq_len,

@@ -147,37 +147,64 @@ template <typename T, int THREADS> __global__ __launch_bounds__(THREADS) void pa
 // tokens the page held, its number in the pool; count = 0: nothing to do.
 struct TouchedPage { int b, p, p0, row0, held, count, id; };
 
-// `slot` of the call's touched pages, by the whole workgroup; the first of a sequence's reports (if `reports`).
-template <int THREADS> __device__ __forceinline__ TouchedPage touched_page(const AppendArgs& a, int slot, bool reports, float* sh_max) {
+// Slot of the first page that sequence i touches, in a ragged call (it touches at most m / ps + 2).
+__device__ __forceinline__ int first_slot(const AppendArgs& a, int i) { return a.new_off[i] / a.page_size + 2 * i; }
+
+// Whether the searches over new_off miss some of sequence b's pages or rows, as they may if it descends somewhere.  The number of
+// sequences that begin at or before an element grows with the element: the first and the last speak for those between.
+__device__ __forceinline__ bool misses(const AppendArgs& a, int b, const Taken& t) {
+    const int ps = a.page_size, slot = first_slot(a, b);
+    const int at[4] = {slot, slot + (t.n - 1) / ps - (t.n - t.m) / ps, t.row0, t.row0 + t.m - 1};
+    int found[4] = {0, 0, 0, 0};
+    bool more[4] = {true, true, true, true};
+    for (int i0 = 1; i0 <= a.batch && (more[0] || more[1] || more[2] || more[3]); i0 += LEOAM_WAVE) {      // (as wave_count_below)
+        const int i = i0 + lane_id(), row = a.new_off[min(i, a.batch)], s = row / ps + 2 * i;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint64_t hit = __ballot(i <= a.batch && (e < 2 ? s : row) <= at[e]);
+            if (more[e]) found[e] += __popcll(hit);
+            more[e] = more[e] && hit == ~0ull;
+        }
+    }
+    return found[0] != b || found[1] != b || found[2] != b || found[3] != b;
+}
+
+// what became of sequence b, by the whole workgroup
+template <int THREADS> __device__ __forceinline__ void report(const AppendArgs& a, int b, float* sh_max) {
+    const int tid = threadIdx.x, ps = a.page_size;
+    Taken t = taken_by(a, b);
+    if (t.status == 0 && a.new_off && t.m > 0 && misses(a, b, t)) t.status = 1;
+    const bool none = t.status || t.m == 0;
+    const int first = none ? 0 : (t.n - t.m) / ps, last = none ? -1 : (t.n - 1) / ps;
+    int bad = 0;
+    for (int p = first + tid; p <= last; p += THREADS) {
+        const int id = a.page_table[(size_t)b * a.max_pages + p];
+        bad |= id < 0 || id >= a.n_pages;
+    }
+    bad = (int)(group_max<THREADS>((float)bad, sh_max));
+    if (tid != 0) return;
+    if (a.status) a.status[b] = t.status ? t.status : bad ? 2 : 0;
+    if (a.n_chunks && !none) a.n_chunks[b] = last + 1;
+}
+
+// `slot` of the call's touched pages, by the whole workgroup
+__device__ __forceinline__ TouchedPage touched_page(const AppendArgs& a, int slot, bool bounds) {
     const int tid = threadIdx.x, ps = a.page_size;
     TouchedPage x = {slot, 0, 0, 0, 0, 0, 0};
     int local = 0;
     if (a.new_off) {
-        // sequence i's pages begin at slot new_off[i] / ps + 2 i: it touches at most m / ps + 2
-        x.b = wave_count_below(a.batch, slot, [&](int i) { return a.new_off[i] / ps + 2 * i; });
+        x.b = wave_count_below(a.batch, slot, [&](int i) { return first_slot(a, i); });
         if (x.b >= a.batch) return x;
-        local = slot - (a.new_off[x.b] / ps + 2 * x.b);
+        local = slot - first_slot(a, x.b);
     }
     const Taken t = taken_by(a, x.b);
     const bool none = t.status || t.m == 0;
     const int first = none ? 0 : (t.n - t.m) / ps, last = none ? -1 : (t.n - 1) / ps;
-    if (local == 0 && reports) {
-        int bad = 0;
-        for (int p = first + tid; p <= last; p += THREADS) {
-            const int id = a.page_table[(size_t)x.b * a.max_pages + p];
-            bad |= id < 0 || id >= a.n_pages;
-        }
-        bad = (int)(group_max<THREADS>((float)bad, sh_max));
-        if (tid == 0) {
-            if (a.status) a.status[x.b] = t.status ? t.status : bad ? 2 : 0;
-            if (a.n_chunks && !none) a.n_chunks[x.b] = (t.n + ps - 1) / ps;
-        }
-    }
     x.p = first + local;
     if (local < 0 || x.p > last) return x;
     x.p0 = max(t.n - t.m, x.p * ps);
     const int p1 = min(t.n, (x.p + 1) * ps);
-    if (reports && tid == 0 && a.chunk_off) {
+    if (bounds && tid == 0 && a.chunk_off) {
         int32_t* off = a.chunk_off + (size_t)x.b * (a.max_pages + 1);
         off[x.p + 1] = p1;
         if (x.p == 0) off[0] = 0;
@@ -332,7 +359,7 @@ __device__ __forceinline__ char* abstract_row(const AppendArgs& a, const Touched
     return a.abstract + (((size_t)x.b * a.n_kv_heads + h) * a.max_pages + x.p) * 2 * row_bytes;
 }
 
-// Prompts: a touched page and a kv head to a workgroup.
+// Prompts: a touched page and a kv head to a workgroup, behind one for each sequence that reports on it.
 //   16 / 32 bits (PASSES = 0): keys, then values, a pass of THREADS / lanes-per-row rows at a time; further workgroups take the
 //     queries.  9K tokens of 32 + 64 heads in fp16: 96 us, 4.6 TB/s (a large copy: 4.7).
 //   8 bits: the scale comes before the codes, so the page's new rows stay in registers, PASSES passes of them; keys and
@@ -347,7 +374,11 @@ __global__ __launch_bounds__(THREADS) void page_append_prompt_kernel(AppendArgs 
     __shared__ float sh_max[WAVES];
     __shared__ float sh_abs[WAVES][2][LEOAM_D];
     const int tid = threadIdx.x, col = (tid % LPR) * EPL, rg = tid / LPR, ps = a.page_size, hkv = a.n_kv_heads;
-    int unit = blockIdx.x, first = 0, last = 1;      // tensors
+    if ((int)blockIdx.x < a.batch) {
+        report<THREADS>(a, blockIdx.x, sh_max);
+        return;
+    }
+    int unit = blockIdx.x - a.batch, first = 0, last = 1;      // tensors
     if constexpr (kStore8) {
         first = last = unit & 1;
         unit >>= 1;
@@ -356,7 +387,7 @@ __global__ __launch_bounds__(THREADS) void page_append_prompt_kernel(AppendArgs 
         return;
     }
     const int h = unit % hkv;
-    const TouchedPage x = touched_page<THREADS>(a, unit / hkv, h == 0 && first == 0, sh_max);
+    const TouchedPage x = touched_page(a, unit / hkv, h == 0 && first == 0);
     if (x.count == 0) return;
     const size_t at = (size_t)x.id * hkv + h;
 #pragma unroll kStore8 ? 1 : 2
@@ -417,16 +448,21 @@ __global__ __launch_bounds__(THREADS) void page_append_prompt_kernel(AppendArgs 
 }
 
 // One token for each sequence: a wave to a (sequence, kv head), lanes of the first row's width hold the key and the value; further
-// waves take the queries.
+// waves report (in the first of these, before its own work, that took 0.25 us longer) and take the queries.
 template <typename T, bool kStore8> __global__ __launch_bounds__(LEOAM_WAVE) void page_append_token_kernel(AppendArgs a) {
     constexpr int EPL = T::kEpl, LPR = Row<T>::kLanesPerRow, ROWB = Row<T>::kRowBytes, STOREB = kStore8 ? LEOAM_D : ROWB, THREADS = LEOAM_WAVE;
     const int hkv = a.n_kv_heads, ps = a.page_size, tid = threadIdx.x, col = (tid % LPR) * EPL;
-    if ((int)blockIdx.x >= a.n_slots * hkv) {
-        append_queries<T, THREADS>(a, blockIdx.x - a.n_slots * hkv);
+    if ((int)blockIdx.x < a.batch) {
+        report<THREADS>(a, blockIdx.x, nullptr);
         return;
     }
-    const int h = blockIdx.x % hkv;
-    const TouchedPage x = touched_page<THREADS>(a, blockIdx.x / hkv, h == 0, nullptr);
+    const int unit = blockIdx.x - a.batch;
+    if (unit >= a.n_slots * hkv) {
+        append_queries<T, THREADS>(a, unit - a.n_slots * hkv);
+        return;
+    }
+    const int h = unit % hkv;
+    const TouchedPage x = touched_page(a, unit / hkv, h == 0);
     if (x.count == 0) return;
     const uint4 raw[2] = {load16(a.k, x.row0 * a.k_stride + (size_t)h * ROWB + col * T::kBytes),
                           load16(a.v, x.row0 * a.v_stride + (size_t)h * ROWB + col * T::kBytes)};
@@ -478,7 +514,7 @@ template <typename T> constexpr int queries_per_unit(int threads) { return 2 * (
 template <typename T, bool kStore8> static hipError_t launch_tokens(const AppendArgs& a, hipStream_t stream) {
     const int per = queries_per_unit<T>(LEOAM_WAVE);
     const long long q_units = a.q ? (long long)a.n_new * ((a.n_q_heads + per - 1) / per) : 0;
-    const long long units = (long long)a.n_slots * a.n_kv_heads + q_units;
+    const long long units = a.batch + (long long)a.n_slots * a.n_kv_heads + q_units;
     if (units > 0x7fffffffll) return hipErrorInvalidValue;
     hipLaunchKernelGGL((page_append_token_kernel<T, kStore8>), dim3((unsigned)units), dim3(LEOAM_WAVE), 0, stream, a);
     return hipGetLastError();
@@ -488,7 +524,7 @@ constexpr int kPromptThreads = 256;
 template <typename T, bool kStore8, int PASSES> static hipError_t launch_prompt(const AppendArgs& a, hipStream_t stream) {
     const int per = queries_per_unit<T>(kPromptThreads);
     const long long q_units = a.q ? (long long)a.n_new * ((a.n_q_heads + per - 1) / per) : 0, kv_units = (long long)a.n_slots * a.n_kv_heads;
-    const long long units = kStore8 ? 2 * kv_units : kv_units + q_units;
+    const long long units = a.batch + (kStore8 ? 2 * kv_units : kv_units + q_units);
     if (units > 0x7fffffffll || q_units > 0x7fffffffll) return hipErrorInvalidValue;
     hipLaunchKernelGGL((page_append_prompt_kernel<T, kStore8, kPromptThreads, PASSES>), dim3((unsigned)units), dim3(kPromptThreads), 0, stream, a);
     hipError_t e = hipGetLastError();

@@ -125,3 +125,34 @@ def test_abstract_of_a_page_begun_without_one(L, dtype, q8, single):
     n = 14 if single else 17
     c.append(make(n - 13), make(n - 13), None if single else i32([0, n - 13]), [n], table)
     c.check_rows(0, table, n)
+
+
+# ---- lists that descend ---------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype,q8", [(BF16, False), (F16, True)], ids=["bf16", "f16-e4m3"])
+@pytest.mark.parametrize("off", [[0, 100, 5, 12], [0, 10, 5, 12], [0, 12, -4, 12], [0, 5, 200, 12], [3, 1, 90, 100], [0, 40, 20, 60, 30, 100],
+                                 [0, 100] + [0] * 70 + [100], [0] * 70 + [90, 80, 100]],
+                         ids=lambda o: "-".join(map(str, o)) if len(o) < 9 else f"{len(o) - 1}-sequences" + str(o[-2]))
+def test_tokens_of_a_descending_list_are_reported(L, dtype, q8, off):
+    """Status 0 says that all of a sequence's tokens are stored and its queries are written."""
+    batch, page, hkv, hq = len(off) - 1, 16, 1, 2
+    new = [max(0, off[b + 1] - off[b]) for b in range(batch)]
+    per = 14
+    table = torch.arange(batch * per, dtype=torch.int32).reshape(batch, per)
+    x = torch.randn(100, hq + 2 * hkv, 128, generator=torch.Generator().manual_seed(7)).to(dtype).cuda()
+    c = Pool(L, dtype, q8, batch, hkv, page, per, batch * per, hq=hq)
+    q_out = torch.full((100, hq, 128), 7.0, dtype=dtype, device="cuda")
+    L.kv_page_append(c.pages, x[:, :hq], x[:, hq: hq + 1], x[:, hq + 1:], i32(off), i32([min(n, per * page) for n in new]), table.cuda(), None, q_out,
+                     c.k, c.v, c.ks, c.vs, c.abstract, c.off, c.n_chunks, c.status)
+    torch.cuda.synchronize()
+    status = c.status.tolist()
+    for b in range(batch):
+        assert status[b] in (0, 1)
+        if off[b] > off[b + 1] or off[b] < 0 or off[b + 1] > 100:
+            assert status[b] == 1, b
+        elif status[b] == 0 and new[b]:
+            K = c.values(0, table[b].long().cuda(), new[b])
+            assert torch.isfinite(K).all(), f"sequence {b} is said to be stored"
+            assert torch.equal(q_out[off[b]: off[b + 1]], x[off[b]: off[b + 1], :hq]), f"queries of sequence {b}"
+    if off == [0, 100, 5, 12]:
+        assert status[1] == 1 and 1 in (status[0], status[2])
