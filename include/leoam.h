@@ -494,7 +494,8 @@ typedef struct {
  *   abstract   [batch, n_kv_heads, max_pages, 2, 128] q_dtype (nullable): the page's rows become the maximum / minimum of
  *              all keys it then holds up to seq_len (as kv_chunk_abstract_build with the pages as chunks, c_max = max_pages),
  *              whatever the rows held: tokens may be taken back (seq_len lowered) and others appended in their places;
- *   chunk_off  [batch, max_pages + 1], n_chunks [batch] int32 (nullable): brought up to date with the pages as chunks,
+ *   chunk_off  [batch, max_pages + 1], n_chunks [batch] int32 (nullable): brought up to date with the pages as chunks (n_chunks[b] = 0
+ *              for a sequence of length 0),
  * so chunk_score and chunk_topk_select run on a leoam_shape with c_max = max_pages and n_ctx = max_pages * page_size.
  *   status[b] (nullable)  0 done; 1 seq_len[b] negative, beyond the capacity or below the number of new tokens, or new_off not
  *             ascending (where it descends, 1 is reported of every sequence that it costs tokens or queries; some of them may

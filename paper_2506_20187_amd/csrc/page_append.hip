@@ -184,7 +184,7 @@ template <int THREADS> __device__ __forceinline__ void report(const AppendArgs& 
     bad = (int)(group_max<THREADS>((float)bad, sh_max));
     if (tid != 0) return;
     if (a.status) a.status[b] = t.status ? t.status : bad ? 2 : 0;
-    if (a.n_chunks && !none) a.n_chunks[b] = last + 1;
+    if (a.n_chunks && (!none || (t.status == 0 && t.n == 0))) a.n_chunks[b] = last + 1;
 }
 
 // `slot` of the call's touched pages, by the whole workgroup

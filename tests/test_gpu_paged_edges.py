@@ -127,6 +127,20 @@ def test_abstract_of_a_page_begun_without_one(L, dtype, q8, single):
     c.check_rows(0, table, n)
 
 
+def test_an_idle_sequence_has_no_chunks(L):
+    c = Pool(L, BF16, False, 3, 2, 16, 3, 8)
+    table = torch.tensor([[0, 1, 2], [3, 4, 5], [6, 7, -1]], dtype=torch.int32)
+    x = torch.randn(60, 2, 128, generator=torch.Generator().manual_seed(1)).to(BF16).cuda()
+    c.append(x, x, i32([0, 20, 40, 60]), [20, 20, 20], table)
+    assert c.n_chunks.tolist() == [2, 2, 2]
+    c.append(x[:3], x[:3], None, [21, 0, 21], table)
+    assert c.n_chunks.tolist() == [2, 0, 2] and c.status.tolist() == [0, 0, 0]
+    c.append(x[:1], x[:1], i32([0, 1, 1, 1]), [22, 0, 21], table)      # (the last takes in nothing and stays as it is)
+    assert c.n_chunks.tolist() == [2, 0, 2]
+    c.append(x[:1], x[:1], i32([0, 1, 1, 1]), [23, 0, 0], table)
+    assert c.n_chunks.tolist() == [2, 0, 0]
+
+
 # ---- lists that descend ---------------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("dtype,q8", [(BF16, False), (F16, True)], ids=["bf16", "f16-e4m3"])
