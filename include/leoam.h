@@ -494,8 +494,12 @@ typedef struct {
  *   abstract   [batch, n_kv_heads, max_pages, 2, 128] q_dtype (nullable): the page's rows become the maximum / minimum of
  *              all keys it then holds up to seq_len (as kv_chunk_abstract_build with the pages as chunks, c_max = max_pages),
  *              whatever the rows held: tokens may be taken back (seq_len lowered) and others appended in their places;
- *   chunk_off  [batch, max_pages + 1], n_chunks [batch] int32 (nullable): brought up to date with the pages as chunks (n_chunks[b] = 0
- *              for a sequence of length 0),
+ *   chunk_off  [batch, max_pages + 1], n_chunks [batch] int32 (nullable): brought up to date with the pages as chunks;
+ *              n_chunks[b] says before the call of how many leading pages the rows and boundaries are here, and afterwards how many
+ *              pages there are (0 for a sequence of length 0).  Full pages from n_chunks[b] on that lie before the first page to
+ *              take a token - another sequence filled them and both list them, or there were no rows for them - are taken in by
+ *              the same call.  Where another sequence takes over a place in the batch, n_chunks[b] has to be 0: set, or left so by
+ *              a call in which the place was idle.  (NULL: only pages that take a token get rows and boundaries.)
  * so chunk_score and chunk_topk_select run on a leoam_shape with c_max = max_pages and n_ctx = max_pages * page_size.
  *   status[b] (nullable)  0 done; 1 seq_len[b] negative, beyond the capacity or below the number of new tokens, or new_off not
  *             ascending (where it descends, 1 is reported of every sequence that it costs tokens or queries; some of them may

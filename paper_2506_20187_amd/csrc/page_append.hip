@@ -169,24 +169,6 @@ __device__ __forceinline__ bool misses(const AppendArgs& a, int b, const Taken& 
     return found[0] != b || found[1] != b || found[2] != b || found[3] != b;
 }
 
-// what became of sequence b, by the whole workgroup
-template <int THREADS> __device__ __forceinline__ void report(const AppendArgs& a, int b, float* sh_max) {
-    const int tid = threadIdx.x, ps = a.page_size;
-    Taken t = taken_by(a, b);
-    if (t.status == 0 && a.new_off && t.m > 0 && misses(a, b, t)) t.status = 1;
-    const bool none = t.status || t.m == 0;
-    const int first = none ? 0 : (t.n - t.m) / ps, last = none ? -1 : (t.n - 1) / ps;
-    int bad = 0;
-    for (int p = first + tid; p <= last; p += THREADS) {
-        const int id = a.page_table[(size_t)b * a.max_pages + p];
-        bad |= id < 0 || id >= a.n_pages;
-    }
-    bad = (int)(group_max<THREADS>((float)bad, sh_max));
-    if (tid != 0) return;
-    if (a.status) a.status[b] = t.status ? t.status : bad ? 2 : 0;
-    if (a.n_chunks && (!none || (t.status == 0 && t.n == 0))) a.n_chunks[b] = last + 1;
-}
-
 // `slot` of the call's touched pages, by the whole workgroup
 __device__ __forceinline__ TouchedPage touched_page(const AppendArgs& a, int slot, bool bounds) {
     const int tid = threadIdx.x, ps = a.page_size;
@@ -281,11 +263,11 @@ __device__ __forceinline__ void store_token(char* page, int slot, int col, const
 // back since, or of whoever had this place in the batch before.  (us for a token each, row folded in : page read; one sequence, 8
 // heads, pages of 64 in bf16 3.5 : 4.2; 96 sequences, pages of 32 in 8 bits 5.4 : 5.5, of 64 5.4 : 5.8, in bf16 4.0 : 4.7, and of 256, 25 MB,
 // 4.0 : 9.4.  Sixteen loads on their way instead of eight: 8.8 for the last, 6.2 against 5.8 for pages of 32.)
-template <typename T, bool kStore8, int THREADS>
+template <typename T, bool kStore8, int THREADS, int BATCH>
 __device__ __forceinline__ void take_in_held(const char* page, int held, float scale, int col, float* mx, float* mn) {
-    constexpr int EPL = T::kEpl, LPR = Row<T>::kLanesPerRow, RPP = THREADS / LPR, BATCH = THREADS == LEOAM_WAVE ? 8 : 4;
+    constexpr int EPL = T::kEpl, LPR = Row<T>::kLanesPerRow, RPP = THREADS / LPR;
     constexpr int STOREB = kStore8 ? LEOAM_D : Row<T>::kRowBytes;
-    const int rg = threadIdx.x / LPR;
+    const int rg = threadIdx.x % THREADS / LPR;
     for (int r0 = 0; r0 < held; r0 += RPP * BATCH) {
         uint4 raw[BATCH];
 #pragma unroll
@@ -321,7 +303,7 @@ __device__ __forceinline__ void take_in_held(const char* page, int held, float s
 template <typename T, int THREADS>
 __device__ __forceinline__ void write_abstract(char* abs_row, int col, float* mx, float* mn, float (*sh)[2][LEOAM_D]) {
     constexpr int EPL = T::kEpl, LPR = Row<T>::kLanesPerRow, WAVES = THREADS / LEOAM_WAVE, ROWB = Row<T>::kRowBytes;
-    const int tid = threadIdx.x, lane = lane_id(), wave = tid / LEOAM_WAVE;
+    const int tid = threadIdx.x % THREADS, lane = lane_id(), wave = tid / LEOAM_WAVE;
 #pragma unroll
     for (int e = 0; e < EPL; ++e) {
 #pragma unroll
@@ -355,8 +337,47 @@ __device__ __forceinline__ void write_abstract(char* abs_row, int col, float* mx
     store16(abs_row, ROWB + col * T::kBytes, round_pack<T>(mn));
 }
 
-__device__ __forceinline__ char* abstract_row(const AppendArgs& a, const TouchedPage& x, int h, int row_bytes) {
-    return a.abstract + (((size_t)x.b * a.n_kv_heads + h) * a.max_pages + x.p) * 2 * row_bytes;
+__device__ __forceinline__ char* abstract_row(const AppendArgs& a, int b, int p, int h, int row_bytes) {
+    return a.abstract + (((size_t)b * a.n_kv_heads + h) * a.max_pages + p) * 2 * row_bytes;
+}
+
+// What became of sequence b, and its full pages from `n_chunks` to the first that takes a token - others filled them, or nobody
+// had rows for them - in the abstract and the boundaries.  One workgroup, since it alone reads and sets n_chunks; once for a
+// sequence and its prefix, so it need not be fast: a wave takes a (page, kv head) at a time (4096 tokens of 8 heads in bf16, pages of 64:
+// 0.3 ms in a prompt's call, 0.85 in a single token's; 64K 5 ms).
+template <typename T, bool kStore8, int THREADS> __device__ __forceinline__ void report(const AppendArgs& a, int b, float* sh_max) {
+    constexpr int EPL = T::kEpl, LPR = Row<T>::kLanesPerRow, ROWB = Row<T>::kRowBytes, STOREB = kStore8 ? LEOAM_D : ROWB;
+    const int tid = threadIdx.x, ps = a.page_size, hkv = a.n_kv_heads;
+    const int32_t* table = a.page_table + (size_t)b * a.max_pages;
+    const int known = a.n_chunks ? max(a.n_chunks[b], 0) : a.max_pages;
+    Taken t = taken_by(a, b);
+    if (t.status == 0 && a.new_off && t.m > 0 && misses(a, b, t)) t.status = 1;
+    const bool none = t.status || t.m == 0;
+    const int first = none ? 0 : (t.n - t.m) / ps, last = none ? -1 : (t.n - 1) / ps;
+    int bad = 0;
+    for (int p = first + tid; p <= last; p += THREADS) bad |= (uint32_t)table[p] >= (uint32_t)a.n_pages;
+    bad = (int)(group_max<THREADS>((float)bad, sh_max));      // (everybody has n_chunks)
+    if (tid == 0) {
+        if (a.status) a.status[b] = t.status ? t.status : bad ? 2 : 0;
+        if (a.n_chunks && (!none || (t.status == 0 && t.n == 0))) a.n_chunks[b] = last + 1;
+    }
+    if (known >= first) return;
+    if (a.chunk_off) {
+        int32_t* off = a.chunk_off + (size_t)b * (a.max_pages + 1);
+        for (int p = known + tid; p < first; p += THREADS) off[p + 1] = (p + 1) * ps;
+        if (known == 0 && tid == 0) off[0] = 0;
+    }
+    if (!a.abstract) return;
+    const int lane = lane_id(), col = (lane % LPR) * EPL;
+    for (int i = tid / LEOAM_WAVE; i < (first - known) * hkv; i += THREADS / LEOAM_WAVE) {
+        const int p = known + i / hkv, h = i % hkv, id = table[p];
+        if ((uint32_t)id >= (uint32_t)a.n_pages) continue;
+        const size_t at = (size_t)id * hkv + h;
+        float mx[EPL], mn[EPL];
+        no_extremes<EPL>(mx, mn);
+        take_in_held<T, kStore8, LEOAM_WAVE, THREADS == LEOAM_WAVE ? 8 : 4>(a.k_pages + at * ps * STOREB, ps, kStore8 ? a.k_scale[at] : 1.f, col, mx, mn);
+        write_abstract<T, LEOAM_WAVE>(abstract_row(a, b, p, h, ROWB), col, mx, mn, nullptr);
+    }
 }
 
 // Prompts: a touched page and a kv head to a workgroup, behind one for each sequence that reports on it.
@@ -375,7 +396,7 @@ __global__ __launch_bounds__(THREADS) void page_append_prompt_kernel(AppendArgs 
     __shared__ float sh_abs[WAVES][2][LEOAM_D];
     const int tid = threadIdx.x, col = (tid % LPR) * EPL, rg = tid / LPR, ps = a.page_size, hkv = a.n_kv_heads;
     if ((int)blockIdx.x < a.batch) {
-        report<THREADS>(a, blockIdx.x, sh_max);
+        report<T, kStore8, THREADS>(a, blockIdx.x, sh_max);
         return;
     }
     int unit = blockIdx.x - a.batch, first = 0, last = 1;      // tensors
@@ -407,7 +428,7 @@ __global__ __launch_bounds__(THREADS) void page_append_prompt_kernel(AppendArgs 
             rotate<EPL, LPR>(a, turn, col, y);
         };
         if constexpr (!kStore8) {
-            if (bounded) take_in_held<T, false, THREADS>(page, x.held, 1.f, col, mx, mn);
+            if (bounded) take_in_held<T, false, THREADS, 4>(page, x.held, 1.f, col, mx, mn);
             for (int r = rg; r < x.count + rg; r += RPP) {      // (uniform trip count)
                 float y[EPL];
                 unpack<T>(row_of(r), y);
@@ -441,9 +462,9 @@ __global__ __launch_bounds__(THREADS) void page_append_prompt_kernel(AppendArgs 
                 const int r = i * RPP + rg;
                 store_token<T, true>(page, x.held + min(r, x.count - 1), col, y[i], now, inv, r < x.count, mx, mn);
             }
-            if (bounded && !grows) take_in_held<T, true, THREADS>(page, x.held, now, col, mx, mn);      // (the rows' registers are free)
+            if (bounded && !grows) take_in_held<T, true, THREADS, 4>(page, x.held, now, col, mx, mn);      // (the rows' registers are free)
         }
-        if (bounded) write_abstract<T, THREADS>(abstract_row(a, x, h, ROWB), col, mx, mn, sh_abs);
+        if (bounded) write_abstract<T, THREADS>(abstract_row(a, x.b, x.p, h, ROWB), col, mx, mn, sh_abs);
     }
 }
 
@@ -453,7 +474,7 @@ template <typename T, bool kStore8> __global__ __launch_bounds__(LEOAM_WAVE) voi
     constexpr int EPL = T::kEpl, LPR = Row<T>::kLanesPerRow, ROWB = Row<T>::kRowBytes, STOREB = kStore8 ? LEOAM_D : ROWB, THREADS = LEOAM_WAVE;
     const int hkv = a.n_kv_heads, ps = a.page_size, tid = threadIdx.x, col = (tid % LPR) * EPL;
     if ((int)blockIdx.x < a.batch) {
-        report<THREADS>(a, blockIdx.x, nullptr);
+        report<T, kStore8, THREADS>(a, blockIdx.x, nullptr);
         return;
     }
     const int unit = blockIdx.x - a.batch;
@@ -476,7 +497,7 @@ template <typename T, bool kStore8> __global__ __launch_bounds__(LEOAM_WAVE) voi
     }
     float held_mx[EPL], held_mn[EPL];      // (read before anybody knows whether the scale grows: one round trip less)
     no_extremes<EPL>(held_mx, held_mn);
-    if (a.abstract) take_in_held<T, kStore8, THREADS>(a.k_pages + at * ps * STOREB, x.held, old[0], col, held_mx, held_mn);
+    if (a.abstract) take_in_held<T, kStore8, THREADS, 8>(a.k_pages + at * ps * STOREB, x.held, old[0], col, held_mx, held_mn);
 #pragma unroll
     for (int which = 0; which < 2; ++which) {
         char* page = (which ? a.v_pages : a.k_pages) + at * ps * STOREB;
@@ -505,7 +526,7 @@ template <typename T, bool kStore8> __global__ __launch_bounds__(LEOAM_WAVE) voi
             if (tid == 0) (which ? a.v_scale : a.k_scale)[at] = scale;
         }
         store_token<T, kStore8>(page, x.held, col, y, scale, inv, tid < LPR, mx, mn);
-        if (bounded) write_abstract<T, THREADS>(abstract_row(a, x, h, ROWB), col, mx, mn, nullptr);
+        if (bounded) write_abstract<T, THREADS>(abstract_row(a, x.b, x.p, h, ROWB), col, mx, mn, nullptr);
     }
 }
 

@@ -23,6 +23,10 @@ class PagedLayer:
       step        append, then attention of one token per sequence: over all pages, or - with `token_budget` or
                   `max_chunks` - chunk_score, chunk_topk_select with the pages as chunks, attention over the kept ones
       prompt      append, then causal attention of the new tokens
+
+    Sequences may list pages that others filled, and tokens may be taken back (`seq_len` lowered before the next append).
+    Under a budget a place in the batch that another sequence takes over must be idle (length 0) for a step in between, or
+    have its `n_chunks` set to 0: the rows of abstracts are the place's, and are made anew from the pages then.
     """
 
     def __init__(self, page_table: torch.Tensor, seq_len: torch.Tensor, n_q_heads: int, n_kv_heads: int, n_pages: int,
@@ -50,7 +54,7 @@ class PagedLayer:
         if self.selects:
             k_max = min(max_pages, int(k_max) or max_pages)
             self.shape = B.make_shape(batch, n_q_heads, n_kv_heads, head_dim, max_pages * page_size, max_pages, k_max, dtype)
-            self.abstract = torch.empty(batch, n_kv_heads, max_pages, 2, head_dim, dtype=dtype, device=dev)
+            self.abstract = torch.zeros(batch, n_kv_heads, max_pages, 2, head_dim, dtype=dtype, device=dev)
             self.chunk_off = torch.zeros(batch, max_pages + 1, dtype=torch.int32, device=dev)
             self.n_chunks = torch.zeros(batch, dtype=torch.int32, device=dev)
             self.score = torch.empty(batch, n_kv_heads, max_pages, dtype=torch.float32, device=dev)

@@ -141,6 +141,91 @@ def test_an_idle_sequence_has_no_chunks(L):
     assert c.n_chunks.tolist() == [2, 0, 0]
 
 
+# ---- pages that others filled ---------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype,q8", KINDS, ids=KIND_IDS)
+@pytest.mark.parametrize("single", [True, False], ids=["tokens", "prompt"])
+def test_rows_of_shared_pages(L, dtype, q8, single):
+    # a sequence that begins behind the pages of another: n_chunks says how many of its rows are there already
+    g = torch.Generator().manual_seed(5)
+    page, hkv = 16, 3
+    c = Pool(L, dtype, q8, 3, hkv, page, 8, 24)
+    table = torch.randperm(24, generator=g).to(torch.int32).reshape(3, 8)
+    make = lambda n: torch.randn(n, hkv, 128, generator=g).to(dtype).cuda()  # noqa: E731
+    c.append(make(100 + 30), make(130), i32([0, 100, 100, 130]), [100, 0, 30], table)
+    table[1, :5], table[2, :6] = table[0, :5], table[0, :6]
+    c.n_chunks[2] = 0      # (it had a sequence of its own before)
+    lens = [101, 81, 97] if single else [100, 85, 120]
+    c.append(make(3) if single else make(29), make(3) if single else make(29), None if single else i32([0, 0, 5, 29]), lens, table)
+    assert c.status.tolist() == [0, 0, 0]
+    for b in range(3):
+        c.check_rows(b, table, lens[b])
+    # rows that are there are not looked at; pages outside the pool are passed over
+    c.abstract[1, :, :2] = 55.0
+    c.abstract[1, :, 3] = 66.0
+    c.n_chunks[1] = 2
+    table[1, 3] = -1
+    lens[1] += 1
+    c.append(make(1), make(1), i32([0, 0, 1, 1]), lens, table)
+    assert (c.abstract[1, :, :2] == 55).all() and (c.abstract[1, :, 3] == 66).all()
+    K = c.values(0, table[1, 2:3].long().cuda(), page)
+    assert torch.equal(c.abstract[1, :, 2, 0].double(), K.amax(1)) and torch.equal(c.abstract[1, :, 2, 1].double(), K.amin(1))
+    assert c.off[1, :7].tolist() == [0, 16, 32, 48, 64, 80, lens[1]]
+
+
+@pytest.mark.parametrize("dtype,q8", [(BF16, False), (F16, True), (F32, False)], ids=["bf16", "f16-e4m3", "f32"])
+@pytest.mark.parametrize("reused", [False, True], ids=["fresh", "reused"])
+def test_layer_selects_among_shared_pages(L, dtype, q8, reused):
+    """A sequence behind another's pages, under a budget, against the same tokens in pages of its own."""
+    g = torch.Generator().manual_seed(6)
+    hq, hkv, page, head = 8, 2, 16, 96      # six pages in common
+    n = [150, 130]
+    x = torch.randn(n[0], hq + 2 * hkv, 128, generator=g)
+    y = torch.randn(n[1] - head, hq + 2 * hkv, 128, generator=g)
+    tail = torch.cat([x[:head], y]).to(dtype).cuda()      # the second sequence, whole
+    x, y = x.to(dtype).cuda(), y.to(dtype).cuda()
+    steps = [torch.randn(2, hq + 2 * hkv, 128, generator=g).to(dtype).cuda() for _ in range(3)]
+    parts = lambda t: (t[:, :hq], t[:, hq: hq + hkv], t[:, hq + hkv:])  # noqa: E731
+    table, n_pages = spread([160, 160], page, g)
+    got = []
+    for shared in (False, True):
+        t = table.clone()
+        seq_len = i32([0, 0])
+        if shared:
+            t[1, : head // page] = t[0, : head // page]
+        layer = L.PagedLayer(t.cuda(), seq_len, hq, hkv, n_pages, page, dtype, L.E4M3 if q8 else None, token_budget=64)
+        if reused:      # somebody was there before, behind pages of his own, and left
+            mine = layer.page_table.clone()
+            layer.page_table.copy_(table)
+            seq_len.copy_(i32([1, 140]))
+            layer.prompt(*parts(torch.cat([x, x])[:141]), i32([0, 1, 141]))
+            seq_len.zero_()
+            layer.step(*parts(x[:2]))
+            layer.page_table.copy_(mine)
+        else:
+            layer.abstract.fill_(9.0)
+        seq_len.copy_(i32([n[0], 0]))
+        layer.prompt(*parts(x), i32([0, n[0], n[0]]))
+        seq_len.copy_(i32(n))
+        new = parts(y) if shared else parts(tail)
+        out = layer.prompt(*new, i32([0, 0, new[0].shape[0]]))[-y.shape[0]:]
+        kept = [out]
+        for s in steps:
+            seq_len.add_(1)
+            layer.step(*parts(s))
+            kept += [layer.out.clone(), layer.lse.clone(), layer.sel_count.clone(), layer.sel_idx.clone()]
+        torch.cuda.synchronize()
+        got.append(kept)
+    for i, (a, b) in enumerate(zip(*got)):
+        if i and i % 4 == 0:      # (entries past the count may be anything)
+            listed = torch.arange(a.shape[2], device="cuda") < got[0][i - 1][..., None]
+            a, b = a[listed], b[listed]
+        if i == 0:
+            assert torch.isfinite(a).all() and float((a.double() - b.double()).abs().max()) < 0.1      # (rows in other tiles)
+        else:
+            assert torch.equal(a, b), i
+
+
 # ---- lists that descend ---------------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("dtype,q8", [(BF16, False), (F16, True)], ids=["bf16", "f16-e4m3"])
