@@ -516,7 +516,8 @@ int kv_page_append(const leoam_pages* pages, const void* q, int64_t q_stride, co
  *   z_t = softmax_scale * (q_j . K_t),  out[b,j,:] = sum_t softmax(z)_t V_t  (float),  lse[b,j] = log sum_t exp(z_t).
  * With sel_idx [batch, n_kv_heads, k_max] and sel_count [batch, n_kv_heads] (both or neither) only over the tokens of
  * the listed pages (places in the sequence, as chunk_topk_select writes them; ids outside the sequence add nothing; a
- * page listed twice counts twice).  Nothing to attend to: out = 0, lse = -inf.  lse may be NULL.
+ * page listed twice counts twice).  Nothing to attend to: out = 0, lse = -inf.  lse may be NULL.  Of a value that is attended to
+ * and not finite the channel becomes infinite or NaN.
  * Workspace: leoam_page_workspace_bytes(pages, 0) gives the intended launch; less gives fewer splits
  * (LEOAM_E_WORKSPACE below leoam_page_workspace_min()).  16-byte aligned, contents irrelevant.
  * Calls that share a workspace must not overlap.
@@ -528,7 +529,9 @@ int page_attention_decode(const leoam_pages* pages, const void* q, const void* k
 
 /*
  * Causal attention of the new tokens (already appended): row r of q [n_new, Hq, 128] has position t and attends to
- * positions 0 .. t of its sequence.  out [n_new, Hq, 128] in q_dtype, rounded once; lse [n_new, Hq] float, nullable.  What
+ * positions 0 .. t of its sequence.  out [n_new, Hq, 128] in q_dtype; lse [n_new, Hq] float, nullable.  Under fp16 and bf16 the
+ * weights are rounded to q_dtype before they meet the values (their sum is not, nor are they in page_attention_decode): out is within
+ * 2^-11 (fp16) or 2^-8 (bf16) of sum_t softmax(z)_t |V_t| from its value in 32 bits, and then rounded itself.  What
  * stands at positions beyond t, NaN and infinities included, does not reach the row.  Rows outside every sequence, and rows
  * of a sequence with seq_len[b] below its number of new tokens whose position is negative, have nothing to attend to: the
  * former are left as they are, the latter get out = 0, lse = -inf.  Workspace as above, of

@@ -6,9 +6,9 @@
 // rounding to the page's type: what a plain evaluation gives, bit for bit.
 //
 // Bytes-bound (a row is read once and written once) for prompts, a chain of dependent round trips
-// (length -> page -> old scale) for single tokens.  One workgroup owns a (touched page, kv head, tensor): the scale
-// of an 8-bit page needs the largest magnitude over all that enters it, and the page's abstract row the maximum and
-// minimum, so nobody else may touch them.
+// (length -> page -> old scale) for single tokens.  One workgroup owns a (touched page, kv head), of 8-bit prompts one of its
+// tensors: the scale of an 8-bit page needs the largest magnitude over all that enters it, and the page's abstract row the
+// maximum and minimum, so nobody else may touch them.
 #include "page_common.h"
 
 namespace leoam {
@@ -36,7 +36,7 @@ __device__ __forceinline__ Taken taken_by(const AppendArgs& a, int b) {
     return Taken{row0, m, n, misfit ? 1 : a.rot_dim && m && n > a.rope_len ? 3 : 0};
 }
 
-// The cosines and sines that the EPL channels from `col` need, 0-channel pairs beyond rot_dim left alone.
+// The cosines and sines that the EPL channels from `col` need (channels from rot_dim on: none).
 template <int EPL> struct Turn {
     float c[EPL], s[EPL];
     __device__ __forceinline__ void load(const AppendArgs& a, int pos, int col) {

@@ -5,7 +5,10 @@
 // 32): the next tile (8 bits: the next two) is on its way to registers while the current one is worked on in LDS.
 // Each of the four waves owns 32 rows.  S^T = K Q^T (32x32 products) leaves lane = row, registers = keys: the row's
 // maximum and sum need no exchange but one with the lane 32 away, and P is already the second operand of O^T = V^T P^T;
-// the first operand, four keys of one channel at a time, comes out of LDS by the transposing read.
+// the first operand, four keys of one channel at a time, comes out of LDS by the transposing read.  For that P is rounded to the
+// model's type, as the stored values are; the row's sum takes it before.  P in two parts, as decoding has it where the matrix cores
+// are idle, doubles the second product: 8192 tokens in bf16 589 -> 772 us, 8-bit prompts behind histories 361 -> 477, for an output of
+// bf16 that is off by 4.9e-4 (its own rounding) instead of 6.6e-4, root mean square; fp16 6.5e-5 instead of 8.5e-5.
 //
 // A unit of work is (128 rows, kv head).  With enough units to fill the chip each takes a workgroup.  With few (a
 // handful of rows behind a long context) the key tiles of all units are laid end to end, each unit's beginning counted as
