@@ -27,11 +27,15 @@ class PagedLayer:
     Sequences may list pages that others filled, and tokens may be taken back (`seq_len` lowered before the next append).
     Under a budget a place in the batch that another sequence takes over must be idle (length 0) for a step in between, or
     have its `n_chunks` set to 0: the rows of abstracts are the place's, and are made anew from the pages then.
+
+    Calls of one layer must not overlap, on two streams or as two graphs: they share its buffers.  Workspaces (up to 66 MiB each)
+    hold nothing between calls: `workspaces_of` another layer makes this one use that one's, as the layers of a model can, whose
+    calls follow one another on one stream.
     """
 
     def __init__(self, page_table: torch.Tensor, seq_len: torch.Tensor, n_q_heads: int, n_kv_heads: int, n_pages: int,
                  page_size: int, dtype: torch.dtype, kv_dtype=None, rope: torch.Tensor = None, interleaved: bool = False,
-                 k_max: int = 0, max_chunks: int = 0, token_budget: int = 0, head_dim: int = 128):
+                 k_max: int = 0, max_chunks: int = 0, token_budget: int = 0, head_dim: int = 128, workspaces_of: "PagedLayer" = None):
         batch, max_pages = page_table.shape
         rope_len, rot_dim = rope.shape if rope is not None else (0, 0)
         self.page_table, self.seq_len, self.rope = page_table, seq_len, rope
@@ -60,8 +64,13 @@ class PagedLayer:
             self.score = torch.empty(batch, n_kv_heads, max_pages, dtype=torch.float32, device=dev)
             self.sel_idx = torch.empty(batch, n_kv_heads, k_max, dtype=torch.int32, device=dev)
             self.sel_count = torch.empty(batch, n_kv_heads, dtype=torch.int32, device=dev)
-        self.workspace = self._new(B.leoam_page_workspace_bytes(self.pages, 0), torch.uint8, None)
-        self.prompt_workspaces = []      # the last is the largest; earlier ones stay, a captured graph may use them
+        need = B.leoam_page_workspace_bytes(self.pages, 0)
+        if workspaces_of is not None and workspaces_of.workspace.numel() >= need:
+            self.workspace = workspaces_of.workspace
+        else:
+            self.workspace = self._new(need, torch.uint8, None)
+        # the last is the largest; earlier ones stay, a captured graph may use them
+        self.prompt_workspaces = [] if workspaces_of is None else workspaces_of.prompt_workspaces
         self.scale = B.default_scale(head_dim)
 
     def _new(self, shape, dtype, stream) -> torch.Tensor:

@@ -255,3 +255,30 @@ def test_tokens_of_a_descending_list_are_reported(L, dtype, q8, off):
             assert torch.equal(q_out[off[b]: off[b + 1]], x[off[b]: off[b + 1], :hq]), f"queries of sequence {b}"
     if off == [0, 100, 5, 12]:
         assert status[1] == 1 and 1 in (status[0], status[2])
+
+
+# ---- layers that share workspaces -------------------------------------------------------------------------------
+
+def test_layers_share_workspaces(L):
+    g = torch.Generator().manual_seed(8)
+    hq, hkv, page, n = 8, 2, 32, [700, 40]
+    table, n_pages = spread([n[0] + 4, n[1] + 4], page, g)
+    x = [torch.randn(sum(n), hq + 2 * hkv, 128, generator=g).to(BF16).cuda() for _ in range(3)]
+    s = [torch.randn(2, hq + 2 * hkv, 128, generator=g).to(BF16).cuda() for _ in range(3)]
+    parts = lambda t: (t[:, :hq], t[:, hq: hq + hkv], t[:, hq + hkv:])  # noqa: E731
+    got = []
+    for together in (False, True):
+        seq_len = i32(n)
+        layers = []
+        for i in range(3):
+            layers.append(L.PagedLayer(table.cuda(), seq_len, hq, hkv, n_pages, page, BF16, L.E4M3 if i == 1 else None, token_budget=96 * (i == 2),
+                                       workspaces_of=layers[0] if together and i else None))
+        out = [layer.prompt(*parts(a), i32([0, n[0], sum(n)])) for layer, a in zip(layers, x)]
+        seq_len.add_(1)
+        out += [layer.step(*parts(a)) for layer, a in zip(layers, s)]
+        torch.cuda.synchronize()
+        got.append(out)
+        held = {w.data_ptr(): w.numel() for layer in layers for w in [layer.workspace] + layer.prompt_workspaces}
+        assert len(held) == (2 if together else 6)
+    for a, b in zip(*got):
+        assert torch.equal(a, b)
