@@ -384,7 +384,7 @@ template <typename T, bool kStore8, int THREADS> __device__ __forceinline__ void
 //   16 / 32 bits (PASSES = 0): keys, then values, a pass of THREADS / lanes-per-row rows at a time; further workgroups take the
 //     queries.  9K tokens of 32 + 64 heads in fp16: 96 us, 4.6 TB/s (a large copy: 4.7).
 //   8 bits: the scale comes before the codes, so the page's new rows stay in registers, PASSES passes of them; keys and
-//     values are workgroups of their own, and so are the queries in a launch of their own.  16K tokens of 32 + 16 heads: 94 us
+//     values are workgroups of their own, and so are the queries in a launch of their own.  16K tokens of 32 + 16 heads: 93 us
 //     against 134 with the former's shape (the queries at a quarter of the occupancy).
 // Workgroups of four heads, which would load the angles of a token once for them, were slower (144 against 93 us for the
 // keys and values of the former, 78 against 58 for the latter): a page then takes longer than there are pages to overlap.
