@@ -485,9 +485,10 @@ typedef struct {
  * receives the rotated query, rounded once; q and q_out may both be NULL.  Keys (rotated) and values go to their places
  * in the pages, rounded once.  n_new == 0: nothing is done.
  * LEOAM_E4M3: scale = the smallest power of two s with |x| <= 448 s for all finite x that the page holds so far (0 for
- * none but zeros; it never falls while a page fills up, nor when tokens are taken back; a page's first token starts it anew), code = round-half-even(x /
- * scale); infinities are stored as +-448 scale (so as 0 where nothing else but zeros is held), NaN as NaN.  What
- * the largest scale does not reach is stored as +-448 of it: beyond 57344 under fp16 (2^7), 1.75 * 2^126 under bf16 (2^118).
+ * none but zeros; it never falls while a page fills up, nor when tokens are taken back; a page's first token starts it anew),
+ * code = round-half-even(x / scale); infinities are stored as +-448 scale (so as 0 where nothing else but zeros is held), NaN as
+ * NaN.  What the largest scale does not reach is stored as +-448 of it: beyond 57344 under fp16 (2^7), 1.75 * 2^126 under bf16
+ * (2^118).
  * When a new token raises a page's scale, its older codes are encoded again from their stored values (exact but for codes that
  * become subnormal).
  * Every page that takes a token must belong to one sequence only.  For each of them

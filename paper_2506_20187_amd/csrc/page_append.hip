@@ -369,8 +369,8 @@ template <typename T, bool kStore8, int THREADS> __device__ __forceinline__ void
     }
     if (!a.abstract) return;
     const int lane = lane_id(), col = (lane % LPR) * EPL;
-    for (int i = tid / LEOAM_WAVE; i < (first - known) * hkv; i += THREADS / LEOAM_WAVE) {
-        const int p = known + i / hkv, h = i % hkv, id = table[p];
+    for (long long i = tid / LEOAM_WAVE; i < (long long)(first - known) * hkv; i += THREADS / LEOAM_WAVE) {
+        const int p = known + (int)(i / hkv), h = (int)(i % hkv), id = table[p];
         if ((uint32_t)id >= (uint32_t)a.n_pages) continue;
         const size_t at = (size_t)id * hkv + h;
         float mx[EPL], mn[EPL];
