@@ -24,6 +24,13 @@
  *   page_attention_decode          Eq. (1) for one token per sequence over all of its
  *                                  pages, or over the pages chunk_topk_select kept.
  *   page_attention_prefill         causal attention of a prompt's tokens.
+ *   kv_page_append_at              kv_page_append with positions of the caller's, on several axes.
+ *   page_attention_decode_shared   page_attention_decode for groups of sequences that begin with
+ *                                  the same pages: those are read once for the group.
+ *   page_weight_add                the attention that each cached token got, added up.
+ *   page_evict_select              which tokens stay (the first, the most recent, those with the
+ *                                  most weight) and which rows move to the places of the others.
+ *   kv_page_move                   those rows moved.
  *
  * Conventions (all entry points)
  *   - Every pointer except `const leoam_shape*` is a DEVICE pointer owned by the
@@ -542,6 +549,101 @@ int page_attention_prefill(const leoam_pages* pages, const void* q, int32_t n_ne
                            const void* k_pages, const void* v_pages, const float* k_scale, const float* v_scale,
                            const int32_t* page_table, const int32_t* seq_len, float softmax_scale, void* out, float* lse,
                            void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * kv_page_append, but for the rotation: with p = position[axis[i]][r] for row r, pair i turns by c_i = rope[p][i],
+ * s_i = rope[p][rot_dim/2 + i].  For tokens whose place in the cache is not their position (after an eviction), and for positions
+ * on several axes, as time, height and width.
+ *   position  [n_axes][n_new] int32, 1 <= n_axes <= LEOAM_MAX_AXES
+ *   axis      [rot_dim/2] int32, the axis that each pair belongs to; not looked at (NULL) if n_axes == 1
+ * A position outside [0, rope_len) is taken as the nearest in it, an axis outside [0, n_axes) as the nearest of them.  status is
+ * as above but for 3: some position of the sequence's rows, on whatever axis, lies outside the table - its tokens are stored all
+ * the same.  (Places may lie beyond rope_len.)  rot_dim == 0: positions are not looked at.
+ */
+#define LEOAM_MAX_AXES 8
+int kv_page_append_at(const leoam_pages* pages, const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
+                      int64_t v_stride, int32_t n_new, const int32_t* new_off, const int32_t* seq_len,
+                      const int32_t* page_table, const float* rope, const int32_t* position, int32_t n_axes, const int32_t* axis,
+                      void* q_out, void* k_pages, void* v_pages, float* k_scale, float* v_scale, void* abstract,
+                      int32_t* chunk_off, int32_t* n_chunks, int32_t* status, void* stream);
+
+/*
+ * page_attention_decode over all pages (same arguments and results), where groups of sequences that follow one another list the
+ * same pages first: what they share is read once for the group.
+ *   group_off    [n_groups + 1] int32, 0 <= off[0] <= ... <= off[n_groups] <= batch, n_groups <= batch: sequences off[g] ..
+ *                off[g + 1] - 1 are group g; a sequence outside of all groups shares nothing
+ *   group_pages  [n_groups] int32: the first so many entries of page_table are the same for the whole group (0: none)
+ * A sequence of a group that is shorter than group_pages[g] * page_size (an idle one among them) is attended to by itself, and
+ * its row of page_table need not be the group's.  A list that descends leaves the results of its sequences undefined.
+ * Workspace: leoam_page_shared_workspace_bytes() gives the intended launch, less gives fewer splits (LEOAM_E_WORKSPACE below
+ * leoam_page_shared_workspace_min()).  16-byte aligned, contents irrelevant.  Calls that share a workspace must not overlap.
+ */
+int page_attention_decode_shared(const leoam_pages* pages, const void* q, const void* k_pages, const void* v_pages,
+                                 const float* k_scale, const float* v_scale, const int32_t* page_table, const int32_t* seq_len,
+                                 int32_t n_groups, const int32_t* group_off, const int32_t* group_pages, float softmax_scale,
+                                 float* out, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+size_t leoam_page_shared_workspace_bytes(const leoam_pages* pages, int32_t n_groups);
+size_t leoam_page_shared_workspace_min(const leoam_pages* pages);
+
+/*
+ * How much of the attention of the call's rows each cached token got.  Row r of q [n_new, Hq, 128] (rotated, as the attention
+ * call took it) has place p in its sequence (new_off as above: the last rows are the sequence's last tokens) and lse [n_new, Hq] is
+ * what the attention call left.  For every sequence b with m rows, kv head h and place t < seq_len[b]:
+ *   weight[b,h,t] = decay * (t < seq_len[b] - m ? weight_before[b,h,t] : 0)
+ *                   + sum over rows r with p >= t, heads j of h's group, of exp(softmax_scale * (q[r,j] . K_t) - lse[r,j]).
+ *   weight, weight_before  [batch, n_kv_heads, max_pages * page_size] float; they may be the same array; weight_before may be NULL
+ *                          (zeros).  Places at or beyond seq_len are left as they are.
+ *   n_seen, token_id       (both or neither) token_id [batch, n_kv_heads, max_pages * page_size] int32 numbers the tokens
+ *                          in the order in which the sequence got them; n_seen [batch] int32 is how many it ever had, these rows
+ *                          counted in.  The rows' own places get n_seen[b] - (seq_len[b] - t); others are left as they are.
+ * Rows with lse = -inf (nothing was attended to) add nothing, nor do rows whose place is negative; tokens of a page that is not in
+ * the pool get nothing.  Of the queries of a long prompt the last ones alone may be given (their logarithms with them): weight_before
+ * then stands for the tokens before them, and their numbers are the caller's to set.  Sums are in binary32, each token's in an order
+ * that depends on the call's shape only.
+ */
+int page_weight_add(const leoam_pages* pages, const void* q, int32_t n_new, const int32_t* new_off, const void* k_pages,
+                    const float* k_scale, const int32_t* page_table, const int32_t* seq_len, float softmax_scale, const float* lse,
+                    float decay, const float* weight_before, float* weight, const int32_t* n_seen, int32_t* token_id, void* stream);
+
+/*
+ * Which tokens stay where a sequence is brought down to keep_len[b] tokens.  Per (sequence, kv head) tokens are ordered: first
+ * the protected ones - places below n_first[b], and the n_recent tokens that came last -, then by weight descending; equal ones
+ * and protected ones by place ascending; NaN is below every weight.  The first keep_len[b] of the order stay.  Those of them at places
+ * below keep_len[b] stay where they are, the others move to the places that become free, both in ascending order:
+ *   moves       [batch, n_kv_heads, m_max, 2] int32: (place that becomes free, place of the token that moves there); entries from
+ *               move_count[b,h] on are left as they are
+ *   move_count  [batch, n_kv_heads] int32
+ *   new_len     [batch] int32: keep_len[b], or seq_len[b] if the sequence is not longer than that
+ *   token_id, n_seen  (both or neither) as page_weight_add keeps them: a token is recent if its number is n_seen[b] - n_recent or
+ *               more.  NULL: places tell (nothing was ever moved).
+ *   n_first     [batch] int32, nullable (0)
+ *   status[b]   (nullable) 0 done; 1 nothing was done, new_len[b] = seq_len[b]: a length is negative or beyond the capacity, or
+ *               min(keep_len[b], seq_len[b] - keep_len[b]) > m_max, the most rows that may move.
+ * Attention does not depend on the order in which a cache holds its tokens, and keys carry their rotation, so nothing else moves.
+ * Places of pages that other sequences list too must be protected (n_first).  Workspace: leoam_page_evict_workspace_bytes(), 16-byte
+ * aligned, contents irrelevant.
+ */
+int page_evict_select(const leoam_pages* pages, const float* weight, const int32_t* token_id, const int32_t* n_seen,
+                      const int32_t* seq_len, const int32_t* keep_len, const int32_t* n_first, int32_t n_recent, int32_t* moves,
+                      int32_t m_max, int32_t* move_count, int32_t* new_len, int32_t* status, void* workspace, size_t workspace_bytes,
+                      void* stream);
+size_t leoam_page_evict_workspace_bytes(const leoam_pages* pages);
+
+/*
+ * Rows moved as page_evict_select lists them: keys, values and - where given - weights and numbers.  For every pair (to, from) of
+ * move_count[b,h], to ascending, to < new_len[b] <= from < old_len[b] (pairs outside of that, and pairs of pages that are not in the
+ * pool, are left out).  Sequences with new_len[b] >= old_len[b] are left alone; seq_len itself is the caller's to set, once for all
+ * layers of a model.  Where n_chunks etc. are given,
+ *   abstract   rows of the pages that tokens moved to, and of the last page, become the maximum / minimum of the keys they then hold
+ *              below new_len[b];
+ *   chunk_off, n_chunks  end at new_len[b].
+ * LEOAM_E4M3: the scale of a page that tokens move to becomes the smallest power of two that is no smaller than it was and reaches
+ * all that moves there; where it rises, the page's older codes are encoded again, as in kv_page_append.
+ * What stands at places from new_len[b] on may change.  Pages that tokens move to must belong to one sequence only.
+ */
+int kv_page_move(const leoam_pages* pages, const int32_t* moves, int32_t m_max, const int32_t* move_count, const int32_t* old_len,
+                 const int32_t* new_len, const int32_t* page_table, void* k_pages, void* v_pages, float* k_scale, float* v_scale,
+                 float* weight, int32_t* token_id, void* abstract, int32_t* chunk_off, int32_t* n_chunks, void* stream);
 
 /* Bytes of workspace for page_attention_decode (n_new <= 0) or page_attention_prefill over n_new rows.  0 on a bad shape. */
 size_t leoam_page_workspace_bytes(const leoam_pages* pages, int32_t n_new);

@@ -13,7 +13,8 @@ from .binding import (  # noqa: F401
     leoam_fused_workspace_bytes, leoam_fused_control_bytes, leoam_workspace_init, kv_chunk_abstract_append, leoam_tree_evaluations, chunk_tree_refine,
     leoam_tree_workspace_bytes, kv_chunk_compress, kv_chunk_recompress, chunk_compression_tags, leoam_compressed_bytes_bound, leoam_compression_share,
     E4M3, Pages, make_pages, kv_page_append, page_attention_decode, page_attention_prefill, leoam_page_workspace_bytes,
-    leoam_page_workspace_min,
+    leoam_page_workspace_min, kv_page_append_at, page_attention_decode_shared, leoam_page_shared_workspace_bytes,
+    leoam_page_shared_workspace_min, page_weight_add, page_evict_select, leoam_page_evict_workspace_bytes, kv_page_move,
     leoam_validate_boundaries, leoam_copy_probe, leoam_read_probe,
     status_string, version, default_scale,
 )

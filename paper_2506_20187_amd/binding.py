@@ -85,6 +85,17 @@ def _load() -> ctypes.CDLL:
     lib.leoam_page_workspace_bytes.restype = sz
     lib.leoam_page_workspace_min.argtypes = [pp]
     lib.leoam_page_workspace_min.restype = sz
+    lib.kv_page_append_at.argtypes = [pp, vp, i64, vp, i64, vp, i64, i32] + [vp] * 5 + [i32] + [vp] * 11
+    lib.page_attention_decode_shared.argtypes = [pp] + [vp] * 7 + [i32, vp, vp, f32, vp, vp, vp, sz, vp]
+    lib.leoam_page_shared_workspace_bytes.argtypes = [pp, i32]
+    lib.leoam_page_shared_workspace_bytes.restype = sz
+    lib.leoam_page_shared_workspace_min.argtypes = [pp]
+    lib.leoam_page_shared_workspace_min.restype = sz
+    lib.page_weight_add.argtypes = [pp, vp, i32] + [vp] * 5 + [f32, vp, f32] + [vp] * 5
+    lib.page_evict_select.argtypes = [pp] + [vp] * 6 + [i32, vp, i32, vp, vp, vp, vp, sz, vp]
+    lib.leoam_page_evict_workspace_bytes.argtypes = [pp]
+    lib.leoam_page_evict_workspace_bytes.restype = sz
+    lib.kv_page_move.argtypes = [pp, vp, i32] + [vp] * 14
     lib.leoam_workspace_init.argtypes = [vp, sz, vp]
     lib.leoam_validate_boundaries.argtypes = [sp, vp, vp, vp]
     lib.leoam_copy_probe.argtypes = [vp, vp, sz, vp]
@@ -96,6 +107,7 @@ def _load() -> ctypes.CDLL:
                  "chunk_select_attention_decode", "chunk_select_attention_decode_static", "kv_chunk_abstract_append", "chunk_tree_refine",
                  "kv_chunk_compress", "kv_chunk_recompress", "chunk_compression_tags", "leoam_workspace_init",
                  "kv_page_append", "page_attention_decode", "page_attention_prefill",
+                 "kv_page_append_at", "page_attention_decode_shared", "page_weight_add", "page_evict_select", "kv_page_move",
                  "leoam_validate_boundaries", "leoam_copy_probe", "leoam_read_probe"):
         getattr(lib, name).restype = ctypes.c_int
     return lib
@@ -111,6 +123,8 @@ EXPORTS = ("kv_chunk_abstract_build", "chunk_score", "chunk_score_pin", "chunk_t
            "kv_chunk_compress", "kv_chunk_recompress", "chunk_compression_tags", "leoam_compressed_bytes_bound", "leoam_compression_share",
            "kv_page_append", "page_attention_decode", "page_attention_prefill", "leoam_page_workspace_bytes",
            "leoam_page_workspace_min",
+           "kv_page_append_at", "page_attention_decode_shared", "leoam_page_shared_workspace_bytes", "leoam_page_shared_workspace_min",
+           "page_weight_add", "page_evict_select", "leoam_page_evict_workspace_bytes", "kv_page_move",
            "leoam_workspace_bytes", "leoam_validate_boundaries", "leoam_copy_probe", "leoam_read_probe", "leoam_status_string",
            "leoam_version")
 
@@ -154,7 +168,8 @@ def _load_bind():
     _bind.setup(Shape, Pages, _p, _stream, *(ctypes.cast(getattr(_lib, n), ctypes.c_void_p).value for n in (
         "chunk_score", "chunk_score_pin", "kv_chunk_abstract_append", "chunk_topk_select",
         "sparse_chunk_attention_decode", "chunk_select_attention_decode",
-        "kv_page_append", "page_attention_decode", "page_attention_prefill")))
+        "kv_page_append", "page_attention_decode", "page_attention_prefill",
+        "kv_page_append_at", "page_attention_decode_shared", "page_weight_add", "page_evict_select", "kv_page_move")))
     return _bind
 
 
@@ -335,6 +350,53 @@ def page_attention_prefill(pages: Pages, q, new_off, k_pages, v_pages, k_scale, 
     """Causal attention of the new tokens, already appended; out in q's type."""
     _check(_bind.page_attention_prefill(pages, q, new_off, k_pages, v_pages, k_scale, v_scale, page_table, seq_len,
                                         softmax_scale, out, lse, workspace, stream), "page_attention_prefill")
+
+
+def kv_page_append_at(pages: Pages, q, k, v, new_off, seq_len, page_table, rope, position, axis, q_out, k_pages, v_pages,
+                      k_scale=None, v_scale=None, abstract=None, chunk_off=None, n_chunks=None, status=None, stream=None) -> None:
+    """kv_page_append with positions of the caller's, [axes, n]; axis [rot_dim / 2]: the axis of each pair (one axis: may be None)."""
+    _check(_bind.kv_page_append_at(pages, q, k, v, new_off, seq_len, page_table, rope, position, axis, q_out, k_pages, v_pages, k_scale,
+                                   v_scale, abstract, chunk_off, n_chunks, status, stream), "kv_page_append_at")
+
+
+def page_attention_decode_shared(pages: Pages, q, k_pages, v_pages, k_scale, v_scale, page_table, seq_len, group_off, group_pages,
+                                 softmax_scale, out, lse, workspace, stream=None) -> None:
+    """page_attention_decode where sequences group_off[g] .. group_off[g + 1] - 1 list the same group_pages[g] pages first."""
+    _check(_bind.page_attention_decode_shared(pages, q, k_pages, v_pages, k_scale, v_scale, page_table, seq_len, group_off, group_pages,
+                                              softmax_scale, out, lse, workspace, stream), "page_attention_decode_shared")
+
+
+def page_weight_add(pages: Pages, q, new_off, k_pages, k_scale, page_table, seq_len, softmax_scale, lse, decay, weight_before, weight,
+                    n_seen=None, token_id=None, stream=None) -> None:
+    """weight [B, Hkv, max_pages * page_size] = decay * weight_before + what each token got of the attention of q's rows."""
+    _check(_bind.page_weight_add(pages, q, new_off, k_pages, k_scale, page_table, seq_len, softmax_scale, lse, decay, weight_before,
+                                 weight, n_seen, token_id, stream), "page_weight_add")
+
+
+def page_evict_select(pages: Pages, weight, token_id, n_seen, seq_len, keep_len, n_first, n_recent, moves, move_count, new_len,
+                      status, workspace, stream=None) -> None:
+    """Which tokens stay where sequences are brought down to keep_len; moves [B, Hkv, m_max, 2]: (free place, place of who moves there)."""
+    _check(_bind.page_evict_select(pages, weight, token_id, n_seen, seq_len, keep_len, n_first, n_recent, moves, move_count, new_len,
+                                   status, workspace, stream), "page_evict_select")
+
+
+def kv_page_move(pages: Pages, moves, move_count, old_len, new_len, page_table, k_pages, v_pages, k_scale=None, v_scale=None,
+                 weight=None, token_id=None, abstract=None, chunk_off=None, n_chunks=None, stream=None) -> None:
+    """The rows that page_evict_select listed to their new places."""
+    _check(_bind.kv_page_move(pages, moves, move_count, old_len, new_len, page_table, k_pages, v_pages, k_scale, v_scale, weight,
+                              token_id, abstract, chunk_off, n_chunks, stream), "kv_page_move")
+
+
+def leoam_page_shared_workspace_bytes(pages: Pages, n_groups: int) -> int:
+    return int(_lib.leoam_page_shared_workspace_bytes(ctypes.byref(pages), int(n_groups)))
+
+
+def leoam_page_shared_workspace_min(pages: Pages) -> int:
+    return int(_lib.leoam_page_shared_workspace_min(ctypes.byref(pages)))
+
+
+def leoam_page_evict_workspace_bytes(pages: Pages) -> int:
+    return int(_lib.leoam_page_evict_workspace_bytes(ctypes.byref(pages)))
 
 
 def leoam_page_workspace_bytes(pages: Pages, n_new: int = 0) -> int:

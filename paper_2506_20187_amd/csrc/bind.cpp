@@ -37,8 +37,13 @@ struct {
     decltype(&::kv_page_append) kv_page_append;
     decltype(&::page_attention_decode) page_attention_decode;
     decltype(&::page_attention_prefill) page_attention_prefill;
+    decltype(&::kv_page_append_at) kv_page_append_at;
+    decltype(&::page_attention_decode_shared) page_attention_decode_shared;
+    decltype(&::page_weight_add) page_weight_add;
+    decltype(&::page_evict_select) page_evict_select;
+    decltype(&::kv_page_move) kv_page_move;
 } g_lib;
-constexpr int kEntryPoints = 9;
+constexpr int kEntryPoints = 14;
 static_assert(sizeof(g_lib) == kEntryPoints * sizeof(void*), "one address each");
 
 // device pointer of a tensor (or None); false with a Python error set
@@ -165,6 +170,16 @@ struct Args {
         } catch (const std::exception& e) {
             refuse(name, e.what());
             return nullptr;
+        }
+    }
+    // of the tensor that is read next (0: none)
+    int64_t elements(const char* name) {
+        if (!ok || a[i] == Py_None || !THPVariable_Check(a[i])) return 0;
+        try {
+            return THPVariable_Unpack(a[i]).numel();
+        } catch (const std::exception& e) {
+            refuse(name, e.what());
+            return 0;
         }
     }
     // bytes of a workspace tensor of any type
@@ -362,7 +377,7 @@ PyObject* py_select_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
-// The pages of the pool and what finds them: k_pages, v_pages, k_scale, v_scale, page_table are arguments of all three calls,
+// The pages of the pool and what finds them: k_pages, v_pages, k_scale, v_scale, page_table are arguments of the calls over them,
 // in this order but for what stands between.
 struct Pool {
     void *k, *v;
@@ -387,8 +402,9 @@ struct Pool {
 // rows of a call fit its 32-bit counts
 bool rows_fit(Args& r, int64_t rows) { return !r.ok || rows <= 0x7fffffff || r.refuse("rows", "more than 2^31 - 1"); }
 
-PyObject* py_page_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
-    Args r(a, n, 18, true);
+// kv_page_append, and kv_page_append_at with position and axis behind rope
+PyObject* append_with(PyObject* const* a, Py_ssize_t n, bool at_positions) {
+    Args r(a, n, at_positions ? 20 : 18, true);
     if (!r.ok) return nullptr;
     const leoam_pages& s = r.pages;
     Pool pool(r);
@@ -402,6 +418,25 @@ PyObject* py_page_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const int32_t* len = r.buffer<int32_t>("seq_len", at::kInt, s.batch);
     const int32_t* table = r.buffer<int32_t>("page_table", at::kInt, (int64_t)s.batch * s.max_pages);
     const float* rope = r.buffer<float>("rope", at::kFloat, (int64_t)s.rope_len * s.rot_dim, s.rot_dim == 0);
+    const int32_t *position = nullptr, *axis = nullptr;
+    int32_t n_axes = 1;
+    if (at_positions) {
+        try {
+            const at::Tensor* t = r.tensor("position", at::kInt, s.rot_dim == 0);
+            if (t) {
+                if (t->dim() != 2 || t->size(0) < 1 || t->size(0) > LEOAM_MAX_AXES || t->size(1) != rows)
+                    r.refuse("position", "expected [axes, rows], one to eight axes");
+                else if (!t->is_contiguous()) r.refuse("position", "expected a contiguous tensor");
+                else {
+                    n_axes = (int32_t)t->size(0);
+                    position = static_cast<const int32_t*>(t->data_ptr());
+                }
+            }
+        } catch (const std::exception& e) {
+            r.refuse("position", e.what());
+        }
+        axis = r.buffer<int32_t>("axis", at::kInt, s.rot_dim / 2, n_axes == 1);
+    }
     void* q_out = r.buffer("q_out", pool.row, q_rows * s.n_q_heads * s.head_dim, true);
     pool.read(r);
     void* abstract = r.buffer("abstract", pool.row, (int64_t)s.batch * s.n_kv_heads * s.max_pages * 2 * s.head_dim, true);
@@ -410,10 +445,16 @@ PyObject* py_page_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
     int32_t* status = r.buffer<int32_t>("status", at::kInt, s.batch, true);
     void* st = r.stream();
     return status_of(r, [&] {
+        if (at_positions)
+            return g_lib.kv_page_append_at(&s, q, q_stride, k, k_stride, v, v_stride, (int32_t)rows, new_off, len, table, rope, position,
+                                           n_axes, axis, q_out, pool.k, pool.v, pool.ks, pool.vs, abstract, off, n_chunks, status, st);
         return g_lib.kv_page_append(&s, q, q_stride, k, k_stride, v, v_stride, (int32_t)rows, new_off, len, table, rope, q_out,
                                     pool.k, pool.v, pool.ks, pool.vs, abstract, off, n_chunks, status, st);
     });
 }
+
+PyObject* py_page_append(PyObject*, PyObject* const* a, Py_ssize_t n) { return append_with(a, n, false); }
+PyObject* py_page_append_at(PyObject*, PyObject* const* a, Py_ssize_t n) { return append_with(a, n, true); }
 
 PyObject* py_page_decode(PyObject*, PyObject* const* a, Py_ssize_t n) {
     Args r(a, n, 15, true);
@@ -479,6 +520,129 @@ PyObject* py_page_prefill(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
+PyObject* py_page_shared(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    Args r(a, n, 15, true);
+    if (!r.ok) return nullptr;
+    const leoam_pages& s = r.pages;
+    Pool pool(r);
+    const int64_t heads = (int64_t)s.batch * s.n_q_heads;
+    const void* q = r.buffer("q", pool.row, heads * s.head_dim);
+    pool.read(r);
+    const int32_t* table = r.buffer<int32_t>("page_table", at::kInt, (int64_t)s.batch * s.max_pages);
+    const int32_t* len = r.buffer<int32_t>("seq_len", at::kInt, s.batch);
+    const int64_t n_off = r.elements("group_off");
+    const int32_t* off = r.buffer<int32_t>("group_off", at::kInt, 2);
+    const int32_t* shared = r.buffer<int32_t>("group_pages", at::kInt, n_off - 1);
+    if (r.ok && n_off - 1 > s.batch) r.refuse("group_off", "more groups than sequences");
+    const float scale = r.f32();
+    float* out = r.buffer<float>("out", at::kFloat, heads * s.head_dim);
+    float* lse = r.buffer<float>("lse", at::kFloat, heads, true);
+    size_t bytes;
+    void* ws = r.scratch("workspace", &bytes);
+    void* st = r.stream();
+    return status_of(r, [&] {
+        return g_lib.page_attention_decode_shared(&s, q, pool.k, pool.v, pool.ks, pool.vs, table, len, (int32_t)(n_off - 1), off, shared,
+                                                  scale, out, lse, ws, bytes, st);
+    });
+}
+
+PyObject* py_page_weight_add(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    Args r(a, n, 15, true);
+    if (!r.ok) return nullptr;
+    const leoam_pages& s = r.pages;
+    Pool pool(r);
+    int64_t rows = -1, stride;
+    const void* q = r.strided_rows("q", pool.row, s.n_q_heads, &rows, &stride);
+    rows_fit(r, rows);
+    if (r.ok && rows > 1 && stride != (int64_t)s.n_q_heads * s.head_dim) r.refuse("q", "expected a contiguous tensor");
+    const int32_t* new_off = r.buffer<int32_t>("new_off", at::kInt, (int64_t)s.batch + 1, true);
+    const void* k = r.buffer("k_pages", pool.kv, pool.elements);
+    const float* ks = r.buffer<float>("k_scale", at::kFloat, pool.scales, pool.kv != at::kFloat8_e4m3fn);
+    const int32_t* table = r.buffer<int32_t>("page_table", at::kInt, (int64_t)s.batch * s.max_pages);
+    const int32_t* len = r.buffer<int32_t>("seq_len", at::kInt, s.batch);
+    const float scale = r.f32();
+    const float* lse = r.buffer<float>("lse", at::kFloat, rows * s.n_q_heads);
+    const float decay = r.f32();
+    const int64_t places = (int64_t)s.batch * s.n_kv_heads * s.max_pages * s.page_size;
+    const float* before = r.buffer<float>("weight_before", at::kFloat, places, true);
+    float* weight = r.buffer<float>("weight", at::kFloat, places);
+    const int32_t* seen = r.buffer<int32_t>("n_seen", at::kInt, s.batch, true);
+    int32_t* ids = r.buffer<int32_t>("token_id", at::kInt, places, true);
+    void* st = r.stream();
+    return status_of(r, [&] {
+        return g_lib.page_weight_add(&s, q, (int32_t)rows, new_off, k, ks, table, len, scale, lse, decay, before, weight, seen, ids, st);
+    });
+}
+
+// [batch, n_kv_heads, m_max, 2]
+int32_t* moves_of(Args& r, int32_t* m_max) {
+    const leoam_pages& s = r.pages;
+    *m_max = 0;
+    try {
+        const at::Tensor* t = r.tensor("moves", at::kInt, false);
+        if (!t) return nullptr;
+        if (t->dim() != 4 || t->size(0) != s.batch || t->size(1) != s.n_kv_heads || t->size(2) > 0x7fffffff || t->size(3) != 2)
+            r.refuse("moves", "expected [batch, n_kv_heads, m_max, 2]");
+        else if (!t->is_contiguous()) r.refuse("moves", "expected a contiguous tensor");
+        if (!r.ok) return nullptr;
+        *m_max = (int32_t)t->size(2);
+        return static_cast<int32_t*>(t->data_ptr());
+    } catch (const std::exception& e) {
+        r.refuse("moves", e.what());
+        return nullptr;
+    }
+}
+
+PyObject* py_page_evict_select(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    Args r(a, n, 14, true);
+    if (!r.ok) return nullptr;
+    const leoam_pages& s = r.pages;
+    const int64_t places = (int64_t)s.batch * s.n_kv_heads * s.max_pages * s.page_size;
+    const float* weight = r.buffer<float>("weight", at::kFloat, places);
+    const int32_t* ids = r.buffer<int32_t>("token_id", at::kInt, places, true);
+    const int32_t* seen = r.buffer<int32_t>("n_seen", at::kInt, s.batch, true);
+    const int32_t* len = r.buffer<int32_t>("seq_len", at::kInt, s.batch);
+    const int32_t* keep = r.buffer<int32_t>("keep_len", at::kInt, s.batch);
+    const int32_t* first = r.buffer<int32_t>("n_first", at::kInt, s.batch, true);
+    const int32_t recent = r.i32();
+    int32_t m_max;
+    int32_t* moves = moves_of(r, &m_max);
+    int32_t* count = r.buffer<int32_t>("move_count", at::kInt, (int64_t)s.batch * s.n_kv_heads);
+    int32_t* new_len = r.buffer<int32_t>("new_len", at::kInt, s.batch);
+    int32_t* status = r.buffer<int32_t>("status", at::kInt, s.batch, true);
+    size_t bytes;
+    void* ws = r.scratch("workspace", &bytes);
+    void* st = r.stream();
+    return status_of(r, [&] {
+        return g_lib.page_evict_select(&s, weight, ids, seen, len, keep, first, recent, moves, m_max, count, new_len, status, ws, bytes, st);
+    });
+}
+
+PyObject* py_page_move(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    Args r(a, n, 16, true);
+    if (!r.ok) return nullptr;
+    const leoam_pages& s = r.pages;
+    Pool pool(r);
+    int32_t m_max;
+    const int32_t* moves = moves_of(r, &m_max);
+    const int32_t* count = r.buffer<int32_t>("move_count", at::kInt, (int64_t)s.batch * s.n_kv_heads);
+    const int32_t* old_len = r.buffer<int32_t>("old_len", at::kInt, s.batch);
+    const int32_t* new_len = r.buffer<int32_t>("new_len", at::kInt, s.batch);
+    const int32_t* table = r.buffer<int32_t>("page_table", at::kInt, (int64_t)s.batch * s.max_pages);
+    pool.read(r);
+    const int64_t places = (int64_t)s.batch * s.n_kv_heads * s.max_pages * s.page_size;
+    float* weight = r.buffer<float>("weight", at::kFloat, places, true);
+    int32_t* ids = r.buffer<int32_t>("token_id", at::kInt, places, true);
+    void* abstract = r.buffer("abstract", pool.row, (int64_t)s.batch * s.n_kv_heads * s.max_pages * 2 * s.head_dim, true);
+    int32_t* off = r.buffer<int32_t>("chunk_off", at::kInt, (int64_t)s.batch * (s.max_pages + 1), true);
+    int32_t* n_chunks = r.buffer<int32_t>("n_chunks", at::kInt, s.batch, true);
+    void* st = r.stream();
+    return status_of(r, [&] {
+        return g_lib.kv_page_move(&s, moves, m_max, count, old_len, new_len, table, pool.k, pool.v, pool.ks, pool.vs, weight, ids, abstract,
+                                  off, n_chunks, st);
+    });
+}
+
 #define LEOAM_METHOD(name, fn) {name, (PyCFunction)(void (*)(void))fn, METH_FASTCALL, nullptr}
 PyMethodDef g_methods[] = {LEOAM_METHOD("setup", py_setup),
                            LEOAM_METHOD("chunk_score", py_chunk_score),
@@ -490,6 +654,11 @@ PyMethodDef g_methods[] = {LEOAM_METHOD("setup", py_setup),
                            LEOAM_METHOD("kv_page_append", py_page_append),
                            LEOAM_METHOD("page_attention_decode", py_page_decode),
                            LEOAM_METHOD("page_attention_prefill", py_page_prefill),
+                           LEOAM_METHOD("kv_page_append_at", py_page_append_at),
+                           LEOAM_METHOD("page_attention_decode_shared", py_page_shared),
+                           LEOAM_METHOD("page_weight_add", py_page_weight_add),
+                           LEOAM_METHOD("page_evict_select", py_page_evict_select),
+                           LEOAM_METHOD("kv_page_move", py_page_move),
                            {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_bind", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 

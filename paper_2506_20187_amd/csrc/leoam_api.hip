@@ -38,8 +38,8 @@ hipError_t recompress_dispatch(const leoam_shape*, const void*, const void*, con
                                const uint8_t*, void*, void*, void*, size_t, long long*, long long*, hipStream_t);
 hipError_t abstract_append_dispatch(const leoam_shape*, const void*, int32_t*, int32_t*, int, void*, int32_t*, hipStream_t);
 hipError_t page_append_dispatch(const leoam_pages*, const void*, int64_t, const void*, int64_t, const void*, int64_t, int,
-                                const int32_t*, const int32_t*, const int32_t*, const float*, void*, void*, void*, float*,
-                                float*, void*, int32_t*, int32_t*, int32_t*, hipStream_t);
+                                const int32_t*, const int32_t*, const int32_t*, const float*, const int32_t*, int, const int32_t*,
+                                void*, void*, void*, float*, float*, void*, int32_t*, int32_t*, int32_t*, hipStream_t);
 hipError_t page_decode_dispatch(const leoam_pages*, const void*, const void*, const void*, const float*, const float*,
                                 const int32_t*, const int32_t*, const int32_t*, const int32_t*, int, float, float*, float*,
                                 void*, size_t, hipStream_t);
@@ -48,6 +48,17 @@ hipError_t page_prefill_dispatch(const leoam_pages*, const void*, int, const int
                                  hipStream_t);
 size_t page_workspace_bytes(const leoam_pages*, int);
 size_t page_min_workspace_bytes(const leoam_pages*);
+hipError_t page_shared_dispatch(const leoam_pages*, const void*, const void*, const void*, const float*, const float*, const int32_t*,
+                                const int32_t*, int, const int32_t*, const int32_t*, float, float*, float*, void*, size_t, hipStream_t);
+size_t page_shared_workspace_bytes(const leoam_pages*, int);
+size_t page_shared_min_workspace_bytes(const leoam_pages*);
+hipError_t page_weight_dispatch(const leoam_pages*, const void*, int, const int32_t*, const void*, const float*, const int32_t*,
+                                const int32_t*, float, const float*, float, const float*, float*, const int32_t*, int32_t*, hipStream_t);
+hipError_t page_evict_dispatch(const leoam_pages*, const float*, const int32_t*, const int32_t*, const int32_t*, const int32_t*,
+                               const int32_t*, int, int32_t*, int, int32_t*, int32_t*, int32_t*, void*, hipStream_t);
+size_t page_evict_workspace_bytes(const leoam_pages*);
+hipError_t page_move_dispatch(const leoam_pages*, const int32_t*, int, const int32_t*, const int32_t*, const int32_t*, const int32_t*,
+                              void*, void*, float*, float*, float*, int32_t*, void*, int32_t*, int32_t*, hipStream_t);
 
 // scores of the first `sink` and the last `tail` chunks of every (b, h) row become FLT_MAX
 __global__ void score_pin_kernel(const int32_t* __restrict__ n_chunks, int sink, int tail, float* __restrict__ score,
@@ -467,10 +478,11 @@ static bool bad_stride(int64_t stride, int q_dtype, int heads, int rows) {
     return stride < (int64_t)heads * LEOAM_D || stride > (1ll << 31) || (stride * e) % 16;
 }
 
-int kv_page_append(const leoam_pages* pages, const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
-                   int64_t v_stride, int32_t n_new, const int32_t* new_off, const int32_t* seq_len,
-                   const int32_t* page_table, const float* rope, void* q_out, void* k_pages, void* v_pages, float* k_scale,
-                   float* v_scale, void* abstract, int32_t* chunk_off, int32_t* n_chunks, int32_t* status, void* stream) {
+static int append_checked(const leoam_pages* pages, const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
+                          int64_t v_stride, int32_t n_new, const int32_t* new_off, const int32_t* seq_len,
+                          const int32_t* page_table, const float* rope, const int32_t* position, int32_t n_axes, const int32_t* axis,
+                          void* q_out, void* k_pages, void* v_pages, float* k_scale, float* v_scale, void* abstract,
+                          int32_t* chunk_off, int32_t* n_chunks, int32_t* status, void* stream) {
     int rc = check_pages(pages);
     if (rc) return rc;
     if (n_new < 0 || (!new_off && n_new != pages->batch)) return LEOAM_E_INVALID_ARG;
@@ -486,8 +498,32 @@ int kv_page_append(const leoam_pages* pages, const void* q, int64_t q_stride, co
         return LEOAM_E_INVALID_ARG;
     if (q && q == q_out && n_new > 1 && q_stride != (int64_t)pages->n_q_heads * LEOAM_D) return LEOAM_E_INVALID_ARG;
     return from_hip(page_append_dispatch(pages, q, q_stride, k, k_stride, v, v_stride, n_new, new_off, seq_len, page_table, rope,
-                                         q_out, k_pages, v_pages, k_scale, v_scale, abstract, chunk_off, n_chunks, status,
-                                         (hipStream_t)stream));
+                                         position, n_axes, axis, q_out, k_pages, v_pages, k_scale, v_scale, abstract, chunk_off,
+                                         n_chunks, status, (hipStream_t)stream));
+}
+
+int kv_page_append(const leoam_pages* pages, const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
+                   int64_t v_stride, int32_t n_new, const int32_t* new_off, const int32_t* seq_len,
+                   const int32_t* page_table, const float* rope, void* q_out, void* k_pages, void* v_pages, float* k_scale,
+                   float* v_scale, void* abstract, int32_t* chunk_off, int32_t* n_chunks, int32_t* status, void* stream) {
+    return append_checked(pages, q, q_stride, k, k_stride, v, v_stride, n_new, new_off, seq_len, page_table, rope, nullptr, 0, nullptr,
+                          q_out, k_pages, v_pages, k_scale, v_scale, abstract, chunk_off, n_chunks, status, stream);
+}
+
+int kv_page_append_at(const leoam_pages* pages, const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
+                      int64_t v_stride, int32_t n_new, const int32_t* new_off, const int32_t* seq_len,
+                      const int32_t* page_table, const float* rope, const int32_t* position, int32_t n_axes, const int32_t* axis,
+                      void* q_out, void* k_pages, void* v_pages, float* k_scale, float* v_scale, void* abstract,
+                      int32_t* chunk_off, int32_t* n_chunks, int32_t* status, void* stream) {
+    int rc = check_pages(pages);
+    if (rc) return rc;
+    if (n_axes < 1) return LEOAM_E_INVALID_ARG;
+    if (n_axes > LEOAM_MAX_AXES) return LEOAM_E_UNSUPPORTED;
+    if (pages->rot_dim && n_new != 0 && (!position || (n_axes > 1 && !axis))) return LEOAM_E_INVALID_ARG;
+    // (nothing is rotated: as an append without positions)
+    return append_checked(pages, q, q_stride, k, k_stride, v, v_stride, n_new, new_off, seq_len, page_table, rope,
+                          pages->rot_dim ? position : nullptr, n_axes, axis, q_out, k_pages, v_pages, k_scale, v_scale, abstract,
+                          chunk_off, n_chunks, status, stream);
 }
 
 static int check_page_attention(const leoam_pages* pages, const void* q, const void* k_pages, const void* v_pages,
@@ -530,6 +566,77 @@ int page_attention_prefill(const leoam_pages* pages, const void* q, int32_t n_ne
     if (rc) return rc;
     return from_hip(page_prefill_dispatch(pages, q, n_new, new_off, k_pages, v_pages, k_scale, v_scale, page_table, seq_len,
                                           softmax_scale, out, lse, workspace, workspace_bytes, (hipStream_t)stream));
+}
+
+int page_attention_decode_shared(const leoam_pages* pages, const void* q, const void* k_pages, const void* v_pages,
+                                 const float* k_scale, const float* v_scale, const int32_t* page_table, const int32_t* seq_len,
+                                 int32_t n_groups, const int32_t* group_off, const int32_t* group_pages, float softmax_scale,
+                                 float* out, float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+    int rc = check_pages(pages);
+    if (rc) return rc;
+    if (n_groups < 1 || n_groups > pages->batch) return LEOAM_E_INVALID_ARG;
+    if (!q || !k_pages || !v_pages || !page_table || !seq_len || !out || !group_off || !group_pages) return LEOAM_E_INVALID_ARG;
+    if (pages->kv_dtype == LEOAM_E4M3 && (!k_scale || !v_scale)) return LEOAM_E_INVALID_ARG;
+    if (misaligned16(q, k_pages, v_pages, out)) return LEOAM_E_INVALID_ARG;
+    if (!workspace || workspace_bytes < page_shared_min_workspace_bytes(pages) || ((uintptr_t)workspace & 15u)) return LEOAM_E_WORKSPACE;
+    return from_hip(page_shared_dispatch(pages, q, k_pages, v_pages, k_scale, v_scale, page_table, seq_len, n_groups, group_off,
+                                         group_pages, softmax_scale, out, lse, workspace, workspace_bytes, (hipStream_t)stream));
+}
+
+size_t leoam_page_shared_workspace_bytes(const leoam_pages* pages, int32_t n_groups) {
+    if (check_pages(pages) || n_groups < 1 || n_groups > pages->batch) return 0;
+    return page_shared_workspace_bytes(pages, n_groups);
+}
+
+size_t leoam_page_shared_workspace_min(const leoam_pages* pages) {
+    if (check_pages(pages)) return 0;
+    return page_shared_min_workspace_bytes(pages);
+}
+
+int page_weight_add(const leoam_pages* pages, const void* q, int32_t n_new, const int32_t* new_off, const void* k_pages,
+                    const float* k_scale, const int32_t* page_table, const int32_t* seq_len, float softmax_scale, const float* lse,
+                    float decay, const float* weight_before, float* weight, const int32_t* n_seen, int32_t* token_id, void* stream) {
+    int rc = check_pages(pages);
+    if (rc) return rc;
+    if (n_new < 0 || (!new_off && n_new != pages->batch)) return LEOAM_E_INVALID_ARG;
+    if (n_new == 0) return LEOAM_OK;
+    if (!q || !k_pages || !page_table || !seq_len || !lse || !weight || !n_seen != !token_id) return LEOAM_E_INVALID_ARG;
+    if (pages->kv_dtype == LEOAM_E4M3 && !k_scale) return LEOAM_E_INVALID_ARG;
+    if (misaligned16(q, k_pages)) return LEOAM_E_INVALID_ARG;
+    return from_hip(page_weight_dispatch(pages, q, n_new, new_off, k_pages, k_scale, page_table, seq_len, softmax_scale, lse, decay,
+                                         weight_before, weight, n_seen, token_id, (hipStream_t)stream));
+}
+
+int page_evict_select(const leoam_pages* pages, const float* weight, const int32_t* token_id, const int32_t* n_seen,
+                      const int32_t* seq_len, const int32_t* keep_len, const int32_t* n_first, int32_t n_recent, int32_t* moves,
+                      int32_t m_max, int32_t* move_count, int32_t* new_len, int32_t* status, void* workspace, size_t workspace_bytes,
+                      void* stream) {
+    int rc = check_pages(pages);
+    if (rc) return rc;
+    if (n_recent < 0 || m_max < 1) return LEOAM_E_INVALID_ARG;
+    if (!weight || !seq_len || !keep_len || !moves || !move_count || !new_len || !token_id != !n_seen) return LEOAM_E_INVALID_ARG;
+    if (((uintptr_t)moves & 7u)) return LEOAM_E_INVALID_ARG;
+    if (!workspace || workspace_bytes < page_evict_workspace_bytes(pages) || ((uintptr_t)workspace & 15u)) return LEOAM_E_WORKSPACE;
+    return from_hip(page_evict_dispatch(pages, weight, token_id, n_seen, seq_len, keep_len, n_first, n_recent, moves, m_max, move_count,
+                                        new_len, status, workspace, (hipStream_t)stream));
+}
+
+size_t leoam_page_evict_workspace_bytes(const leoam_pages* pages) {
+    if (check_pages(pages)) return 0;
+    return page_evict_workspace_bytes(pages);
+}
+
+int kv_page_move(const leoam_pages* pages, const int32_t* moves, int32_t m_max, const int32_t* move_count, const int32_t* old_len,
+                 const int32_t* new_len, const int32_t* page_table, void* k_pages, void* v_pages, float* k_scale, float* v_scale,
+                 float* weight, int32_t* token_id, void* abstract, int32_t* chunk_off, int32_t* n_chunks, void* stream) {
+    int rc = check_pages(pages);
+    if (rc) return rc;
+    if (m_max < 1) return LEOAM_E_INVALID_ARG;
+    if (!moves || !move_count || !old_len || !new_len || !page_table || !k_pages || !v_pages) return LEOAM_E_INVALID_ARG;
+    if (pages->kv_dtype == LEOAM_E4M3 && (!k_scale || !v_scale)) return LEOAM_E_INVALID_ARG;
+    if (misaligned16(k_pages, v_pages, abstract) || ((uintptr_t)moves & 7u)) return LEOAM_E_INVALID_ARG;
+    return from_hip(page_move_dispatch(pages, moves, m_max, move_count, old_len, new_len, page_table, k_pages, v_pages, k_scale, v_scale,
+                                       weight, token_id, abstract, chunk_off, n_chunks, (hipStream_t)stream));
 }
 
 size_t leoam_page_workspace_bytes(const leoam_pages* pages, int32_t n_new) {

@@ -3,7 +3,8 @@
 //
 // Rotation of channel pair (a, b) at a token's position: (a c - b s, b c + a s) with c, s from a table; every
 // product and the sum is one binary32 operation (contraction is off there), then one
-// rounding to the page's type: what a plain evaluation gives, bit for bit.
+// rounding to the page's type: what a plain evaluation gives, bit for bit.  The position is the token's place in the sequence, or
+// (kAt) what the caller gives for each row and axis.
 //
 // Bytes-bound (a row is read once and written once) for prompts, a chain of dependent round trips
 // (length -> page -> old scale) for single tokens.  One workgroup owns a (touched page, kv head), of 8-bit prompts one of its
@@ -24,6 +25,9 @@ struct AppendArgs {
     char* abstract;
     int32_t *chunk_off, *n_chunks, *status;
     int batch, n_q_heads, n_kv_heads, n_pages, page_size, max_pages, rot_dim, interleaved, rope_len;
+    // positions that the caller gives (kAt): [n_axes][n_new], and the axis of each pair (nullptr: the first)
+    const int32_t *position, *axis;
+    int n_axes;
 };
 
 // what a sequence takes in: rows [row0, row0 + m) of the call become its tokens [n - m, n); status as reported
@@ -33,23 +37,62 @@ __device__ __forceinline__ Taken taken_by(const AppendArgs& a, int b) {
     const bool ragged = a.new_off != nullptr;
     const int n = a.seq_len[b], row0 = ragged ? a.new_off[b] : b, m = ragged ? a.new_off[b + 1] - row0 : n > 0 ? 1 : 0;
     const bool misfit = m < 0 || row0 < 0 || m > a.n_new - row0 || n < m || n > a.max_pages * a.page_size;
-    return Taken{row0, m, n, misfit ? 1 : a.rot_dim && m && n > a.rope_len ? 3 : 0};
+    return Taken{row0, m, n, misfit ? 1 : a.rot_dim && m && n > a.rope_len && !a.position ? 3 : 0};
 }
 
-// The cosines and sines that the EPL channels from `col` need (channels from rot_dim on: none).
-template <int EPL> struct Turn {
+// a row's position on an axis, as near to it as the table has one
+__device__ __forceinline__ int position_of(const AppendArgs& a, int axis, int row) {
+    return min(max(a.position[(size_t)axis * a.n_new + row], 0), a.rope_len - 1);
+}
+
+// The cosines and sines that the EPL channels from `col` need (channels from rot_dim on: none): those of place `pos`, or (kAt) of
+// the positions that the call's row `row` was given.
+template <int EPL, bool kAt> struct Turn {
     float c[EPL], s[EPL];
-    __device__ __forceinline__ void load(const AppendArgs& a, int pos, int col) {
+    __device__ __forceinline__ void load(const AppendArgs& a, int pos, int row, int col) {
         if (col >= a.rot_dim) return;
         // pairs (2i, 2i+1): EPL / 2 angles from col / 2; pairs (i, i + half): EPL from col or col - half (half is a multiple of EPL)
         constexpr int N = EPL / 2;
         const int half = a.rot_dim >> 1, at = a.interleaved ? col >> 1 : col < half ? col : col - half, more = a.interleaved ? 0 : N;
-        const float* row = a.rope + (size_t)pos * a.rot_dim + at;
         float c0[N], c1[N], s0[N], s1[N];
-        angles(row, c0);
-        angles(row + more, c1);
-        angles(row + half, s0);
-        angles(row + half + more, s1);
+        auto of_position = [&](int p) {
+            const float* angle = a.rope + (size_t)p * a.rot_dim + at;
+            angles(angle, c0);
+            angles(angle + more, c1);
+            angles(angle + half, s0);
+            angles(angle + half + more, s1);
+        };
+        if constexpr (!kAt) {
+            of_position(pos);
+        } else if (!a.axis) {
+            of_position(position_of(a, 0, row));
+        } else {
+            // The pieces of every axis that some of the lane's pairs belong to (mostly one: axes come in sections); each pair then
+            // keeps its own.
+            int ax0[N], ax1[N];
+            uint32_t wanted = 0;
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                ax0[e] = min(max(a.axis[at + e], 0), a.n_axes - 1);
+                ax1[e] = min(max(a.axis[at + more + e], 0), a.n_axes - 1);
+                wanted |= 1u << ax0[e] | 1u << ax1[e];
+            }
+            float k0[N], k1[N], t0[N], t1[N];
+            for (int x = 0; x < a.n_axes; ++x) {
+                if (!(wanted >> x & 1)) continue;
+                of_position(position_of(a, x, row));
+#pragma unroll
+                for (int e = 0; e < N; ++e) {
+                    if (ax0[e] == x) { k0[e] = c0[e]; t0[e] = s0[e]; }
+                    if (ax1[e] == x) { k1[e] = c1[e]; t1[e] = s1[e]; }
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                c0[e] = k0[e]; s0[e] = t0[e];
+                c1[e] = k1[e]; s1[e] = t1[e];
+            }
+        }
 #pragma unroll
         for (int e = 0; e < EPL; ++e) {
             c[e] = a.interleaved ? c0[e / 2] : e < N ? c0[e % N] : c1[e % N];
@@ -68,8 +111,8 @@ template <int EPL> struct Turn {
 };
 
 // x: this lane's EPL channels from `col` of a row that LPR neighbouring lanes hold (all of them are here)
-template <int EPL, int LPR>
-__device__ __forceinline__ void rotate(const AppendArgs& a, const Turn<EPL>& t, int col, float* x) {
+template <int EPL, int LPR, bool kAt>
+__device__ __forceinline__ void rotate(const AppendArgs& a, const Turn<EPL, kAt>& t, int col, float* x) {
 #pragma clang fp contract(off)
     const int half = a.rot_dim >> 1;
     float other[EPL];
@@ -117,7 +160,7 @@ template <int THREADS> __device__ __forceinline__ float group_max(float v, float
 }
 
 // Query rows: a token and 2 * (rows of a pass) of its heads.
-template <typename T, int THREADS> __device__ __forceinline__ void append_queries(const AppendArgs& a, int unit) {
+template <typename T, int THREADS, bool kAt> __device__ __forceinline__ void append_queries(const AppendArgs& a, int unit) {
     constexpr int EPL = T::kEpl, LPR = Row<T>::kLanesPerRow, RPP = THREADS / LPR, ROWB = Row<T>::kRowBytes;
     const int tid = threadIdx.x, col = (tid % LPR) * EPL, rg = tid / LPR;
     const int per_token = (a.n_q_heads + 2 * RPP - 1) / (2 * RPP);
@@ -127,20 +170,20 @@ template <typename T, int THREADS> __device__ __forceinline__ void append_querie
     if (b >= a.batch) return;
     const Taken t = taken_by(a, b);
     if (t.status || row < t.row0 || row >= t.row0 + t.m) return;
-    Turn<EPL> turn;
-    turn.load(a, t.n - t.m + (row - t.row0), col);
+    Turn<EPL, kAt> turn;
+    turn.load(a, t.n - t.m + (row - t.row0), row, col);
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         const int h = h0 + i * RPP + rg, hc = min(h, a.n_q_heads - 1);
         float x[EPL];
         unpack<T>(load16(a.q, row * a.q_stride + (size_t)hc * ROWB + col * T::kBytes), x);
-        rotate<EPL, LPR>(a, turn, col, x);
+        rotate<EPL, LPR, kAt>(a, turn, col, x);
         if (h < a.n_q_heads) store16(a.q_out, ((size_t)row * a.n_q_heads + h) * ROWB + col * T::kBytes, round_pack<T>(x));
     }
 }
 
-template <typename T, int THREADS> __global__ __launch_bounds__(THREADS) void page_append_queries_kernel(AppendArgs a) {
-    append_queries<T, THREADS>(a, blockIdx.x);
+template <typename T, int THREADS, bool kAt> __global__ __launch_bounds__(THREADS) void page_append_queries_kernel(AppendArgs a) {
+    append_queries<T, THREADS, kAt>(a, blockIdx.x);
 }
 
 // A touched page of a sequence: logical page, the positions [p0, p1) that enter it, the row of the call that p0 is, how many
@@ -345,7 +388,7 @@ __device__ __forceinline__ char* abstract_row(const AppendArgs& a, int b, int p,
 // had rows for them - in the abstract and the boundaries.  One workgroup, since it alone reads and sets n_chunks; once for a
 // sequence and its prefix, so it need not be fast: a wave takes a (page, kv head) at a time (4096 tokens of 8 heads in bf16, pages of 64:
 // 0.3 ms in a prompt's call, 0.85 in a single token's; 64K 5 ms).
-template <typename T, bool kStore8, int THREADS> __device__ __forceinline__ void report(const AppendArgs& a, int b, float* sh_max) {
+template <typename T, bool kStore8, int THREADS, bool kAt> __device__ __forceinline__ void report(const AppendArgs& a, int b, float* sh_max) {
     constexpr int EPL = T::kEpl, LPR = Row<T>::kLanesPerRow, ROWB = Row<T>::kRowBytes, STOREB = kStore8 ? LEOAM_D : ROWB;
     const int tid = threadIdx.x, ps = a.page_size, hkv = a.n_kv_heads;
     const int32_t* table = a.page_table + (size_t)b * a.max_pages;
@@ -356,9 +399,17 @@ template <typename T, bool kStore8, int THREADS> __device__ __forceinline__ void
     const int first = none ? 0 : (t.n - t.m) / ps, last = none ? -1 : (t.n - 1) / ps;
     int bad = 0;
     for (int p = first + tid; p <= last; p += THREADS) bad |= (uint32_t)table[p] >= (uint32_t)a.n_pages;
+    if constexpr (kAt) {      // 1: a position that the table does not have, 2: a page that the pool does not have
+        bad <<= 1;
+        if (a.status && a.rot_dim && !none)
+            for (int x = 0; x < a.n_axes; ++x) {
+                const int32_t* position = a.position + (size_t)x * a.n_new + t.row0;
+                for (int r = tid; r < t.m; r += THREADS) bad = max(bad, (uint32_t)position[r] >= (uint32_t)a.rope_len ? 1 : 0);
+            }
+    }
     bad = (int)(group_max<THREADS>((float)bad, sh_max));      // (everybody has n_chunks)
     if (tid == 0) {
-        if (a.status) a.status[b] = t.status ? t.status : bad ? 2 : 0;
+        if (a.status) a.status[b] = t.status ? t.status : kAt && bad == 1 ? 3 : bad ? 2 : 0;
         if (a.n_chunks && (!none || (t.status == 0 && t.n == 0))) a.n_chunks[b] = last + 1;
     }
     if (known >= first) return;
@@ -388,7 +439,7 @@ template <typename T, bool kStore8, int THREADS> __device__ __forceinline__ void
 //     against 134 with the former's shape (the queries at a quarter of the occupancy).
 // Workgroups of four heads, which would load the angles of a token once for them, were slower (144 against 93 us for the
 // keys and values of the former, 78 against 58 for the latter): a page then takes longer than there are pages to overlap.
-template <typename T, bool kStore8, int THREADS, int PASSES>
+template <typename T, bool kStore8, int THREADS, int PASSES, bool kAt>
 __global__ __launch_bounds__(THREADS) void page_append_prompt_kernel(AppendArgs a) {
     constexpr int EPL = T::kEpl, LPR = Row<T>::kLanesPerRow, RPP = THREADS / LPR, WAVES = THREADS / LEOAM_WAVE;
     constexpr int ROWB = Row<T>::kRowBytes, STOREB = kStore8 ? LEOAM_D : ROWB;
@@ -396,7 +447,7 @@ __global__ __launch_bounds__(THREADS) void page_append_prompt_kernel(AppendArgs 
     __shared__ float sh_abs[WAVES][2][LEOAM_D];
     const int tid = threadIdx.x, col = (tid % LPR) * EPL, rg = tid / LPR, ps = a.page_size, hkv = a.n_kv_heads;
     if ((int)blockIdx.x < a.batch) {
-        report<T, kStore8, THREADS>(a, blockIdx.x, sh_max);
+        report<T, kStore8, THREADS, kAt>(a, blockIdx.x, sh_max);
         return;
     }
     int unit = blockIdx.x - a.batch, first = 0, last = 1;      // tensors
@@ -404,7 +455,7 @@ __global__ __launch_bounds__(THREADS) void page_append_prompt_kernel(AppendArgs 
         first = last = unit & 1;
         unit >>= 1;
     } else if (unit >= a.n_slots * hkv) {
-        append_queries<T, THREADS>(a, unit - a.n_slots * hkv);
+        append_queries<T, THREADS, kAt>(a, unit - a.n_slots * hkv);
         return;
     }
     const int h = unit % hkv;
@@ -423,9 +474,9 @@ __global__ __launch_bounds__(THREADS) void page_append_prompt_kernel(AppendArgs 
         auto row_of = [&](int r) { return load16(src, (x.row0 + min(r, x.count - 1)) * stride); };
         auto turn_row = [&](int r, float* y) {
             if (!turned) return;
-            Turn<EPL> turn;
-            turn.load(a, x.p0 + min(r, x.count - 1), col);
-            rotate<EPL, LPR>(a, turn, col, y);
+            Turn<EPL, kAt> turn;
+            turn.load(a, x.p0 + min(r, x.count - 1), x.row0 + min(r, x.count - 1), col);
+            rotate<EPL, LPR, kAt>(a, turn, col, y);
         };
         if constexpr (!kStore8) {
             if (bounded) take_in_held<T, false, THREADS, 4>(page, x.held, 1.f, col, mx, mn);
@@ -470,16 +521,16 @@ __global__ __launch_bounds__(THREADS) void page_append_prompt_kernel(AppendArgs 
 
 // One token for each sequence: a wave to a (sequence, kv head), lanes of the first row's width hold the key and the value; further
 // waves report (in the first of these, before its own work, that took 0.25 us longer) and take the queries.
-template <typename T, bool kStore8> __global__ __launch_bounds__(LEOAM_WAVE) void page_append_token_kernel(AppendArgs a) {
+template <typename T, bool kStore8, bool kAt> __global__ __launch_bounds__(LEOAM_WAVE) void page_append_token_kernel(AppendArgs a) {
     constexpr int EPL = T::kEpl, LPR = Row<T>::kLanesPerRow, ROWB = Row<T>::kRowBytes, STOREB = kStore8 ? LEOAM_D : ROWB, THREADS = LEOAM_WAVE;
     const int hkv = a.n_kv_heads, ps = a.page_size, tid = threadIdx.x, col = (tid % LPR) * EPL;
     if ((int)blockIdx.x < a.batch) {
-        report<T, kStore8, THREADS>(a, blockIdx.x, nullptr);
+        report<T, kStore8, THREADS, kAt>(a, blockIdx.x, nullptr);
         return;
     }
     const int unit = blockIdx.x - a.batch;
     if (unit >= a.n_slots * hkv) {
-        append_queries<T, THREADS>(a, unit - a.n_slots * hkv);
+        append_queries<T, THREADS, kAt>(a, unit - a.n_slots * hkv);
         return;
     }
     const int h = unit % hkv;
@@ -487,8 +538,8 @@ template <typename T, bool kStore8> __global__ __launch_bounds__(LEOAM_WAVE) voi
     if (x.count == 0) return;
     const uint4 raw[2] = {load16(a.k, x.row0 * a.k_stride + (size_t)h * ROWB + col * T::kBytes),
                           load16(a.v, x.row0 * a.v_stride + (size_t)h * ROWB + col * T::kBytes)};
-    Turn<EPL> turn;
-    if (a.rot_dim) turn.load(a, x.p0, col);
+    Turn<EPL, kAt> turn;
+    if (a.rot_dim) turn.load(a, x.p0, x.row0, col);
     const size_t at = (size_t)x.id * hkv + h;
     float old[2] = {0.f, 0.f};
     if (kStore8 && x.held > 0) {
@@ -504,7 +555,7 @@ template <typename T, bool kStore8> __global__ __launch_bounds__(LEOAM_WAVE) voi
         const bool bounded = which == 0 && a.abstract;
         float y[EPL], mx[EPL], mn[EPL], scale = 1.f, inv = 1.f;
         unpack<T>(raw[which], y);
-        if (which == 0 && a.rot_dim) rotate<EPL, LPR>(a, turn, col, y);
+        if (which == 0 && a.rot_dim) rotate<EPL, LPR, kAt>(a, turn, col, y);
 #pragma unroll
         for (int e = 0; e < EPL; ++e) {
             mx[e] = held_mx[e];
@@ -532,49 +583,49 @@ template <typename T, bool kStore8> __global__ __launch_bounds__(LEOAM_WAVE) voi
 
 template <typename T> constexpr int queries_per_unit(int threads) { return 2 * (threads / Row<T>::kLanesPerRow); }
 
-template <typename T, bool kStore8> static hipError_t launch_tokens(const AppendArgs& a, hipStream_t stream) {
+template <typename T, bool kStore8, bool kAt> static hipError_t launch_tokens(const AppendArgs& a, hipStream_t stream) {
     const int per = queries_per_unit<T>(LEOAM_WAVE);
     const long long q_units = a.q ? (long long)a.n_new * ((a.n_q_heads + per - 1) / per) : 0;
     const long long units = a.batch + (long long)a.n_slots * a.n_kv_heads + q_units;
     if (units > 0x7fffffffll) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((page_append_token_kernel<T, kStore8>), dim3((unsigned)units), dim3(LEOAM_WAVE), 0, stream, a);
+    hipLaunchKernelGGL((page_append_token_kernel<T, kStore8, kAt>), dim3((unsigned)units), dim3(LEOAM_WAVE), 0, stream, a);
     return hipGetLastError();
 }
 
 constexpr int kPromptThreads = 256;
-template <typename T, bool kStore8, int PASSES> static hipError_t launch_prompt(const AppendArgs& a, hipStream_t stream) {
+template <typename T, bool kStore8, int PASSES, bool kAt> static hipError_t launch_prompt(const AppendArgs& a, hipStream_t stream) {
     const int per = queries_per_unit<T>(kPromptThreads);
     const long long q_units = a.q ? (long long)a.n_new * ((a.n_q_heads + per - 1) / per) : 0, kv_units = (long long)a.n_slots * a.n_kv_heads;
     const long long units = a.batch + (kStore8 ? 2 * kv_units : kv_units + q_units);
     if (units > 0x7fffffffll || q_units > 0x7fffffffll) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((page_append_prompt_kernel<T, kStore8, kPromptThreads, PASSES>), dim3((unsigned)units), dim3(kPromptThreads), 0, stream, a);
+    hipLaunchKernelGGL((page_append_prompt_kernel<T, kStore8, kPromptThreads, PASSES, kAt>), dim3((unsigned)units), dim3(kPromptThreads), 0, stream, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || !kStore8 || q_units == 0) return e;
-    hipLaunchKernelGGL((page_append_queries_kernel<T, kPromptThreads>), dim3((unsigned)q_units), dim3(kPromptThreads), 0, stream, a);
+    hipLaunchKernelGGL((page_append_queries_kernel<T, kPromptThreads, kAt>), dim3((unsigned)q_units), dim3(kPromptThreads), 0, stream, a);
     return hipGetLastError();
 }
 
-template <typename T> static hipError_t append_of(const AppendArgs& a, bool store8, bool single, hipStream_t stream) {
+template <typename T, bool kAt> static hipError_t append_of(const AppendArgs& a, bool store8, bool single, hipStream_t stream) {
     if constexpr (T::kTag != LEOAM_F32) {
         if (store8) {
-            if (single) return launch_tokens<T, true>(a, stream);
+            if (single) return launch_tokens<T, true, kAt>(a, stream);
             switch (a.page_size) {
-            case 16: return launch_prompt<T, true, 1>(a, stream);
-            case 32: return launch_prompt<T, true, 2>(a, stream);
-            case 64: return launch_prompt<T, true, 4>(a, stream);
-            case 128: return launch_prompt<T, true, 8>(a, stream);
-            default: return launch_prompt<T, true, 16>(a, stream);
+            case 16: return launch_prompt<T, true, 1, kAt>(a, stream);
+            case 32: return launch_prompt<T, true, 2, kAt>(a, stream);
+            case 64: return launch_prompt<T, true, 4, kAt>(a, stream);
+            case 128: return launch_prompt<T, true, 8, kAt>(a, stream);
+            default: return launch_prompt<T, true, 16, kAt>(a, stream);
             }
         }
     }
-    return single ? launch_tokens<T, false>(a, stream) : launch_prompt<T, false, 0>(a, stream);
+    return single ? launch_tokens<T, false, kAt>(a, stream) : launch_prompt<T, false, 0, kAt>(a, stream);
 }
 
 hipError_t page_append_dispatch(const leoam_pages* s, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
                                 const void* v, int64_t v_stride, int n_new, const int32_t* new_off, const int32_t* seq_len,
-                                const int32_t* page_table, const float* rope, void* q_out, void* k_pages, void* v_pages,
-                                float* k_scale, float* v_scale, void* abstract, int32_t* chunk_off, int32_t* n_chunks,
-                                int32_t* status, hipStream_t stream) {
+                                const int32_t* page_table, const float* rope, const int32_t* position, int n_axes,
+                                const int32_t* axis, void* q_out, void* k_pages, void* v_pages, float* k_scale, float* v_scale,
+                                void* abstract, int32_t* chunk_off, int32_t* n_chunks, int32_t* status, hipStream_t stream) {
     const int e = s->q_dtype == LEOAM_F32 ? 4 : 2;
     AppendArgs a;
     a.q = (const char*)q; a.k = (const char*)k; a.v = (const char*)v;
@@ -588,11 +639,12 @@ hipError_t page_append_dispatch(const leoam_pages* s, const void* q, int64_t q_s
     a.batch = s->batch; a.n_q_heads = s->n_q_heads; a.n_kv_heads = s->n_kv_heads; a.n_pages = s->n_pages;
     a.page_size = s->page_size; a.max_pages = s->max_pages; a.rot_dim = s->rot_dim; a.interleaved = s->rope_interleaved;
     a.rope_len = s->rope_len;
+    a.position = position; a.n_axes = n_axes; a.axis = n_axes > 1 ? axis : nullptr;
     const bool store8 = s->kv_dtype == LEOAM_E4M3, single = new_off == nullptr;
     switch (s->q_dtype) {
-    case LEOAM_F32: return append_of<F32>(a, store8, single, stream);
-    case LEOAM_F16: return append_of<F16>(a, store8, single, stream);
-    default: return append_of<BF16>(a, store8, single, stream);
+    case LEOAM_F32: return position ? append_of<F32, true>(a, store8, single, stream) : append_of<F32, false>(a, store8, single, stream);
+    case LEOAM_F16: return position ? append_of<F16, true>(a, store8, single, stream) : append_of<F16, false>(a, store8, single, stream);
+    default: return position ? append_of<BF16, true>(a, store8, single, stream) : append_of<BF16, false>(a, store8, single, stream);
     }
 }
 

@@ -24,6 +24,20 @@ class PagedLayer:
                   `max_chunks` - chunk_score, chunk_topk_select with the pages as chunks, attention over the kept ones
       prompt      append, then causal attention of the new tokens
 
+and, for caches that are shared and kept within bounds,
+
+      attend_shared  attention of one token per sequence where groups of sequences begin with the same pages (`groups`: the most
+                     groups of a call)
+      weigh          what each cached token got of the attention of some rows, added to `weight`
+      evict          the sequences brought down to `keep_len` tokens, by `weight` (`evicts`: the most rows of a sequence that
+                     may move in a call); returns the new lengths, which become seq_len once all layers have evicted
+
+After an eviction a token's place is not its position: `append`, `step` and `prompt` then want `position` ([axes, rows]; with several
+axes `axis` [rot_dim / 2] says whose each pair is).  `n_seen` [B] int32 is how many tokens a sequence ever had, brought up to date by
+whoever schedules, as seq_len is.  A place in the batch that another sequence takes over needs nothing: `weigh` starts its new tokens
+anew.  A sequence whose tokens were not all weighed (`weigh` of a prompt's last queries only) has `weight` and `token_id` of the
+others set by the caller: to 0 and to their places.
+
     Sequences may list pages that others filled, and tokens may be taken back (`seq_len` lowered before the next append).
     Under a budget a place in the batch that another sequence takes over must be idle (length 0) for a step in between, or
     have its `n_chunks` set to 0: the rows of abstracts are the place's, and are made anew from the pages then.
@@ -35,7 +49,8 @@ class PagedLayer:
 
     def __init__(self, page_table: torch.Tensor, seq_len: torch.Tensor, n_q_heads: int, n_kv_heads: int, n_pages: int,
                  page_size: int, dtype: torch.dtype, kv_dtype=None, rope: torch.Tensor = None, interleaved: bool = False,
-                 k_max: int = 0, max_chunks: int = 0, token_budget: int = 0, head_dim: int = 128, workspaces_of: "PagedLayer" = None):
+                 k_max: int = 0, max_chunks: int = 0, token_budget: int = 0, head_dim: int = 128, workspaces_of: "PagedLayer" = None,
+                 axis: torch.Tensor = None, groups: int = 0, evicts: int = 0):
         batch, max_pages = page_table.shape
         rope_len, rot_dim = rope.shape if rope is not None else (0, 0)
         self.page_table, self.seq_len, self.rope = page_table, seq_len, rope
@@ -72,6 +87,21 @@ class PagedLayer:
         # the last is the largest; earlier ones stay, a captured graph may use them
         self.prompt_workspaces = [] if workspaces_of is None else workspaces_of.prompt_workspaces
         self.scale = B.default_scale(head_dim)
+        self.axis, self.groups, self.evicts = axis, int(groups), int(evicts)
+        self.weight = self.token_id = self.shared_workspace = None
+        if self.groups:
+            need = B.leoam_page_shared_workspace_bytes(self.pages, self.groups)
+            other = getattr(workspaces_of, "shared_workspace", None)
+            self.shared_workspace = other if other is not None and other.numel() >= need else self._new(need, torch.uint8, None)
+        if self.evicts:
+            places = (batch, n_kv_heads, max_pages * page_size)
+            self.weight = torch.zeros(places, dtype=torch.float32, device=dev)
+            self.token_id = torch.zeros(places, dtype=torch.int32, device=dev)
+            self.moves = torch.empty(batch, n_kv_heads, self.evicts, 2, dtype=torch.int32, device=dev)
+            self.move_count = torch.empty(batch, n_kv_heads, dtype=torch.int32, device=dev)
+            self.new_len = torch.zeros(batch, dtype=torch.int32, device=dev)
+            self.evict_status = torch.zeros(batch, dtype=torch.int32, device=dev)
+            self.evict_workspace = self._new(B.leoam_page_evict_workspace_bytes(self.pages), torch.uint8, None)
 
     def _new(self, shape, dtype, stream) -> torch.Tensor:
         """Of the stream's own memory: freed before its kernels have run, it is given to later ones of that stream only."""
@@ -81,9 +111,14 @@ class PagedLayer:
         with torch.cuda.stream(stream):      # (None: as it is)
             return torch.empty(shape, dtype=dtype, device=device)
 
-    def append(self, q, k, v, new_off=None, q_out=None, stream=None) -> torch.Tensor:
+    def append(self, q, k, v, new_off=None, q_out=None, stream=None, position=None) -> torch.Tensor:
         if q_out is None:
             q_out = self._new(q.shape, q.dtype, stream)
+        if position is not None:
+            B.kv_page_append_at(self.pages, q, k, v, new_off, self.seq_len, self.page_table, self.rope, position, self.axis, q_out,
+                                self.k_pages, self.v_pages, self.k_scale, self.v_scale, self.abstract, self.chunk_off, self.n_chunks,
+                                self.status, stream)
+            return q_out
         B.kv_page_append(self.pages, q, k, v, new_off, self.seq_len, self.page_table, self.rope, q_out, self.k_pages,
                          self.v_pages, self.k_scale, self.v_scale, self.abstract, self.chunk_off, self.n_chunks, self.status,
                          stream)
@@ -101,13 +136,38 @@ class PagedLayer:
                                 self.seq_len, idx, count, self.scale, self.out, self.lse, self.workspace, stream)
         return self.out
 
-    def step(self, q, k, v, q_out=None, stream=None) -> torch.Tensor:
-        """One new token per sequence: q [B, Hq, 128], k, v [B, Hkv, 128]."""
-        return self.attend(self.append(q, k, v, None, q_out, stream), stream)
+    def attend_shared(self, q, group_off, group_pages, stream=None) -> torch.Tensor:
+        """As attend over all pages; sequences group_off[g] .. group_off[g + 1] - 1 list the same group_pages[g] pages first."""
+        if self.shared_workspace is None or group_pages.numel() > self.groups:
+            raise ValueError("PagedLayer was made for %d groups" % self.groups)
+        B.page_attention_decode_shared(self.pages, q, self.k_pages, self.v_pages, self.k_scale, self.v_scale, self.page_table, self.seq_len,
+                                       group_off, group_pages, self.scale, self.out, self.lse, self.shared_workspace, stream)
+        return self.out
 
-    def prompt(self, q, k, v, new_off, out=None, lse=None, q_out=None, stream=None) -> torch.Tensor:
+    def weigh(self, q, n_seen, new_off=None, lse=None, decay: float = 1.0, stream=None) -> None:
+        """q (rotated) and lse of an attention call of this step; lse None: what attend or attend_shared left."""
+        if self.weight is None:
+            raise ValueError("PagedLayer was made without evictions")
+        B.page_weight_add(self.pages, q, new_off, self.k_pages, self.k_scale, self.page_table, self.seq_len, self.scale,
+                          self.lse if lse is None else lse, decay, self.weight, self.weight, n_seen, self.token_id, stream)
+
+    def evict(self, keep_len, n_seen, n_first=None, n_recent: int = 0, stream=None) -> torch.Tensor:
+        """keep_len, n_seen, n_first [B] int32; new lengths [B] int32 (evict_status says where nothing could be done)."""
+        if self.weight is None:
+            raise ValueError("PagedLayer was made without evictions")
+        B.page_evict_select(self.pages, self.weight, self.token_id, n_seen, self.seq_len, keep_len, n_first, n_recent, self.moves,
+                            self.move_count, self.new_len, self.evict_status, self.evict_workspace, stream)
+        B.kv_page_move(self.pages, self.moves, self.move_count, self.seq_len, self.new_len, self.page_table, self.k_pages, self.v_pages,
+                       self.k_scale, self.v_scale, self.weight, self.token_id, self.abstract, self.chunk_off, self.n_chunks, stream)
+        return self.new_len
+
+    def step(self, q, k, v, q_out=None, stream=None, position=None) -> torch.Tensor:
+        """One new token per sequence: q [B, Hq, 128], k, v [B, Hkv, 128]."""
+        return self.attend(self.append(q, k, v, None, q_out, stream, position), stream)
+
+    def prompt(self, q, k, v, new_off, out=None, lse=None, q_out=None, stream=None, position=None) -> torch.Tensor:
         """Sequence b's new tokens are rows new_off[b] .. new_off[b + 1]; out [n, Hq, 128] in q's type."""
-        q_out = self.append(q, k, v, new_off, q_out, stream)
+        q_out = self.append(q, k, v, new_off, q_out, stream, position)
         out = self._new(q_out.shape, q_out.dtype, stream) if out is None else out
         need = B.leoam_page_workspace_bytes(self.pages, q_out.shape[0])
         if not self.prompt_workspaces or self.prompt_workspaces[-1].numel() < need:
