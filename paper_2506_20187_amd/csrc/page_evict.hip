@@ -5,10 +5,10 @@
 // many of the one as of the other, the i-th moves to the i-th.  With kept(t) = tokens before t that stay, t < keep is free place
 // number t - kept(t), and t >= keep is mover number kept(t) - kept(keep): one count in order gives both.
 //
-// A weight becomes a 32-bit key of the same order, and the lowest key that stays is found by histograms.  What is read is 8 bytes
-// a token; bound by latency.  Where a row fits, one workgroup holds its keys in registers and narrows down their range, 11 bits at
-// a time.  Longer rows are cut into parts of 16384 places (at `keep`, too, so that what stays before it is a sum over parts): three
-// launches make histograms of the parts' keys by 11, 11 and 10 bits, each beginning with the sums of the last one's, a fourth one lists.
+// A weight becomes a 32-bit key of the same order, protected ones the highest, and the lowest key that stays is found by histograms of
+// 11, 11 and 10 of its bits.  What is read is 8 bytes a token; bound by latency.  Where a row fits, one workgroup holds its keys in
+// registers.  Longer rows are cut into parts of 8192 places (at `keep`, too, so that what stays before it is a sum over parts): three
+// launches make the parts' histograms, each beginning with the sums of the last one's, a fourth one lists.
 #include "page_common.h"
 
 namespace leoam {
@@ -25,7 +25,8 @@ struct EvictArgs {
 
 constexpr int kEvictThreads = 1024;
 constexpr int kEvictHeld = 16;                     // keys of a thread
-constexpr int kEvictPart = kEvictThreads * kEvictHeld;
+constexpr int kEvictRowMost = kEvictThreads * kEvictHeld;      // longest row of a workgroup
+constexpr int kPartThreads = 512, kEvictPart = kPartThreads * kEvictHeld;
 constexpr int kEvictBins = 2048;
 constexpr uint32_t kProtected = 0xffffffffu;       // above every weight's key
 
@@ -42,27 +43,26 @@ struct EvictRow {
     long long newest;      // numbers from here on are recent
     const float* weight;
     const int32_t* ids;
-    bool bad, none;
+    bool none, bad;
     __device__ __forceinline__ EvictRow(const EvictArgs& a, int bh) {
         const int b = bh / a.n_kv_heads;
         n = uniform(a.seq_len[b]);
         keep = uniform(a.keep_len[b]);
         bad = n < 0 || n > a.capacity || keep < 0 || (keep < n && min(keep, n - keep) > a.m_max);
-        none = bad || keep >= n;
+        none = bad || keep >= n || keep == 0;
         first = a.n_first ? a.n_first[b] : 0;
         weight = a.weight + (size_t)bh * a.capacity;
         ids = a.token_id ? a.token_id + (size_t)bh * a.capacity : nullptr;
         newest = (long long)(ids ? a.n_seen[b] : n) - a.n_recent;
     }
-    __device__ __forceinline__ uint32_t key(int t) const {
-        const int id = ids ? ids[t] : t;
-        const uint32_t k = key_of_weight(weight[t]);
+    __device__ __forceinline__ uint32_t key(int t, int id, float w) const {
+        const uint32_t k = key_of_weight(w);
         return t < first || id >= newest ? kProtected : k;
     }
     __device__ __forceinline__ void report(const EvictArgs& a, int bh) const {
         const int b = bh / a.n_kv_heads;
         if (bh == b * a.n_kv_heads) {
-            a.new_len[b] = none ? n : keep;
+            a.new_len[b] = bad || keep >= n ? n : keep;
             if (a.status) a.status[b] = bad ? 1 : 0;
         }
         if (none) a.move_count[bh] = 0;
@@ -77,11 +77,17 @@ template <int THREADS> struct HeldKeys {
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / LEOAM_WAVE), seg = (hi - lo + THREADS - 1) / THREADS * LEOAM_WAVE;
         begin = min(hi, lo + wave * seg);
         end = min(hi, begin + seg);
+        float w[kEvictHeld];
+        int id[kEvictHeld];
 #pragma unroll
-        for (int i = 0; i < kEvictHeld; ++i) {
-            const int t = begin + i * LEOAM_WAVE + lane_id();
-            keys[i] = t < end ? row.key(t) : 0u;
+        for (int i = 0; i < kEvictHeld; ++i) {      // (all on their way together; places past the last repeat it)
+            if (begin + i * LEOAM_WAVE >= end) break;
+            const int t = min(begin + i * LEOAM_WAVE + lane_id(), end - 1);
+            w[i] = row.weight[t];
+            id[i] = row.ids ? row.ids[t] : t;
         }
+#pragma unroll
+        for (int i = 0; i < kEvictHeld; ++i) keys[i] = row.key(min(begin + i * LEOAM_WAVE + lane_id(), end - 1), id[i], w[i]);
     }
     template <typename F> __device__ __forceinline__ void each(F&& f) const {      // f(place, key, counts), by whole waves
 #pragma unroll
@@ -92,23 +98,29 @@ template <int THREADS> struct HeldKeys {
     }
 };
 
-// The bin, from the top, in which the `need`-th entry of a histogram is: bin, entries above it, entries in it.  count(bin): by
-// thread i the bins kEvictBins - 1 - i * PER - (0 .. PER - 1).  The workgroup's `sh`: waves + 3 words.
-template <int THREADS, typename F> __device__ __forceinline__ int3 find_bin(int need, int* sh, F&& count) {
+// the sum of the waves' words before this wave's
+template <int WAVES> __device__ __forceinline__ int before_wave(const int* sh, int wave) {
+    const uint32_t incl = wave_incl_scan_u32(lane_id() < WAVES ? (uint32_t)sh[lane_id()] : 0u);
+    return wave ? __builtin_amdgcn_readlane((int)incl, wave - 1) : 0;
+}
+
+// The bin, from the top, in which the `need`-th entry of a histogram is: bin, entries above it, entries in it.  counts(first, c): the
+// counts of PER bins from `first` (a multiple of PER) on.  The workgroup's `sh`: waves + 3 words.
+template <int THREADS, typename F> __device__ __forceinline__ int3 find_bin(int need, int* sh, F&& counts) {
     constexpr int PER = kEvictBins / THREADS, WAVES = THREADS / LEOAM_WAVE;
-    const int tid = threadIdx.x, lane = lane_id(), wave = tid / LEOAM_WAVE, top = kEvictBins - 1 - tid * PER;
+    const int tid = threadIdx.x, lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(tid / LEOAM_WAVE), first = kEvictBins - (tid + 1) * PER;
     uint32_t c[PER], sum = 0;
+    counts(first, c);
 #pragma unroll
-    for (int i = 0; i < PER; ++i) sum += c[i] = count(top - i);
+    for (int i = 0; i < PER; ++i) sum += c[i];
     const uint32_t incl = wave_incl_scan_u32(sum);
     if (lane == LEOAM_WAVE - 1) sh[wave] = (int)incl;
     __syncthreads();
-    int before = (int)(incl - sum);
-    for (int w = 0; w < wave; ++w) before += sh[w];
+    int before = before_wave<WAVES>(sh, wave) + (int)(incl - sum);
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
+    for (int i = PER - 1; i >= 0; --i) {
         if (before < need && before + (int)c[i] >= need) {
-            sh[WAVES] = top - i;
+            sh[WAVES] = first + i;
             sh[WAVES + 1] = before;
             sh[WAVES + 2] = (int)c[i];
         }
@@ -118,6 +130,19 @@ template <int THREADS, typename F> __device__ __forceinline__ int3 find_bin(int 
     const int3 found = make_int3(sh[WAVES], sh[WAVES + 1], sh[WAVES + 2]);
     __syncthreads();
     return found;
+}
+
+// The histogram of a stage in LDS: stage 0: bits 31..21 of all keys; 1: bits 20..10 of those that begin as `prefix`; 2: bits 9..0.
+// (Protected ones come by the wave, all of them into the last bin: counted by the wave.)
+template <int STAGE, int THREADS> __device__ __forceinline__ void count_keys(const HeldKeys<THREADS>& held, uint32_t prefix, uint32_t* hist) {
+    constexpr int kShift = STAGE == 0 ? 21 : STAGE == 1 ? 10 : 0, kKnown = STAGE == 1 ? 21 : 10;
+    int guarded = 0;
+    held.each([&](int, uint32_t k, bool in) {
+        const bool last = in && k == kProtected;
+        guarded += __popcll(__ballot(last));
+        if (in && !last && (STAGE == 0 || (k ^ prefix) >> kKnown == 0)) atomicAdd(&hist[k >> kShift & (STAGE == 2 ? 1023u : 2047u)], 1u);
+    });
+    if (lane_id() == 0 && guarded && (STAGE == 0 || (kProtected ^ prefix) >> kKnown == 0)) atomicAdd(&hist[STAGE == 2 ? 1023 : 2047], (uint32_t)guarded);
 }
 
 // The moves of places [begin, end): keys above `bound` stay, and the first `ties` of those equal to it.  above, equal: how many of either
@@ -142,65 +167,39 @@ __device__ __forceinline__ void list_moves(const HeldKeys<THREADS>& held, int ke
 // (Rows of up to 8192 places: 512 threads, so that four workgroups share a compute unit.)
 template <int THREADS> __global__ __launch_bounds__(THREADS, THREADS == 512 ? 8 : 4) void page_evict_row_kernel(EvictArgs a) {
     constexpr int WAVES = THREADS / LEOAM_WAVE;
-    __shared__ uint32_t hist[kEvictBins];
-    __shared__ uint32_t sh_low, sh_high;
-    __shared__ int sh_protected, sh_find[WAVES + 3], sh_above[WAVES], sh_equal[WAVES], sh_kept_low[2];
+    __shared__ uint32_t hist[3][kEvictBins];
+    __shared__ int sh_find[WAVES + 3], sh_above[WAVES], sh_equal[WAVES], sh_kept_low[2];
     const int tid = threadIdx.x, lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(tid / LEOAM_WAVE), bh = blockIdx.x;
     const EvictRow row(a, bh);
     if (tid == 0) row.report(a, bh);
     if (row.none) return;
     const HeldKeys<THREADS> held(row, 0, row.n);
     const int keep = row.keep;
-
-    // ---- protected ones, and the range of the others' keys
-    if (tid == 0) {
-        sh_low = 0xffffffffu;
-        sh_high = 0u;
-        sh_protected = sh_kept_low[0] = sh_kept_low[1] = 0;
-    }
-    __syncthreads();
-    {
-        uint32_t low = 0xffffffffu, high = 0u;
-        int count = 0;
-        held.each([&](int, uint32_t k, bool in) {
-            const bool guarded = in && k == kProtected;
-            count += __popcll(__ballot(guarded));
-            if (in && !guarded) {
-                low = min(low, k);
-                high = max(high, k);
-            }
-        });
-        low = wave_min_u32(low);
-        high = wave_max_u32(high);
-        if (lane == 0) {
-            atomicMin(&sh_low, low);
-            atomicMax(&sh_high, high);
-            atomicAdd(&sh_protected, count);
-        }
-    }
-    __syncthreads();
+    for (int i = tid; i < 3 * kEvictBins; i += THREADS) hist[0][i] = 0;
+    if (tid < 2) sh_kept_low[tid] = 0;
 
     // ---- keys above `bound` stay, and `ties` of those equal to it
-    uint32_t bound = kProtected, low = sh_low, high = sh_high;
-    int ties = keep, need = keep - sh_protected;      // (all of the protected ones or more than fit: the first of them)
-    while (need > 0) {
-        const int shift = max(0, 21 - __builtin_clz((high - low) | 1u));
-        for (int i = tid; i < kEvictBins; i += THREADS) hist[i] = 0;
+    uint32_t bound = 0;
+    int ties = keep;
+    auto stage = [&](auto which) {      // whether the bound is found: the key itself, or a bin that stays whole
+        constexpr int STAGE = decltype(which)::value, kShift = STAGE == 0 ? 21 : STAGE == 1 ? 10 : 0;
         __syncthreads();
-        held.each([&](int, uint32_t k, bool in) {
-            if (in && k >= low && k <= high) atomicAdd(&hist[(k - low) >> shift], 1u);
+        count_keys<STAGE, THREADS>(held, bound, hist[STAGE]);
+        __syncthreads();
+        const int3 found = find_bin<THREADS>(ties, sh_find, [&](int bin, uint32_t* c) {
+#pragma unroll
+            for (int i = 0; i < kEvictBins / THREADS; ++i) c[i] = hist[STAGE][bin + i];
         });
-        __syncthreads();
-        const int3 found = find_bin<THREADS>(need, sh_find, [&](int bin) { return hist[bin]; });
-        need -= found.y;
-        low += (uint32_t)found.x << shift;
-        high = min(high, low + ((1u << shift) - 1u));
-        if (shift == 0 || (need == found.z && low > 0u)) {      // the key itself, or the whole bin stays
-            bound = shift == 0 ? low : low - 1u;
-            ties = shift == 0 ? need : 0;
-            break;
+        ties -= found.y;
+        bound |= (uint32_t)found.x << kShift;
+        if (STAGE < 2 && ties == found.z && bound > 0u) {
+            bound -= 1u;
+            ties = 0;
+            return true;
         }
-    }
+        return STAGE == 2;
+    };
+    if (!stage(std::integral_constant<int, 0>{}) && !stage(std::integral_constant<int, 1>{})) stage(std::integral_constant<int, 2>{});
 
     // ---- how many stay before each wave's places, and before `keep`
     {
@@ -220,24 +219,19 @@ template <int THREADS> __global__ __launch_bounds__(THREADS, THREADS == 512 ? 8 
         }
     }
     __syncthreads();
-    int above = 0, equal = 0;
-    for (int w = 0; w < wave; ++w) {
-        above += sh_above[w];
-        equal += sh_equal[w];
-    }
+    const int above = before_wave<WAVES>(sh_above, wave), equal = before_wave<WAVES>(sh_equal, wave);
     const int kept_low = sh_kept_low[0] + min(sh_kept_low[1], ties);
     if (tid == 0) a.move_count[bh] = keep - kept_low;
     list_moves<THREADS>(held, keep, bound, ties, above, equal, kept_low, a.moves + (size_t)bh * a.m_max * 2);
 }
 
 // ---- a part of a row to a workgroup -------------------------------------------------------------------------
-// Of each part: histograms of two stages in turn, and how many of its keys are above all bins that were found so far (protected ones
-// included).  Of each row, stage by stage: the bits of the bound that are known, and how many entries of the bin are still needed.
-struct EvictPart { int above, guarded; };
+// Of each part: histograms of two stages in turn, and how many of its keys are above all bins that were found so far.  Of each row,
+// stage by stage: the bits of the bound that are known, and how many entries of the bin are still needed.
 struct EvictFound { uint32_t prefix; int need; };
 struct EvictLong {
     uint32_t* hist;         // [2][row][part][kEvictBins]
-    EvictPart* part;        // [2][row][part]
+    int* above;             // [2][row][part]
     EvictFound* found;      // [2][row]
     int rows, parts;
 };
@@ -254,67 +248,72 @@ struct PartOf {
     }
 };
 
-// stage 0: bits 31..21 of all keys; 1: bits 20..10 of those that the first stage's bin holds; 2: bits 9..0
-template <int STAGE> __global__ __launch_bounds__(kEvictThreads, 4) void page_evict_hist_kernel(EvictArgs a, EvictLong s) {
-    constexpr int kShift = STAGE == 0 ? 21 : STAGE == 1 ? 10 : 0, kLast = STAGE == 1 ? 21 : 10;
-    __shared__ uint32_t hist[kEvictBins];
-    __shared__ int sh_find[kEvictThreads / LEOAM_WAVE + 3], sh_guarded, sh_above;
+// neighbouring bins summed over a row's parts, eight parts on their way together
+constexpr int kPartBins = kEvictBins / kPartThreads;
+static_assert(kPartBins == 4, "a thread's bins are loaded by 16 bytes");
+__device__ __forceinline__ void sum_parts(const uint32_t* hist, int n_parts, int first, uint32_t* c) {
+    c[0] = c[1] = c[2] = c[3] = 0;
+    for (int p0 = 0; p0 < n_parts; p0 += 8) {
+        uint4 x[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) x[u] = load16(hist, ((size_t)min(p0 + u, n_parts - 1) * kEvictBins + first) * sizeof(uint32_t));
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            if (p0 + u >= n_parts) break;
+            c[0] += x[u].x;
+            c[1] += x[u].y;
+            c[2] += x[u].z;
+            c[3] += x[u].w;
+        }
+    }
+}
+// of four neighbouring bins, the entries above `bin`
+__device__ __forceinline__ int above_bin(const uint4& x, int first, int bin) {
+    return (first > bin ? (int)x.x : 0) + (first + 1 > bin ? (int)x.y : 0) + (first + 2 > bin ? (int)x.z : 0) + (first + 3 > bin ? (int)x.w : 0);
+}
+
+template <int STAGE> __global__ __launch_bounds__(kPartThreads, 4) void page_evict_hist_kernel(EvictArgs a, EvictLong s) {
+    __shared__ __align__(16) uint32_t hist[kEvictBins];
+    __shared__ int sh_find[kPartThreads / LEOAM_WAVE + 3], sh_above;
     const int tid = threadIdx.x, bh = blockIdx.x / s.parts, p = blockIdx.x % s.parts;
     const EvictRow row(a, bh);
     if (STAGE == 0 && tid == 0 && p == 0) row.report(a, bh);
     if (row.none) return;
     const PartOf part(row, p);
     if (p >= part.n_parts) return;
-    const HeldKeys<kEvictThreads> held(row, part.begin, part.end);
+    const HeldKeys<kPartThreads> held(row, part.begin, part.end);
     uint32_t* mine = s.hist + (((size_t)(STAGE & 1) * s.rows + bh) * s.parts + p) * kEvictBins;
-    const uint32_t* last = s.hist + ((size_t)((STAGE & 1) ^ 1) * s.rows + bh) * s.parts * kEvictBins;
-    EvictPart* state = s.part + ((size_t)(STAGE & 1) * s.rows + bh) * s.parts;
-    const EvictPart* was = s.part + ((size_t)((STAGE & 1) ^ 1) * s.rows + bh) * s.parts;
-    for (int i = tid; i < kEvictBins; i += kEvictThreads) hist[i] = 0;
-    if (tid == 0) sh_guarded = sh_above = 0;
+    for (int i = tid; i < kEvictBins; i += kPartThreads) hist[i] = 0;
+    if (tid == 0) sh_above = 0;
     uint32_t prefix = 0;
-    EvictPart now = {0, 0};
+    int above = 0;
     if constexpr (STAGE > 0) {
+        constexpr int kKnown = STAGE == 1 ? 21 : 10;
+        const size_t before = (size_t)((STAGE & 1) ^ 1) * s.rows + bh;      // the last stage's
+        const uint32_t* last = s.hist + before * s.parts * kEvictBins;
+        above = s.above[before * s.parts + p];
+        const uint4 own = load16(last, ((size_t)p * kEvictBins + 4 * tid) * sizeof(uint32_t));
         int need = row.keep;
-        now = was[p];
-        if (STAGE == 1)
-            for (int i = 0; i < part.n_parts; ++i) need -= was[i].guarded;
-        else need = s.found[(STAGE - 2) * s.rows + bh].need;
-        if (need <= 0) {      // (the protected ones alone are as many as stay)
-            if (tid == 0 && p == 0) s.found[(STAGE - 1) * s.rows + bh] = EvictFound{0u, need};
-            if (tid == 0) state[p] = now;
-            return;
+        if (STAGE == 2) {
+            const EvictFound f = s.found[bh];
+            need = f.need;
+            prefix = f.prefix;
         }
-        const int3 found = find_bin<kEvictThreads>(need, sh_find, [&](int bin) {
-            uint32_t sum = 0;
-            for (int i = 0; i < part.n_parts; ++i) sum += last[(size_t)i * kEvictBins + bin];
-            return sum;
-        });
-        need -= found.y;
-        prefix = (STAGE == 2 ? s.found[bh].prefix : 0u) | (uint32_t)found.x << kLast;
-        if (tid == 0 && p == 0) s.found[(STAGE - 1) * s.rows + bh] = EvictFound{prefix, need};
-        int above = 0;
-        for (int bin = found.x + 1 + tid; bin < kEvictBins; bin += kEvictThreads) above += (int)last[(size_t)p * kEvictBins + bin];
-        if (above) atomicAdd(&sh_above, above);
+        const int3 found = find_bin<kPartThreads>(need, sh_find, [&](int bin, uint32_t* c) { sum_parts(last, part.n_parts, bin, c); });
+        prefix |= (uint32_t)found.x << kKnown;
+        if (tid == 0 && p == 0) s.found[(size_t)(STAGE - 1) * s.rows + bh] = EvictFound{prefix, need - found.y};
+        const int more = above_bin(own, 4 * tid, found.x);
+        if (more) atomicAdd(&sh_above, more);
     }
     __syncthreads();
-    held.each([&](int, uint32_t k, bool in) {
-        const bool guarded = in && k == kProtected;
-        if (STAGE == 0) {
-            const uint64_t g = __ballot(guarded);
-            if (lane_id() == 0 && g) atomicAdd(&sh_guarded, (int)__popcll(g));
-        }
-        if (!in || guarded) return;
-        if (STAGE > 0 && (k ^ prefix) >> kLast) return;
-        atomicAdd(&hist[(k >> kShift) & (STAGE == 2 ? 1023u : 2047u)], 1u);
-    });
+    count_keys<STAGE, kPartThreads>(held, prefix, hist);
     __syncthreads();
-    for (int i = tid; i < kEvictBins; i += kEvictThreads) mine[i] = hist[i];
-    if (tid == 0) state[p] = STAGE == 0 ? EvictPart{sh_guarded, sh_guarded} : EvictPart{now.above + sh_above, now.guarded};
+    *reinterpret_cast<uint4*>(mine + 4 * tid) = *reinterpret_cast<const uint4*>(hist + 4 * tid);
+    if (tid == 0) s.above[((size_t)(STAGE & 1) * s.rows + bh) * s.parts + p] = above + sh_above;
 }
 
-__global__ __launch_bounds__(kEvictThreads, 4) void page_evict_list_kernel(EvictArgs a, EvictLong s) {
-    constexpr int WAVES = kEvictThreads / LEOAM_WAVE;
+__global__ __launch_bounds__(kPartThreads, 4) void page_evict_list_kernel(EvictArgs a, EvictLong s) {
+    constexpr int WAVES = kPartThreads / LEOAM_WAVE;
     __shared__ int sh_find[WAVES + 3], sh_above[WAVES], sh_equal[WAVES], sh_sums[4];
     const int tid = threadIdx.x, lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(tid / LEOAM_WAVE);
     const int bh = blockIdx.x / s.parts, p = blockIdx.x % s.parts;
@@ -322,45 +321,33 @@ __global__ __launch_bounds__(kEvictThreads, 4) void page_evict_list_kernel(Evict
     if (row.none) return;
     const PartOf part(row, p);
     if (p >= part.n_parts) return;
-    const HeldKeys<kEvictThreads> held(row, part.begin, part.end);
+    const HeldKeys<kPartThreads> held(row, part.begin, part.end);
     const uint32_t* last = s.hist + (size_t)bh * s.parts * kEvictBins;      // (stage 2's)
-    const EvictPart* state = s.part + (size_t)bh * s.parts;
+    const int* state = s.above + (size_t)bh * s.parts;
     if (tid < 4) sh_sums[tid] = 0;
-    uint32_t bound = kProtected;
-    int ties = row.keep, bin = kEvictBins;
     const EvictFound before = s.found[s.rows + bh];
-    if (before.need > 0) {
-        const int3 found = find_bin<kEvictThreads>(before.need, sh_find, [&](int i) {
-            uint32_t sum = 0;
-            for (int q = 0; q < part.n_parts; ++q) sum += last[(size_t)q * kEvictBins + i];
-            return sum;
-        });
-        bin = found.x;
-        bound = before.prefix | (uint32_t)bin;
-        ties = before.need - found.y;
-    }
-    __syncthreads();
+    const int3 found = find_bin<kPartThreads>(before.need, sh_find, [&](int i, uint32_t* c) { sum_parts(last, part.n_parts, i, c); });
+    const uint32_t bound = before.prefix | (uint32_t)found.x;
+    const int ties = before.need - found.y;
     // the parts' keys above the bound and equal to it: those of parts before this one, those of parts below `keep`; a wave to a part
     for (int q = wave; q < part.n_parts; q += WAVES) {
         if (q >= p && q >= part.n_low) continue;
-        int above = 0, equal = 0;
-        if (bin < kEvictBins) {
-            for (int i = lane; i < 1024; i += LEOAM_WAVE) above += i > bin ? (int)last[(size_t)q * kEvictBins + i] : 0;
-            for (int d = 32; d > 0; d >>= 1) above += __shfl_xor(above, d, LEOAM_WAVE);
-            above += state[q].above;
-            equal = (int)last[(size_t)q * kEvictBins + bin];
-        } else {
-            equal = state[q].guarded;
+        const uint32_t* mine = last + (size_t)q * kEvictBins;
+        const int equal = (int)mine[found.x];
+        int above = lane == 0 ? state[q] : 0;
+        uint4 x[4];      // (stage 2 has 1024 bins)
+#pragma unroll
+        for (int u = 0; u < 4; ++u) x[u] = *reinterpret_cast<const uint4*>(mine + 256 * u + 4 * lane);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) above += above_bin(x[u], 256 * u + 4 * lane, found.x);
+        above = __builtin_amdgcn_readlane((int)wave_incl_scan_u32((uint32_t)above), LEOAM_WAVE - 1);
+        if (lane == 0 && q < p) {
+            atomicAdd(&sh_sums[0], above);
+            atomicAdd(&sh_sums[1], equal);
         }
-        if (lane == 0) {
-            if (q < p) {
-                atomicAdd(&sh_sums[0], above);
-                atomicAdd(&sh_sums[1], equal);
-            }
-            if (q < part.n_low) {
-                atomicAdd(&sh_sums[2], above);
-                atomicAdd(&sh_sums[3], equal);
-            }
+        if (lane == 0 && q < part.n_low) {
+            atomicAdd(&sh_sums[2], above);
+            atomicAdd(&sh_sums[3], equal);
         }
     }
     int above = 0, equal = 0;
@@ -373,27 +360,23 @@ __global__ __launch_bounds__(kEvictThreads, 4) void page_evict_list_kernel(Evict
         sh_equal[wave] = equal;
     }
     __syncthreads();
-    above = sh_sums[0];
-    equal = sh_sums[1];
-    for (int w = 0; w < wave; ++w) {
-        above += sh_above[w];
-        equal += sh_equal[w];
-    }
+    above = sh_sums[0] + before_wave<WAVES>(sh_above, wave);
+    equal = sh_sums[1] + before_wave<WAVES>(sh_equal, wave);
     const int kept_low = sh_sums[2] + min(sh_sums[3], ties);
     if (tid == 0 && p == 0) a.move_count[bh] = row.keep - kept_low;
-    list_moves<kEvictThreads>(held, row.keep, bound, ties, above, equal, kept_low, a.moves + (size_t)bh * a.m_max * 2);
+    list_moves<kPartThreads>(held, row.keep, bound, ties, above, equal, kept_low, a.moves + (size_t)bh * a.m_max * 2);
 }
 
 static int evict_parts(const leoam_pages* s) {
     const int capacity = s->max_pages * s->page_size;
-    return capacity <= kEvictPart ? 0 : capacity / kEvictPart + 2;      // (0: a row to a workgroup)
+    return capacity <= kEvictRowMost ? 0 : capacity / kEvictPart + 2;      // (0: a row to a workgroup)
 }
 static size_t evict_hist_bytes(const leoam_pages* s) {
     return 2 * (size_t)s->batch * s->n_kv_heads * evict_parts(s) * kEvictBins * sizeof(uint32_t);
 }
-static size_t evict_part_bytes(const leoam_pages* s) { return 2 * (size_t)s->batch * s->n_kv_heads * evict_parts(s) * sizeof(EvictPart); }
+static size_t evict_above_bytes(const leoam_pages* s) { return 2 * (size_t)s->batch * s->n_kv_heads * evict_parts(s) * sizeof(int); }
 size_t page_evict_workspace_bytes(const leoam_pages* s) {
-    return evict_hist_bytes(s) + evict_part_bytes(s) + 2 * (size_t)s->batch * s->n_kv_heads * sizeof(EvictFound);
+    return evict_hist_bytes(s) + evict_above_bytes(s) + 2 * (size_t)s->batch * s->n_kv_heads * sizeof(EvictFound);
 }
 
 hipError_t page_evict_dispatch(const leoam_pages* s, const float* weight, const int32_t* token_id, const int32_t* n_seen,
@@ -412,10 +395,10 @@ hipError_t page_evict_dispatch(const leoam_pages* s, const float* weight, const 
     if ((long long)rows * parts > 0x7fffffffll) return hipErrorInvalidValue;
     EvictLong l;
     l.hist = (uint32_t*)workspace;
-    l.part = (EvictPart*)((char*)workspace + evict_hist_bytes(s));
-    l.found = (EvictFound*)((char*)workspace + evict_hist_bytes(s) + evict_part_bytes(s));
+    l.above = (int*)((char*)workspace + evict_hist_bytes(s));
+    l.found = (EvictFound*)((char*)workspace + evict_hist_bytes(s) + evict_above_bytes(s));
     l.rows = rows; l.parts = parts;
-    const dim3 grid((unsigned)(rows * parts)), block(kEvictThreads);
+    const dim3 grid((unsigned)(rows * parts)), block(kPartThreads);
     hipLaunchKernelGGL(page_evict_hist_kernel<0>, grid, block, 0, stream, a, l);
     hipLaunchKernelGGL(page_evict_hist_kernel<1>, grid, block, 0, stream, a, l);
     hipLaunchKernelGGL(page_evict_hist_kernel<2>, grid, block, 0, stream, a, l);

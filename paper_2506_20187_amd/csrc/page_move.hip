@@ -50,7 +50,7 @@ template <typename T> __device__ __forceinline__ float move_scale_of(float amax)
     return bits_to_float((uint32_t)(e + 127) << 23);
 }
 
-template <typename T, typename S> __global__ __launch_bounds__(kMoveThreads) void page_move_kernel(MoveArgs a) {
+template <typename T, typename S> __global__ __launch_bounds__(kMoveThreads, 4) void page_move_kernel(MoveArgs a) {
     constexpr bool k8 = std::is_same<S, E4M3>::value;
     constexpr int EPL = T::kEpl, LPR = LEOAM_D / EPL, RPL = LEOAM_WAVE / LPR;      // lanes to a row, rows to a load
     constexpr int ROWB = LEOAM_D * S::kBytes, BATCH = 8;                             // loads that are on their way together
@@ -79,19 +79,20 @@ template <typename T, typename S> __global__ __launch_bounds__(kMoveThreads) voi
 
     // page p, whose pairs begin at i0 (i0 == n: none)
     auto take = [&](int p, int i0) {
-        const int id = uniform(table[p]);
+        const int entry = table[p];
+        int2 pair = moves[min(i0 + lane, max(n - 1, 0))];      // (m_max >= 1: there is an entry)
+        for (int r = lane; r < ps; r += LEOAM_WAVE) from[r] = -1;
+        const int id = uniform(entry);
         if ((uint32_t)id >= (uint32_t)a.n_pages) return;
         const size_t row_of_page = (size_t)id * hkv + h;
         const float old = k8 ? scales[row_of_page] : 1.f;
-        for (int r = lane; r < ps; r += LEOAM_WAVE) from[r] = -1;
         int n_rows = 0;
         for (int j0 = 0; j0 < ps; j0 += LEOAM_WAVE) {
             const int i = i0 + j0 + lane;
-            const bool listed = i < n && j0 + lane < ps;
-            const int2 pair = moves[min(i, n - 1 < 0 ? 0 : n - 1)];      // (m_max >= 1: there is an entry)
-            const bool mine = listed && pair.x >> a.page_shift == p, inside = mine && pair.x < new_len && pair.y >= new_len && pair.y < old_len;
-            const int src_id = inside ? table[pair.y >> a.page_shift] : -1;
-            const bool fits = (uint32_t)src_id < (uint32_t)a.n_pages;
+            if (j0 > 0) pair = moves[min(i, n - 1)];
+            const bool mine = i < n && j0 + lane < ps && pair.x >> a.page_shift == p, inside = mine && pair.x < new_len && pair.y >= new_len && pair.y < old_len;
+            const int src_id = table[inside ? pair.y >> a.page_shift : p];
+            const bool fits = inside && (uint32_t)src_id < (uint32_t)a.n_pages;
             const uint64_t hit = __ballot(fits);
             if (fits) {
                 const size_t row = (size_t)src_id * hkv + h;
@@ -99,9 +100,13 @@ template <typename T, typename S> __global__ __launch_bounds__(kMoveThreads) voi
                 from[to] = (long long)(((row << a.page_shift) + (pair.y & (ps - 1))) * ROWB);
                 if constexpr (k8) from_scale[to] = scales[row];
                 rows[n_rows + __popcll(hit & ((1ull << lane) - 1))] = (int16_t)to;
-                const size_t at = (size_t)bh * cap;
-                if (which == 0 && a.weight) a.weight[at + pair.x] = a.weight[at + pair.y];
-                if (which == 0 && a.token_id) a.token_id[at + pair.x] = a.token_id[at + pair.y];
+                if (which) {      // (the keys' waves have the abstracts to see to)
+                    const size_t at = (size_t)bh * cap;
+                    const float moved_weight = a.weight ? a.weight[at + pair.y] : 0.f;
+                    const int moved_id = a.token_id ? a.token_id[at + pair.y] : 0;
+                    if (a.weight) a.weight[at + pair.x] = moved_weight;
+                    if (a.token_id) a.token_id[at + pair.x] = moved_id;
+                }
             }
             n_rows += __popcll(hit);
             if (__ballot(mine) != ~0ull) break;
