@@ -11,6 +11,8 @@
 // tokens, then O^T = V^T P^T with the weights in two fp16 or three bf16 parts.  Here a wave has two blocks of 16 columns, so what it
 // fetches is used twice; up to 32 columns the four waves take a quarter of the tokens each, up to 64 two waves
 // share tokens, up to 128 all four do, with a quarter of the columns each, and the first-level cache serves them.
+#include <cfloat>
+
 #include "page_common.h"
 
 namespace leoam {
@@ -30,15 +32,22 @@ struct PageSharedArgs {
     const float *k_scale, *v_scale;
     const int32_t *page_table, *seq_len, *group_off, *group_pages;
     int n_groups;
-    float scale_log2;
+    float scale_log2;      // of |softmax_scale|
+    uint32_t flip;         // sign bits of the queries, turned if softmax_scale is negative
     float *out, *lse;
     SharedRow* rows;
-    float *own, *pre, *slots;      // whole states of (sequence, head), pieces
+    // States: 128 accumulators, and apart from them the maximum and the sum.  First the whole ones of each head over its own tokens, then
+    // those over its group's prefix, then the slots of pieces, of kSharedColumns columns each.
+    float *acc, *ml;
+    int n_heads;
     int sharers;
     int batch, n_kv_heads, group_shift, n_pages, page_shift, max_pages;
 };
 
-template <typename T> constexpr int shared_bias() { return T::kTag == LEOAM_F16 ? 15 : 0; }      // as decode_bias
+// The reference of a column's weights may lag its maximum by 2^kSharedLag, so that the accumulators are rarely scaled; fp16 weights take
+// it 2^7 lower, so that small ones stay clear of fp16's subnormals and the largest below its maximum.
+constexpr float kSharedLag = 8.f;
+template <typename T> constexpr int shared_bias() { return T::kTag == LEOAM_F16 ? 7 : 0; }
 
 // a 16-token tile of the walk (wave-uniform)
 struct SharedTile {
@@ -55,10 +64,23 @@ template <typename T, typename S> struct SharedStep {
     typename std::conditional<k8, uint2, uint4>::type v[8];
 };
 
-// What a unit's beginning costs a workgroup, in tiles.
-constexpr int kSharedStart = 2;
+// What a tile costs a workgroup whose waves go `ways` over the columns, and what a unit's beginning does: shares are measured in that.
+// (Every wave of a workgroup that goes four ways multiplies all of a tile.)
+template <bool k8> __device__ __forceinline__ int tile_cost(int ways) { return ways == 1 ? 2 : ways == 2 ? (k8 ? 4 : 3) : (k8 ? 8 : 5); }
+constexpr int kSharedStart = 4;
+constexpr int kMostTileCost = 8;
 
 __device__ __forceinline__ int shared_tiles(int tokens) { return max(1, (tokens + kSharedTile - 1) / kSharedTile); }
+// of the waves, over a unit's columns
+__device__ __forceinline__ int ways_of(int n_cols) { return n_cols <= kWaveColumns ? 1 : n_cols <= 2 * kWaveColumns ? 2 : 4; }
+
+// Units of an entry (a group's prefix, or a sequence's own tokens): `full` ones of most columns, then `rest` of the others.
+struct SharedEntry {
+    int full, rest, tiles, cost_full, cost_rest;
+    __device__ __forceinline__ long long length(int unit) const { return kSharedStart + (long long)tiles * cost(unit); }
+    __device__ __forceinline__ int cost(int unit) const { return unit < full ? cost_full : cost_rest; }
+    __device__ __forceinline__ long long total() const { return full * length(0) + rest * (kSharedStart + (long long)tiles * cost_rest); }
+};
 
 template <typename T, typename S>
 __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))) void page_shared_kernel(PageSharedArgs a) {
@@ -67,7 +89,8 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
     constexpr int ROWB = LEOAM_D * S::kBytes, QROWB = Row<T>::kRowBytes, NT = Step::NT, NK = Step::NK, STEP = 16 * NT, NQ = k32 ? 8 : 4;
     constexpr float kBias = shared_bias<T>();
     constexpr int kParts = T::kTag == LEOAM_F16 ? 2 : 3;
-    __shared__ float xw[kAttWaves][kWaveColumns][kPartStride];
+    constexpr int kStride = LEOAM_D + 4;      // of a column in LDS: its accumulators, maximum and sum
+    __shared__ __align__(16) float xw[kAttWaves][kWaveColumns][kStride];
     __shared__ int sh_off[kGroupsInLds + 1], sh_pages[kGroupsInLds];
     __shared__ long long sh_sum[kAttWaves], sh_at;
     __shared__ int sh_entry;
@@ -100,27 +123,24 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
         const int shared = prefix_of(lo - 1);
         return len >= shared ? shared : 0;      // (a sequence that is shorter has all of its tokens to itself)
     };
-    // entries: groups, then sequences.  Units of an entry, and tiles of each.
-    struct Entry { int units, tiles; };
+    // entries: groups, then sequences
     auto entry_of = [&](int e) {
         if (e < a.n_groups) {
             const int members = off_of(e + 1) - off_of(e), tokens = prefix_of(e);
-            if (members <= 0 || tokens == 0) return Entry{0, 0};
-            return Entry{(members + most_members - 1) / most_members * hkv, shared_tiles(tokens) + kSharedStart};
+            if (members <= 0 || tokens == 0) return SharedEntry{0, 0, 0, 1, 1};
+            const int full = members / most_members, rest = members - full * most_members;
+            return SharedEntry{full * hkv, rest ? hkv : 0, shared_tiles(tokens), tile_cost<k8>(4), tile_cost<k8>(ways_of(rest << a.group_shift))};
         }
         const int b = e - a.n_groups, len = length_of(b);
-        return Entry{hkv, shared_tiles(len - before_of(b, len)) + kSharedStart};
+        return SharedEntry{0, hkv, shared_tiles(len - before_of(b, len)), 1, tile_cost<k8>(1)};
     };
     const int n_entries = a.n_groups + a.batch;
-    long long pos, end, share;
-    int entry, unit, off;
+    long long pos, end, share, off;      // off: how far into the unit pos is
+    int entry, unit;
     {
         const int per = (n_entries + kAttThreads - 1) / kAttThreads, e0 = min(tid * per, n_entries), e1 = min(e0 + per, n_entries);
         long long mine = 0;
-        for (int e = e0; e < e1; ++e) {
-            const Entry x = entry_of(e);
-            mine += (long long)x.units * x.tiles;
-        }
+        for (int e = e0; e < e1; ++e) mine += entry_of(e).total();
         long long incl = mine;
 #pragma unroll
         for (int d = 1; d < LEOAM_WAVE; d <<= 1) {
@@ -135,15 +155,14 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
             if (w < wave) before += sh_sum[w];
             total += sh_sum[w];
         }
-        share = (total + a.sharers - 1) / a.sharers;
+        share = max((total + a.sharers - 1) / a.sharers, (long long)kMostTileCost);      // (so that a tile begins in each)
         pos = share * blockIdx.x;
         end = min(total, pos + share);
         if (pos >= end) return;
         if (pos >= before && pos < before + mine) {
             int e = e0;
             for (;;) {
-                const Entry x = entry_of(e);
-                const long long n = (long long)x.units * x.tiles;
+                const long long n = entry_of(e).total();
                 if (pos < before + n) break;
                 before += n;
                 ++e;
@@ -153,14 +172,16 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
         }
         __syncthreads();
         entry = uniform(sh_entry);
-        const Entry x = entry_of(entry);
-        unit = uniform((int)(sh_at / x.tiles));
-        off = uniform((int)(sh_at - (long long)unit * x.tiles));
+        const SharedEntry x = entry_of(entry);
+        const long long at = sh_at, full = x.full * x.length(0), in = at < full ? at : at - full, length = at < full ? x.length(0) : x.length(x.full);
+        unit = uniform((int)(in / length));
+        off = in - unit * length;
+        if (at >= full) unit += x.full;
     }
 
     // One stretch of a unit: tokens [t_begin, t_end) of row b_table, for this wave's columns, NB blocks of 16; `col_row`: the lane's
     // row of q in each block, < 0: none.
-    auto walk = [&](auto blocks, int b_table, int h, int t_begin, int t_end, int stream, int n_streams, const long long* col_row) {
+    auto walk = [&](auto blocks, int b_table, int h, int t_begin, int t_end, int way, int ways, int n_cols, const long long* col_row, auto&& leave) {
         constexpr int NB = decltype(blocks)::value;
         uint4 qb[NB][NQ];
 #pragma unroll
@@ -171,7 +192,9 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
                 const int byte = k32 ? 64 * s + 16 * grp : k8 ? 128 * (s >> 1) + 32 * grp + 16 * (s & 1) : 64 * s + 16 * grp;
                 qb[n][s] = make_uint4(0, 0, 0, 0);
                 if (col_row[n] >= 0) qb[n][s] = load16(a.q, (size_t)col_row[n] * QROWB + byte);
+                qb[n][s].x ^= a.flip; qb[n][s].y ^= a.flip; qb[n][s].z ^= a.flip; qb[n][s].w ^= a.flip;
             }
+        const int n_streams = kAttWaves / ways, stream = wave / ways;
         const int n_steps = (t_end - t_begin + STEP - 1) / STEP, per = (n_steps + n_streams - 1) / n_streams;
         const int s0 = min(n_steps, stream * per), s1 = min(n_steps, s0 + per);
 
@@ -282,19 +305,20 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
             bool partial = false;      // some tile has tokens that do not count
 #pragma unroll
             for (int j = 0; j < NT; ++j) partial |= at[j].valid < 16;
+            if (partial) {
+#pragma unroll
+                for (int n = 0; n < NB; ++n)
+#pragma unroll
+                    for (int i = 0; i < 4 * NT; ++i)
+                        if (4 * grp + i % 4 >= at[i / 4].valid) x[n][i] = -INFINITY;
+            }
 #pragma unroll
             for (int n = 0; n < NB; ++n) {
-                float z[4 * NT];
+                float mt = x[n][0];
 #pragma unroll
-                for (int i = 0; i < 4 * NT; ++i) {
-                    z[i] = x[n][i] * a.scale_log2;
-                    if (partial && 4 * grp + i % 4 >= at[i / 4].valid) z[i] = -INFINITY;
-                }
-                float mt = z[0];
-#pragma unroll
-                for (int i = 1; i < 4 * NT; ++i) mt = fmaxf(mt, z[i]);
-                mt = rows_max4(mt) - kBias;
-                if (__ballot(mt > m_run[n])) {
+                for (int i = 1; i < 4 * NT; ++i) mt = fmaxf(mt, x[n][i]);
+                mt = rows_max4(mt) * a.scale_log2 - kBias;
+                if (__ballot(mt > m_run[n] + kSharedLag)) {
                     const float m = fmaxf(m_run[n], mt), c = exp2_or_zero(m_run[n], m);
                     m_run[n] = m;
                     l_run[n] *= c;
@@ -307,7 +331,6 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
 #pragma unroll
                 for (int i = 0; i < 4 * NT; ++i) {
                     x[n][i] = exp2_raw(fmaf(x[n][i], a.scale_log2, -ref));
-                    if (partial && z[i] == -INFINITY) x[n][i] = 0.f;
                     l_run[n] += x[n][i];
                 }
             }
@@ -397,45 +420,84 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
                 for (int j = 0; j < NT; ++j) at[j] = next[j];
             }
         }
-        // ---- this wave's states ---------------------------------------------------------------------------
-        __syncthreads();      // (the previous stretch's states have been read)
+        // ---- the columns' states: leave(column, first of four channels, accumulators, maximum, sum) ------------
 #pragma unroll
         for (int n = 0; n < NB; ++n) {
             l_run[n] += shfl_xor_f(l_run[n], 16);
             l_run[n] += shfl_xor_f(l_run[n], 32);
+        }
+        // accumulator i, row 4 grp + r: its channel is 8 (4 grp + r) + i (fp32: 64 (i / 4) + 4 (4 grp + r) + i % 4)
+        auto four = [&](int n, int r, int half) {
+            return make_float4(acc[n][4 * half][r], acc[n][4 * half + 1][r], acc[n][4 * half + 2][r], acc[n][4 * half + 3][r]);
+        };
+        auto channel = [&](int r, int half) { return k32 ? 64 * half + 4 * (4 * grp + r) : 8 * (4 * grp + r) + 4 * half; };
+        if (n_streams == 1) {      // a wave has all of its columns' tokens
+#pragma unroll
+            for (int n = 0; n < NB; ++n) {
+                const int c = kWaveColumns * way + 16 * n + l16;
+                if (c >= n_cols) continue;
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) leave(c, channel(r, half), four(n, r, half), m_run[n], l_run[n]);
+            }
+            return;
+        }
+        __syncthreads();      // (the previous stretch's states have been read)
+#pragma unroll
+        for (int n = 0; n < NB; ++n) {
             float* x = xw[wave][16 * n + l16];
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
+            for (int r = 0; r < 4; ++r)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    // row 4 grp + r of accumulator i: its channel
-                    const int d = k32 ? 64 * (i / 4) + 4 * (4 * grp + r) + (i & 3) : 8 * (4 * grp + r) + i;
-                    x[d] = acc[n][i][r];
-                }
+                for (int half = 0; half < 2; ++half) *reinterpret_cast<float4*>(x + channel(r, half)) = four(n, r, half);
             if (grp == 0) {
                 x[LEOAM_D] = m_run[n];
                 x[LEOAM_D + 1] = l_run[n];
             }
         }
         __syncthreads();
+        for (int i = tid; i < n_cols * (LEOAM_D / 4); i += kAttThreads) {
+            const int c = i / (LEOAM_D / 4), d = 4 * (i % (LEOAM_D / 4)), w0 = c / kWaveColumns, in = c % kWaveColumns;
+            float ms[kAttWaves], m = -INFINITY;
+#pragma unroll
+            for (int k = 0; k < kAttWaves; ++k) {      // (two ways: waves w0 and w0 + 2)
+                ms[k] = k < n_streams ? xw[w0 + k * ways][in][LEOAM_D] : -INFINITY;
+                m = fmaxf(m, ms[k]);
+            }
+            float l = 0.f;
+            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int k = 0; k < kAttWaves; ++k) {
+                if (k >= n_streams) break;
+                const float f = exp2_or_zero(ms[k], m);
+                const float4 x = *reinterpret_cast<const float4*>(&xw[w0 + k * ways][in][d]);
+                l += f * xw[w0 + k * ways][in][LEOAM_D + 1];
+                v.x += f * x.x; v.y += f * x.y; v.z += f * x.z; v.w += f * x.w;
+            }
+            leave(c, d, v, m, l);
+        }
     };
 
     bool first_piece = true;
     while (pos < end) {
-        const Entry x = entry_of(entry);
-        const int units = uniform(x.units), tiles = uniform(x.tiles) - kSharedStart;
+        const SharedEntry x = entry_of(entry);
+        const int units = uniform(x.full + x.rest);
         if (units == 0) {      // (a group without a prefix)
             ++entry;
             continue;
         }
-        const int take = uniform((int)min((long long)(kSharedStart + tiles - off), end - pos));
-        const int tile0 = max(off - kSharedStart, 0), tile1 = off + take - kSharedStart;
-        if (tile0 < tile1) {      // (the share may end before the unit's first tile)
+        const int tiles = uniform(x.tiles), cost = uniform(x.cost(unit));
+        const long long length = kSharedStart + (long long)tiles * cost, take = min(length - off, end - pos);
+        // tiles that begin in the share
+        auto tiles_before = [&](long long at) { return at <= kSharedStart ? 0 : (int)((at - kSharedStart + cost - 1) / cost); };
+        const int tile0 = uniform(tiles_before(off)), tile1 = uniform(min(tiles, tiles_before(off + take)));
+        if (tile0 < tile1) {
             const int h = unit % hkv;
             const bool prefix = entry < a.n_groups, whole = tile1 - tile0 == tiles;
             const int slot = 2 * (int)blockIdx.x + (first_piece ? 0 : 1);      // opens the share, or closes it
             // pieces of the unit, and where the first lies, if it begins here
-            const int count = whole ? kWhole : (int)((pos - off + kSharedStart + tiles - 1) / share - blockIdx.x) + 1;
+            const int count = whole ? kWhole : (int)((pos - off + kSharedStart + (long long)(tiles - 1) * cost) / share - blockIdx.x) + 1;
             int n_cols, b0, tokens, before = 0, b_table;
             bool work = true;
             if (prefix) {
@@ -474,8 +536,8 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
                 if (before == 0) r->pre_count = 0;
             }
             if (work && (tokens > 0 || final_)) {
-                const int ways = n_cols <= kWaveColumns ? 1 : n_cols <= 2 * kWaveColumns ? 2 : 4;      // of the waves, over the columns
-                const int way = wave & (ways - 1), stream = wave / ways;
+                const int ways = ways_of(n_cols);
+                const int way = wave & (ways - 1);
                 long long col_row[2];
 #pragma unroll
                 for (int n = 0; n < 2; ++n) {
@@ -484,30 +546,20 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
                     col_row[n] = counts ? (((long long)b * hkv + h) << a.group_shift) + (c & (group - 1)) : -1;
                 }
                 const int t_begin = before + tile0 * kSharedTile, t_end = before + min(tokens, tile1 * kSharedTile);
-                if (n_cols <= 16) walk(std::integral_constant<int, 1>{}, b_table, h, t_begin, t_end, stream, kAttWaves / ways, col_row);
-                else walk(std::integral_constant<int, 2>{}, b_table, h, t_begin, t_end, stream, kAttWaves / ways, col_row);
-                // ---- the streams' states into one -----------------------------------------------------------
-                for (int i = tid; i < n_cols * kPartStride; i += kAttThreads) {
-                    const int c = i / kPartStride, d = i % kPartStride, w0 = c / kWaveColumns, in = c % kWaveColumns;
-                    float m = -INFINITY;
-                    for (int w = w0; w < kAttWaves; w += ways) m = fmaxf(m, xw[w][in][LEOAM_D]);
-                    float v = 0.f, l = 0.f;
-                    for (int w = w0; w < kAttWaves; w += ways) {
-                        const float f = exp2_or_zero(xw[w][in][LEOAM_D], m);
-                        l += f * xw[w][in][LEOAM_D + 1];
-                        if (d < LEOAM_D) v += f * xw[w][in][d];
-                    }
-                    const float state = d < LEOAM_D ? v : d == LEOAM_D ? m : l;
+                auto leave = [&](int c, int d, const float4& v, float m, float l) {
                     const size_t j = (((size_t)(b0 + (c >> a.group_shift)) * hkv + h) << a.group_shift) + (c & (group - 1));
                     if (final_) {
-                        if (d < LEOAM_D) a.out[j * LEOAM_D + d] = l == 0.f ? 0.f : v / l;      // (NaN stays)
-                        else if (d == LEOAM_D && a.lse) a.lse[j] = log_sum_exp(m, l, shared_bias<T>());
-                    } else if (whole) {
-                        (prefix ? a.pre : a.own)[j * kPartStride + d] = state;
-                    } else {
-                        a.slots[((size_t)slot * kSharedColumns + c) * kPartStride + d] = state;
+                        const float inv = l == 0.f ? 0.f : 1.f / l;      // (NaN stays)
+                        *reinterpret_cast<float4*>(a.out + j * LEOAM_D + d) = make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
+                        if (d == 0 && a.lse) a.lse[j] = log_sum_exp(m, l, shared_bias<T>());
+                        return;
                     }
-                }
+                    const size_t at = !whole ? 2 * (size_t)a.n_heads + (size_t)slot * kSharedColumns + c : prefix ? a.n_heads + j : j;
+                    *reinterpret_cast<float4*>(a.acc + at * LEOAM_D + d) = v;
+                    if (d == 0) *reinterpret_cast<float2*>(a.ml + 2 * at) = make_float2(m, l);
+                };
+                if (n_cols <= 16) walk(std::integral_constant<int, 1>{}, b_table, h, t_begin, t_end, way, ways, n_cols, col_row, leave);
+                else walk(std::integral_constant<int, 2>{}, b_table, h, t_begin, t_end, way, ways, n_cols, col_row, leave);
             }
             first_piece = false;
         }
@@ -521,9 +573,8 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
 }
 
 // A head's pieces: those of its group's unit, then its own.  128 threads take eight at a time, all on their way together.
-__global__ __launch_bounds__(2 * LEOAM_D) void page_shared_merge_kernel(const SharedRow* __restrict__ rows, const float* __restrict__ own,
-                                                                       const float* __restrict__ pre, const float* __restrict__ slots,
-                                                                       int group_shift, int n_heads, int sharers, int bias,
+__global__ __launch_bounds__(2 * LEOAM_D) void page_shared_merge_kernel(const SharedRow* __restrict__ rows, const float* __restrict__ acc,
+                                                                       const float* __restrict__ ml, int group_shift, int n_heads, int sharers, int bias,
                                                                        float* __restrict__ out, float* __restrict__ lse) {
     constexpr int kBatch = 8;
     const int d = threadIdx.x % LEOAM_D, j = 2 * blockIdx.x + threadIdx.x / LEOAM_D;
@@ -536,21 +587,22 @@ __global__ __launch_bounds__(2 * LEOAM_D) void page_shared_merge_kernel(const Sh
     auto state = [&](int i) {
         const bool mine = i >= n_pre;
         const int k = mine ? i - n_pre : i, count = mine ? r.own_count : r.pre_count;
-        if (count == kWhole) return (mine ? own : pre) + (size_t)j * kPartStride;
+        if (count == kWhole) return (size_t)(mine ? j : n_heads + j);
         // (each further piece opens the next workgroup's share)
         const int slot0 = mine ? r.own_slot : r.pre_slot, slot = min(max(k == 0 ? slot0 : 2 * (slot0 / 2 + k), 0), last);
         const int col = min(max(mine ? 0 : r.pre_col, 0), kSharedColumns - (1 << group_shift)) + g;
-        return slots + ((size_t)slot * kSharedColumns + col) * kPartStride;
+        return 2 * (size_t)n_heads + (size_t)slot * kSharedColumns + col;
     };
     float m = -INFINITY, l = 0.f, o = 0.f;
     for (int i0 = 0; i0 < n_pre + n_own; i0 += kBatch) {
         float ms[kBatch], ls[kBatch], os[kBatch];
 #pragma unroll
         for (int u = 0; u < kBatch; ++u) {
-            const float* p = state(min(i0 + u, n_pre + n_own - 1));
-            ms[u] = p[LEOAM_D];
-            ls[u] = p[LEOAM_D + 1];
-            os[u] = p[d];
+            const size_t at = state(min(i0 + u, n_pre + n_own - 1));
+            const float2 x = *reinterpret_cast<const float2*>(ml + 2 * at);
+            ms[u] = x.x;
+            ls[u] = x.y;
+            os[u] = acc[at * LEOAM_D + d];
         }
         float mb = m;
 #pragma unroll
@@ -577,9 +629,9 @@ __global__ __launch_bounds__(2 * LEOAM_D) void page_shared_merge_kernel(const Sh
 constexpr int kSharedGroups = 512;      // workgroups: two fill a compute unit
 
 static size_t shared_rows_bytes(const leoam_pages* s) { return ((size_t)s->batch * s->n_kv_heads * sizeof(SharedRow) + 255) / 256 * 256; }
-static size_t shared_state_bytes(const leoam_pages* s) { return ((size_t)s->batch * s->n_q_heads * kPartStride * sizeof(float) + 255) / 256 * 256; }
-static size_t shared_slot_bytes() { return 2 * (size_t)kSharedColumns * kPartStride * sizeof(float); }
-static size_t shared_fixed_bytes(const leoam_pages* s) { return shared_rows_bytes(s) + 2 * shared_state_bytes(s); }
+constexpr size_t kStateBytes = (LEOAM_D + 2) * sizeof(float);
+static size_t shared_fixed_bytes(const leoam_pages* s) { return shared_rows_bytes(s) + 2 * (size_t)s->batch * s->n_q_heads * kStateBytes; }
+static size_t shared_slot_bytes() { return 2 * (size_t)kSharedColumns * kStateBytes; }      // of a workgroup
 size_t page_shared_workspace_bytes(const leoam_pages* s, int) { return shared_fixed_bytes(s) + kSharedGroups * shared_slot_bytes(); }
 size_t page_shared_min_workspace_bytes(const leoam_pages* s) { return shared_fixed_bytes(s) + shared_slot_bytes(); }
 
@@ -587,9 +639,8 @@ template <typename T, typename S> static hipError_t launch_shared(const PageShar
     hipLaunchKernelGGL((page_shared_kernel<T, S>), dim3(a.sharers), dim3(kAttThreads), 0, stream, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    const int n_heads = a.batch * a.n_kv_heads << a.group_shift;
-    hipLaunchKernelGGL(page_shared_merge_kernel, dim3((n_heads + 1) / 2), dim3(2 * LEOAM_D), 0, stream, a.rows, a.own, a.pre, a.slots,
-                       a.group_shift, n_heads, a.sharers, shared_bias<T>(), a.out, a.lse);
+    hipLaunchKernelGGL(page_shared_merge_kernel, dim3((a.n_heads + 1) / 2), dim3(2 * LEOAM_D), 0, stream, a.rows, a.acc, a.ml,
+                       a.group_shift, a.n_heads, a.sharers, shared_bias<T>(), a.out, a.lse);
     return hipGetLastError();
 }
 
@@ -601,15 +652,17 @@ hipError_t page_shared_dispatch(const leoam_pages* s, const void* q, const void*
     a.q = (const char*)q; a.k_pages = (const char*)k_pages; a.v_pages = (const char*)v_pages;
     a.k_scale = k_scale; a.v_scale = v_scale; a.page_table = page_table; a.seq_len = seq_len;
     a.group_off = group_off; a.group_pages = group_pages; a.n_groups = n_groups;
-    a.scale_log2 = softmax_scale * kLog2e;
+    // (tokens that do not count have -inf before it is scaled: a scale of zero is the smallest there is instead)
+    a.scale_log2 = fmaxf(fabsf(softmax_scale) * kLog2e, FLT_MIN);
+    a.flip = softmax_scale < 0.f ? (s->q_dtype == LEOAM_F32 ? 0x80000000u : 0x80008000u) : 0u;
     a.out = out; a.lse = lse;
     char* ws = (char*)workspace;
     a.rows = (SharedRow*)ws;
-    a.own = (float*)(ws + shared_rows_bytes(s));
-    a.pre = (float*)(ws + shared_rows_bytes(s) + shared_state_bytes(s));
-    a.slots = (float*)(ws + shared_fixed_bytes(s));
     const size_t fit = (workspace_bytes - shared_fixed_bytes(s)) / shared_slot_bytes();
     a.sharers = (int)(fit < (size_t)kSharedGroups ? fit : (size_t)kSharedGroups);
+    a.n_heads = s->batch * s->n_q_heads;
+    a.acc = (float*)(ws + shared_rows_bytes(s));
+    a.ml = a.acc + (2 * (size_t)a.n_heads + 2 * (size_t)a.sharers * kSharedColumns) * LEOAM_D;
     a.batch = s->batch; a.n_kv_heads = s->n_kv_heads; a.group_shift = __builtin_ctz((unsigned)(s->n_q_heads / s->n_kv_heads));
     a.n_pages = s->n_pages; a.page_shift = __builtin_ctz((unsigned)s->page_size); a.max_pages = s->max_pages;
     const bool k8 = s->kv_dtype == LEOAM_E4M3;
