@@ -104,4 +104,31 @@ __device__ __forceinline__ float log_sum_exp(float m, float l, int bias) {
     return l == 0.f ? -INFINITY : ((m + (float)bias) + log2f(ldexpf(l, -bias))) * kLn2;
 }
 
+// ---- tiles of keys and values in LDS, 32x32 products ----------------------------------------------------
+typedef __attribute__((ext_vector_type(16))) float f32x16_t;
+typedef __attribute__((ext_vector_type(4))) short s16x4_t;
+
+template <typename T> __device__ __forceinline__ f32x16_t mfma_32x32x16(const uint4& a, const uint4& b, f32x16_t c);
+template <> __device__ __forceinline__ f32x16_t mfma_32x32x16<BF16>(const uint4& a, const uint4& b, f32x16_t c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
+}
+template <> __device__ __forceinline__ f32x16_t mfma_32x32x16<F16>(const uint4& a, const uint4& b, f32x16_t c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8_t, a), __builtin_bit_cast(f16x8_t, b), c, 0, 0, 0);
+}
+
+// four keys of one channel: lane l of 16 gives the address of channels 4 (l % 4) .. + 3 of key l / 4 and gets channel l
+__device__ __forceinline__ uint2 transposed(const char* at) {
+    return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)at));
+}
+
+// how the scheduler is to interleave what stands before it: n instructions of a kind
+enum : int { kMfma = 0x8, kValu = 0x2, kTrans = 0x400, kLdsRead = 0x100 };
+template <int KIND, int N> __device__ __forceinline__ void then() { __builtin_amdgcn_sched_group_barrier(KIND, N, 0); }
+
+// Bytes from one row to the next of a tile in LDS.  Keys are read 16 bytes of eight rows at a time: a row further is
+// four banks further.  Values are read, by half a wave, as 64 bytes of four rows (fp32: 128 bytes of two rows four apart): 16 banks
+// further (fp32: eight).  All offsets within a tile are constants that way.
+template <typename T> constexpr int kKeyStride = LEOAM_D * T::kBytes + 16;
+template <typename T> constexpr int kValueStride = LEOAM_D * T::kBytes + (T::kTag == LEOAM_F32 ? 32 : 64);
+
 }  // namespace leoam

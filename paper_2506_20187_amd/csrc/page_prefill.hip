@@ -20,9 +20,6 @@
 
 namespace leoam {
 
-typedef __attribute__((ext_vector_type(16))) float f32x16_t;
-typedef __attribute__((ext_vector_type(4))) short s16x4_t;
-
 constexpr int kRows = 128;            // query rows of a workgroup, 32 a wave
 
 // fp16 weights: the reference is taken 2^7 lower, so that small weights stay clear of fp16's subnormals
@@ -72,32 +69,9 @@ struct Shares {
 // a piece: [32 groups of 4 channels][128 rows][4], maxima, sums
 constexpr int kPieceFloats = kRows * (LEOAM_D + 2);
 
-// four keys of one channel: lane l of 16 gives the address of channels 4 (l % 4) .. + 3 of key l / 4 and gets channel l
-__device__ __forceinline__ uint2 transposed(const char* at) {
-    return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)at));
-}
-
-// how the scheduler is to interleave what stands before it: n instructions of a kind
-enum : int { kMfma = 0x8, kValu = 0x2, kTrans = 0x400, kLdsRead = 0x100 };
-template <int KIND, int N> __device__ __forceinline__ void then() { __builtin_amdgcn_sched_group_barrier(KIND, N, 0); }
-
 // the rows of a slot: sequence, its first row in the call, its number of rows, which tile of them, the sequence's length
 struct Unit { int b, row0, m, local, len; };
 __device__ __forceinline__ int first_slot_of(int row0, int i, int group) { return (int)((long long)row0 * group / kRows) + i; }
-
-template <typename T> __device__ __forceinline__ f32x16_t mfma_32x32x16(const uint4& a, const uint4& b, f32x16_t c);
-template <> __device__ __forceinline__ f32x16_t mfma_32x32x16<BF16>(const uint4& a, const uint4& b, f32x16_t c) {
-    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
-}
-template <> __device__ __forceinline__ f32x16_t mfma_32x32x16<F16>(const uint4& a, const uint4& b, f32x16_t c) {
-    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8_t, a), __builtin_bit_cast(f16x8_t, b), c, 0, 0, 0);
-}
-
-// Bytes from one row to the next of a tile in LDS.  Keys are read 16 bytes of eight rows at a time: a row further is
-// four banks further.  Values are read, by half a wave, as 64 bytes of four rows (fp32: 128 bytes of two rows four apart): 16 banks
-// further (fp32: eight).  All offsets within a tile are constants that way.
-template <typename T> constexpr int kKeyStride = LEOAM_D * T::kBytes + 16;
-template <typename T> constexpr int kValueStride = LEOAM_D * T::kBytes + (T::kTag == LEOAM_F32 ? 32 : 64);
 
 // the values of a register that are not finite become zero; whether there were any
 template <typename T> __device__ __forceinline__ bool silence(uint32_t& w) {

@@ -1,16 +1,18 @@
 // page_attention_decode_shared: softmax(scale q K^T) V of one token per sequence where groups of sequences list the same leading
 // pages: a group's prefix is read once for all of its members, each sequence's further pages by itself.
 //
-// HBM-bound up to some hundred (member, head) columns per kv head, by the matrix cores and the exponentials beyond.  A unit of work
+// HBM-bound up to some 64 (member, head) columns per kv head, by the matrix cores and the exponentials beyond.  A unit of work
 // is (up to 128 columns of a group, kv head) over the group's prefix, or (sequence, kv head) over its own tokens.  The tiles of all
 // units are laid end to end, each unit's beginning counted as some more, and shared out equally: the host does not know the
 // lengths.  A unit cut by the ends of shares leaves its pieces, (acc[128], m, l) per column, in the workspace; a second
 // kernel folds a head's pieces of its group's unit and of its own, in order, so results do not depend on scheduling.
 //
-// As in page_attention_decode everything runs on the matrix cores without passing through LDS: S^T = K Q^T, lane = column, registers =
-// tokens, then O^T = V^T P^T with the weights in two fp16 or three bf16 parts.  Here a wave has two blocks of 16 columns, so what it
-// fetches is used twice; up to 32 columns the four waves take a quarter of the tokens each, up to 64 two waves
-// share tokens, up to 128 all four do, with a quarter of the columns each, and the first-level cache serves them.
+// Up to 64 columns everything runs on the matrix cores without passing through LDS, as in page_attention_decode: S^T = K Q^T, lane =
+// column, registers = tokens, then O^T = V^T P^T.  A wave has one or two blocks of 16 columns, so what it fetches is used twice; beyond 32
+// columns two waves share tokens, with half of the columns each.  Beyond 64 the waves have 32 columns each and tiles of 64 keys go
+// through LDS, with 32x32 products as in page_attention_prefill: a key row from the caches is 16 bytes of 16 rows a load, which
+// the first-level cache serves at a quarter of its rate, four times over.  Weights go in as two fp16 or three bf16 numbers that add up to
+// them (22 or 24 bits), so the float output keeps its precision, at twice the cost of rounded ones beyond 64 columns.
 #include <cfloat>
 
 #include "page_common.h"
@@ -65,21 +67,36 @@ template <typename T, typename S> struct SharedStep {
 };
 
 // What a tile costs a workgroup whose waves go `ways` over the columns, and what a unit's beginning does: shares are measured in that.
-// (Every wave of a workgroup that goes four ways multiplies all of a tile.)
-template <bool k8> __device__ __forceinline__ int tile_cost(int ways) { return ways == 1 ? 2 : ways == 2 ? (k8 ? 4 : 3) : (k8 ? 8 : 5); }
+// (us for 48 sequences behind 32K in bf16, 70 in nine groups in 8 bits: 91, 87 with 5 for four ways; 89, 86 with 4; 98, 97 with all
+// half as much.)
+__device__ __forceinline__ int tile_cost(int ways) { return ways == 1 ? 2 : ways == 2 ? 3 : 4; }
 constexpr int kSharedStart = 4;
-constexpr int kMostTileCost = 8;
+constexpr int kMostTileCost = 4;
 
 __device__ __forceinline__ int shared_tiles(int tokens) { return max(1, (tokens + kSharedTile - 1) / kSharedTile); }
 // of the waves, over a unit's columns
 __device__ __forceinline__ int ways_of(int n_cols) { return n_cols <= kWaveColumns ? 1 : n_cols <= 2 * kWaveColumns ? 2 : 4; }
 
+// a / b of numbers that are not negative; a division in 64 bits takes a microsecond, and they rarely need it
+__device__ __forceinline__ long long quotient(long long a, long long b) {
+    return (unsigned long long)(a | b) >> 32 ? a / b : (long long)((uint32_t)a / (uint32_t)b);
+}
+
+// A value that the compiler takes for a new one, so that what is computed from it stays where it is used: what depends on the lane
+// alone it would compute for all walks ahead of the loop over units, in more registers than there are (51 of them in scratch memory,
+// 27 MB a launch).
+__device__ __forceinline__ int here(int v) {
+    asm volatile("" : "+v"(v));
+    return v;
+}
+
 // Units of an entry (a group's prefix, or a sequence's own tokens): `full` ones of most columns, then `rest` of the others.
 struct SharedEntry {
     int full, rest, tiles, cost_full, cost_rest;
-    __device__ __forceinline__ long long length(int unit) const { return kSharedStart + (long long)tiles * cost(unit); }
+    // (fewer than 2^23 tiles)
+    __device__ __forceinline__ int length(int unit) const { return kSharedStart + tiles * cost(unit); }
     __device__ __forceinline__ int cost(int unit) const { return unit < full ? cost_full : cost_rest; }
-    __device__ __forceinline__ long long total() const { return full * length(0) + rest * (kSharedStart + (long long)tiles * cost_rest); }
+    __device__ __forceinline__ long long total() const { return (long long)full * length(0) + (long long)rest * (kSharedStart + tiles * cost_rest); }
 };
 
 template <typename T, typename S>
@@ -90,12 +107,15 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
     constexpr float kBias = shared_bias<T>();
     constexpr int kParts = T::kTag == LEOAM_F16 ? 2 : 3;
     constexpr int kStride = LEOAM_D + 4;      // of a column in LDS: its accumulators, maximum and sum
-    __shared__ __align__(16) float xw[kAttWaves][kWaveColumns][kStride];
+    constexpr int KEYS = k32 ? 32 : 64, KSTR = kKeyStride<T>, VSTR = kValueStride<T>;      // of a tile in LDS
+    constexpr int kTilesBytes = 2 * KEYS * (KSTR + VSTR), kStatesBytes = kAttWaves * kWaveColumns * kStride * (int)sizeof(float);
+    __shared__ __align__(16) char smem[kTilesBytes > kStatesBytes ? kTilesBytes : kStatesBytes];
+    float (*xw)[kWaveColumns][kStride] = reinterpret_cast<float (*)[kWaveColumns][kStride]>(smem);
     __shared__ int sh_off[kGroupsInLds + 1], sh_pages[kGroupsInLds];
     __shared__ long long sh_sum[kAttWaves], sh_at;
     __shared__ int sh_entry;
 
-    const int tid = threadIdx.x, lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(tid / LEOAM_WAVE), grp = lane >> 4, l16 = lane & 15;
+    const int tid = threadIdx.x, lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(tid / LEOAM_WAVE);
     const int hkv = a.n_kv_heads, group = 1 << a.group_shift, cap = a.max_pages << a.page_shift;
     const int most_members = kSharedColumns >> a.group_shift;
 
@@ -129,14 +149,14 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
             const int members = off_of(e + 1) - off_of(e), tokens = prefix_of(e);
             if (members <= 0 || tokens == 0) return SharedEntry{0, 0, 0, 1, 1};
             const int full = members / most_members, rest = members - full * most_members;
-            return SharedEntry{full * hkv, rest ? hkv : 0, shared_tiles(tokens), tile_cost<k8>(4), tile_cost<k8>(ways_of(rest << a.group_shift))};
+            return SharedEntry{full * hkv, rest ? hkv : 0, shared_tiles(tokens), tile_cost(4), tile_cost(ways_of(rest << a.group_shift))};
         }
         const int b = e - a.n_groups, len = length_of(b);
-        return SharedEntry{0, hkv, shared_tiles(len - before_of(b, len)), 1, tile_cost<k8>(1)};
+        return SharedEntry{0, hkv, shared_tiles(len - before_of(b, len)), 1, tile_cost(1)};
     };
     const int n_entries = a.n_groups + a.batch;
-    long long pos, end, share, off;      // off: how far into the unit pos is
-    int entry, unit;
+    long long pos, end, share, first;      // its places on the line of all costs, [first, end), and where on it the work is
+    int entry, unit, off;                   // off: how far into the unit
     {
         const int per = (n_entries + kAttThreads - 1) / kAttThreads, e0 = min(tid * per, n_entries), e1 = min(e0 + per, n_entries);
         long long mine = 0;
@@ -155,8 +175,8 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
             if (w < wave) before += sh_sum[w];
             total += sh_sum[w];
         }
-        share = max((total + a.sharers - 1) / a.sharers, (long long)kMostTileCost);      // (so that a tile begins in each)
-        pos = share * blockIdx.x;
+        share = max(quotient(total + a.sharers - 1, a.sharers), (long long)kMostTileCost);      // (so that a tile begins in each)
+        pos = first = share * blockIdx.x;
         end = min(total, pos + share);
         if (pos >= end) return;
         if (pos >= before && pos < before + mine) {
@@ -173,16 +193,23 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
         __syncthreads();
         entry = uniform(sh_entry);
         const SharedEntry x = entry_of(entry);
-        const long long at = sh_at, full = x.full * x.length(0), in = at < full ? at : at - full, length = at < full ? x.length(0) : x.length(x.full);
-        unit = uniform((int)(in / length));
-        off = in - unit * length;
-        if (at >= full) unit += x.full;
+        const long long at = sh_at, full = (long long)x.full * x.length(0), in = at < full ? at : at - full;
+        const int length = at < full ? x.length(0) : x.length(x.full);
+        unit = uniform((int)quotient(in, length));
+        off = uniform((int)(in - (long long)unit * length));
+        if (at >= full) unit += uniform(x.full);
     }
 
-    // One stretch of a unit: tokens [t_begin, t_end) of row b_table, for this wave's columns, NB blocks of 16; `col_row`: the lane's
-    // row of q in each block, < 0: none.
-    auto walk = [&](auto blocks, int b_table, int h, int t_begin, int t_end, int way, int ways, int n_cols, const long long* col_row, auto&& leave) {
-        constexpr int NB = decltype(blocks)::value;
+    // a piece of a query as it takes part: with its sign turned, or zero
+    auto settle = [&](uint4& q, bool counts) {
+        q = counts ? make_uint4(q.x ^ a.flip, q.y ^ a.flip, q.z ^ a.flip, q.w ^ a.flip) : make_uint4(0, 0, 0, 0);
+    };
+    // One stretch of a unit: tokens [t_begin, t_end) of row b_table, for this wave's columns, NB blocks of 16, WAYS of the four waves on
+    // columns of their own.  rows, counts: the lane's row of q in each block, and whether the column is one.
+    auto walk = [&](auto blocks, auto apart, int b_table, int h, int t_begin, int t_end, int n_cols, const size_t* rows, const bool* counts,
+                    auto&& leave) {
+        const int lane = here(lane_id()), tid = here(threadIdx.x), grp = lane >> 4, l16 = lane & 15;
+        constexpr int NB = decltype(blocks)::value, WAYS = decltype(apart)::value, STREAMS = kAttWaves / WAYS;
         uint4 qb[NB][NQ];
 #pragma unroll
         for (int n = 0; n < NB; ++n)
@@ -190,13 +217,10 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
             for (int s = 0; s < NQ; ++s) {
                 // 16-byte pieces in the order in which a key row's loads hold the channels
                 const int byte = k32 ? 64 * s + 16 * grp : k8 ? 128 * (s >> 1) + 32 * grp + 16 * (s & 1) : 64 * s + 16 * grp;
-                qb[n][s] = make_uint4(0, 0, 0, 0);
-                if (col_row[n] >= 0) qb[n][s] = load16(a.q, (size_t)col_row[n] * QROWB + byte);
-                qb[n][s].x ^= a.flip; qb[n][s].y ^= a.flip; qb[n][s].z ^= a.flip; qb[n][s].w ^= a.flip;
+                qb[n][s] = load16(a.q, rows[n] * QROWB + byte);
             }
-        const int n_streams = kAttWaves / ways, stream = wave / ways;
-        const int n_steps = (t_end - t_begin + STEP - 1) / STEP, per = (n_steps + n_streams - 1) / n_streams;
-        const int s0 = min(n_steps, stream * per), s1 = min(n_steps, s0 + per);
+        const int n_steps = (t_end - t_begin + STEP - 1) / STEP, per = (n_steps + STREAMS - 1) / STREAMS;
+        const int s0 = min(n_steps, wave / WAYS * per), s1 = min(n_steps, s0 + per);
 
         // lane i holds entry held0 + i of the row's pages (-1: none)
         int held0 = -(1 << 30), held_page = -1;
@@ -408,6 +432,10 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
             where(s0, at);
             fetch_keys(at, st);
             fetch_values(at, st);
+#pragma unroll
+            for (int n = 0; n < NB; ++n)
+#pragma unroll
+                for (int s = 0; s < NQ; ++s) settle(qb[n][s], counts[n]);
             for (int s = s0; s < s1; ++s) {
                 float x[NB][4 * NT];
                 where(min(s + 1, s1 - 1), next);
@@ -431,19 +459,7 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
             return make_float4(acc[n][4 * half][r], acc[n][4 * half + 1][r], acc[n][4 * half + 2][r], acc[n][4 * half + 3][r]);
         };
         auto channel = [&](int r, int half) { return k32 ? 64 * half + 4 * (4 * grp + r) : 8 * (4 * grp + r) + 4 * half; };
-        if (n_streams == 1) {      // a wave has all of its columns' tokens
-#pragma unroll
-            for (int n = 0; n < NB; ++n) {
-                const int c = kWaveColumns * way + 16 * n + l16;
-                if (c >= n_cols) continue;
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-#pragma unroll
-                    for (int half = 0; half < 2; ++half) leave(c, channel(r, half), four(n, r, half), m_run[n], l_run[n]);
-            }
-            return;
-        }
-        __syncthreads();      // (the previous stretch's states have been read)
+        __syncthreads();      // (what the previous stretch left in LDS has been read)
 #pragma unroll
         for (int n = 0; n < NB; ++n) {
             float* x = xw[wave][16 * n + l16];
@@ -458,29 +474,250 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
         }
         __syncthreads();
         for (int i = tid; i < n_cols * (LEOAM_D / 4); i += kAttThreads) {
-            const int c = i / (LEOAM_D / 4), d = 4 * (i % (LEOAM_D / 4)), w0 = c / kWaveColumns, in = c % kWaveColumns;
-            float ms[kAttWaves], m = -INFINITY;
+            const int c = i / (LEOAM_D / 4), d = 4 * (i % (LEOAM_D / 4)), in = c % kWaveColumns;
+            const int w0 = WAYS == 1 ? 0 : c / kWaveColumns;
+            float ms[STREAMS], ls[STREAMS], m = -INFINITY, l = 0.f;
+            float4 x[STREAMS], v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-            for (int k = 0; k < kAttWaves; ++k) {      // (two ways: waves w0 and w0 + 2)
-                ms[k] = k < n_streams ? xw[w0 + k * ways][in][LEOAM_D] : -INFINITY;
+            for (int k = 0; k < STREAMS; ++k) {
+                const float* state = xw[w0 + k * WAYS][in];
+                x[k] = *reinterpret_cast<const float4*>(state + d);
+                ms[k] = state[LEOAM_D];
+                ls[k] = state[LEOAM_D + 1];
                 m = fmaxf(m, ms[k]);
             }
-            float l = 0.f;
-            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-            for (int k = 0; k < kAttWaves; ++k) {
-                if (k >= n_streams) break;
+            for (int k = 0; k < STREAMS; ++k) {
                 const float f = exp2_or_zero(ms[k], m);
-                const float4 x = *reinterpret_cast<const float4*>(&xw[w0 + k * ways][in][d]);
-                l += f * xw[w0 + k * ways][in][LEOAM_D + 1];
-                v.x += f * x.x; v.y += f * x.y; v.z += f * x.z; v.w += f * x.w;
+                l += f * ls[k];
+                v.x += f * x[k].x; v.y += f * x[k].y; v.z += f * x[k].z; v.w += f * x[k].w;
             }
             leave(c, d, v, m, l);
         }
     };
 
+    // The same for more than 64 columns, 32 of them a wave's: the workgroup's tiles of 64 keys (fp32: 32) go through LDS, the next (8 bits:
+    // the next two) on its way to registers.
+    auto walk_tiles = [&](int b_table, int h, int t_begin, int t_end, int n_cols, size_t my_row, bool counts, auto&& leave) {
+        constexpr int KB = KEYS / 32, PIECES = ROWB / 16, LOADS = KEYS * PIECES / kAttThreads, ROWS_PER_LOAD = kAttThreads / PIECES;
+        constexpr int GROUPS = KEYS / 16, AHEAD = k8 ? 2 : 1, NQ32 = k32 ? 16 : 8;      // (16 keys never straddle a page)
+        constexpr uint32_t kAllOk = (1u << GROUPS) - 1;
+        char *sh_k = smem, *sh_v = smem + 2 * KEYS * KSTR;
+        const int lane = here(lane_id()), tid = here(threadIdx.x), half = lane >> 5, l32 = lane & 31;
+        const int32_t* table = a.page_table + (size_t)b_table * a.max_pages;
+        const uint32_t head_bytes = (uint32_t)ROWB << a.page_shift, page_bytes = head_bytes * (uint32_t)hkv, in_page = (1u << a.page_shift) - 1;
+        const char *kh = a.k_pages + (size_t)h * head_bytes, *vh = a.v_pages + (size_t)h * head_bytes;
+        const int n_tiles = (t_end - t_begin + KEYS - 1) / KEYS;
+        // lane l looks after 16-key group l % GROUPS of a tile; groups behind the end have no page
+        auto pages_of = [&](int j) {
+            const int t = t_begin + j * KEYS + 16 * (lane % GROUPS);
+            return t < t_end ? table[t >> a.page_shift] : -1;
+        };
+        int id = pages_of(0);
+        uint4 qb[NQ32];
+#pragma unroll
+        for (int s = 0; s < NQ32; ++s) qb[s] = load16(a.q, my_row * QROWB + 32 * s + 16 * half);
+        struct Tile {
+            uint4 k[LOADS], v[LOADS];
+            float ks[LOADS], vs[LOADS];
+            uint32_t ok;      // bit g: group g has a page
+        };
+        // id: the lane's page in tile j; afterwards - on its way ahead of the rows - in the tile behind it
+        auto fetch = [&](int j, int& id, Tile& t) {
+            const bool ok = (uint32_t)id < (uint32_t)a.n_pages;
+            t.ok = (uint32_t)__ballot(ok) & kAllOk;
+            const uint32_t page = ok ? (uint32_t)id : 0u;
+            const uint64_t begin = (uint64_t)page * page_bytes;
+            const int lo = (int)(uint32_t)begin, hi = (int)(uint32_t)(begin >> 32);
+            id = pages_of(min(j + 1, n_tiles - 1));
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) {
+                // a load's 16-key group is the same for the wave
+                constexpr int kPerLoad = ROWS_PER_LOAD > 16 ? ROWS_PER_LOAD / 16 : 1;      // groups of one load: waves differ
+                const int r = i * ROWS_PER_LOAD + tid / PIECES;
+                const int g = i * ROWS_PER_LOAD / 16 + (kPerLoad > 1 ? wave * (LEOAM_WAVE / PIECES) / 16 : 0);
+                const uint32_t at = ((uint32_t)(t_begin + j * KEYS + r) & in_page) * ROWB + 16 * (tid % PIECES);
+                const uint64_t base = (uint64_t)(uint32_t)__builtin_amdgcn_readlane(hi, g) << 32 | (uint32_t)__builtin_amdgcn_readlane(lo, g);
+                t.k[i] = load16(kh + base, at);
+                t.v[i] = load16(vh + base, at);
+                if (k8) {
+                    const size_t row = (size_t)(uint32_t)__builtin_amdgcn_readlane((int)page, g) * hkv + h;
+                    t.ks[i] = a.k_scale[row];
+                    t.vs[i] = a.v_scale[row];
+                }
+            }
+        };
+        auto stage = [&](int buf, Tile& t) {
+            if (t.ok != kAllOk) {
+#pragma unroll
+                for (int i = 0; i < LOADS; ++i) {
+                    if (t.ok >> ((i * ROWS_PER_LOAD + tid / PIECES) / 16) & 1) continue;
+                    t.v[i] = make_uint4(0, 0, 0, 0);      // nothing there: no value may matter
+                    t.vs[i] = 1.f;
+                }
+            }
+            char *kt = sh_k + buf * KEYS * KSTR, *vt = sh_v + buf * KEYS * VSTR;
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) {
+                const int r = i * ROWS_PER_LOAD + tid / PIECES, piece = tid % PIECES;
+                if constexpr (k8) {
+                    store16(kt, r * KSTR + 32 * piece, widen8<T>(t.k[i].x, t.k[i].y, t.ks[i]));
+                    store16(kt, r * KSTR + 32 * piece + 16, widen8<T>(t.k[i].z, t.k[i].w, t.ks[i]));
+                    store16(vt, r * VSTR + 32 * piece, widen8<T>(t.v[i].x, t.v[i].y, t.vs[i]));
+                    store16(vt, r * VSTR + 32 * piece + 16, widen8<T>(t.v[i].z, t.v[i].w, t.vs[i]));
+                } else {
+                    store16(kt, r * KSTR + 16 * piece, t.k[i]);
+                    store16(vt, r * VSTR + 16 * piece, t.v[i]);
+                }
+            }
+        };
+
+        f32x16_t acc[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[i][r] = 0.f;
+        float m_run = -INFINITY, l_run = 0.f;
+        const uint32_t k_lane = l32 * KSTR + 16 * half;
+        const uint32_t v_lane = k32 ? 4 * half * VSTR + 4 * l32
+                                    : (4 * half + (lane & 15) / 4) * VSTR + 32 * ((lane >> 4) & 1) + 8 * (lane & 3);
+        // lane = column, register r of key block kb = key 32 kb + 8 (r / 4) + 4 half + r % 4
+        auto work = [&](int buf, uint32_t ok) {
+            constexpr int NB = KB;
+            const char *kt = sh_k + buf * KEYS * KSTR + k_lane, *vt = sh_v + buf * KEYS * VSTR + v_lane;
+            f32x16_t s[NB];
+#pragma unroll
+            for (int kb = 0; kb < NB; ++kb) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[kb][r] = 0.f;
+#pragma unroll
+                for (int i = 0; i < NQ32; ++i) {
+                    const uint4 ka = load16(kt, 32 * kb * KSTR + 32 * i);
+                    if constexpr (k32) {
+                        float kx[4], qx[4];
+                        unpack<F32>(ka, kx);
+                        unpack<F32>(qb[i], qx);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) s[kb] = __builtin_amdgcn_mfma_f32_32x32x2f32(kx[e], qx[e], s[kb], 0, 0, 0);
+                    } else {
+                        s[kb] = mfma_32x32x16<T>(ka, qb[i], s[kb]);
+                    }
+                }
+            }
+            if (ok != kAllOk) {
+#pragma unroll
+                for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        if (!(ok >> (2 * kb + r / 8) & 1)) s[kb][r] = -INFINITY;
+            }
+            float mt = s[0][0];
+#pragma unroll
+            for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) mt = fmaxf(mt, s[kb][r]);
+            {
+                float x = mt, y = mt;
+                permlane32_swap(x, y);
+                mt = fmaxf(x, y) * a.scale_log2 - kBias;
+            }
+            if (__ballot(mt > m_run + kSharedLag)) {
+                const float m = fmaxf(m_run, mt), c = exp2_or_zero(m_run, m);
+                m_run = m;
+                l_run *= c;
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) acc[i][r] *= c;
+            }
+            const float ref = m_run == -INFINITY ? 0.f : m_run;
+            if constexpr (k32) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    s[0][r] = exp2_raw(fmaf(s[0][r], a.scale_log2, -ref));
+                    l_run += s[0][r];
+#pragma unroll
+                    for (int db = 0; db < 4; ++db) {
+                        const float v = *reinterpret_cast<const float*>(vt + (8 * (r / 4) + r % 4) * VSTR + 128 * db);
+                        acc[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, s[0][r], acc[db], 0, 0, 0);
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int t = 0; t < 2 * NB; ++t) {      // 16 keys
+                    float p[8];
+#pragma unroll
+                    for (int r = 0; r < 8; ++r) {
+                        p[r] = exp2_raw(fmaf(s[t / 2][8 * (t % 2) + r], a.scale_log2, -ref));
+                        l_run += p[r];
+                    }
+                    uint4 parts[kParts];
+#pragma unroll
+                    for (int k = 0; k < kParts; ++k) {
+                        uint32_t w[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            float u, v;
+                            w[i] = pair_of(T{}, p[2 * i], p[2 * i + 1]);
+                            pair_back(T{}, w[i], u, v);
+                            p[2 * i] -= u;      // (exact: what is left has fewer bits)
+                            p[2 * i + 1] -= v;
+                        }
+                        parts[k] = make_uint4(w[0], w[1], w[2], w[3]);
+                    }
+#pragma unroll
+                    for (int db = 0; db < 4; ++db) {
+                        // the lane's address is that of 4 channels of one key; what it gets is one channel of 4 keys
+                        const uint2 w0 = transposed(vt + 16 * t * VSTR + 64 * db), w1 = transposed(vt + (16 * t + 8) * VSTR + 64 * db);
+#pragma unroll
+                        for (int k = 0; k < kParts; ++k) acc[db] = mfma_32x32x16<T>(make_uint4(w0.x, w0.y, w1.x, w1.y), parts[k], acc[db]);
+                    }
+                }
+            }
+        };
+
+        const bool idle = kWaveColumns * wave >= n_cols;      // none of the wave's columns is one
+        __syncthreads();                                       // (what the previous stretch left in LDS has been read)
+        {
+            Tile even, odd;
+            fetch(0, id, even);
+            if constexpr (AHEAD == 2) fetch(min(1, n_tiles - 1), id, odd);
+#pragma unroll
+            for (int s = 0; s < NQ32; ++s) settle(qb[s], counts);
+            stage(0, even);
+            uint32_t ok = even.ok;
+            __syncthreads();
+            // Tile j is worked on, then `in` is staged; `to` takes in tile j + AHEAD.  (No branch around the loads and none that leads
+            // back, or the compiler has everybody wait for the second tile too.)
+            int j = 0;
+            auto step = [&](Tile& in, Tile& to) {
+                if (AHEAD == 2 || j + 1 < n_tiles) fetch(min(j + AHEAD, n_tiles - 1), id, to);
+                if (!idle) work(j & 1, ok);
+                if (++j == n_tiles) return false;
+                stage(j & 1, in);
+                ok = in.ok;
+                __syncthreads();
+                return true;
+            };
+            if constexpr (AHEAD == 1) {
+                while (step(even, even)) {}
+            } else {
+                while (step(odd, even) && step(even, odd)) {}
+            }
+        }
+        l_run += shfl_xor_f(l_run, 32);
+        const int c = kWaveColumns * wave + l32;
+        if (c >= n_cols) return;
+#pragma unroll
+        for (int db = 0; db < 4; ++db)
+#pragma unroll
+            for (int r = 0; r < 16; r += 4)
+                leave(c, 32 * db + 2 * r + 4 * half, make_float4(acc[db][r], acc[db][r + 1], acc[db][r + 2], acc[db][r + 3]), m_run, l_run);
+    };
+
     bool first_piece = true;
     while (pos < end) {
+        const int lane = here(lane_id()), tid = here(threadIdx.x), l16 = lane & 15;
         const SharedEntry x = entry_of(entry);
         const int units = uniform(x.full + x.rest);
         if (units == 0) {      // (a group without a prefix)
@@ -488,16 +725,16 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
             continue;
         }
         const int tiles = uniform(x.tiles), cost = uniform(x.cost(unit));
-        const long long length = kSharedStart + (long long)tiles * cost, take = min(length - off, end - pos);
+        const int take = uniform((int)min((long long)(kSharedStart + tiles * cost - off), end - pos));
         // tiles that begin in the share
-        auto tiles_before = [&](long long at) { return at <= kSharedStart ? 0 : (int)((at - kSharedStart + cost - 1) / cost); };
-        const int tile0 = uniform(tiles_before(off)), tile1 = uniform(min(tiles, tiles_before(off + take)));
+        auto tiles_before = [&](int at) { return at <= kSharedStart ? 0 : (int)((uint32_t)(at - kSharedStart + cost - 1) / (uint32_t)cost); };
+        const int tile0 = tiles_before(off), tile1 = min(tiles, tiles_before(off + take));
         if (tile0 < tile1) {
             const int h = unit % hkv;
             const bool prefix = entry < a.n_groups, whole = tile1 - tile0 == tiles;
             const int slot = 2 * (int)blockIdx.x + (first_piece ? 0 : 1);      // opens the share, or closes it
             // pieces of the unit, and where the first lies, if it begins here
-            const int count = whole ? kWhole : (int)((pos - off + kSharedStart + (long long)(tiles - 1) * cost) / share - blockIdx.x) + 1;
+            const int count = whole ? kWhole : tile0 ? 1 : (int)quotient(pos - first - off + kSharedStart + (long long)(tiles - 1) * cost, share) + 1;
             int n_cols, b0, tokens, before = 0, b_table;
             bool work = true;
             if (prefix) {
@@ -505,14 +742,12 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
                 const int members = min(off_of(entry + 1) - b0, most_members);
                 n_cols = members << a.group_shift;
                 tokens = prefix_of(entry);
-                b_table = -1;      // the first member that has the whole prefix
-                for (int i = 0; i < members && b_table < 0; i += LEOAM_WAVE) {
-                    const uint64_t has = __ballot(i + lane < members && length_of(b0 + i + lane) >= tokens);
-                    if (has) b_table = b0 + i + __builtin_ctzll(has);
-                }
                 b0 = uniform(b0);
                 n_cols = uniform(n_cols);
-                b_table = uniform(b_table);
+                // the first member that has the whole prefix (at most 128 members, two a lane)
+                const int len0 = lane < members ? length_of(b0 + lane) : -1, len1 = lane + LEOAM_WAVE < members ? length_of(b0 + lane + LEOAM_WAVE) : -1;
+                const uint64_t has0 = __ballot(len0 >= tokens), has1 = __ballot(len1 >= tokens);
+                b_table = has0 ? b0 + __builtin_ctzll(has0) : has1 ? b0 + LEOAM_WAVE + __builtin_ctzll(has1) : -1;
                 work = b_table >= 0;
                 if (tile0 == 0 && tid < members && length_of(b0 + tid) >= tokens) {
                     SharedRow* r = a.rows + (size_t)(b0 + tid) * hkv + h;
@@ -536,18 +771,15 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
                 if (before == 0) r->pre_count = 0;
             }
             if (work && (tokens > 0 || final_)) {
-                const int ways = ways_of(n_cols);
-                const int way = wave & (ways - 1);
-                long long col_row[2];
-#pragma unroll
-                for (int n = 0; n < 2; ++n) {
-                    const int c = kWaveColumns * way + 16 * n + l16, b = b0 + (c >> a.group_shift);
-                    const bool counts = c < n_cols && (!prefix || length_of(b) >= tokens);
-                    col_row[n] = counts ? (((long long)b * hkv + h) << a.group_shift) + (c & (group - 1)) : -1;
-                }
+                // (columns past the last repeat it; what is asked for does not wait for whether it counts)
+                auto row_of = [&](int c) {
+                    c = min(c, n_cols - 1);
+                    return (((size_t)(b0 + (c >> a.group_shift)) * hkv + h) << a.group_shift) + (c & (group - 1));
+                };
+                auto counts_of = [&](int c) { return c < n_cols && (!prefix || length_of(b0 + (c >> a.group_shift)) >= tokens); };
                 const int t_begin = before + tile0 * kSharedTile, t_end = before + min(tokens, tile1 * kSharedTile);
                 auto leave = [&](int c, int d, const float4& v, float m, float l) {
-                    const size_t j = (((size_t)(b0 + (c >> a.group_shift)) * hkv + h) << a.group_shift) + (c & (group - 1));
+                    const size_t j = row_of(c);
                     if (final_) {
                         const float inv = l == 0.f ? 0.f : 1.f / l;      // (NaN stays)
                         *reinterpret_cast<float4*>(a.out + j * LEOAM_D + d) = make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
@@ -558,8 +790,19 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
                     *reinterpret_cast<float4*>(a.acc + at * LEOAM_D + d) = v;
                     if (d == 0) *reinterpret_cast<float2*>(a.ml + 2 * at) = make_float2(m, l);
                 };
-                if (n_cols <= 16) walk(std::integral_constant<int, 1>{}, b_table, h, t_begin, t_end, way, ways, n_cols, col_row, leave);
-                else walk(std::integral_constant<int, 2>{}, b_table, h, t_begin, t_end, way, ways, n_cols, col_row, leave);
+                constexpr std::integral_constant<int, 1> one{};
+                constexpr std::integral_constant<int, 2> two{};
+                if (n_cols <= 2 * kWaveColumns) {
+                    const int c0 = (n_cols <= kWaveColumns ? 0 : kWaveColumns * (wave & 1)) + l16;
+                    const size_t rows[2] = {row_of(c0), row_of(c0 + 16)};
+                    const bool counts[2] = {counts_of(c0), counts_of(c0 + 16)};
+                    if (n_cols <= 16) walk(one, one, b_table, h, t_begin, t_end, n_cols, rows, counts, leave);
+                    else if (n_cols <= kWaveColumns) walk(two, one, b_table, h, t_begin, t_end, n_cols, rows, counts, leave);
+                    else walk(two, two, b_table, h, t_begin, t_end, n_cols, rows, counts, leave);
+                } else {
+                    const int c = kWaveColumns * wave + (lane & 31);
+                    walk_tiles(b_table, h, t_begin, t_end, n_cols, row_of(c), counts_of(c), leave);
+                }
             }
             first_piece = false;
         }
@@ -572,58 +815,82 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
     }
 }
 
-// A head's pieces: those of its group's unit, then its own.  128 threads take eight at a time, all on their way together.
-__global__ __launch_bounds__(2 * LEOAM_D) void page_shared_merge_kernel(const SharedRow* __restrict__ rows, const float* __restrict__ acc,
-                                                                       const float* __restrict__ ml, int group_shift, int n_heads, int sharers, int bias,
-                                                                       float* __restrict__ out, float* __restrict__ lse) {
+// A head's pieces: those of its group's unit, then its own.  32 threads take four channels each of eight pieces at a time, all on their
+// way together; four such groups share a head's pieces, in order.
+constexpr int kMergeParts = 4, kMergeHeads = 2;
+__global__ __launch_bounds__(kMergeHeads * kMergeParts * 32) void page_shared_merge_kernel(const SharedRow* __restrict__ rows, const float* __restrict__ acc,
+                                                                                          const float* __restrict__ ml, int group_shift, int n_heads,
+                                                                                          int sharers, int bias, float* __restrict__ out,
+                                                                                          float* __restrict__ lse) {
     constexpr int kBatch = 8;
-    const int d = threadIdx.x % LEOAM_D, j = 2 * blockIdx.x + threadIdx.x / LEOAM_D;
-    if (j >= n_heads) return;
+    __shared__ float sh_m[kMergeHeads][kMergeParts], sh_l[kMergeHeads][kMergeParts];
+    __shared__ __align__(16) float sh_o[kMergeHeads][kMergeParts][LEOAM_D];
+    const int t = threadIdx.x % 32, part = threadIdx.x / 32 % kMergeParts, mine = threadIdx.x / (32 * kMergeParts), d = 4 * t;
+    const int j = min(kMergeHeads * (int)blockIdx.x + mine, n_heads - 1);      // (the last one twice)
     const SharedRow r = rows[j >> group_shift];
-    if (r.own_count == kFinal) return;
+    const bool done = r.own_count == kFinal;
     // (counts and slots that no kernel wrote - lists of groups that overlap - stay within the workspace)
     const int g = j & ((1 << group_shift) - 1), last = 2 * sharers - 1;
     const int n_pre = r.pre_count == kWhole ? 1 : min(max(r.pre_count, 0), sharers), n_own = r.own_count == kWhole ? 1 : min(max(r.own_count, 0), sharers);
+    const int n = done ? 0 : n_pre + n_own;
     auto state = [&](int i) {
-        const bool mine = i >= n_pre;
-        const int k = mine ? i - n_pre : i, count = mine ? r.own_count : r.pre_count;
-        if (count == kWhole) return (size_t)(mine ? j : n_heads + j);
+        const bool own = i >= n_pre;
+        const int k = own ? i - n_pre : i, count = own ? r.own_count : r.pre_count;
+        if (count == kWhole) return (size_t)(own ? j : n_heads + j);
         // (each further piece opens the next workgroup's share)
-        const int slot0 = mine ? r.own_slot : r.pre_slot, slot = min(max(k == 0 ? slot0 : 2 * (slot0 / 2 + k), 0), last);
-        const int col = min(max(mine ? 0 : r.pre_col, 0), kSharedColumns - (1 << group_shift)) + g;
+        const int slot0 = own ? r.own_slot : r.pre_slot, slot = min(max(k == 0 ? slot0 : 2 * (slot0 / 2 + k), 0), last);
+        const int col = min(max(own ? 0 : r.pre_col, 0), kSharedColumns - (1 << group_shift)) + g;
         return 2 * (size_t)n_heads + (size_t)slot * kSharedColumns + col;
     };
-    float m = -INFINITY, l = 0.f, o = 0.f;
-    for (int i0 = 0; i0 < n_pre + n_own; i0 += kBatch) {
-        float ms[kBatch], ls[kBatch], os[kBatch];
+    float m = -INFINITY, l = 0.f;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int i0 = part * kBatch; i0 < n; i0 += kMergeParts * kBatch) {
+        float ms[kBatch], ls[kBatch];
+        float4 os[kBatch];
 #pragma unroll
         for (int u = 0; u < kBatch; ++u) {
-            const size_t at = state(min(i0 + u, n_pre + n_own - 1));
+            const size_t at = state(min(i0 + u, n - 1));
             const float2 x = *reinterpret_cast<const float2*>(ml + 2 * at);
-            ms[u] = x.x;
+            ms[u] = i0 + u < n ? x.x : -INFINITY;
             ls[u] = x.y;
-            os[u] = acc[at * LEOAM_D + d];
+            os[u] = *reinterpret_cast<const float4*>(acc + at * LEOAM_D + d);
         }
         float mb = m;
 #pragma unroll
-        for (int u = 0; u < kBatch; ++u) {
-            if (i0 + u >= n_pre + n_own) ms[u] = -INFINITY;
-            mb = fmaxf(mb, ms[u]);
-        }
+        for (int u = 0; u < kBatch; ++u) mb = fmaxf(mb, ms[u]);
         const float c = exp2_or_zero(m, mb);
         m = mb;
         l *= c;
-        o *= c;
+        o.x *= c; o.y *= c; o.z *= c; o.w *= c;
 #pragma unroll
         for (int u = 0; u < kBatch; ++u) {
-            if (i0 + u >= n_pre + n_own) continue;
+            if (i0 + u >= n) continue;
             const float w = exp2_or_zero(ms[u], m);
             l += w * ls[u];
-            o += w * os[u];
+            o.x += w * os[u].x; o.y += w * os[u].y; o.z += w * os[u].z; o.w += w * os[u].w;
         }
     }
-    out[(size_t)j * LEOAM_D + d] = l == 0.f ? 0.f : o / l;      // (NaN stays)
-    if (lse && d == 0) lse[j] = log_sum_exp(m, l, bias);
+    if (t == 0) {
+        sh_m[mine][part] = m;
+        sh_l[mine][part] = l;
+    }
+    *reinterpret_cast<float4*>(&sh_o[mine][part][d]) = o;
+    __syncthreads();
+    if (part || done) return;
+    for (int p = 1; p < kMergeParts; ++p) m = fmaxf(m, sh_m[mine][p]);
+    l = 0.f;
+    o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int p = 0; p < kMergeParts; ++p) {
+        const float w = exp2_or_zero(sh_m[mine][p], m);
+        const float4 x = *reinterpret_cast<const float4*>(&sh_o[mine][p][d]);
+        if (sh_m[mine][p] == -INFINITY) continue;      // (a part without pieces)
+        l += w * sh_l[mine][p];
+        o.x += w * x.x; o.y += w * x.y; o.z += w * x.z; o.w += w * x.w;
+    }
+    const float inv = l == 0.f ? 0.f : 1.f / l;      // (NaN stays)
+    *reinterpret_cast<float4*>(out + (size_t)j * LEOAM_D + d) = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+    if (lse && t == 0) lse[j] = log_sum_exp(m, l, bias);
 }
 
 constexpr int kSharedGroups = 512;      // workgroups: two fill a compute unit
@@ -639,7 +906,7 @@ template <typename T, typename S> static hipError_t launch_shared(const PageShar
     hipLaunchKernelGGL((page_shared_kernel<T, S>), dim3(a.sharers), dim3(kAttThreads), 0, stream, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(page_shared_merge_kernel, dim3((a.n_heads + 1) / 2), dim3(2 * LEOAM_D), 0, stream, a.rows, a.acc, a.ml,
+    hipLaunchKernelGGL(page_shared_merge_kernel, dim3((a.n_heads + kMergeHeads - 1) / kMergeHeads), dim3(kMergeHeads * kMergeParts * 32), 0, stream, a.rows, a.acc, a.ml,
                        a.group_shift, a.n_heads, a.sharers, shared_bias<T>(), a.out, a.lse);
     return hipGetLastError();
 }
