@@ -58,6 +58,12 @@ template <typename F> __device__ __forceinline__ int wave_count_below(int n, int
 // a value that is the same in every lane, held once for the wave
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
+// p[i] of a list that no kernel writes meanwhile, i the same in every lane: a scalar load, which is not waited for in turn with the
+// wave's other loads (in a kernel that stores anything the compiler takes a vector load, behind all that are on their way)
+template <typename V> __device__ __forceinline__ V scalar_at(const V* p, size_t i) {
+    return ((const __attribute__((address_space(4))) V*)p)[i];
+}
+
 __device__ __forceinline__ float exp2_raw(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // eight codes to the operand type, times a power of two (exact)

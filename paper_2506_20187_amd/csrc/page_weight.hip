@@ -1,11 +1,14 @@
 // page_weight_add: what every cached token got of the attention of the call's rows, added to what it got before:
 // weight[t] = decay weight[t] + sum over the rows that see t and the group's heads of exp(scale q.k_t - lse).
 //
-// S = K Q^T on the matrix cores, keys as the first operand: a wave holds its keys in registers (64; fp32: 32) and goes through the
-// rows sixteen (row, head) columns at a time, so the sums of a token stay in registers too and nothing is added by atomics.  One row
-// for each sequence: every key is read once, bound by that; the four waves of a workgroup take four stretches of keys.
-// Many rows: bound by the exponentials; the four waves share the keys and take every fourth block of columns each, their sums are
-// added in order at the end.
+// S = K Q^T on the matrix cores, keys as the first operand: a wave holds its keys in registers and goes through the rows sixteen
+// (row, head) columns at a time, so the sums of a token stay in registers too and nothing is added by atomics.
+// Few rows for each sequence: every key is read once, bound by that.  The stretches of 32 keys (fp32: 16) of all sequences and heads
+// are laid end to end and shared out equally to the waves; a wave has the next one's keys on their way while it works on one.  They
+// come as whole rows, which the caches serve at four times the rate of an operand's 16 bytes of 16 rows, and become operands
+// in LDS.
+// Many rows: bound by the exponentials.  The eight waves of a workgroup share 64 keys (fp32: 32) and take every eighth block of
+// columns each; their sums are added in order at the end.  Queries, too, come as whole rows.
 #include "page_common.h"
 
 namespace leoam {
@@ -25,180 +28,364 @@ struct PageWeightArgs {
     int total;      // (block of keys, sequence, kv head) triples of a full table
 };
 
-template <typename T> constexpr int kWeightTiles = T::kTag == LEOAM_F32 ? 2 : 4;      // 16-key tiles of a wave
+template <typename T, bool kSplitRows> constexpr int kWeightTiles = (T::kTag == LEOAM_F32 ? 1 : 2) * (kSplitRows ? 2 : 1);      // of 16 keys, of a wave
 
-template <typename T, typename S, int G, bool kSplitRows> __global__ __launch_bounds__(kAttThreads) void page_weight_kernel(PageWeightArgs a) {
-    constexpr bool k8 = std::is_same<S, E4M3>::value, k32 = T::kTag == LEOAM_F32;
-    constexpr int ROWB = LEOAM_D * S::kBytes, QROWB = Row<T>::kRowBytes, NT = kWeightTiles<T>, KEYS = 16 * NT, NQ = k32 ? 8 : 4;
-    constexpr int BLOCK = kSplitRows ? KEYS : kAttWaves * KEYS;
-    __shared__ float sh[kAttWaves][KEYS];
-    const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / LEOAM_WAVE), grp = lane >> 4, l16 = lane & 15;
-    const int hkv = a.n_kv_heads, rows_bh = a.batch * hkv;
+// A stretch of keys: (sequence, kv head), its first key, the sequence's length, its rows of the call and the place of the first one's token.
+struct WeightUnit { int bh, b, h, t0, len, row0, m, first; };
 
-    // A grid that goes round several times stops behind the longest sequence.
-    int longest = 0x7fffffff;
-    if ((int)gridDim.x < a.total) {
-        longest = 0;
-        for (int i = lane; i < a.batch; i += LEOAM_WAVE) longest = max(longest, a.seq_len[i]);
-        longest = (int)wave_max_u32((uint32_t)longest);
-    }
-    for (int unit = blockIdx.x; unit < a.total; unit += gridDim.x) {
-        const int bh = unit % rows_bh, b = bh / hkv, h = bh - b * hkv;
-        const long long block0 = (long long)(unit / rows_bh) * BLOCK;
-        if (block0 >= longest) return;
-        const int len = uniform(min(max(a.seq_len[b], 0), a.max_pages << a.page_shift));
-        const int t0 = (int)block0 + (kSplitRows ? 0 : wave * KEYS);
-        if (t0 >= len) continue;      // (kSplitRows: all waves)
-        int row0 = b, m = 1;
+// 16 (row, head) columns
+template <typename T> struct WeightColumns {
+    static constexpr int NQ = T::kTag == LEOAM_F32 ? 8 : 4;
+    uint4 q[NQ];
+    float base;      // lse, log2 domain
+    int pos;         // the row's place, -1: no column, or a row that attended to nothing
+};
+
+template <typename T, typename S, int G, bool kSplitRows> struct Weighing {
+    static constexpr bool k8 = std::is_same<S, E4M3>::value, k32 = T::kTag == LEOAM_F32;
+    static constexpr int ROWB = LEOAM_D * S::kBytes, QROWB = Row<T>::kRowBytes, NT = kWeightTiles<T, kSplitRows>, KEYS = 16 * NT;
+    static constexpr int NQ = WeightColumns<T>::NQ, NK = k32 ? 8 : k8 ? 2 : 4;
+    // Tile j, token l16; a token that does not count re-reads the last one that does.  (Few rows: as they lie in the page, a row by
+    // kPieces neighbouring lanes.)
+    static constexpr int kPieces = ROWB / 16, kRowsOfLoad = LEOAM_WAVE / kPieces;
+    static constexpr int kQPieces = QROWB / 16, kColumnsOfLoad = LEOAM_WAVE / kQPieces;
+    struct Keys {
+        uint4 k[NT * NK];
+        float ks[NT];
+        uint32_t have;      // bit j: the tile has a page
+    };
+
+    static __device__ __forceinline__ WeightUnit unit_at(const PageWeightArgs& a, int bh, long long t0) {
+        WeightUnit u;
+        u.bh = bh;
+        u.b = bh / a.n_kv_heads;
+        u.h = bh - u.b * a.n_kv_heads;
+        u.len = min(max(scalar_at(a.seq_len, u.b), 0), a.max_pages << a.page_shift);
+        u.t0 = (int)t0;
+        u.row0 = u.b;
+        u.m = 1;
         if (a.new_off) {
-            row0 = uniform(a.new_off[b]);
-            m = uniform(a.new_off[b + 1]) - row0;
-            if (row0 < 0 || m < 0 || m > a.n_new - row0) m = 0;
+            u.row0 = scalar_at(a.new_off, u.b);
+            u.m = scalar_at(a.new_off, u.b + 1) - u.row0;
+            if (u.row0 < 0 || u.m < 0 || u.m > a.n_new - u.row0) u.m = 0;
         }
-        const int first = len - m;      // place of the first row's token
+        u.first = u.len - u.m;
+        return u;
+    }
+    // columns from the first row that sees a key of the stretch on
+    // (few rows: all of them, so that a wave's columns stay what they are)
+    static __device__ __forceinline__ int first_row(const WeightUnit& u) { return kSplitRows ? max(0, u.t0 - u.first) : 0; }
+    static __device__ __forceinline__ int columns(const WeightUnit& u) { return (u.m - first_row(u)) * G; }
 
-        // ---- keys: tile j, token l16; a token that does not count re-reads the last one that does --------------
-        uint4 kb[NT * NQ];
-        uint32_t have = 0;      // bit j: the tile has a page
+    static __device__ __forceinline__ void fetch_keys(const PageWeightArgs& a, const WeightUnit& u, Keys& x) {
+        const int lane = lane_id(), grp = lane >> 4, l16 = lane & 15;
+        x.have = 0;
+        int id[NT];
+#pragma unroll
+        for (int j = 0; j < NT; ++j) id[j] = scalar_at(a.page_table, (size_t)u.b * a.max_pages + (min(u.t0 + 16 * j, u.len - 1) >> a.page_shift));
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
-            const int t = min(t0 + 16 * j, len - 1), valid = min(len - (t0 + 16 * j), 16);
-            const int id = uniform(a.page_table[(size_t)b * a.max_pages + (t >> a.page_shift)]);
-            const bool ok = (uint32_t)id < (uint32_t)a.n_pages && valid > 0;
-            have |= (ok ? 1u : 0u) << j;
-            const size_t row = (size_t)(ok ? id : 0) * hkv + h;
+            const int t = min(u.t0 + 16 * j, u.len - 1), valid = min(u.len - (u.t0 + 16 * j), 16), page = id[j];
+            const bool ok = (uint32_t)page < (uint32_t)a.n_pages && valid > 0;
+            x.have |= (ok ? 1u : 0u) << j;
+            const size_t row = (size_t)(ok ? page : 0) * a.n_kv_heads + u.h;
             const char* kp = a.k_pages + (row << a.page_shift) * ROWB;
-            const uint32_t at = (uint32_t)((t & ((1 << a.page_shift) - 1) & ~15) + min(l16, max(valid - 1, 0))) * ROWB;
-            if constexpr (k8) {
-                const float ks = a.k_scale[row];
+            const uint32_t row0 = t & ((1 << a.page_shift) - 1) & ~15, last = max(valid - 1, 0);
+            if constexpr (k8) x.ks[j] = scalar_at(a.k_scale, row);
 #pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    const uint4 w = load16(kp, at + 64 * c + 16 * grp);
-                    kb[NQ * j + 2 * c] = widen8<T>(w.x, w.y, ks);
-                    kb[NQ * j + 2 * c + 1] = widen8<T>(w.z, w.w, ks);
-                }
-            } else {
-#pragma unroll
-                for (int s = 0; s < NQ; ++s) kb[NQ * j + s] = load16(kp, at + 64 * s + 16 * grp);
+            for (int s = 0; s < NK; ++s) {
+                if constexpr (kSplitRows) x.k[NK * j + s] = load16(kp, (row0 + min((uint32_t)l16, last)) * ROWB + 64 * s + 16 * grp);
+                else x.k[NK * j + s] = load16(kp, (row0 + min((uint32_t)(s * kRowsOfLoad + lane / kPieces), last)) * ROWB + 16 * (lane % kPieces));
             }
         }
-
-        float w[NT][4];
+    }
+    static __device__ __forceinline__ void fetch_columns(const PageWeightArgs& a, const WeightUnit& u, int cb, WeightColumns<T>& c) {
+        const int lane = lane_id(), grp = lane >> 4, l16 = lane & 15, n_cols = columns(u);
+        const int i0 = first_row(u);
+        auto row_of = [&](int col) {      // (columns past the last repeat it)
+            col = max(min(16 * cb + col, n_cols - 1), 0);
+            return n_cols > 0 ? ((size_t)(u.row0 + i0 + col / G) * a.n_kv_heads + u.h) * G + col % G : 0;
+        };
+#pragma unroll
+        for (int s = 0; s < NQ; ++s) {
+            if constexpr (kSplitRows) c.q[s] = load16(a.q, row_of(s * kColumnsOfLoad + lane / kQPieces) * QROWB + 16 * (lane % kQPieces));
+            else c.q[s] = load16(a.q, row_of(l16) * QROWB + 16 * query_piece(s, grp));
+        }
+        const int i = i0 + max(min(16 * cb + l16, n_cols - 1), 0) / G;
+        c.base = a.lse[row_of(l16)];
+        c.pos = 16 * cb + l16 < n_cols ? u.first + i : -1;
+    }
+    // Rows into a wave's LDS, and out again as operands: 16-byte piece p of row r lies at p ^ r (low bits), so that a piece of 16 rows is
+    // in banks of its own.
+    static __device__ __forceinline__ uint32_t lds_at(int r, int p) { return r * ROWB + 16 * (p ^ (r & (kPieces - 1))); }
+    static __device__ __forceinline__ void turn(Keys& x, char* lds) {
+        const int lane = lane_id(), grp = lane >> 4, l16 = lane & 15;
 #pragma unroll
         for (int j = 0; j < NT; ++j)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) w[j][r] = 0.f;
-
-        // ---- columns: (row, head) pairs from the first row that sees a key of this wave on ---------------------
-        const int i0 = max(0, t0 - first), n_cols = (m - i0) * G, n_blocks = (n_cols + 15) / 16;
-        const int last_key = min(t0 + KEYS, len) - 1;
-        struct Columns {
-            uint4 q[NQ];
-            float base;      // lse, log2 domain
-            int pos;         // the row's place, -1: no column, or a row that attended to nothing
-        };
-        auto fetch = [&](int cb, Columns& c) {
-            const int col = min(16 * cb + l16, n_cols - 1), i = i0 + col / G;
-            const size_t at = ((size_t)(row0 + i) * hkv + h) * G + col % G;
+            for (int s = 0; s < NK; ++s) store16(lds, lds_at(16 * j + s * kRowsOfLoad + lane / kPieces, lane % kPieces), x.k[NK * j + s]);
 #pragma unroll
-            for (int s = 0; s < NQ; ++s) {
-                // 16-byte pieces in the order in which a key row's registers hold the channels
-                const int byte = k32 ? 64 * s + 16 * grp : k8 ? 128 * (s >> 1) + 32 * grp + 16 * (s & 1) : 64 * s + 16 * grp;
-                c.q[s] = load16(a.q, at * QROWB + byte);
-            }
-            const float lse = a.lse[at];
-            c.base = lse * kLog2e;
-            c.pos = 16 * cb + l16 < n_cols && lse != -INFINITY ? first + i : -1;
-        };
-        auto add = [&](const Columns& c) {
-            const bool masked = __ballot(c.pos < last_key) != 0;
+        for (int j = 0; j < NT; ++j)
 #pragma unroll
-            for (int j = 0; j < NT; ++j) {
-                f32x4_t s = {0.f, 0.f, 0.f, 0.f};
-                if constexpr (k32) {
-                    f32x4_t chain[4];
+            for (int s = 0; s < NK; ++s) x.k[NK * j + s] = load16(lds, lds_at(16 * j + l16, 4 * s + grp));
+    }
+    // the 16-byte piece of a query that goes with register i of a key's
+    static __device__ __forceinline__ int query_piece(int i, int grp) { return k8 ? 8 * (i >> 1) + 2 * grp + (i & 1) : 4 * i + grp; }
+    // queries that came as rows, by a wave's LDS (of 16 of them) to operands
+    static __device__ __forceinline__ void turn(WeightColumns<T>& c, char* lds) {
+        const int lane = lane_id(), grp = lane >> 4, l16 = lane & 15;
+        auto at = [&](int r, int p) { return r * QROWB + 16 * (p ^ r); };
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) chain[e] = s;
+        for (int s = 0; s < NQ; ++s) store16(lds, at(s * kColumnsOfLoad + lane / kQPieces, lane % kQPieces), c.q[s]);
 #pragma unroll
-                    for (int i = 0; i < NQ; ++i) {
-                        float kx[4], qx[4];
-                        unpack<F32>(kb[NQ * j + i], kx);
-                        unpack<F32>(c.q[i], qx);
+        for (int s = 0; s < NQ; ++s) c.q[s] = load16(lds, at(l16, query_piece(s, grp)));
+    }
+    // the operand's eight channels (fp32: four) of register i of tile j
+    static __device__ __forceinline__ uint4 key(const Keys& x, int j, int i) {
+        if constexpr (k8) {
+            const uint4 w = x.k[NK * j + i / 2];
+            return i & 1 ? widen8<T>(w.z, w.w, x.ks[j]) : widen8<T>(w.x, w.y, x.ks[j]);
+        } else {
+            return x.k[NK * j + i];
+        }
+    }
+    template <typename K> static __device__ __forceinline__ void add(const PageWeightArgs& a, const WeightUnit& u, K&& key_of, const WeightColumns<T>& c, float (*w)[4]) {
+        const int pos = c.base != -INFINITY ? c.pos : -1;
+        const float base = c.base * kLog2e;
+        if (__ballot(pos < min(u.t0 + KEYS, u.len) - 1)) add_products<true>(a, u, key_of, c, pos, base, w);
+        else add_products<false>(a, u, key_of, c, pos, base, w);
+    }
+    template <bool kMasked, typename K>
+    static __device__ __forceinline__ void add_products(const PageWeightArgs& a, const WeightUnit& u, K&& key_of, const WeightColumns<T>& c, int pos,
+                                                        float base, float (*w)[4]) {
+        const int grp = lane_id() >> 4;
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) chain[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(kx[e], qx[e], chain[e], 0, 0, 0);
-                    }
-                    s = (chain[0] + chain[1]) + (chain[2] + chain[3]);
-                } else {
+        for (int j = 0; j < NT; ++j) {
+            f32x4_t s = {0.f, 0.f, 0.f, 0.f};
+            if constexpr (k32) {
+                f32x4_t chain[4];
 #pragma unroll
-                    for (int i = 0; i < NQ; ++i) s = mfma_16x16x32<T>(kb[NQ * j + i], c.q[i], s);
+                for (int e = 0; e < 4; ++e) chain[e] = s;
+#pragma unroll
+                for (int i = 0; i < NQ; ++i) {
+                    float kx[4], qx[4];
+                    unpack<F32>(key_of(j, i), kx);
+                    unpack<F32>(c.q[i], qx);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) chain[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(kx[e], qx[e], chain[e], 0, 0, 0);
                 }
+                s = (chain[0] + chain[1]) + (chain[2] + chain[3]);
+            } else {
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    float p = exp2_raw(fmaf(s[r], a.scale_log2, -c.base));
-                    if (masked && t0 + 16 * j + 4 * grp + r > c.pos) p = 0.f;
-                    w[j][r] += p;
-                }
+                for (int i = 0; i < NQ; ++i) s = mfma_16x16x32<T>(key_of(j, i), c.q[i], s);
             }
-        };
-        constexpr int kStep = kSplitRows ? kAttWaves : 1;
-        const int begin = kSplitRows ? wave : 0;
-        if (begin < n_blocks) {
-            Columns c[2];
-            fetch(begin, c[0]);
-            for (int cb = begin; cb < n_blocks; cb += 2 * kStep) {
-                fetch(min(cb + kStep, n_blocks - 1), c[1]);
-                add(c[0]);
-                if (cb + kStep >= n_blocks) break;
-                fetch(min(cb + 2 * kStep, n_blocks - 1), c[0]);
-                add(c[1]);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                float p = exp2_raw(fmaf(s[r], a.scale_log2, -base));
+                if (kMasked && u.t0 + 16 * j + 4 * grp + r > pos) p = 0.f;
+                w[j][r] += p;
             }
         }
-
-        // ---- the columns' sums; lane l16 keeps that of register l16 % 4 of tile l16 / 4 ------------------------
+    }
+    // The columns' sums: lane l16 keeps that of register l16 % 4 of tile l16 / 4, token `slot` of the stretch.
+    static __device__ __forceinline__ int slot() { return 16 * ((lane_id() & 15) >> 2) + 4 * (lane_id() >> 4) + (lane_id() & 3); }
+    static __device__ __forceinline__ bool keeps(const WeightUnit& u) { return (lane_id() & 15) < 4 * NT && u.t0 + slot() < u.len; }
+    static __device__ __forceinline__ size_t place(const PageWeightArgs& a, const WeightUnit& u) {
+        return (size_t)u.bh * ((size_t)a.max_pages << a.page_shift) + min(u.t0 + slot(), u.len - 1);
+    }
+    static __device__ __forceinline__ float sums(uint32_t have, const float (*w)[4]) {
         float mine = 0.f;
-        bool counts = false;
 #pragma unroll
         for (int j = 0; j < NT; ++j)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const float sum = row16_sum(w[j][r]);
-                if (l16 == 4 * j + r) {
-                    mine = have >> j & 1 ? sum : 0.f;      // (no page: nobody attended to it)
-                    counts = true;
+                if ((lane_id() & 15) == 4 * j + r && have >> j & 1) mine = sum;      // (no page: nobody attended to it)
+            }
+        return mine;
+    }
+    static __device__ __forceinline__ void store(const PageWeightArgs& a, const WeightUnit& u, float was, float mine) {
+        const int t = u.t0 + slot();
+        const size_t at = place(a, u);
+        a.weight[at] = t < u.first && a.before ? fmaf(a.decay, was, mine) : mine;
+        if (a.token_id && t >= u.first) a.token_id[at] = a.n_seen[u.b] - (u.len - t);
+    }
+};
+
+// ---- few rows for each sequence -------------------------------------------------------------------------------
+template <typename T, typename S, int G> __global__ __launch_bounds__(kAttThreads, 2) void page_weight_few_kernel(PageWeightArgs a) {
+    using W = Weighing<T, S, G, false>;
+    __shared__ long long sh_sum[kAttWaves], sh_in[kAttWaves];
+    __shared__ int sh_entry[kAttWaves];
+    __shared__ __align__(16) char sh_keys[kAttWaves][W::KEYS * W::ROWB];
+    const int tid = threadIdx.x, lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(tid / LEOAM_WAVE), hkv = a.n_kv_heads;
+    auto blocks_of = [&](int len) { return (min(max(len, 0), a.max_pages << a.page_shift) + W::KEYS - 1) / W::KEYS; };
+
+    // ---- this wave's share of the stretches: `left` of them, from stretch `block` of head h of sequence b on -------
+    int b, h, block, left;
+    {
+        const int per = (a.batch + kAttThreads - 1) / kAttThreads, b0 = min(tid * per, a.batch), b1 = min(b0 + per, a.batch);
+        long long mine = 0;
+        for (int i = b0; i < b1; ++i) mine += (long long)blocks_of(a.seq_len[i]) * hkv;
+        long long incl = mine;
+#pragma unroll
+        for (int d = 1; d < LEOAM_WAVE; d <<= 1) {
+            const long long o = __shfl_up(incl, d, LEOAM_WAVE);
+            if (lane >= d) incl += o;
+        }
+        if (lane == LEOAM_WAVE - 1) sh_sum[wave] = incl;
+        __syncthreads();
+        long long total = 0, before = incl - mine;
+#pragma unroll
+        for (int w = 0; w < kAttWaves; ++w) {
+            if (w < wave) before += sh_sum[w];
+            total += sh_sum[w];
+        }
+        // (the first `more` waves take one more than the others)
+        const int waves = gridDim.x * kAttWaves, each = (int)(total / waves), more = (int)(total - (long long)each * waves);
+        auto begin_of = [&](int w) { return (long long)w * each + min(w, more); };
+        long long at = before;
+        for (int i = b0; i < b1; ++i) {
+            const long long n = (long long)blocks_of(a.seq_len[i]) * hkv;
+#pragma unroll
+            for (int w = 0; w < kAttWaves; ++w) {
+                const long long p = begin_of(blockIdx.x * kAttWaves + w);
+                if (p >= at && p < at + n) {
+                    sh_entry[w] = i;
+                    sh_in[w] = p - at;
                 }
             }
-        const int slot = 16 * (l16 >> 2) + 4 * grp + (l16 & 3), t = t0 + slot;
-        if constexpr (kSplitRows) {
-            if (counts) sh[wave][slot] = mine;
-            __syncthreads();
-            if (wave == 0 && counts) {
-                mine = sh[0][slot];
+            at += n;
+        }
+        __syncthreads();
+        const int w = blockIdx.x * kAttWaves + wave;
+        left = each + (w < more ? 1 : 0);
+        if (left == 0) return;
+        b = uniform(sh_entry[wave]);
+        const int n = blocks_of(scalar_at(a.seq_len, b));
+        h = uniform((int)(sh_in[wave] / n));
+        block = uniform((int)(sh_in[wave] - (long long)h * n));
+    }
+
+    struct Fetched {
+        WeightUnit u;
+        typename W::Keys keys;
+        float was;
+    };
+    auto fetch = [&](Fetched& x) __attribute__((always_inline)) {
+        x.u = W::unit_at(a, b * hkv + h, (long long)block * W::KEYS);
+        W::fetch_keys(a, x.u, x.keys);
+        x.was = a.before ? a.before[W::place(a, x.u)] : 0.f;
+        // to the next stretch
+        --left;
+        if (left == 0 || (++block) * W::KEYS < x.u.len) return;
+        block = 0;
+        if (++h < hkv) return;
+        h = 0;
+        do ++b;
+        while (blocks_of(scalar_at(a.seq_len, b)) == 0);      // (there is one: the share is not at its end)
+    };
+    WeightColumns<T> cols;
+    int cols_of = -1;      // which (sequence, kv head) they are of
+    // works on x while y is on its way; false: x was the last one
+    auto step = [&](Fetched& x, Fetched& y) __attribute__((always_inline)) {
+        if (x.u.bh != cols_of) {
+            cols_of = x.u.bh;
+            W::fetch_columns(a, x.u, 0, cols);
+        }
+        const bool last = left == 0;
+        if (!last) fetch(y);
+        float w[W::NT][4];
 #pragma unroll
-                for (int v = 1; v < kAttWaves; ++v) mine += sh[v][slot];
+        for (int j = 0; j < W::NT; ++j)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) w[j][r] = 0.f;
+        W::turn(x.keys, sh_keys[wave]);
+        auto key_of = [&](int j, int i) { return W::key(x.keys, j, i); };
+        const int n_cols = W::columns(x.u);
+        if (n_cols > 0) W::add(a, x.u, key_of, cols, w);
+        for (int cb = 1; 16 * cb < n_cols; ++cb) {
+            WeightColumns<T> more;
+            W::fetch_columns(a, x.u, cb, more);
+            W::add(a, x.u, key_of, more, w);
+        }
+        const float mine = W::sums(x.keys.have, w);
+        if (W::keeps(x.u)) W::store(a, x.u, x.was, mine);
+        return !last;
+    };
+    Fetched even, odd;
+    fetch(even);
+    while (step(even, odd) && step(odd, even)) {}
+}
+
+// ---- many rows ------------------------------------------------------------------------------------------------
+constexpr int kManyWaves = 8;
+template <typename T, typename S, int G> __global__ __launch_bounds__(kManyWaves * LEOAM_WAVE, 2) void page_weight_many_kernel(PageWeightArgs a) {
+    using W = Weighing<T, S, G, true>;
+    __shared__ float sh[kManyWaves][W::KEYS];
+    __shared__ __align__(16) char sh_queries[kManyWaves][16 * W::QROWB];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / LEOAM_WAVE), rows_bh = a.batch * a.n_kv_heads;
+    for (int unit = blockIdx.x; unit < a.total; unit += gridDim.x) {
+        const int block = unit / rows_bh;
+        const WeightUnit u = W::unit_at(a, unit - block * rows_bh, (long long)block * W::KEYS);
+        if (u.t0 >= u.len) continue;
+        typename W::Keys keys;
+        W::fetch_keys(a, u, keys);
+        const float was = a.before ? a.before[W::place(a, u)] : 0.f;
+        uint4 wide[W::NT * W::NQ];      // (8 bits: widened once)
+#pragma unroll
+        for (int j = 0; j < W::NT; ++j)
+#pragma unroll
+            for (int i = 0; i < W::NQ; ++i) wide[W::NQ * j + i] = W::key(keys, j, i);
+        auto key_of = [&](int j, int i) { return wide[W::NQ * j + i]; };
+        float w[W::NT][4];
+#pragma unroll
+        for (int j = 0; j < W::NT; ++j)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) w[j][r] = 0.f;
+        const int n_cols = W::columns(u), n_blocks = n_cols > 0 ? (n_cols + 15) / 16 : 0;
+        if (wave < n_blocks) {
+            // (two blocks a turn, of which the second may be behind the last column and add nothing: were there a branch, the loads would
+            // be moved behind it, where they are waited for at once)
+            WeightColumns<T> even, odd;
+            W::fetch_columns(a, u, wave, even);
+            for (int cb = wave; cb < n_blocks; cb += 2 * kManyWaves) {
+                W::fetch_columns(a, u, cb + kManyWaves, odd);
+                W::turn(even, sh_queries[wave]);
+                W::add(a, u, key_of, even, w);
+                W::fetch_columns(a, u, cb + 2 * kManyWaves, even);
+                W::turn(odd, sh_queries[wave]);
+                W::add(a, u, key_of, odd, w);
             }
         }
-        if ((!kSplitRows || wave == 0) && counts && t < len) {
-            const size_t at = (size_t)bh * ((size_t)a.max_pages << a.page_shift) + t;
-            a.weight[at] = t < first && a.before ? fmaf(a.decay, a.before[at], mine) : mine;
-            if (a.token_id && t >= first) a.token_id[at] = a.n_seen[b] - (len - t);
+        float mine = W::sums(keys.have, w);
+        if ((lane_id() & 15) < 4 * W::NT) sh[wave][W::slot()] = mine;
+        __syncthreads();
+        if (wave == 0 && W::keeps(u)) {
+            mine = sh[0][W::slot()];
+#pragma unroll
+            for (int v = 1; v < kManyWaves; ++v) mine += sh[v][W::slot()];
+            W::store(a, u, was, mine);
         }
-        if constexpr (kSplitRows) __syncthreads();      // (the sums have been read)
+        __syncthreads();      // (the sums have been read)
     }
 }
 
-// Four or more blocks of columns for each sequence on average: the waves share keys.
+// Four or more blocks of columns for each sequence on average: many rows.
 constexpr int kManyColumns = 64;
-constexpr int kMostWeightGroups = 8192;
+constexpr int kFewGroups = 512;             // workgroups: two fill a compute unit (three, with fewer registers each: 150 against 136 us, 16 sequences to 33001)
+constexpr int kManyGroups = 65536;
 
 template <typename T, typename S, int G> static hipError_t launch_weight(PageWeightArgs a, hipStream_t stream) {
-    const bool split = (long long)a.n_new * G >= (long long)kManyColumns * a.batch;
-    const long long block = 16 * kWeightTiles<T> * (split ? 1 : kAttWaves), capacity = (long long)a.max_pages << a.page_shift;
+    const bool many = (long long)a.n_new * G >= (long long)kManyColumns * a.batch;
+    const long long block = 16 * (many ? kWeightTiles<T, true> : kWeightTiles<T, false>), capacity = (long long)a.max_pages << a.page_shift;
     const long long total = (capacity + block - 1) / block * a.batch * a.n_kv_heads;
-    if (total > 0x7fffffffll - kMostWeightGroups) return hipErrorInvalidValue;
+    if (total > 0x7fffffffll - kManyGroups) return hipErrorInvalidValue;
     a.total = (int)total;
-    const dim3 grid((unsigned)(total < kMostWeightGroups ? total : kMostWeightGroups)), threads(kAttThreads);
-    if (split) hipLaunchKernelGGL((page_weight_kernel<T, S, G, true>), grid, threads, 0, stream, a);
-    else hipLaunchKernelGGL((page_weight_kernel<T, S, G, false>), grid, threads, 0, stream, a);
+    const long long groups = many ? total : (total + kAttWaves - 1) / kAttWaves, most = many ? kManyGroups : kFewGroups;
+    const dim3 grid((unsigned)(groups < most ? groups : most)), threads(kAttThreads);
+    if (many) hipLaunchKernelGGL((page_weight_many_kernel<T, S, G>), grid, dim3(kManyWaves * LEOAM_WAVE), 0, stream, a);
+    else hipLaunchKernelGGL((page_weight_few_kernel<T, S, G>), grid, threads, 0, stream, a);
     return hipGetLastError();
 }
 template <typename T, typename S> static hipError_t weight_of(const PageWeightArgs& a, int group, hipStream_t stream) {
