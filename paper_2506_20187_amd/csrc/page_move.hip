@@ -2,10 +2,10 @@
 // weights and the tokens' numbers; scales of 8-bit pages, abstracts and boundaries are kept up.
 //
 // Bytes-bound: a row is read once and written once.  With abstracts the pages that rows move to are read whole, since the key
-// that was replaced may have been the page's largest or smallest.  A wave owns a (page that rows move to, kv head, tensor): an
+// that was replaced may have been the page's largest or smallest.  A wave owns a (page that rows move to, kv head): an
 // 8-bit page's scale may have to grow, and its codes with it.  The pairs are listed by their new place, so a page's pairs
 // are neighbours; the waves of a (sequence, kv head) share its pairs equally and take the pages that begin in their share.  A wave
-// first looks up all rows that come (a lane each), then has as many of them on their way as its registers hold.
+// first looks up all rows that come (a lane each), then has as many of them on their way as its registers hold, keys and values.
 // Sources lie behind the kept length and are not written, but in the page that the kept length cuts: 8 bits leave that page to
 // a second launch, when nobody reads it any more.
 #include "page_common.h"
@@ -50,69 +50,73 @@ template <typename T> __device__ __forceinline__ float move_scale_of(float amax)
     return bits_to_float((uint32_t)(e + 127) << 23);
 }
 
-template <typename T, typename S> __global__ __launch_bounds__(kMoveThreads, 4) void page_move_kernel(MoveArgs a) {
+template <typename T, typename S> __global__ __launch_bounds__(kMoveThreads, 3) void page_move_kernel(MoveArgs a) {
     constexpr bool k8 = std::is_same<S, E4M3>::value;
     constexpr int EPL = T::kEpl, LPR = LEOAM_D / EPL, RPL = LEOAM_WAVE / LPR;      // lanes to a row, rows to a load
     constexpr int ROWB = LEOAM_D * S::kBytes, BATCH = 8;                             // loads that are on their way together
-    // a wave's page: where each row comes from (bytes into the pool, -1: it stays), by which scale, and the rows that come
+    // a wave's page: where each row comes from (bytes into a pool, -1: it stays), by which scales, and the rows that come
     __shared__ long long sh_from[kMoveWaves][kMostRows];
-    __shared__ float sh_scale[k8 ? kMoveWaves : 1][kMostRows];
+    __shared__ float sh_scale[k8 ? 2 : 1][k8 ? kMoveWaves : 1][kMostRows];
     __shared__ int16_t sh_rows[kMoveWaves][kMostRows];
     const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / LEOAM_WAVE);
     const int col = (lane % LPR) * EPL, rg = lane / LPR, ps = 1 << a.page_shift, hkv = a.n_kv_heads;
-    const int which = blockIdx.x & 1, task = (int)(blockIdx.x >> 1) * kMoveWaves + wave, bh = task / a.per_row, sharer = task - bh * a.per_row;
+    const int task = (int)blockIdx.x * kMoveWaves + wave, bh = task / a.per_row, sharer = task - bh * a.per_row;
     if (bh >= a.n_rows) return;
     const int b = bh / hkv, h = bh - b * hkv;
     const int cap = a.max_pages << a.page_shift;
-    const int old_len = uniform(min(max(a.old_len[b], 0), cap)), new_len = uniform(min(max(a.new_len[b], 0), old_len));
+    const int old_len = min(max(scalar_at(a.old_len, b), 0), cap), new_len = min(max(scalar_at(a.new_len, b), 0), old_len);
+    const int n = min(max(scalar_at(a.move_count, bh), 0), min(a.m_max, new_len));
     if (new_len >= old_len) return;
-    const int n = uniform(min(max(a.move_count[bh], 0), min(a.m_max, new_len)));
     const int2* moves = reinterpret_cast<const int2*>(a.moves) + (size_t)bh * a.m_max;
     const int32_t* table = a.page_table + (size_t)b * a.max_pages;
     const int cut_page = new_len & (ps - 1) ? new_len >> a.page_shift : -1;
-    const bool bounded = which == 0 && a.abstract;
-    char* pool = (which ? a.v_pages : a.k_pages) + col * S::kBytes;
-    float* scales = which ? a.v_scale : a.k_scale;
+    const bool bounded = a.abstract != nullptr;
+    char* const pools[2] = {a.k_pages + col * S::kBytes, a.v_pages + col * S::kBytes};
+    float* const scales[2] = {a.k_scale, a.v_scale};
     long long* from = sh_from[wave];
-    float* from_scale = sh_scale[k8 ? wave : 0];
+    float* const from_scale[2] = {sh_scale[0][k8 ? wave : 0], sh_scale[k8 ? 1 : 0][k8 ? wave : 0]};
     int16_t* rows = sh_rows[wave];
 
     // page p, whose pairs begin at i0 (i0 == n: none)
     auto take = [&](int p, int i0) {
-        const int entry = table[p];
+        const int id = scalar_at(table, p);
         int2 pair = moves[min(i0 + lane, max(n - 1, 0))];      // (m_max >= 1: there is an entry)
-        for (int r = lane; r < ps; r += LEOAM_WAVE) from[r] = -1;
-        const int id = uniform(entry);
         if ((uint32_t)id >= (uint32_t)a.n_pages) return;
         const size_t row_of_page = (size_t)id * hkv + h;
-        const float old = k8 ? scales[row_of_page] : 1.f;
+        float old[2] = {1.f, 1.f};
+        if constexpr (k8) {
+            old[0] = a.k_scale[row_of_page];
+            old[1] = a.v_scale[row_of_page];
+        }
+        for (int r = lane; r < ps; r += LEOAM_WAVE) from[r] = -1;
         int n_rows = 0;
         for (int j0 = 0; j0 < ps; j0 += LEOAM_WAVE) {
             const int i = i0 + j0 + lane;
             if (j0 > 0) pair = moves[min(i, n - 1)];
-            const bool mine = i < n && j0 + lane < ps && pair.x >> a.page_shift == p, inside = mine && pair.x < new_len && pair.y >= new_len && pair.y < old_len;
+            const bool mine = i < n && j0 + lane < ps && pair.x >> a.page_shift == p;
+            const bool inside = mine && pair.x < new_len && pair.y >= new_len && pair.y < old_len;
             const int src_id = table[inside ? pair.y >> a.page_shift : p];
             const bool fits = inside && (uint32_t)src_id < (uint32_t)a.n_pages;
             const uint64_t hit = __ballot(fits);
             if (fits) {
-                const size_t row = (size_t)src_id * hkv + h;
+                const size_t row = (size_t)src_id * hkv + h, at = (size_t)bh * cap;
                 const int to = pair.x & (ps - 1);
                 from[to] = (long long)(((row << a.page_shift) + (pair.y & (ps - 1))) * ROWB);
-                if constexpr (k8) from_scale[to] = scales[row];
                 rows[n_rows + __popcll(hit & ((1ull << lane) - 1))] = (int16_t)to;
-                if (which) {      // (the keys' waves have the abstracts to see to)
-                    const size_t at = (size_t)bh * cap;
-                    const float moved_weight = a.weight ? a.weight[at + pair.y] : 0.f;
-                    const int moved_id = a.token_id ? a.token_id[at + pair.y] : 0;
-                    if (a.weight) a.weight[at + pair.x] = moved_weight;
-                    if (a.token_id) a.token_id[at + pair.x] = moved_id;
+                const float moved_weight = a.weight ? a.weight[at + pair.y] : 0.f;
+                const int moved_id = a.token_id ? a.token_id[at + pair.y] : 0;
+                if constexpr (k8) {
+                    from_scale[0][to] = a.k_scale[row];
+                    from_scale[1][to] = a.v_scale[row];
                 }
+                if (a.weight) a.weight[at + pair.x] = moved_weight;
+                if (a.token_id) a.token_id[at + pair.x] = moved_id;
             }
             n_rows += __popcll(hit);
             if (__ballot(mine) != ~0ull) break;
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");      // (the lists are the wave's own)
-        char* page = pool + (row_of_page << a.page_shift) * ROWB;
+        char* const page[2] = {pools[0] + (row_of_page << a.page_shift) * ROWB, pools[1] + (row_of_page << a.page_shift) * ROWB};
         float mx[EPL], mn[EPL];
 #pragma unroll
         for (int e = 0; e < EPL; ++e) {
@@ -128,104 +132,107 @@ template <typename T, typename S> __global__ __launch_bounds__(kMoveThreads, 4) 
         };
         const int valid = min(ps, new_len - (p << a.page_shift));
         if constexpr (!k8) {
-            // every row of the page, from where it is or from where it comes; without abstracts the rows that come
-            const int count = bounded ? valid : n_rows;
-            for (int j0 = 0; j0 < count; j0 += RPL * BATCH) {
-                uint4 w[BATCH];
-                int to[BATCH];
+            // the rows that come; with abstracts every key of the page, from where it is or from where it comes
+            auto move_rows = [&](auto tensor) __attribute__((always_inline)) {
+                constexpr int W = decltype(tensor)::value;
+                const bool all = W == 0 && bounded;
+                const int count = all ? valid : n_rows;
+                for (int j0 = 0; j0 < count; j0 += RPL * BATCH) {
+                    uint4 w[BATCH];
+                    int to[BATCH];
 #pragma unroll
-                for (int u = 0; u < BATCH; ++u) {      // (rows past the last repeat it)
-                    const int j = min(j0 + u * RPL + rg, count - 1), r = bounded ? j : rows[j];
-                    const long long src = from[r];
-                    to[u] = src < 0 ? -1 : r;
-                    w[u] = load16(src < 0 ? page + (size_t)r * ROWB : pool + src, 0);
-                }
-#pragma unroll
-                for (int u = 0; u < BATCH; ++u) {
-                    if (bounded) {
-                        float y[EPL];
-                        unpack<T>(w[u], y);
-                        extremes(y);
+                    for (int u = 0; u < BATCH; ++u) {      // (rows past the last repeat it)
+                        const int j = min(j0 + u * RPL + rg, count - 1), r = all ? j : rows[j];
+                        const long long src = from[r];
+                        to[u] = src < 0 ? -1 : r;
+                        w[u] = load16(src < 0 ? page[W] + (size_t)r * ROWB : pools[W] + src, 0);
                     }
-                    if (to[u] >= 0) store16(page, (size_t)to[u] * ROWB, w[u]);
+#pragma unroll
+                    for (int u = 0; u < BATCH; ++u) {
+                        if (all) {
+                            float y[EPL];
+                            unpack<T>(w[u], y);
+                            extremes(y);
+                        }
+                        if (to[u] >= 0) store16(page[W], (size_t)to[u] * ROWB, w[u]);
+                    }
                 }
-            }
+            };
+            move_rows(std::integral_constant<int, 1>{});
+            move_rows(std::integral_constant<int, 0>{});
         } else {
             // The scale comes before the codes: rows that come are read for their largest magnitude, and again if they are more than
             // the registers hold (from the cache).
-            uint2 w[2 * BATCH];
-            auto fetch = [&](int j0) {
+            constexpr int HELD = 2 * BATCH, kHeld = RPL * HELD;
+            uint2 held[2][HELD];
+            auto row_of = [&](int j) { return (int)rows[min(j, n_rows - 1)]; };
+            auto fetch = [&](auto tensor, int j0) __attribute__((always_inline)) {
+                constexpr int W = decltype(tensor)::value;
 #pragma unroll
-                for (int u = 0; u < 2 * BATCH; ++u) {
-                    const int r = rows[min(j0 + u * RPL + rg, n_rows - 1)];
-                    w[u] = *reinterpret_cast<const uint2*>(pool + from[r]);
-                }
+                for (int u = 0; u < HELD; ++u) held[W][u] = *reinterpret_cast<const uint2*>(pools[W] + from[row_of(j0 + u * RPL + rg)]);
             };
-            auto value = [&](int u, int r, float* y) {
-                unpack_e4m3(w[u].x, y);
-                unpack_e4m3(w[u].y, y + 4);
-                const float f = from_scale[r];
+            auto encode_rows = [&](auto tensor) __attribute__((always_inline)) {
+                constexpr int W = decltype(tensor)::value;
+                const bool keys = W == 0 && bounded;
+                float top = 0.f;
+                for (int j0 = 0; j0 < n_rows; j0 += kHeld) {
+                    if (j0 > 0) fetch(tensor, j0);
 #pragma unroll
-                for (int e = 0; e < EPL; ++e) y[e] *= f;
-            };
-            constexpr int kHeld = RPL * 2 * BATCH;
-            float top = 0.f;
-            for (int j0 = 0; j0 < n_rows; j0 += kHeld) {
-                fetch(j0);
+                    for (int u = 0; u < HELD; ++u) {      // (a code's magnitude, NaN left out by the maximum, and 8 bits have no infinity)
+                        float y[8];
+                        unpack_e4m3(held[W][u].x, y);
+                        unpack_e4m3(held[W][u].y, y + 4);
+                        float m = fmaxf(fabsf(y[0]), fabsf(y[1]));
 #pragma unroll
-                for (int u = 0; u < 2 * BATCH; ++u) {
-                    float y[EPL];
-                    value(u, rows[min(j0 + u * RPL + rg, n_rows - 1)], y);
-#pragma unroll
-                    for (int e = 0; e < EPL; ++e) {
-                        const float m = fabsf(y[e]);
-                        top = fmaxf(top, m < INFINITY ? m : 0.f);
+                        for (int e = 2; e < 8; ++e) m = fmaxf(m, fabsf(y[e]));
+                        top = fmaxf(top, m * from_scale[W][row_of(j0 + u * RPL + rg)]);
                     }
                 }
-            }
-            const float now = fmaxf(old, move_scale_of<T>(wave_extreme_f<true>(top))), inv = now > 0.f ? 1.f / now : 0.f, f = old * inv;
-            const bool grows = now > old;
-            if (lane == 0 && grows) scales[row_of_page] = now;
-            auto put = [&](int r, const float* y, bool store) {
-                const uint2 c = make_uint2(pack_e4m3(y), pack_e4m3(y + 4));
-                if (store) *reinterpret_cast<uint2*>(page + (size_t)r * ROWB) = c;
-                if (bounded && r < valid) {
-                    float z[EPL];
-                    stored_values<T, S>(make_uint4(c.x, c.y, 0, 0), now, z);
-                    extremes(z);
+                const float now = fmaxf(old[W], move_scale_of<T>(wave_extreme_f<true>(top))), inv = now > 0.f ? 1.f / now : 0.f;
+                const bool grows = now > old[W];
+                if (lane == 0 && grows) scales[W][row_of_page] = now;
+                // (what is stored is at most 448 of the new scale, and the quotient of two scales a power of two)
+                auto put = [&](int r, const uint2& code, float f, bool store) __attribute__((always_inline)) {
+                    float y[8];
+                    unpack_e4m3(code.x, y);
+                    unpack_e4m3(code.y, y + 4);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) y[e] *= f;
+                    const uint2 c = make_uint2(pack_e4m3(y), pack_e4m3(y + 4));
+                    if (store) *reinterpret_cast<uint2*>(page[W] + (size_t)r * ROWB) = c;
+                    if (keys && r < valid) {
+                        stored_values<T, S>(make_uint4(c.x, c.y, 0, 0), now, y);
+                        extremes(y);
+                    }
+                };
+                for (int j0 = 0; j0 < n_rows; j0 += kHeld) {
+                    if (n_rows > kHeld) fetch(tensor, j0);
+#pragma unroll
+                    for (int u = 0; u < HELD; ++u) {
+                        const int j = j0 + u * RPL + rg, r = row_of(j);
+                        put(r, held[W][u], from_scale[W][r] * inv, j < n_rows);
+                    }
+                }
+                // the rows that stay (those behind the kept length, too, that others may have been read from)
+                const int count = grows ? min(ps, old_len - (p << a.page_shift)) : keys ? valid : 0;
+                const float f = grows ? old[W] * inv : 1.f;
+                for (int r0 = 0; r0 < count; r0 += kHeld) {
+#pragma unroll
+                    for (int u = 0; u < HELD; ++u)
+                        held[W][u] = *reinterpret_cast<const uint2*>(page[W] + (size_t)min(r0 + u * RPL + rg, count - 1) * ROWB);
+#pragma unroll
+                    for (int u = 0; u < HELD; ++u) {
+                        const int r = r0 + u * RPL + rg;
+                        if (r < count && from[r] < 0) put(r, held[W][u], f, grows);
+                    }
                 }
             };
-            for (int j0 = 0; j0 < n_rows; j0 += kHeld) {
-                if (n_rows > kHeld) fetch(j0);
-#pragma unroll
-                for (int u = 0; u < 2 * BATCH; ++u) {
-                    const int j = j0 + u * RPL + rg, r = rows[min(j, n_rows - 1)];
-                    float y[EPL];
-                    value(u, r, y);
-#pragma unroll
-                    for (int e = 0; e < EPL; ++e) y[e] = clamp_nan(y[e], 448.f * now) * inv;
-                    put(r, y, j < n_rows);
-                }
+            if (n_rows > 0) {
+                fetch(std::integral_constant<int, 0>{}, 0);
+                fetch(std::integral_constant<int, 1>{}, 0);
             }
-            // the rows that stay (those behind the kept length, too, that others may have been read from)
-            const int count = grows ? min(ps, old_len - (p << a.page_shift)) : bounded ? valid : 0;
-            for (int r0 = 0; r0 < count; r0 += kHeld) {
-#pragma unroll
-                for (int u = 0; u < 2 * BATCH; ++u) w[u] = *reinterpret_cast<const uint2*>(page + (size_t)min(r0 + u * RPL + rg, count - 1) * ROWB);
-#pragma unroll
-                for (int u = 0; u < 2 * BATCH; ++u) {
-                    const int r = r0 + u * RPL + rg;
-                    if (r >= count || from[r] >= 0) continue;
-                    float y[EPL];
-                    unpack_e4m3(w[u].x, y);
-                    unpack_e4m3(w[u].y, y + 4);
-                    if (grows) {
-#pragma unroll
-                        for (int e = 0; e < EPL; ++e) y[e] *= f;
-                    }
-                    put(r, y, grows);
-                }
-            }
+            encode_rows(std::integral_constant<int, 0>{});
+            encode_rows(std::integral_constant<int, 1>{});
         }
         if (bounded) {
 #pragma unroll
@@ -270,7 +277,7 @@ template <typename T, typename S> __global__ __launch_bounds__(kMoveThreads, 4) 
             take(__builtin_amdgcn_readlane(p, l), base + l);
         }
     }
-    if (sharer + 1 < a.per_row || which) return;
+    if (sharer + 1 < a.per_row) return;
     // what the sequence loses beside the rows that moved: the last page holds fewer tokens
     if (bounded && last_page >= 0 && (a.cut < 0 || last_page != cut_page) &&
         (n == 0 || uniform(moves[n - 1].x) >> a.page_shift != last_page))
@@ -281,13 +288,13 @@ template <typename T, typename S> __global__ __launch_bounds__(kMoveThreads, 4) 
     }
 }
 
-constexpr int kMoveTasks = 16384;      // waves of a tensor
+constexpr int kMoveTasks = 16384;      // waves
 
 template <typename T, typename S> static hipError_t launch_move(MoveArgs a, hipStream_t stream) {
     a.per_row = (kMoveTasks + a.n_rows - 1) / a.n_rows;
     if (a.per_row > a.m_max) a.per_row = a.m_max;
     a.cut = std::is_same<S, E4M3>::value ? 0 : -1;
-    auto grid = [&] { return dim3(2 * (unsigned)(((long long)a.n_rows * a.per_row + kMoveWaves - 1) / kMoveWaves)); };
+    auto grid = [&] { return dim3((unsigned)(((long long)a.n_rows * a.per_row + kMoveWaves - 1) / kMoveWaves)); };
     hipLaunchKernelGGL((page_move_kernel<T, S>), grid(), dim3(kMoveThreads), 0, stream, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.cut < 0) return e;
