@@ -45,52 +45,63 @@ __device__ __forceinline__ int position_of(const AppendArgs& a, int axis, int ro
     return min(max(a.position[(size_t)axis * a.n_new + row], 0), a.rope_len - 1);
 }
 
+// The axes of the pairs that the EPL channels from `col` belong to, four bits each (kAt).  They are the lane's, whatever the row: looked
+// up once, ahead of the rows' positions.
+template <int EPL, bool kAt> struct Axes {
+    uint32_t packed = 0;
+    bool mixed = false;      // some lane of the wave has pairs of several axes
+    __device__ __forceinline__ Axes(const AppendArgs& a, int col) {
+        if constexpr (kAt) {
+            if (!a.axis) return;
+            constexpr int N = EPL / 2;
+            const int half = a.rot_dim >> 1, at = a.interleaved ? col >> 1 : col < half ? col : col - half, more = a.interleaved ? 0 : N;
+            if (col < a.rot_dim) {
+#pragma unroll
+                for (int e = 0; e < N; ++e) {
+                    packed |= (uint32_t)min(max(a.axis[at + e], 0), a.n_axes - 1) << 4 * e;
+                    packed |= (uint32_t)min(max(a.axis[at + more + e], 0), a.n_axes - 1) << 4 * (e + N);
+                }
+            }
+            constexpr uint32_t kAll = EPL == 8 ? 0x11111111u : 0x1111u;
+            mixed = __ballot(packed != (packed & 15u) * kAll) != 0;
+        }
+    }
+    // the row's position on the axis of the first of the pairs
+    __device__ __forceinline__ int position(const AppendArgs& a, int row) const { return kAt ? position_of(a, packed & 15u, row) : 0; }
+};
+
 // The cosines and sines that the EPL channels from `col` need (channels from rot_dim on: none): those of place `pos`, or (kAt) of
-// the positions that the call's row `row` was given.
+// the positions that the call's row `row` was given, `pos` on the axis of the first pair.
 template <int EPL, bool kAt> struct Turn {
     float c[EPL], s[EPL];
-    __device__ __forceinline__ void load(const AppendArgs& a, int pos, int row, int col) {
+    __device__ __forceinline__ void load(const AppendArgs& a, int pos, int row, int col, const Axes<EPL, kAt>& axes) {
         if (col >= a.rot_dim) return;
         // pairs (2i, 2i+1): EPL / 2 angles from col / 2; pairs (i, i + half): EPL from col or col - half (half is a multiple of EPL)
         constexpr int N = EPL / 2;
         const int half = a.rot_dim >> 1, at = a.interleaved ? col >> 1 : col < half ? col : col - half, more = a.interleaved ? 0 : N;
         float c0[N], c1[N], s0[N], s1[N];
-        auto of_position = [&](int p) {
+        auto of_position = [&](int p, float* c0, float* c1, float* s0, float* s1) {
             const float* angle = a.rope + (size_t)p * a.rot_dim + at;
             angles(angle, c0);
             angles(angle + more, c1);
             angles(angle + half, s0);
             angles(angle + half + more, s1);
         };
-        if constexpr (!kAt) {
-            of_position(pos);
-        } else if (!a.axis) {
-            of_position(position_of(a, 0, row));
-        } else {
-            // The pieces of every axis that some of the lane's pairs belong to (mostly one: axes come in sections); each pair then
-            // keeps its own.
-            int ax0[N], ax1[N];
-            uint32_t wanted = 0;
-#pragma unroll
-            for (int e = 0; e < N; ++e) {
-                ax0[e] = min(max(a.axis[at + e], 0), a.n_axes - 1);
-                ax1[e] = min(max(a.axis[at + more + e], 0), a.n_axes - 1);
-                wanted |= 1u << ax0[e] | 1u << ax1[e];
-            }
+        of_position(pos, c0, c1, s0, s1);
+        if (kAt && axes.mixed) {
+            // The pieces of all axes, and each pair keeps its own.  (Where axes come in sections whose borders are multiples of EPL there
+            // are no such pairs.)
             float k0[N], k1[N], t0[N], t1[N];
             for (int x = 0; x < a.n_axes; ++x) {
-                if (!(wanted >> x & 1)) continue;
-                of_position(position_of(a, x, row));
+                of_position(position_of(a, x, row), k0, k1, t0, t1);
 #pragma unroll
                 for (int e = 0; e < N; ++e) {
-                    if (ax0[e] == x) { k0[e] = c0[e]; t0[e] = s0[e]; }
-                    if (ax1[e] == x) { k1[e] = c1[e]; t1[e] = s1[e]; }
+                    const bool first = (axes.packed >> 4 * e & 15u) == (uint32_t)x, second = (axes.packed >> 4 * (e + N) & 15u) == (uint32_t)x;
+                    c0[e] = first ? k0[e] : c0[e];
+                    s0[e] = first ? t0[e] : s0[e];
+                    c1[e] = second ? k1[e] : c1[e];
+                    s1[e] = second ? t1[e] : s1[e];
                 }
-            }
-#pragma unroll
-            for (int e = 0; e < N; ++e) {
-                c0[e] = k0[e]; s0[e] = t0[e];
-                c1[e] = k1[e]; s1[e] = t1[e];
             }
         }
 #pragma unroll
@@ -165,13 +176,15 @@ template <typename T, int THREADS, bool kAt> __device__ __forceinline__ void app
     const int tid = threadIdx.x, col = (tid % LPR) * EPL, rg = tid / LPR;
     const int per_token = (a.n_q_heads + 2 * RPP - 1) / (2 * RPP);
     const int row = unit / per_token, h0 = (unit % per_token) * 2 * RPP;
+    const Axes<EPL, kAt> axes(a, col);
+    const int given = axes.position(a, row);
     int b = row;
     if (a.new_off) b = wave_count_below(a.batch, row, [&](int i) { return a.new_off[i]; });
     if (b >= a.batch) return;
     const Taken t = taken_by(a, b);
     if (t.status || row < t.row0 || row >= t.row0 + t.m) return;
     Turn<EPL, kAt> turn;
-    turn.load(a, t.n - t.m + (row - t.row0), row, col);
+    turn.load(a, kAt ? given : t.n - t.m + (row - t.row0), row, col, axes);
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         const int h = h0 + i * RPP + rg, hc = min(h, a.n_q_heads - 1);
@@ -440,7 +453,7 @@ template <typename T, bool kStore8, int THREADS, bool kAt> __device__ __forceinl
 // Workgroups of four heads, which would load the angles of a token once for them, were slower (144 against 93 us for the
 // keys and values of the former, 78 against 58 for the latter): a page then takes longer than there are pages to overlap.
 template <typename T, bool kStore8, int THREADS, int PASSES, bool kAt>
-__global__ __launch_bounds__(THREADS) void page_append_prompt_kernel(AppendArgs a) {
+__global__ __launch_bounds__(THREADS, kAt && !kStore8 ? 5 : 1) void page_append_prompt_kernel(AppendArgs a) {
     constexpr int EPL = T::kEpl, LPR = Row<T>::kLanesPerRow, RPP = THREADS / LPR, WAVES = THREADS / LEOAM_WAVE;
     constexpr int ROWB = Row<T>::kRowBytes, STOREB = kStore8 ? LEOAM_D : ROWB;
     __shared__ float sh_max[WAVES];
@@ -459,6 +472,7 @@ __global__ __launch_bounds__(THREADS) void page_append_prompt_kernel(AppendArgs 
         return;
     }
     const int h = unit % hkv;
+    const Axes<EPL, kAt> axes(a, col);
     const TouchedPage x = touched_page(a, unit / hkv, h == 0 && first == 0);
     if (x.count == 0) return;
     const size_t at = (size_t)x.id * hkv + h;
@@ -472,18 +486,23 @@ __global__ __launch_bounds__(THREADS) void page_append_prompt_kernel(AppendArgs 
         no_extremes<EPL>(mx, mn);
         // (rows past the last repeat it: rotation exchanges lanes, so all of them are here)
         auto row_of = [&](int r) { return load16(src, (x.row0 + min(r, x.count - 1)) * stride); };
-        auto turn_row = [&](int r, float* y) {
+        auto given = [&](int r) { return axes.position(a, x.row0 + min(r, x.count - 1)); };
+        auto turn_row = [&](int r, int pos, float* y) {
             if (!turned) return;
             Turn<EPL, kAt> turn;
-            turn.load(a, x.p0 + min(r, x.count - 1), x.row0 + min(r, x.count - 1), col);
+            turn.load(a, kAt ? pos : x.p0 + min(r, x.count - 1), x.row0 + min(r, x.count - 1), col, axes);
             rotate<EPL, LPR, kAt>(a, turn, col, y);
         };
         if constexpr (!kStore8) {
             if (bounded) take_in_held<T, false, THREADS, 4>(page, x.held, 1.f, col, mx, mn);
+            int pos = kAt && turned ? given(rg) : 0;
             for (int r = rg; r < x.count + rg; r += RPP) {      // (uniform trip count)
                 float y[EPL];
-                unpack<T>(row_of(r), y);
-                turn_row(r, y);
+                const uint4 raw = row_of(r);
+                const int next = kAt && turned ? given(r + RPP) : 0;      // (a row ahead of the angles that it leads to)
+                unpack<T>(raw, y);
+                turn_row(r, pos, y);
+                pos = next;
                 store_token<T, false>(page, x.held + min(r, x.count - 1), col, y, 1.f, 1.f, r < x.count, mx, mn);
             }
         } else {
@@ -491,12 +510,15 @@ __global__ __launch_bounds__(THREADS) void page_append_prompt_kernel(AppendArgs 
             float y[PASSES][EPL], top = 0.f;
 #pragma unroll
             for (int i = 0; i < PASSES; ++i) raw[i] = row_of(i * RPP + rg);
+            int pos = kAt && turned ? given(rg) : 0;
             float* scales = which ? a.v_scale : a.k_scale;
             const float old = x.held > 0 ? scales[at] : 0.f;
 #pragma unroll
             for (int i = 0; i < PASSES; ++i) {
                 unpack<T>(raw[i], y[i]);
-                turn_row(i * RPP + rg, y[i]);
+                const int next = kAt && turned && i + 1 < PASSES ? given((i + 1) * RPP + rg) : 0;
+                turn_row(i * RPP + rg, pos, y[i]);
+                pos = next;
 #pragma unroll
                 for (int e = 0; e < EPL; ++e) {
                     const float m = fabsf(y[i][e]);
@@ -534,12 +556,14 @@ template <typename T, bool kStore8, bool kAt> __global__ __launch_bounds__(LEOAM
         return;
     }
     const int h = unit % hkv;
+    const Axes<EPL, kAt> axes(a, col);
+    const int given = kAt && a.rot_dim ? axes.position(a, unit / hkv) : 0;      // (a token each: its row is its sequence's)
     const TouchedPage x = touched_page(a, unit / hkv, h == 0);
     if (x.count == 0) return;
     const uint4 raw[2] = {load16(a.k, x.row0 * a.k_stride + (size_t)h * ROWB + col * T::kBytes),
                           load16(a.v, x.row0 * a.v_stride + (size_t)h * ROWB + col * T::kBytes)};
     Turn<EPL, kAt> turn;
-    if (a.rot_dim) turn.load(a, x.p0, x.row0, col);
+    if (a.rot_dim) turn.load(a, kAt ? given : x.p0, x.row0, col, axes);
     const size_t at = (size_t)x.id * hkv + h;
     float old[2] = {0.f, 0.f};
     if (kStore8 && x.held > 0) {

@@ -122,7 +122,7 @@ def test_weigh_scales_of_any_sign_and_without_numbers(L):
 def test_weigh_rows_of_negative_places_and_lists_that_descend(L):
     # more rows than tokens: those before the first token see nothing; a list that descends brings no rows
     made = Made(BF16, False, [3, 20], 1, 16, seed=5)
-    q = torch.randn(8, 2, 128).to(BF16).cuda()
+    q = torch.randn(8, 2, 128, generator=torch.Generator().manual_seed(5)).to(BF16).cuda()
     lse, pages = torch.zeros(8, 2).cuda(), made.pages(L, 2)
     one, two = torch.full((2, 1, 48), 7.0).cuda(), torch.full((2, 1, 48), 7.0).cuda()
     pages.max_pages = 3
@@ -131,7 +131,10 @@ def test_weigh_rows_of_negative_places_and_lists_that_descend(L):
     L.page_weight_add(pages, q, i32([0, 8, 8]), made.k_pages, None, table.cuda(), made.seq_len, SCALE, lse, 1.0, None, one)
     L.page_weight_add(pages, q[5:].contiguous(), i32([0, 3, 3]), made.k_pages, None, table.cuda(), made.seq_len, SCALE, lse[5:].contiguous(), 1.0,
                       None, two)
-    assert torch.equal(one, two) and (one[0, 0, :3] > 0).all() and (one[1, 0, :20] == 0).all()
+    # The two calls bring different numbers of rows, so a token's sum may be taken in another order.  It has at most six terms that are
+    # not zero (three rows, two heads), all positive and the same in both calls: five additions, each off by at most 2^-24 of the sum, so
+    # two orders differ by at most 10 * 2^-24 of it, below 2^-20.
+    assert ((one - two).abs() <= 2.0 ** -20 * one).all() and (one[0, 0, :3] > 0).all() and (one[1, 0, :20] == 0).all()
     L.page_weight_add(pages, q, i32([5, 2, 99]), made.k_pages, None, table.cuda(), made.seq_len, SCALE, lse, 0.5, one, two)
     assert torch.equal(two[0, 0, :3], one[0, 0, :3] * 0.5) and (two[1, 0, :20] == 0).all()
 
