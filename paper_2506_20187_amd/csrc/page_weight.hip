@@ -3,12 +3,14 @@
 //
 // S = K Q^T on the matrix cores, keys as the first operand: a wave holds its keys in registers and goes through the rows sixteen
 // (row, head) columns at a time, so the sums of a token stay in registers too and nothing is added by atomics.
-// Few rows for each sequence: every key is read once, bound by that.  The stretches of 32 keys (fp32: 16) of all sequences and heads
-// are laid end to end and shared out equally to the waves; a wave has the next one's keys on their way while it works on one.  They
-// come as whole rows, which the caches serve at four times the rate of an operand's 16 bytes of 16 rows, and become operands
-// in LDS.
-// Many rows: bound by the exponentials.  The eight waves of a workgroup share 64 keys (fp32: 32) and take every eighth block of
-// columns each; their sums are added in order at the end.  Queries, too, come as whole rows.
+// Few rows for each sequence: every key is read once, bound by that.  The stretches of 64 keys (fp32: 32) of all sequences and heads
+// are laid end to end and shared out equally to the waves; a wave works on half of one while the next half's keys are on their
+// way.  They come as whole rows, which the caches serve at four times the rate of an operand's 16 bytes of 16 rows, and become
+// operands in LDS.  Sixteen tokens of sequences to 33001 (617 MB): 128 us, 4.8 TB/s; with operands straight from the loads and no
+// equal shares 187; with weights written for 32 keys at a time 134.
+// Many rows: bound by the exponentials and the instructions around them.  The waves of a workgroup share 64 keys (fp32: 32) and go
+// through the blocks of columns in turn; their sums are added in order at the end.  Queries, too, come as whole rows.  A prompt of
+// 4096 with 32 heads: 115 us (268 M exponentials, 69 GFLOP); with operands straight from the loads 191.
 #include "page_common.h"
 
 namespace leoam {
@@ -28,9 +30,11 @@ struct PageWeightArgs {
     int total;      // (block of keys, sequence, kv head) triples of a full table
 };
 
-template <typename T, bool kSplitRows> constexpr int kWeightTiles = (T::kTag == LEOAM_F32 ? 1 : 2) * (kSplitRows ? 2 : 1);      // of 16 keys, of a wave
+// tiles of 16 keys that a wave has in registers
+template <typename T, bool kSplitRows> constexpr int kWeightTiles = (T::kTag == LEOAM_F32 ? 1 : 2) * (kSplitRows ? 2 : 1);
 
-// A stretch of keys: (sequence, kv head), its first key, the sequence's length, its rows of the call and the place of the first one's token.
+// A stretch of keys: (sequence, kv head), its first key, the sequence's length, its rows of the call and the place of the first
+// one's token.
 struct WeightUnit { int bh, b, h, t0, len, row0, m, first; };
 
 // 16 (row, head) columns
@@ -55,13 +59,13 @@ template <typename T, typename S, int G, bool kSplitRows> struct Weighing {
         uint32_t have;      // bit j: the tile has a page
     };
 
-    static __device__ __forceinline__ WeightUnit unit_at(const PageWeightArgs& a, int bh, long long t0) {
+    static __device__ __forceinline__ WeightUnit unit_at(const PageWeightArgs& a, int bh, int t0) {
         WeightUnit u;
         u.bh = bh;
         u.b = bh / a.n_kv_heads;
         u.h = bh - u.b * a.n_kv_heads;
         u.len = min(max(scalar_at(a.seq_len, u.b), 0), a.max_pages << a.page_shift);
-        u.t0 = (int)t0;
+        u.t0 = t0;
         u.row0 = u.b;
         u.m = 1;
         if (a.new_off) {
@@ -82,7 +86,8 @@ template <typename T, typename S, int G, bool kSplitRows> struct Weighing {
         x.have = 0;
         int id[NT];
 #pragma unroll
-        for (int j = 0; j < NT; ++j) id[j] = scalar_at(a.page_table, (size_t)u.b * a.max_pages + (min(u.t0 + 16 * j, u.len - 1) >> a.page_shift));
+        for (int j = 0; j < NT; ++j)
+            id[j] = scalar_at(a.page_table, (size_t)u.b * a.max_pages + (min(u.t0 + 16 * j, u.len - 1) >> a.page_shift));
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
             const int t = min(u.t0 + 16 * j, u.len - 1), valid = min(u.len - (u.t0 + 16 * j), 16), page = id[j];
@@ -94,8 +99,8 @@ template <typename T, typename S, int G, bool kSplitRows> struct Weighing {
             if constexpr (k8) x.ks[j] = scalar_at(a.k_scale, row);
 #pragma unroll
             for (int s = 0; s < NK; ++s) {
-                if constexpr (kSplitRows) x.k[NK * j + s] = load16(kp, (row0 + min((uint32_t)l16, last)) * ROWB + 64 * s + 16 * grp);
-                else x.k[NK * j + s] = load16(kp, (row0 + min((uint32_t)(s * kRowsOfLoad + lane / kPieces), last)) * ROWB + 16 * (lane % kPieces));
+                const uint32_t r = kSplitRows ? l16 : s * kRowsOfLoad + lane / kPieces, p = kSplitRows ? 4 * s + grp : lane % kPieces;
+                x.k[NK * j + s] = load16(kp, (row0 + min(r, last)) * ROWB + 16 * p);
             }
         }
     }
@@ -149,15 +154,18 @@ template <typename T, typename S, int G, bool kSplitRows> struct Weighing {
             return x.k[NK * j + i];
         }
     }
-    template <typename K> static __device__ __forceinline__ void add(const PageWeightArgs& a, const WeightUnit& u, K&& key_of, const WeightColumns<T>& c, float (*w)[4]) {
+    // One block of columns onto the sums: p = exp2(s q.k - base) where the column sees the key; one that attended to nothing adds 0.
+    template <typename K>
+    static __device__ __forceinline__ void add(const PageWeightArgs& a, const WeightUnit& u, K&& key_of, const WeightColumns<T>& c,
+                                               float (*w)[4]) {
         const int pos = c.base != -INFINITY ? c.pos : -1;
         const float base = c.base * kLog2e;
         if (__ballot(pos < min(u.t0 + KEYS, u.len) - 1)) add_products<true>(a, u, key_of, c, pos, base, w);
         else add_products<false>(a, u, key_of, c, pos, base, w);
     }
     template <bool kMasked, typename K>
-    static __device__ __forceinline__ void add_products(const PageWeightArgs& a, const WeightUnit& u, K&& key_of, const WeightColumns<T>& c, int pos,
-                                                        float base, float (*w)[4]) {
+    static __device__ __forceinline__ void add_products(const PageWeightArgs& a, const WeightUnit& u, K&& key_of,
+                                                        const WeightColumns<T>& c, int pos, float base, float (*w)[4]) {
         const int grp = lane_id() >> 4;
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
@@ -187,16 +195,18 @@ template <typename T, typename S, int G, bool kSplitRows> struct Weighing {
             }
         }
     }
-    // The columns' sums: lane l16 keeps that of register l16 % 4 of tile l16 / 4, token `slot` of the stretch.
+    // The columns' sums of TILES tiles: lane l16 keeps that of register l16 % 4 of tile l16 / 4, token `slot` of the stretch.
     static __device__ __forceinline__ int slot() { return 16 * ((lane_id() & 15) >> 2) + 4 * (lane_id() >> 4) + (lane_id() & 3); }
-    static __device__ __forceinline__ bool keeps(const WeightUnit& u) { return (lane_id() & 15) < 4 * NT && u.t0 + slot() < u.len; }
+    static __device__ __forceinline__ bool keeps(const WeightUnit& u, int tiles) {
+        return (lane_id() & 15) < 4 * tiles && u.t0 + slot() < u.len;
+    }
     static __device__ __forceinline__ size_t place(const PageWeightArgs& a, const WeightUnit& u) {
         return (size_t)u.bh * ((size_t)a.max_pages << a.page_shift) + min(u.t0 + slot(), u.len - 1);
     }
-    static __device__ __forceinline__ float sums(uint32_t have, const float (*w)[4]) {
+    template <int TILES> static __device__ __forceinline__ float sums(uint32_t have, const float (*w)[4]) {
         float mine = 0.f;
 #pragma unroll
-        for (int j = 0; j < NT; ++j)
+        for (int j = 0; j < TILES; ++j)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const float sum = row16_sum(w[j][r]);
@@ -219,7 +229,8 @@ template <typename T, typename S, int G> __global__ __launch_bounds__(kAttThread
     __shared__ int sh_entry[kAttWaves];
     __shared__ __align__(16) char sh_keys[kAttWaves][W::KEYS * W::ROWB];
     const int tid = threadIdx.x, lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(tid / LEOAM_WAVE), hkv = a.n_kv_heads;
-    auto blocks_of = [&](int len) { return (min(max(len, 0), a.max_pages << a.page_shift) + W::KEYS - 1) / W::KEYS; };
+    constexpr int STRETCH = 2 * W::KEYS;
+    auto blocks_of = [&](int len) { return (min(max(len, 0), a.max_pages << a.page_shift) + STRETCH - 1) / STRETCH; };
 
     // ---- this wave's share of the stretches: `left` of them, from stretch `block` of head h of sequence b on -------
     int b, h, block, left;
@@ -267,67 +278,64 @@ template <typename T, typename S, int G> __global__ __launch_bounds__(kAttThread
         block = uniform((int)(sh_in[wave] - (long long)h * n));
     }
 
-    struct Fetched {
-        WeightUnit u;
-        typename W::Keys keys;
-        float was;
-    };
-    auto fetch = [&](Fetched& x) __attribute__((always_inline)) {
-        x.u = W::unit_at(a, b * hkv + h, (long long)block * W::KEYS);
-        W::fetch_keys(a, x.u, x.keys);
-        x.was = a.before ? a.before[W::place(a, x.u)] : 0.f;
-        // to the next stretch
-        --left;
-        if (left == 0 || (++block) * W::KEYS < x.u.len) return;
-        block = 0;
-        if (++h < hkv) return;
-        h = 0;
-        do ++b;
-        while (blocks_of(scalar_at(a.seq_len, b)) == 0);      // (there is one: the share is not at its end)
-    };
+    // half `half` of stretch `block`
+    auto half_at = [&](int half) __attribute__((always_inline)) { return W::unit_at(a, b * hkv + h, block * STRETCH + half * W::KEYS); };
+    typename W::Keys even, odd;
     WeightColumns<T> cols;
     int cols_of = -1;      // which (sequence, kv head) they are of
-    // works on x while y is on its way; false: x was the last one
-    auto step = [&](Fetched& x, Fetched& y) __attribute__((always_inline)) {
-        if (x.u.bh != cols_of) {
-            cols_of = x.u.bh;
-            W::fetch_columns(a, x.u, 0, cols);
+    W::fetch_keys(a, half_at(0), even);
+    while (left > 0) {
+        const WeightUnit u = half_at(0), v = half_at(1);      // (the second may lie behind the last token)
+        if (u.bh != cols_of) {
+            cols_of = u.bh;
+            W::fetch_columns(a, u, 0, cols);
         }
-        const bool last = left == 0;
-        if (!last) fetch(y);
-        float w[W::NT][4];
+        W::fetch_keys(a, v, odd);
+        const float was = a.before ? a.before[W::place(a, u)] : 0.f;
+        float w[2 * W::NT][4];
 #pragma unroll
-        for (int j = 0; j < W::NT; ++j)
+        for (int j = 0; j < 2 * W::NT; ++j)
 #pragma unroll
             for (int r = 0; r < 4; ++r) w[j][r] = 0.f;
-        W::turn(x.keys, sh_keys[wave]);
-        auto key_of = [&](int j, int i) { return W::key(x.keys, j, i); };
-        const int n_cols = W::columns(x.u);
-        if (n_cols > 0) W::add(a, x.u, key_of, cols, w);
-        for (int cb = 1; 16 * cb < n_cols; ++cb) {
-            WeightColumns<T> more;
-            W::fetch_columns(a, x.u, cb, more);
-            W::add(a, x.u, key_of, more, w);
+        auto work = [&](const WeightUnit& x, typename W::Keys& keys, float (*sums)[4]) __attribute__((always_inline)) {
+            W::turn(keys, sh_keys[wave]);
+            auto key_of = [&](int j, int i) { return W::key(keys, j, i); };
+            const int n_cols = W::columns(x);
+            if (n_cols > 0) W::add(a, x, key_of, cols, sums);
+            for (int cb = 1; 16 * cb < n_cols; ++cb) {
+                WeightColumns<T> more;
+                W::fetch_columns(a, x, cb, more);
+                W::add(a, x, key_of, more, sums);
+            }
+        };
+        work(u, even, w);
+        const uint32_t have = even.have;
+        // to the next stretch (behind the share's last: that one again, from the caches)
+        if (--left > 0 && ++block * STRETCH >= u.len) {
+            block = 0;
+            if (++h == hkv) {
+                h = 0;
+                do ++b;
+                while (blocks_of(scalar_at(a.seq_len, b)) == 0);      // (there is one: the share is not at its end)
+            }
         }
-        const float mine = W::sums(x.keys.have, w);
-        if (W::keeps(x.u)) W::store(a, x.u, x.was, mine);
-        return !last;
-    };
-    Fetched even, odd;
-    fetch(even);
-    while (step(even, odd) && step(odd, even)) {}
+        W::fetch_keys(a, half_at(0), even);
+        work(v, odd, w + W::NT);
+        const float mine = W::template sums<2 * W::NT>(have | odd.have << W::NT, w);
+        if (W::keeps(u, 2 * W::NT)) W::store(a, u, was, mine);
+    }
 }
 
 // ---- many rows ------------------------------------------------------------------------------------------------
-constexpr int kManyWaves = 8;
-template <typename T, typename S, int G> __global__ __launch_bounds__(kManyWaves * LEOAM_WAVE, 2) void page_weight_many_kernel(PageWeightArgs a) {
+template <typename T, typename S, int G, int WAVES>
+__global__ __launch_bounds__(WAVES * LEOAM_WAVE, 2) void page_weight_many_kernel(PageWeightArgs a) {
     using W = Weighing<T, S, G, true>;
-    __shared__ float sh[kManyWaves][W::KEYS];
-    __shared__ __align__(16) char sh_queries[kManyWaves][16 * W::QROWB];
+    __shared__ float sh[WAVES][W::KEYS];
+    __shared__ __align__(16) char sh_queries[WAVES][16 * W::QROWB];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / LEOAM_WAVE), rows_bh = a.batch * a.n_kv_heads;
     for (int unit = blockIdx.x; unit < a.total; unit += gridDim.x) {
         const int block = unit / rows_bh;
-        const WeightUnit u = W::unit_at(a, unit - block * rows_bh, (long long)block * W::KEYS);
+        const WeightUnit u = W::unit_at(a, unit - block * rows_bh, block * W::KEYS);
         if (u.t0 >= u.len) continue;
         typename W::Keys keys;
         W::fetch_keys(a, u, keys);
@@ -349,43 +357,62 @@ template <typename T, typename S, int G> __global__ __launch_bounds__(kManyWaves
             // be moved behind it, where they are waited for at once)
             WeightColumns<T> even, odd;
             W::fetch_columns(a, u, wave, even);
-            for (int cb = wave; cb < n_blocks; cb += 2 * kManyWaves) {
-                W::fetch_columns(a, u, cb + kManyWaves, odd);
+            for (int cb = wave; cb < n_blocks; cb += 2 * WAVES) {
+                W::fetch_columns(a, u, cb + WAVES, odd);
                 W::turn(even, sh_queries[wave]);
                 W::add(a, u, key_of, even, w);
-                W::fetch_columns(a, u, cb + 2 * kManyWaves, even);
+                W::fetch_columns(a, u, cb + 2 * WAVES, even);
                 W::turn(odd, sh_queries[wave]);
                 W::add(a, u, key_of, odd, w);
             }
         }
-        float mine = W::sums(keys.have, w);
+        float mine = W::template sums<W::NT>(keys.have, w);
         if ((lane_id() & 15) < 4 * W::NT) sh[wave][W::slot()] = mine;
         __syncthreads();
-        if (wave == 0 && W::keeps(u)) {
+        if (wave == 0 && W::keeps(u, W::NT)) {
             mine = sh[0][W::slot()];
 #pragma unroll
-            for (int v = 1; v < kManyWaves; ++v) mine += sh[v][W::slot()];
+            for (int v = 1; v < WAVES; ++v) mine += sh[v][W::slot()];
             W::store(a, u, was, mine);
         }
         __syncthreads();      // (the sums have been read)
     }
 }
 
-// Four or more blocks of columns for each sequence on average: many rows.
-constexpr int kManyColumns = 64;
-constexpr int kFewGroups = 512;             // workgroups: two fill a compute unit (three, with fewer registers each: 150 against 136 us, 16 sequences to 33001)
+// More than a block of columns for each sequence on average: many rows.
+constexpr int kFewColumns = 16;
+// workgroups of few rows: two fill a compute unit (three, with fewer registers each: 150 against 136 us, 16 sequences to 33001)
+constexpr int kFewGroups = 512;
 constexpr int kManyGroups = 65536;
 
+// Waves that share a stretch of many rows: one, where the stretches by themselves fill the card (a workgroup of eight is alone on its
+// compute unit, and its loads are waited for at each stretch: 64 rows behind 32001 tokens 39 us, four waves 58, eight 110); more,
+// where few stretches would leave it idle (256 rows behind 2000 36, 14, 13; prompt of 4096 530, 168, 129).  Prompts without much
+// before them take more: the last stretches have few rows, the first ones all (8 prompts of 4096 1078, 865, 888).
+static int waves_of(long long stretches, long long columns, bool prompts) {
+    if (columns >= 512 && stretches <= (prompts ? 1024 : 256)) return 8;
+    return columns >= 256 && (prompts || stretches <= 1024) ? 4 : 1;
+}
+
 template <typename T, typename S, int G> static hipError_t launch_weight(PageWeightArgs a, hipStream_t stream) {
-    const bool many = (long long)a.n_new * G >= (long long)kManyColumns * a.batch;
-    const long long block = 16 * (many ? kWeightTiles<T, true> : kWeightTiles<T, false>), capacity = (long long)a.max_pages << a.page_shift;
+    const long long capacity = (long long)a.max_pages << a.page_shift, columns = (long long)a.n_new * G;
+    const bool many = columns > (long long)kFewColumns * a.batch;
+    const int block = 16 * (many ? kWeightTiles<T, true> : 2 * kWeightTiles<T, false>);
     const long long total = (capacity + block - 1) / block * a.batch * a.n_kv_heads;
     if (total > 0x7fffffffll - kManyGroups) return hipErrorInvalidValue;
     a.total = (int)total;
-    const long long groups = many ? total : (total + kAttWaves - 1) / kAttWaves, most = many ? kManyGroups : kFewGroups;
-    const dim3 grid((unsigned)(groups < most ? groups : most)), threads(kAttThreads);
-    if (many) hipLaunchKernelGGL((page_weight_many_kernel<T, S, G>), grid, dim3(kManyWaves * LEOAM_WAVE), 0, stream, a);
-    else hipLaunchKernelGGL((page_weight_few_kernel<T, S, G>), grid, threads, 0, stream, a);
+    if (!many) {
+        const long long groups = (total + kAttWaves - 1) / kAttWaves;
+        hipLaunchKernelGGL((page_weight_few_kernel<T, S, G>), dim3((unsigned)(groups < kFewGroups ? groups : kFewGroups)), dim3(kAttThreads), 0,
+                           stream, a);
+        return hipGetLastError();
+    }
+    const dim3 grid((unsigned)(total < kManyGroups ? total : kManyGroups));
+    switch (waves_of(total, columns / a.batch, 2ll * a.n_new >= a.batch * capacity)) {
+    case 8: hipLaunchKernelGGL((page_weight_many_kernel<T, S, G, 8>), grid, dim3(8 * LEOAM_WAVE), 0, stream, a); break;
+    case 4: hipLaunchKernelGGL((page_weight_many_kernel<T, S, G, 4>), grid, dim3(4 * LEOAM_WAVE), 0, stream, a); break;
+    default: hipLaunchKernelGGL((page_weight_many_kernel<T, S, G, 1>), grid, dim3(LEOAM_WAVE), 0, stream, a);
+    }
     return hipGetLastError();
 }
 template <typename T, typename S> static hipError_t weight_of(const PageWeightArgs& a, int group, hipStream_t stream) {

@@ -97,6 +97,13 @@ def test_weigh_page_sizes(L, dtype, q8, page):
     run_weigh(L, Made(dtype, q8, [5 * page + 7, page, 1, 1025], 2, page, seed=page), 8, [100, 1, 1, 40], seed=page, decay=0.0)
 
 
+@pytest.mark.parametrize("dtype,q8", KINDS, ids=KIND_IDS)
+@pytest.mark.parametrize("rows,history", [(4, 700), (5, 700), (33, 1200), (65, 900), (65, 0), (130, 800), (150, 10)])
+def test_weigh_rows_behind_a_history(L, dtype, q8, rows, history):
+    """One, four and eight waves to a stretch of keys, and the borders between them."""
+    run_weigh(L, Made(dtype, q8, [rows + history, rows], 2, 32, seed=rows), 8, [rows, rows], seed=rows)
+
+
 def test_weigh_long_prompt(L):
     run_weigh(L, Made(BF16, False, [1500], 1, 64, seed=2), 8, [1500], before=False)
 
