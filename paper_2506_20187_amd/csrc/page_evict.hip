@@ -6,9 +6,11 @@
 // number t - kept(t), and t >= keep is mover number kept(t) - kept(keep): one count in order gives both.
 //
 // A weight becomes a 32-bit key of the same order, protected ones the highest, and the lowest key that stays is found by histograms of
-// 11, 11 and 10 of its bits.  What is read is 8 bytes a token; bound by latency.  Where a row fits, one workgroup holds its keys in
-// registers.  Longer rows are cut into parts of 8192 places (at `keep`, too, so that what stays before it is a sum over parts): three
-// launches make the parts' histograms, each beginning with the sums of the last one's, a fourth one lists.
+// 11, 11 and 10 of its bits.  What is read is 8 bytes a token; bound by latency, where there are many rows by the instructions for each
+// key.  A workgroup holds the keys of a row in registers (16 rows of 4200 tokens 9.6 us, of 32000 31, 512 rows of 20000 52).  Longer
+// rows are cut into parts of 8192 places (at `keep`, too, so that what stays before it is a sum over parts): three launches make the
+// parts' histograms, each beginning with the sums of the last one's, a fourth one lists (16 rows of 64000 29 us; 35 when every
+// workgroup read all bins of its row's parts).
 #include "page_common.h"
 
 namespace leoam {
@@ -23,10 +25,7 @@ struct EvictArgs {
     int n_kv_heads, capacity;
 };
 
-constexpr int kEvictThreads = 1024;
-constexpr int kEvictHeld = 16;                     // keys of a thread
-constexpr int kEvictRowMost = kEvictThreads * kEvictHeld;      // longest row of a workgroup
-constexpr int kPartThreads = 512, kEvictPart = kPartThreads * kEvictHeld;
+constexpr int kPartThreads = 512, kPartHeld = 16, kEvictPart = kPartThreads * kPartHeld;      // threads, keys of a thread
 constexpr int kEvictBins = 2048;
 constexpr uint32_t kProtected = 0xffffffffu;       // above every weight's key
 
@@ -70,28 +69,34 @@ struct EvictRow {
 };
 
 // Places [begin, end) of a row, dealt out to the waves in order, 64 at a time, with their keys.
-template <int THREADS> struct HeldKeys {
-    uint32_t keys[kEvictHeld];
+template <int THREADS, int HELD> struct HeldKeys {
+    uint32_t keys[HELD];
     int begin, end;
     __device__ __forceinline__ HeldKeys(const EvictRow& row, int lo, int hi) {
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / LEOAM_WAVE), seg = (hi - lo + THREADS - 1) / THREADS * LEOAM_WAVE;
         begin = min(hi, lo + wave * seg);
         end = min(hi, begin + seg);
-        float w[kEvictHeld];
-        int id[kEvictHeld];
+        constexpr int TOGETHER = 16;      // on their way together; places past the last repeat it
 #pragma unroll
-        for (int i = 0; i < kEvictHeld; ++i) {      // (all on their way together; places past the last repeat it)
-            if (begin + i * LEOAM_WAVE >= end) break;
-            const int t = min(begin + i * LEOAM_WAVE + lane_id(), end - 1);
-            w[i] = row.weight[t];
-            id[i] = row.ids ? row.ids[t] : t;
+        for (int i0 = 0; i0 < HELD; i0 += TOGETHER) {
+            if (begin + i0 * LEOAM_WAVE >= end) break;
+            float w[TOGETHER];
+            int id[TOGETHER];
+#pragma unroll
+            for (int i = 0; i < TOGETHER; ++i) {
+                if (begin + (i0 + i) * LEOAM_WAVE >= end) break;
+                const int t = min(begin + (i0 + i) * LEOAM_WAVE + lane_id(), end - 1);
+                w[i] = row.weight[t];
+                id[i] = row.ids ? row.ids[t] : t;
+            }
+#pragma unroll
+            for (int i = 0; i < TOGETHER; ++i)
+                keys[i0 + i] = row.key(min(begin + (i0 + i) * LEOAM_WAVE + lane_id(), end - 1), id[i], w[i]);
         }
-#pragma unroll
-        for (int i = 0; i < kEvictHeld; ++i) keys[i] = row.key(min(begin + i * LEOAM_WAVE + lane_id(), end - 1), id[i], w[i]);
     }
     template <typename F> __device__ __forceinline__ void each(F&& f) const {      // f(place, key, counts), by whole waves
 #pragma unroll
-        for (int i = 0; i < kEvictHeld; ++i) {
+        for (int i = 0; i < HELD; ++i) {
             const int t = begin + i * LEOAM_WAVE + lane_id();
             if (begin + i * LEOAM_WAVE < end) f(t, keys[i], t < end);
         }
@@ -104,13 +109,15 @@ template <int WAVES> __device__ __forceinline__ int before_wave(const int* sh, i
     return wave ? __builtin_amdgcn_readlane((int)incl, wave - 1) : 0;
 }
 
-// The bin, from the top, in which the `need`-th entry of a histogram is: bin, entries above it, entries in it.  counts(first, c): the
-// counts of PER bins from `first` (a multiple of PER) on.  The workgroup's `sh`: waves + 3 words.
-template <int THREADS, typename F> __device__ __forceinline__ int3 find_bin(int need, int* sh, F&& counts) {
+// The bin, from the top, in which the `need`-th entry of a histogram is: bin, entries above it, entries in it.  The workgroup's `sh`:
+// waves + 3 words.
+template <int THREADS> __device__ __forceinline__ int3 find_bin(int need, int* sh, const uint32_t* hist) {
     constexpr int PER = kEvictBins / THREADS, WAVES = THREADS / LEOAM_WAVE;
-    const int tid = threadIdx.x, lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(tid / LEOAM_WAVE), first = kEvictBins - (tid + 1) * PER;
+    const int tid = threadIdx.x, lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(tid / LEOAM_WAVE);
+    const int first = kEvictBins - (tid + 1) * PER;
     uint32_t c[PER], sum = 0;
-    counts(first, c);
+#pragma unroll
+    for (int i = 0; i < PER; ++i) c[i] = hist[first + i];
 #pragma unroll
     for (int i = 0; i < PER; ++i) sum += c[i];
     const uint32_t incl = wave_incl_scan_u32(sum);
@@ -134,7 +141,8 @@ template <int THREADS, typename F> __device__ __forceinline__ int3 find_bin(int 
 
 // The histogram of a stage in LDS: stage 0: bits 31..21 of all keys; 1: bits 20..10 of those that begin as `prefix`; 2: bits 9..0.
 // (Protected ones come by the wave, all of them into the last bin: counted by the wave.)
-template <int STAGE, int THREADS> __device__ __forceinline__ void count_keys(const HeldKeys<THREADS>& held, uint32_t prefix, uint32_t* hist) {
+template <int STAGE, int THREADS, int HELD>
+__device__ __forceinline__ void count_keys(const HeldKeys<THREADS, HELD>& held, uint32_t prefix, uint32_t* hist) {
     constexpr int kShift = STAGE == 0 ? 21 : STAGE == 1 ? 10 : 0, kKnown = STAGE == 1 ? 21 : 10;
     int guarded = 0;
     held.each([&](int, uint32_t k, bool in) {
@@ -142,14 +150,15 @@ template <int STAGE, int THREADS> __device__ __forceinline__ void count_keys(con
         guarded += __popcll(__ballot(last));
         if (in && !last && (STAGE == 0 || (k ^ prefix) >> kKnown == 0)) atomicAdd(&hist[k >> kShift & (STAGE == 2 ? 1023u : 2047u)], 1u);
     });
-    if (lane_id() == 0 && guarded && (STAGE == 0 || (kProtected ^ prefix) >> kKnown == 0)) atomicAdd(&hist[STAGE == 2 ? 1023 : 2047], (uint32_t)guarded);
+    if (lane_id() == 0 && guarded && (STAGE == 0 || (kProtected ^ prefix) >> kKnown == 0))
+        atomicAdd(&hist[STAGE == 2 ? 1023 : 2047], (uint32_t)guarded);
 }
 
 // The moves of places [begin, end): keys above `bound` stay, and the first `ties` of those equal to it.  above, equal: how many of either
 // are before the wave's places; kept_low: how many stay below `keep`.
-template <int THREADS>
-__device__ __forceinline__ void list_moves(const HeldKeys<THREADS>& held, int keep, uint32_t bound, int ties, int above, int equal, int kept_low,
-                                           int32_t* moves) {
+template <int THREADS, int HELD>
+__device__ __forceinline__ void list_moves(const HeldKeys<THREADS, HELD>& held, int keep, uint32_t bound, int ties, int above, int equal,
+                                           int kept_low, int32_t* moves) {
     const uint64_t below = (1ull << lane_id()) - 1;
     held.each([&](int t, uint32_t k, bool in) {
         const uint64_t ab = __ballot(in && k > bound), eq = __ballot(in && k == bound);
@@ -165,7 +174,8 @@ __device__ __forceinline__ void list_moves(const HeldKeys<THREADS>& held, int ke
 
 // ---- a row to a workgroup ---------------------------------------------------------------------------------
 // (Rows of up to 8192 places: 512 threads, so that four workgroups share a compute unit.)
-template <int THREADS> __global__ __launch_bounds__(THREADS, THREADS == 512 ? 8 : 4) void page_evict_row_kernel(EvictArgs a) {
+template <int THREADS, int HELD>
+__global__ __launch_bounds__(THREADS, THREADS == 512 ? 8 : 4) void page_evict_row_kernel(EvictArgs a) {
     constexpr int WAVES = THREADS / LEOAM_WAVE;
     __shared__ uint32_t hist[3][kEvictBins];
     __shared__ int sh_find[WAVES + 3], sh_above[WAVES], sh_equal[WAVES], sh_kept_low[2];
@@ -173,7 +183,7 @@ template <int THREADS> __global__ __launch_bounds__(THREADS, THREADS == 512 ? 8 
     const EvictRow row(a, bh);
     if (tid == 0) row.report(a, bh);
     if (row.none) return;
-    const HeldKeys<THREADS> held(row, 0, row.n);
+    const HeldKeys<THREADS, HELD> held(row, 0, row.n);
     const int keep = row.keep;
     for (int i = tid; i < 3 * kEvictBins; i += THREADS) hist[0][i] = 0;
     if (tid < 2) sh_kept_low[tid] = 0;
@@ -184,12 +194,9 @@ template <int THREADS> __global__ __launch_bounds__(THREADS, THREADS == 512 ? 8 
     auto stage = [&](auto which) {      // whether the bound is found: the key itself, or a bin that stays whole
         constexpr int STAGE = decltype(which)::value, kShift = STAGE == 0 ? 21 : STAGE == 1 ? 10 : 0;
         __syncthreads();
-        count_keys<STAGE, THREADS>(held, bound, hist[STAGE]);
+        count_keys<STAGE, THREADS, HELD>(held, bound, hist[STAGE]);
         __syncthreads();
-        const int3 found = find_bin<THREADS>(ties, sh_find, [&](int bin, uint32_t* c) {
-#pragma unroll
-            for (int i = 0; i < kEvictBins / THREADS; ++i) c[i] = hist[STAGE][bin + i];
-        });
+        const int3 found = find_bin<THREADS>(ties, sh_find, hist[STAGE]);
         ties -= found.y;
         bound |= (uint32_t)found.x << kShift;
         if (STAGE < 2 && ties == found.z && bound > 0u) {
@@ -222,15 +229,17 @@ template <int THREADS> __global__ __launch_bounds__(THREADS, THREADS == 512 ? 8 
     const int above = before_wave<WAVES>(sh_above, wave), equal = before_wave<WAVES>(sh_equal, wave);
     const int kept_low = sh_kept_low[0] + min(sh_kept_low[1], ties);
     if (tid == 0) a.move_count[bh] = keep - kept_low;
-    list_moves<THREADS>(held, keep, bound, ties, above, equal, kept_low, a.moves + (size_t)bh * a.m_max * 2);
+    list_moves<THREADS, HELD>(held, keep, bound, ties, above, equal, kept_low, a.moves + (size_t)bh * a.m_max * 2);
 }
 
 // ---- a part of a row to a workgroup -------------------------------------------------------------------------
 // Of each part: histograms of two stages in turn, and how many of its keys are above all bins that were found so far.  Of each row,
 // stage by stage: the bits of the bound that are known, and how many entries of the bin are still needed.
+constexpr int kCoarse = 64, kFine = kEvictBins / kCoarse;
 struct EvictFound { uint32_t prefix; int need; };
 struct EvictLong {
     uint32_t* hist;         // [2][row][part][kEvictBins]
+    uint32_t* coarse;       // [2][row][part][kCoarse]: its bins by 32
     int* above;             // [2][row][part]
     EvictFound* found;      // [2][row]
     int rows, parts;
@@ -248,108 +257,135 @@ struct PartOf {
     }
 };
 
-// neighbouring bins summed over a row's parts, eight parts on their way together
-constexpr int kPartBins = kEvictBins / kPartThreads;
-static_assert(kPartBins == 4, "a thread's bins are loaded by 16 bytes");
-__device__ __forceinline__ void sum_parts(const uint32_t* hist, int n_parts, int first, uint32_t* c) {
-    c[0] = c[1] = c[2] = c[3] = 0;
-    for (int p0 = 0; p0 < n_parts; p0 += 8) {
-        uint4 x[8];
+// The bin of a row's histogram, from the top, that holds the `need`-th entry, out of those of its parts: first among the coarse bins,
+// then among the 32 that one is made of, so that little more is read than 384 bytes of each part.  of(q, k): whether part q belongs to
+// set k of K.
+constexpr int kPartWaves = kPartThreads / LEOAM_WAVE;
+template <int K> struct PartSums { uint32_t x[2][kPartWaves][K + 1][LEOAM_WAVE]; };
+template <int K> struct PartBin {
+    int bin, above, above_of[K], equal_of[K];      // entries above the bin: of the row, of the sets; entries in it
+    template <typename F>
+    __device__ __forceinline__ PartBin(const uint32_t* hist, const uint32_t* coarse, int n_parts, int need, PartSums<K>& sh, F&& of) {
+        const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / LEOAM_WAVE);
+        above = 0;
 #pragma unroll
-        for (int u = 0; u < 8; ++u) x[u] = load16(hist, ((size_t)min(p0 + u, n_parts - 1) * kEvictBins + first) * sizeof(uint32_t));
+        for (int k = 0; k < K; ++k) above_of[k] = 0;
+        auto look = [&](int level, int lanes_of_part, const uint32_t* from, int stride) __attribute__((always_inline)) {
+            // lane i of a part's: its i-th bin from the top
+            const int per = LEOAM_WAVE / lanes_of_part, i = lane % lanes_of_part;
+            uint32_t sums[K + 1];
 #pragma unroll
-        for (int u = 0; u < 8; ++u) {
-            if (p0 + u >= n_parts) break;
-            c[0] += x[u].x;
-            c[1] += x[u].y;
-            c[2] += x[u].z;
-            c[3] += x[u].w;
-        }
+            for (int k = 0; k <= K; ++k) sums[k] = 0;
+            for (int q0 = wave * per + lane / lanes_of_part; q0 < n_parts; q0 += 4 * kPartWaves * per) {
+                uint32_t x[4];
+#pragma unroll
+                for (int u = 0; u < 4; ++u)
+                    x[u] = from[(size_t)min(q0 + u * kPartWaves * per, n_parts - 1) * stride + lanes_of_part - 1 - i];
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    const int q = q0 + u * kPartWaves * per;
+                    if (q >= n_parts) break;
+#pragma unroll
+                    for (int k = 0; k < K; ++k) sums[k] += of(q, k) ? x[u] : 0u;
+                    sums[K] += x[u];
+                }
+            }
+#pragma unroll
+            for (int k = 0; k <= K; ++k) sh.x[level][wave][k][lane] = sums[k];
+            __syncthreads();
+#pragma unroll
+            for (int k = 0; k <= K; ++k) {
+                sums[k] = 0;
+#pragma unroll
+                for (int w = 0; w < kPartWaves; ++w)
+                    for (int r = 0; r < per; ++r) sums[k] += sh.x[level][w][k][r * lanes_of_part + i];
+                if (lane >= lanes_of_part) sums[k] = 0;
+            }
+            const uint32_t upto = wave_incl_scan_u32(sums[K]), left = (uint32_t)(need - above);
+            const int hit = min(__builtin_ctzll(__ballot(upto >= left && upto - sums[K] < left) | 1ull << 63), lanes_of_part - 1);
+            above += __builtin_amdgcn_readlane((int)(upto - sums[K]), hit);
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                above_of[k] += __builtin_amdgcn_readlane((int)(wave_incl_scan_u32(sums[k]) - sums[k]), hit);
+                equal_of[k] = __builtin_amdgcn_readlane((int)sums[k], hit);
+            }
+            return lanes_of_part - 1 - hit;
+        };
+        const int big = look(0, kCoarse, coarse, kCoarse);
+        bin = big * kFine + look(1, kFine, hist + big * kFine, kEvictBins);
     }
-}
-// of four neighbouring bins, the entries above `bin`
-__device__ __forceinline__ int above_bin(const uint4& x, int first, int bin) {
-    return (first > bin ? (int)x.x : 0) + (first + 1 > bin ? (int)x.y : 0) + (first + 2 > bin ? (int)x.z : 0) + (first + 3 > bin ? (int)x.w : 0);
-}
+};
 
 template <int STAGE> __global__ __launch_bounds__(kPartThreads, 4) void page_evict_hist_kernel(EvictArgs a, EvictLong s) {
     __shared__ __align__(16) uint32_t hist[kEvictBins];
-    __shared__ int sh_find[kPartThreads / LEOAM_WAVE + 3], sh_above;
+    __shared__ PartSums<1> sh_find;
     const int tid = threadIdx.x, bh = blockIdx.x / s.parts, p = blockIdx.x % s.parts;
     const EvictRow row(a, bh);
     if (STAGE == 0 && tid == 0 && p == 0) row.report(a, bh);
     if (row.none) return;
     const PartOf part(row, p);
     if (p >= part.n_parts) return;
-    const HeldKeys<kPartThreads> held(row, part.begin, part.end);
-    uint32_t* mine = s.hist + (((size_t)(STAGE & 1) * s.rows + bh) * s.parts + p) * kEvictBins;
+    const HeldKeys<kPartThreads, kPartHeld> held(row, part.begin, part.end);
+    const size_t here = ((size_t)(STAGE & 1) * s.rows + bh) * s.parts + p;
     for (int i = tid; i < kEvictBins; i += kPartThreads) hist[i] = 0;
-    if (tid == 0) sh_above = 0;
     uint32_t prefix = 0;
     int above = 0;
     if constexpr (STAGE > 0) {
         constexpr int kKnown = STAGE == 1 ? 21 : 10;
         const size_t before = (size_t)((STAGE & 1) ^ 1) * s.rows + bh;      // the last stage's
-        const uint32_t* last = s.hist + before * s.parts * kEvictBins;
         above = s.above[before * s.parts + p];
-        const uint4 own = load16(last, ((size_t)p * kEvictBins + 4 * tid) * sizeof(uint32_t));
         int need = row.keep;
         if (STAGE == 2) {
             const EvictFound f = s.found[bh];
             need = f.need;
             prefix = f.prefix;
         }
-        const int3 found = find_bin<kPartThreads>(need, sh_find, [&](int bin, uint32_t* c) { sum_parts(last, part.n_parts, bin, c); });
-        prefix |= (uint32_t)found.x << kKnown;
-        if (tid == 0 && p == 0) s.found[(size_t)(STAGE - 1) * s.rows + bh] = EvictFound{prefix, need - found.y};
-        const int more = above_bin(own, 4 * tid, found.x);
-        if (more) atomicAdd(&sh_above, more);
+        const PartBin<1> found(s.hist + before * s.parts * kEvictBins, s.coarse + before * s.parts * kCoarse, part.n_parts, need, sh_find,
+                               [&](int q, int) { return q == p; });
+        prefix |= (uint32_t)found.bin << kKnown;
+        above += found.above_of[0];
+        if (tid == 0 && p == 0) s.found[(size_t)(STAGE - 1) * s.rows + bh] = EvictFound{prefix, need - found.above};
     }
     __syncthreads();
-    count_keys<STAGE, kPartThreads>(held, prefix, hist);
+    count_keys<STAGE, kPartThreads, kPartHeld>(held, prefix, hist);
     __syncthreads();
-    *reinterpret_cast<uint4*>(mine + 4 * tid) = *reinterpret_cast<const uint4*>(hist + 4 * tid);
-    if (tid == 0) s.above[((size_t)(STAGE & 1) * s.rows + bh) * s.parts + p] = above + sh_above;
+    static_assert(kEvictBins == 4 * kPartThreads && kFine == 32, "a thread writes four bins, eight threads a coarse one");
+    const uint4 mine = *reinterpret_cast<const uint4*>(hist + 4 * tid);
+    *reinterpret_cast<uint4*>(s.hist + here * kEvictBins + 4 * tid) = mine;
+    uint32_t sum = (mine.x + mine.y) + (mine.z + mine.w);
+#pragma unroll
+    for (int d = 1; d < 8; d <<= 1) sum += __shfl_xor(sum, d, LEOAM_WAVE);
+    if ((tid & 7) == 0) s.coarse[here * kCoarse + (tid >> 3)] = sum;
+    if (tid == 0) s.above[here] = above;
 }
 
 __global__ __launch_bounds__(kPartThreads, 4) void page_evict_list_kernel(EvictArgs a, EvictLong s) {
     constexpr int WAVES = kPartThreads / LEOAM_WAVE;
-    __shared__ int sh_find[WAVES + 3], sh_above[WAVES], sh_equal[WAVES], sh_sums[4];
+    __shared__ PartSums<2> sh_find;
+    __shared__ int sh_above[WAVES], sh_equal[WAVES];
     const int tid = threadIdx.x, lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(tid / LEOAM_WAVE);
     const int bh = blockIdx.x / s.parts, p = blockIdx.x % s.parts;
     const EvictRow row(a, bh);
     if (row.none) return;
     const PartOf part(row, p);
     if (p >= part.n_parts) return;
-    const HeldKeys<kPartThreads> held(row, part.begin, part.end);
-    const uint32_t* last = s.hist + (size_t)bh * s.parts * kEvictBins;      // (stage 2's)
-    const int* state = s.above + (size_t)bh * s.parts;
-    if (tid < 4) sh_sums[tid] = 0;
+    const HeldKeys<kPartThreads, kPartHeld> held(row, part.begin, part.end);
+    // of the parts before this one, and of those below `keep`: keys above the bound and equal to it
+    const size_t first = (size_t)bh * s.parts;      // (stage 2's)
     const EvictFound before = s.found[s.rows + bh];
-    const int3 found = find_bin<kPartThreads>(before.need, sh_find, [&](int i, uint32_t* c) { sum_parts(last, part.n_parts, i, c); });
-    const uint32_t bound = before.prefix | (uint32_t)found.x;
-    const int ties = before.need - found.y;
-    // the parts' keys above the bound and equal to it: those of parts before this one, those of parts below `keep`; a wave to a part
-    for (int q = wave; q < part.n_parts; q += WAVES) {
-        if (q >= p && q >= part.n_low) continue;
-        const uint32_t* mine = last + (size_t)q * kEvictBins;
-        const int equal = (int)mine[found.x];
-        int above = lane == 0 ? state[q] : 0;
-        uint4 x[4];      // (stage 2 has 1024 bins)
-#pragma unroll
-        for (int u = 0; u < 4; ++u) x[u] = *reinterpret_cast<const uint4*>(mine + 256 * u + 4 * lane);
-#pragma unroll
-        for (int u = 0; u < 4; ++u) above += above_bin(x[u], 256 * u + 4 * lane, found.x);
-        above = __builtin_amdgcn_readlane((int)wave_incl_scan_u32((uint32_t)above), LEOAM_WAVE - 1);
-        if (lane == 0 && q < p) {
-            atomicAdd(&sh_sums[0], above);
-            atomicAdd(&sh_sums[1], equal);
-        }
-        if (lane == 0 && q < part.n_low) {
-            atomicAdd(&sh_sums[2], above);
-            atomicAdd(&sh_sums[3], equal);
-        }
+    const PartBin<2> found(s.hist + first * kEvictBins, s.coarse + first * kCoarse, part.n_parts, before.need, sh_find,
+                           [&](int q, int k) { return q < (k == 0 ? p : part.n_low); });
+    const uint32_t bound = before.prefix | (uint32_t)found.bin;
+    const int ties = before.need - found.above;
+    uint32_t above_of[2] = {0, 0};
+    for (int q = lane; q < part.n_parts; q += LEOAM_WAVE) {
+        const int x = s.above[first + q];
+        above_of[0] += q < p ? x : 0;
+        above_of[1] += q < part.n_low ? x : 0;
     }
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+        above_of[k] = __builtin_amdgcn_readlane((int)wave_incl_scan_u32(above_of[k]), LEOAM_WAVE - 1) + found.above_of[k];
     int above = 0, equal = 0;
     held.each([&](int, uint32_t k, bool in) {
         above += __popcll(__ballot(in && k > bound));
@@ -360,23 +396,28 @@ __global__ __launch_bounds__(kPartThreads, 4) void page_evict_list_kernel(EvictA
         sh_equal[wave] = equal;
     }
     __syncthreads();
-    above = sh_sums[0] + before_wave<WAVES>(sh_above, wave);
-    equal = sh_sums[1] + before_wave<WAVES>(sh_equal, wave);
-    const int kept_low = sh_sums[2] + min(sh_sums[3], ties);
+    above = above_of[0] + before_wave<WAVES>(sh_above, wave);
+    equal = found.equal_of[0] + before_wave<WAVES>(sh_equal, wave);
+    const int kept_low = above_of[1] + min(found.equal_of[1], ties);
     if (tid == 0 && p == 0) a.move_count[bh] = row.keep - kept_low;
-    list_moves<kPartThreads>(held, row.keep, bound, ties, above, equal, kept_low, a.moves + (size_t)bh * a.m_max * 2);
+    list_moves<kPartThreads, kPartHeld>(held, row.keep, bound, ties, above, equal, kept_low, a.moves + (size_t)bh * a.m_max * 2);
 }
 
+// Into how many parts rows are cut at most; 0: a row to a workgroup.  That takes a microsecond for a thousand tokens, four launches take
+// 28 whatever the length if there are few rows (16 of 20000 24 against 28, of 32000 31 / 28, of 64000 60 / 29), but more work in all
+// (128 rows of 32000 33 / 57, of 60000 61 / 74, 512 of those 142 / 221).
+constexpr int kRowHeld = 64;      // keys of a thread, at most
 static int evict_parts(const leoam_pages* s) {
-    const int capacity = s->max_pages * s->page_size;
-    return capacity <= kEvictRowMost ? 0 : capacity / kEvictPart + 2;      // (0: a row to a workgroup)
+    const int capacity = s->max_pages * s->page_size, rows = s->batch * s->n_kv_heads;
+    return capacity <= (rows < 128 ? 32 : kRowHeld) * 1024 ? 0 : capacity / kEvictPart + 2;
 }
 static size_t evict_hist_bytes(const leoam_pages* s) {
     return 2 * (size_t)s->batch * s->n_kv_heads * evict_parts(s) * kEvictBins * sizeof(uint32_t);
 }
 static size_t evict_above_bytes(const leoam_pages* s) { return 2 * (size_t)s->batch * s->n_kv_heads * evict_parts(s) * sizeof(int); }
+static size_t evict_coarse_bytes(const leoam_pages* s) { return evict_hist_bytes(s) / kFine; }
 size_t page_evict_workspace_bytes(const leoam_pages* s) {
-    return evict_hist_bytes(s) + evict_above_bytes(s) + 2 * (size_t)s->batch * s->n_kv_heads * sizeof(EvictFound);
+    return evict_hist_bytes(s) + evict_coarse_bytes(s) + evict_above_bytes(s) + 2 * (size_t)s->batch * s->n_kv_heads * sizeof(EvictFound);
 }
 
 hipError_t page_evict_dispatch(const leoam_pages* s, const float* weight, const int32_t* token_id, const int32_t* n_seen,
@@ -388,15 +429,18 @@ hipError_t page_evict_dispatch(const leoam_pages* s, const float* weight, const 
     a.n_kv_heads = s->n_kv_heads; a.capacity = s->max_pages * s->page_size;
     const int rows = s->batch * s->n_kv_heads, parts = evict_parts(s);
     if (parts == 0) {
-        if (a.capacity <= 512 * kEvictHeld) hipLaunchKernelGGL(page_evict_row_kernel<512>, dim3(rows), dim3(512), 0, stream, a);
-        else hipLaunchKernelGGL(page_evict_row_kernel<kEvictThreads>, dim3(rows), dim3(kEvictThreads), 0, stream, a);
+        if (a.capacity <= 16 * 512) hipLaunchKernelGGL((page_evict_row_kernel<512, 16>), dim3(rows), dim3(512), 0, stream, a);
+        else if (a.capacity <= 16 * 1024) hipLaunchKernelGGL((page_evict_row_kernel<1024, 16>), dim3(rows), dim3(1024), 0, stream, a);
+        else if (a.capacity <= 32 * 1024) hipLaunchKernelGGL((page_evict_row_kernel<1024, 32>), dim3(rows), dim3(1024), 0, stream, a);
+        else hipLaunchKernelGGL((page_evict_row_kernel<1024, kRowHeld>), dim3(rows), dim3(1024), 0, stream, a);
         return hipGetLastError();
     }
     if ((long long)rows * parts > 0x7fffffffll) return hipErrorInvalidValue;
     EvictLong l;
     l.hist = (uint32_t*)workspace;
-    l.above = (int*)((char*)workspace + evict_hist_bytes(s));
-    l.found = (EvictFound*)((char*)workspace + evict_hist_bytes(s) + evict_above_bytes(s));
+    l.coarse = (uint32_t*)((char*)l.hist + evict_hist_bytes(s));
+    l.above = (int*)((char*)l.coarse + evict_coarse_bytes(s));
+    l.found = (EvictFound*)((char*)l.above + evict_above_bytes(s));
     l.rows = rows; l.parts = parts;
     const dim3 grid((unsigned)(rows * parts)), block(kPartThreads);
     hipLaunchKernelGGL(page_evict_hist_kernel<0>, grid, block, 0, stream, a, l);

@@ -254,12 +254,12 @@ def test_select_lengths(L, ids):
     run_select(L, lengths, keeps, first=[0, 1, 4, 4, 4, 4, 1, 4, 4, 4, 4, 4, 4, 4], recent=10, ids=ids)
 
 
-@pytest.mark.parametrize("n", [16383, 16384, 16385, 20000, 50000, 131072])
+@pytest.mark.parametrize("n", [8191, 8193, 16383, 16384, 16385, 20000, 32703, 32769, 50000, 131072])
 def test_select_long_rows(L, n):
     run_select(L, [n, n - 1, n // 2], [n // 3, n - 2, n // 2 - 1], hkv=3, first=[64, 0, 1], recent=1000, seed=n)
 
 
-@pytest.mark.parametrize("n", [300, 20000])
+@pytest.mark.parametrize("n", [300, 20000, 40000])
 def test_select_ties_and_special_weights(L, n):
     def make(w, ids):
         w[0] = 1.0                                                      # all the same: by place
@@ -273,6 +273,12 @@ def test_select_ties_and_special_weights(L, n):
     for part in (2, 3, 10):
         run_select(L, [n] * 7, [n // part] * 7, make=make, recent=7, first=[3] * 7)
         run_select(L, [n] * 7, [n - n // part] * 7, make=make, ids=False)
+
+
+@pytest.mark.parametrize("n", [40000, 65400, 70000])
+def test_select_many_long_rows(L, n):
+    lengths = [n, 40, n - 1, 33000] + 28 * [700]
+    run_select(L, lengths, [n // 2, 39, n - 300, 1] + 28 * [5], hkv=4, first=[4] * 3 + [0] * 29, recent=100, seed=n)
 
 
 def test_select_more_protected_than_stay(L):
@@ -292,7 +298,7 @@ def test_select_lists_that_are_too_short_and_lengths_that_do_not_fit(L):
 
 
 def test_select_replays_from_a_graph(L):
-    call, moves, count = run_select(L, [3000, 40000], [1000, 39000], recent=20)
+    call, moves, count = run_select(L, [3000, 40000], [1000, 39000], recent=20)      # (four launches)
     want = moves.clone()
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):
