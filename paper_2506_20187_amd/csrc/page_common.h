@@ -137,4 +137,15 @@ template <int KIND, int N> __device__ __forceinline__ void then() { __builtin_am
 template <typename T> constexpr int kKeyStride = LEOAM_D * T::kBytes + 16;
 template <typename T> constexpr int kValueStride = LEOAM_D * T::kBytes + (T::kTag == LEOAM_F32 ? 32 : 64);
 
+// the smallest power of two s with amax <= 448 s, as a float; its exponent stays where s * code is a number of T
+template <typename T> __device__ __forceinline__ float scale_of(float amax) {
+    if (!(amax > 0.f)) return 0.f;
+    constexpr int kLow = T::kTag == LEOAM_F16 ? -15 : -100, kHigh = T::kTag == LEOAM_F16 ? 7 : 118;
+    const uint32_t u = float_to_bits(amax);
+    // amax = 1.f * 2^e, 448 = 1.75 * 2^8   (a subnormal amax is below the smallest exponent anyway)
+    int e = (int)(u >> 23) - 127 - 8 + ((u & 0x7fffffu) > 0x600000u ? 1 : 0);
+    e = min(max(e, kLow), kHigh);
+    return bits_to_float((uint32_t)(e + 127) << 23);
+}
+
 }  // namespace leoam

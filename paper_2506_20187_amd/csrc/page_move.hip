@@ -8,6 +8,8 @@
 // first looks up all rows that come (a lane each), then has as many of them on their way as its registers hold, keys and values.
 // Sources lie behind the kept length and are not written, but in the page that the kept length cuts: 8 bits leave that page to
 // a second launch, when nobody reads it any more.
+// 40 sequences of 4.2K in bf16 (265 MB) 64 us, 4.1 TB/s; six of 60K in 8 bits (295 MB) 102 us: there the largest magnitudes, codes
+// to numbers for the abstracts and, where scales differ, new codes keep the vector units busy.
 #include "page_common.h"
 
 namespace leoam {
@@ -29,28 +31,9 @@ struct MoveArgs {
 constexpr int kMoveThreads = 256, kMoveWaves = kMoveThreads / LEOAM_WAVE;
 constexpr int kMostRows = 256;      // of a page
 
-// eight channels (fp32: four) of a row as floats, of the stored type
-template <typename T, typename S> __device__ __forceinline__ void stored_values(const uint4& w, float scale, float* y) {
-    if constexpr (std::is_same<S, E4M3>::value) {
-        unpack_e4m3(w.x, y);
-        unpack_e4m3(w.y, y + 4);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] *= scale;
-    } else {
-        unpack<T>(w, y);
-    }
-}
-
-// The smallest power of two s with amax <= 448 s, its exponent where s * code is a number of T (as an append has it).
-template <typename T> __device__ __forceinline__ float move_scale_of(float amax) {
-    if (!(amax > 0.f)) return 0.f;
-    constexpr int kLow = T::kTag == LEOAM_F16 ? -15 : -100, kHigh = T::kTag == LEOAM_F16 ? 7 : 118;
-    const uint32_t u = float_to_bits(amax);
-    const int e = min(max((int)(u >> 23) - 127 - 8 + ((u & 0x7fffffu) > 0x600000u ? 1 : 0), kLow), kHigh);
-    return bits_to_float((uint32_t)(e + 127) << 23);
-}
-
-template <typename T, typename S> __global__ __launch_bounds__(kMoveThreads, 3) void page_move_kernel(MoveArgs a) {
+// (Waves for each SIMD, and loads of a wave's that are on their way together in 8 bits: 12000 pairs of six sequences behind 48000, 8
+// heads: 3 and 16 182 us, 3 and 8 164, 4 and 8 161, 4 and 4 154, 6 and 4 153 but in 16 bits 40 x 4.2K 73 instead of 64.)
+template <typename T, typename S> __global__ __launch_bounds__(kMoveThreads, 4) void page_move_kernel(MoveArgs a) {
     constexpr bool k8 = std::is_same<S, E4M3>::value;
     constexpr int EPL = T::kEpl, LPR = LEOAM_D / EPL, RPL = LEOAM_WAVE / LPR;      // lanes to a row, rows to a load
     constexpr int ROWB = LEOAM_D * S::kBytes, BATCH = 8;                             // loads that are on their way together
@@ -163,13 +146,16 @@ template <typename T, typename S> __global__ __launch_bounds__(kMoveThreads, 3) 
         } else {
             // The scale comes before the codes: rows that come are read for their largest magnitude, and again if they are more than
             // the registers hold (from the cache).
-            constexpr int HELD = 2 * BATCH, kHeld = RPL * HELD;
+            constexpr int HELD = 4, kHeld = RPL * HELD;
             uint2 held[2][HELD];
             auto row_of = [&](int j) { return (int)rows[min(j, n_rows - 1)]; };
             auto fetch = [&](auto tensor, int j0) __attribute__((always_inline)) {
                 constexpr int W = decltype(tensor)::value;
 #pragma unroll
-                for (int u = 0; u < HELD; ++u) held[W][u] = *reinterpret_cast<const uint2*>(pools[W] + from[row_of(j0 + u * RPL + rg)]);
+                for (int u = 0; u < HELD; ++u) {
+                    if (j0 + u * RPL >= n_rows) break;
+                    held[W][u] = *reinterpret_cast<const uint2*>(pools[W] + from[row_of(j0 + u * RPL + rg)]);
+                }
             };
             auto encode_rows = [&](auto tensor) __attribute__((always_inline)) {
                 constexpr int W = decltype(tensor)::value;
@@ -179,6 +165,7 @@ template <typename T, typename S> __global__ __launch_bounds__(kMoveThreads, 3) 
                     if (j0 > 0) fetch(tensor, j0);
 #pragma unroll
                     for (int u = 0; u < HELD; ++u) {      // (a code's magnitude, NaN left out by the maximum, and 8 bits have no infinity)
+                        if (j0 + u * RPL >= n_rows) break;
                         float y[8];
                         unpack_e4m3(held[W][u].x, y);
                         unpack_e4m3(held[W][u].y, y + 4);
@@ -188,20 +175,24 @@ template <typename T, typename S> __global__ __launch_bounds__(kMoveThreads, 3) 
                         top = fmaxf(top, m * from_scale[W][row_of(j0 + u * RPL + rg)]);
                     }
                 }
-                const float now = fmaxf(old[W], move_scale_of<T>(wave_extreme_f<true>(top))), inv = now > 0.f ? 1.f / now : 0.f;
+                const float now = fmaxf(old[W], scale_of<T>(wave_extreme_f<true>(top))), inv = now > 0.f ? 1.f / now : 0.f;
                 const bool grows = now > old[W];
                 if (lane == 0 && grows) scales[W][row_of_page] = now;
-                // (what is stored is at most 448 of the new scale, and the quotient of two scales a power of two)
-                auto put = [&](int r, const uint2& code, float f, bool store) __attribute__((always_inline)) {
+                // (what is stored is at most 448 of the new scale, and the quotient of two scales a power of two: mostly 1, and codes
+                // stay what they are)
+                auto put = [&](int r, uint2 c, float f, bool store) __attribute__((always_inline)) {
                     float y[8];
-                    unpack_e4m3(code.x, y);
-                    unpack_e4m3(code.y, y + 4);
+                    if (__ballot(f != 1.f)) {
+                        unpack_e4m3(c.x, y);
+                        unpack_e4m3(c.y, y + 4);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) y[e] *= f;
-                    const uint2 c = make_uint2(pack_e4m3(y), pack_e4m3(y + 4));
+                        for (int e = 0; e < 8; ++e) y[e] *= f;
+                        c = make_uint2(pack_e4m3(y), pack_e4m3(y + 4));
+                    }
                     if (store) *reinterpret_cast<uint2*>(page[W] + (size_t)r * ROWB) = c;
-                    if (keys && r < valid) {
-                        stored_values<T, S>(make_uint4(c.x, c.y, 0, 0), now, y);
+                    if (keys && r < valid) {      // (of codes: the scale comes at the end)
+                        unpack_e4m3(c.x, y);
+                        unpack_e4m3(c.y, y + 4);
                         extremes(y);
                     }
                 };
@@ -210,7 +201,8 @@ template <typename T, typename S> __global__ __launch_bounds__(kMoveThreads, 3) 
 #pragma unroll
                     for (int u = 0; u < HELD; ++u) {
                         const int j = j0 + u * RPL + rg, r = row_of(j);
-                        put(r, held[W][u], from_scale[W][r] * inv, j < n_rows);
+                        if (j0 + u * RPL >= n_rows) break;
+                        put(r, held[W][u], fminf(from_scale[W][r] * inv, 0x1p30f), j < n_rows);      // (more: a row of zeros)
                     }
                 }
                 // the rows that stay (those behind the kept length, too, that others may have been read from)
@@ -223,7 +215,15 @@ template <typename T, typename S> __global__ __launch_bounds__(kMoveThreads, 3) 
 #pragma unroll
                     for (int u = 0; u < HELD; ++u) {
                         const int r = r0 + u * RPL + rg;
+                        if (r0 + u * RPL >= count) break;
                         if (r < count && from[r] < 0) put(r, held[W][u], f, grows);
+                    }
+                }
+                if (keys) {
+#pragma unroll
+                    for (int e = 0; e < EPL; ++e) {      // (infinite: the lane saw no number)
+                        mx[e] = mx[e] == -INFINITY ? mx[e] : mx[e] * now;
+                        mn[e] = mn[e] == INFINITY ? mn[e] : mn[e] * now;
                     }
                 }
             };

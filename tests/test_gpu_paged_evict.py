@@ -447,6 +447,20 @@ def test_every_row_moves_or_none_does(L, dtype, q8, page):
     cache.run(keeps, lists)
 
 
+def test_move_zeros_from_a_page_of_far_larger_numbers(L):
+    """The quotient of the scales is beyond 32 bits, the row's codes are zero: so are they afterwards."""
+    pages = L.make_pages(1, 1, 1, 128, 2, 16, 2, BF16, kv_dtype=L.E4M3)
+    k, v = (torch.randint(0, 0x7e, (2, 1, 16, 128), dtype=torch.uint8, device="cuda") for _ in range(2))
+    k[1, 0, 3], v[1, 0, 3] = 0, 0x80      # (-0, too)
+    ks, vs = (torch.tensor([[2.0 ** -90], [2.0 ** 110]], device="cuda") for _ in range(2))
+    want = [x.clone() for x in (k, v, ks, vs)]
+    want[0][0, 0, 5], want[1][0, 0, 5] = 0, 0x80
+    kf, vf = k.view(torch.float8_e4m3fn), v.view(torch.float8_e4m3fn)
+    L.kv_page_move(pages, i32([[[[5, 19]]]]), i32([[1]]), i32([32]), i32([16]), i32([[0, 1]]), kf, vf, ks, vs, None, None, None, None, None)
+    for got, expected in zip((k, v, ks, vs), want):
+        assert torch.equal(got, expected)
+
+
 @pytest.mark.parametrize("dtype", [F16, BF16])
 def test_scales_that_rise_from_zero_and_by_far(L, dtype):
     cache = Moving(L, dtype, True, [64, 64], 2, 16, seed=2)
