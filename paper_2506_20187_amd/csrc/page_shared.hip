@@ -13,6 +13,10 @@
 // through LDS, with 32x32 products as in page_attention_prefill: a key row from the caches is 16 bytes of 16 rows a load, which
 // the first-level cache serves at a quarter of its rate, four times over.  Weights go in as two fp16 or three bf16 numbers that add up to
 // them (22 or 24 bits), so the float output keeps its precision, at twice the cost of rounded ones beyond 64 columns.
+//
+// 48 sequences behind 32768 tokens, 32 of 8 heads, bf16: 89 us (221 MB and 26 GFLOP; each by itself, as page_attention_decode has it,
+// would read 6.6 GB); 70 of 64 heads in nine groups behind 9000, 8 bits: 85; four of 8 heads behind 1024, fp32: 15, launches and
+// dependent round trips.
 #include <cfloat>
 
 #include "page_common.h"
@@ -24,10 +28,12 @@ namespace leoam {
 constexpr int kWhole = -1, kFinal = -2;
 struct SharedRow { int32_t own_count, own_slot, pre_count, pre_slot, pre_col; };
 
-constexpr int kSharedTile = 128;          // unit of the partition, tokens
+constexpr int kSharedTile = 64;           // unit of the partition, tokens
 constexpr int kSharedColumns = 128;       // most columns of a unit
 constexpr int kWaveColumns = 32;
 constexpr int kGroupsInLds = 512;
+
+constexpr int kSharedStart = 6, kMostTileCost = 6;
 
 struct PageSharedArgs {
     const char *q, *k_pages, *v_pages;
@@ -67,11 +73,9 @@ template <typename T, typename S> struct SharedStep {
 };
 
 // What a tile costs a workgroup whose waves go `ways` over the columns, and what a unit's beginning does: shares are measured in that.
-// (us for 48 sequences behind 32K in bf16, 70 in nine groups in 8 bits: 91, 87 with 5 for four ways; 89, 86 with 4; 98, 97 with all
-// half as much.)
-__device__ __forceinline__ int tile_cost(int ways) { return ways == 1 ? 2 : ways == 2 ? 3 : 4; }
-constexpr int kSharedStart = 4;
-constexpr int kMostTileCost = 4;
+// (us for 48 sequences behind 32K in bf16, 70 in nine groups in 8 bits, 128 behind 8000, 19 of 16 heads in four groups in fp32: 91, 89, 68,
+// 24; with beginnings of 4 99, 100, 72, 24, of 8 92, 91, 70, 24; two and four ways at 3 and 4 95, 89, 73, 26; tiles of 128 93, 88, 77, 34.)
+__device__ __forceinline__ int tile_cost(int ways) { return ways == 1 ? 2 : ways == 2 ? 4 : kMostTileCost; }
 
 __device__ __forceinline__ int shared_tiles(int tokens) { return max(1, (tokens + kSharedTile - 1) / kSharedTile); }
 // of the waves, over a unit's columns
@@ -96,7 +100,9 @@ struct SharedEntry {
     // (fewer than 2^23 tiles)
     __device__ __forceinline__ int length(int unit) const { return kSharedStart + tiles * cost(unit); }
     __device__ __forceinline__ int cost(int unit) const { return unit < full ? cost_full : cost_rest; }
-    __device__ __forceinline__ long long total() const { return (long long)full * length(0) + (long long)rest * (kSharedStart + tiles * cost_rest); }
+    __device__ __forceinline__ long long total() const {
+        return (long long)full * length(0) + (long long)rest * (kSharedStart + tiles * cost_rest);
+    }
 };
 
 template <typename T, typename S>
@@ -505,7 +511,8 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
         char *sh_k = smem, *sh_v = smem + 2 * KEYS * KSTR;
         const int lane = here(lane_id()), tid = here(threadIdx.x), half = lane >> 5, l32 = lane & 31;
         const int32_t* table = a.page_table + (size_t)b_table * a.max_pages;
-        const uint32_t head_bytes = (uint32_t)ROWB << a.page_shift, page_bytes = head_bytes * (uint32_t)hkv, in_page = (1u << a.page_shift) - 1;
+        const uint32_t head_bytes = (uint32_t)ROWB << a.page_shift, page_bytes = head_bytes * (uint32_t)hkv;
+        const uint32_t in_page = (1u << a.page_shift) - 1;
         const char *kh = a.k_pages + (size_t)h * head_bytes, *vh = a.v_pages + (size_t)h * head_bytes;
         const int n_tiles = (t_end - t_begin + KEYS - 1) / KEYS;
         // lane l looks after 16-key group l % GROUPS of a tile; groups behind the end have no page
@@ -537,7 +544,8 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
                 const int r = i * ROWS_PER_LOAD + tid / PIECES;
                 const int g = i * ROWS_PER_LOAD / 16 + (kPerLoad > 1 ? wave * (LEOAM_WAVE / PIECES) / 16 : 0);
                 const uint32_t at = ((uint32_t)(t_begin + j * KEYS + r) & in_page) * ROWB + 16 * (tid % PIECES);
-                const uint64_t base = (uint64_t)(uint32_t)__builtin_amdgcn_readlane(hi, g) << 32 | (uint32_t)__builtin_amdgcn_readlane(lo, g);
+                const uint64_t base =
+                    (uint64_t)(uint32_t)__builtin_amdgcn_readlane(hi, g) << 32 | (uint32_t)__builtin_amdgcn_readlane(lo, g);
                 t.k[i] = load16(kh + base, at);
                 t.v[i] = load16(vh + base, at);
                 if (k8) {
@@ -727,14 +735,17 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
         const int tiles = uniform(x.tiles), cost = uniform(x.cost(unit));
         const int take = uniform((int)min((long long)(kSharedStart + tiles * cost - off), end - pos));
         // tiles that begin in the share
-        auto tiles_before = [&](int at) { return at <= kSharedStart ? 0 : (int)((uint32_t)(at - kSharedStart + cost - 1) / (uint32_t)cost); };
+        auto tiles_before = [&](int at) {
+            return at <= kSharedStart ? 0 : (int)((uint32_t)(at - kSharedStart + cost - 1) / (uint32_t)cost);
+        };
         const int tile0 = tiles_before(off), tile1 = min(tiles, tiles_before(off + take));
         if (tile0 < tile1) {
             const int h = unit % hkv;
             const bool prefix = entry < a.n_groups, whole = tile1 - tile0 == tiles;
             const int slot = 2 * (int)blockIdx.x + (first_piece ? 0 : 1);      // opens the share, or closes it
             // pieces of the unit, and where the first lies, if it begins here
-            const int count = whole ? kWhole : tile0 ? 1 : (int)quotient(pos - first - off + kSharedStart + (long long)(tiles - 1) * cost, share) + 1;
+            const long long last_at = pos - first - off + kSharedStart + (long long)(tiles - 1) * cost;
+            const int count = whole ? kWhole : tile0 ? 1 : (int)quotient(last_at, share) + 1;
             int n_cols, b0, tokens, before = 0, b_table;
             bool work = true;
             if (prefix) {
@@ -745,7 +756,8 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
                 b0 = uniform(b0);
                 n_cols = uniform(n_cols);
                 // the first member that has the whole prefix (at most 128 members, two a lane)
-                const int len0 = lane < members ? length_of(b0 + lane) : -1, len1 = lane + LEOAM_WAVE < members ? length_of(b0 + lane + LEOAM_WAVE) : -1;
+                const int len0 = lane < members ? length_of(b0 + lane) : -1;
+                const int len1 = lane + LEOAM_WAVE < members ? length_of(b0 + lane + LEOAM_WAVE) : -1;
                 const uint64_t has0 = __ballot(len0 >= tokens), has1 = __ballot(len1 >= tokens);
                 b_table = has0 ? b0 + __builtin_ctzll(has0) : has1 ? b0 + LEOAM_WAVE + __builtin_ctzll(has1) : -1;
                 work = b_table >= 0;
@@ -818,10 +830,11 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
 // A head's pieces: those of its group's unit, then its own.  32 threads take four channels each of eight pieces at a time, all on their
 // way together; four such groups share a head's pieces, in order.
 constexpr int kMergeParts = 4, kMergeHeads = 2;
-__global__ __launch_bounds__(kMergeHeads * kMergeParts * 32) void page_shared_merge_kernel(const SharedRow* __restrict__ rows, const float* __restrict__ acc,
-                                                                                          const float* __restrict__ ml, int group_shift, int n_heads,
-                                                                                          int sharers, int bias, float* __restrict__ out,
-                                                                                          float* __restrict__ lse) {
+constexpr int kMergeThreads = kMergeHeads * kMergeParts * 32;
+__global__ __launch_bounds__(kMergeThreads) void page_shared_merge_kernel(const SharedRow* __restrict__ rows, const float* __restrict__ acc,
+                                                                          const float* __restrict__ ml, int group_shift, int n_heads,
+                                                                          int sharers, int bias, float* __restrict__ out,
+                                                                          float* __restrict__ lse) {
     constexpr int kBatch = 8;
     __shared__ float sh_m[kMergeHeads][kMergeParts], sh_l[kMergeHeads][kMergeParts];
     __shared__ __align__(16) float sh_o[kMergeHeads][kMergeParts][LEOAM_D];
@@ -831,7 +844,8 @@ __global__ __launch_bounds__(kMergeHeads * kMergeParts * 32) void page_shared_me
     const bool done = r.own_count == kFinal;
     // (counts and slots that no kernel wrote - lists of groups that overlap - stay within the workspace)
     const int g = j & ((1 << group_shift) - 1), last = 2 * sharers - 1;
-    const int n_pre = r.pre_count == kWhole ? 1 : min(max(r.pre_count, 0), sharers), n_own = r.own_count == kWhole ? 1 : min(max(r.own_count, 0), sharers);
+    const int n_pre = r.pre_count == kWhole ? 1 : min(max(r.pre_count, 0), sharers);
+    const int n_own = r.own_count == kWhole ? 1 : min(max(r.own_count, 0), sharers);
     const int n = done ? 0 : n_pre + n_own;
     auto state = [&](int i) {
         const bool own = i >= n_pre;
@@ -906,8 +920,8 @@ template <typename T, typename S> static hipError_t launch_shared(const PageShar
     hipLaunchKernelGGL((page_shared_kernel<T, S>), dim3(a.sharers), dim3(kAttThreads), 0, stream, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(page_shared_merge_kernel, dim3((a.n_heads + kMergeHeads - 1) / kMergeHeads), dim3(kMergeHeads * kMergeParts * 32), 0, stream, a.rows, a.acc, a.ml,
-                       a.group_shift, a.n_heads, a.sharers, shared_bias<T>(), a.out, a.lse);
+    hipLaunchKernelGGL(page_shared_merge_kernel, dim3((a.n_heads + kMergeHeads - 1) / kMergeHeads), dim3(kMergeThreads), 0, stream, a.rows,
+                       a.acc, a.ml, a.group_shift, a.n_heads, a.sharers, shared_bias<T>(), a.out, a.lse);
     return hipGetLastError();
 }
 
