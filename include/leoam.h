@@ -613,7 +613,7 @@ int page_weight_add(const leoam_pages* pages, const void* q, int32_t n_new, cons
  *   moves       [batch, n_kv_heads, m_max, 2] int32: (place that becomes free, place of the token that moves there); entries from
  *               move_count[b,h] on are left as they are
  *   move_count  [batch, n_kv_heads] int32
- *   new_len     [batch] int32: keep_len[b], or seq_len[b] if the sequence is not longer than that
+ *   new_len     [batch] int32: keep_len[b], or seq_len[b] if the sequence is not longer than that; an array of its own
  *   token_id, n_seen  (both or neither) as page_weight_add keeps them: a token is recent if its number is n_seen[b] - n_recent or
  *               more.  NULL: places tell (nothing was ever moved).
  *   n_first     [batch] int32, nullable (0)
@@ -621,7 +621,7 @@ int page_weight_add(const leoam_pages* pages, const void* q, int32_t n_new, cons
  *               min(keep_len[b], seq_len[b] - keep_len[b]) > m_max, the most rows that may move.
  * Attention does not depend on the order in which a cache holds its tokens, and keys carry their rotation, so nothing else moves.
  * Places of pages that other sequences list too must be protected (n_first).  Workspace: leoam_page_evict_workspace_bytes(), 16-byte
- * aligned, contents irrelevant.
+ * aligned, contents irrelevant.  Calls that share a workspace must not overlap.
  */
 int page_evict_select(const leoam_pages* pages, const float* weight, const int32_t* token_id, const int32_t* n_seen,
                       const int32_t* seq_len, const int32_t* keep_len, const int32_t* n_first, int32_t n_recent, int32_t* moves,

@@ -615,7 +615,8 @@ int page_evict_select(const leoam_pages* pages, const float* weight, const int32
     if (rc) return rc;
     if (n_recent < 0 || m_max < 1) return LEOAM_E_INVALID_ARG;
     if (!weight || !seq_len || !keep_len || !moves || !move_count || !new_len || !token_id != !n_seen) return LEOAM_E_INVALID_ARG;
-    if (((uintptr_t)moves & 7u)) return LEOAM_E_INVALID_ARG;
+    // (other workgroups still read the lengths when new_len is written)
+    if (((uintptr_t)moves & 7u) || new_len == seq_len || new_len == keep_len) return LEOAM_E_INVALID_ARG;
     if (!workspace || workspace_bytes < page_evict_workspace_bytes(pages) || ((uintptr_t)workspace & 15u)) return LEOAM_E_WORKSPACE;
     return from_hip(page_evict_dispatch(pages, weight, token_id, n_seen, seq_len, keep_len, n_first, n_recent, moves, m_max, move_count,
                                         new_len, status, workspace, (hipStream_t)stream));

@@ -96,7 +96,8 @@ template <int EPL, bool kAt> struct Turn {
                 of_position(position_of(a, x, row), k0, k1, t0, t1);
 #pragma unroll
                 for (int e = 0; e < N; ++e) {
-                    const bool first = (axes.packed >> 4 * e & 15u) == (uint32_t)x, second = (axes.packed >> 4 * (e + N) & 15u) == (uint32_t)x;
+                    const bool first = (axes.packed >> 4 * e & 15u) == (uint32_t)x;
+                    const bool second = (axes.packed >> 4 * (e + N) & 15u) == (uint32_t)x;
                     c0[e] = first ? k0[e] : c0[e];
                     s0[e] = first ? t0[e] : s0[e];
                     c1[e] = second ? k1[e] : c1[e];
@@ -390,7 +391,8 @@ __device__ __forceinline__ char* abstract_row(const AppendArgs& a, int b, int p,
 // had rows for them - in the abstract and the boundaries.  One workgroup, since it alone reads and sets n_chunks; once for a
 // sequence and its prefix, so it need not be fast: a wave takes a (page, kv head) at a time (4096 tokens of 8 heads in bf16, pages of 64:
 // 0.3 ms in a prompt's call, 0.85 in a single token's; 64K 5 ms).
-template <typename T, bool kStore8, int THREADS, bool kAt> __device__ __forceinline__ void report(const AppendArgs& a, int b, float* sh_max) {
+template <typename T, bool kStore8, int THREADS, bool kAt>
+__device__ __forceinline__ void report(const AppendArgs& a, int b, float* sh_max) {
     constexpr int EPL = T::kEpl, LPR = Row<T>::kLanesPerRow, ROWB = Row<T>::kRowBytes, STOREB = kStore8 ? LEOAM_D : ROWB;
     const int tid = threadIdx.x, ps = a.page_size, hkv = a.n_kv_heads;
     const int32_t* table = a.page_table + (size_t)b * a.max_pages;
@@ -441,6 +443,8 @@ template <typename T, bool kStore8, int THREADS, bool kAt> __device__ __forceinl
 //     against 134 with the former's shape (the queries at a quarter of the occupancy).
 // Workgroups of four heads, which would load the angles of a token once for them, were slower (144 against 93 us for the
 // keys and values of the former, 78 against 58 for the latter): a page then takes longer than there are pages to overlap.
+// Positions of the caller's: three prompts of 4097 of 5001 tokens, 32 / 8 heads, fp16 (285 MB), waves for each SIMD 4, 5, 6, 7: three axes
+// in sections 94, 84, 83, 79 us, by turns 114, 105, 111, 116, one axis 82, 74, 73, 73 (63 without positions).
 template <typename T, bool kStore8, int THREADS, int PASSES, bool kAt>
 __global__ __launch_bounds__(THREADS, kAt && !kStore8 ? 5 : 1) void page_append_prompt_kernel(AppendArgs a) {
     constexpr int EPL = T::kEpl, LPR = Row<T>::kLanesPerRow, RPP = THREADS / LPR, WAVES = THREADS / LEOAM_WAVE;
@@ -533,7 +537,8 @@ __global__ __launch_bounds__(THREADS, kAt && !kStore8 ? 5 : 1) void page_append_
 // One token for each sequence: a wave to a (sequence, kv head), lanes of the first row's width hold the key and the value; further
 // waves report (in the first of these, before its own work, that took 0.25 us longer) and take the queries.
 template <typename T, bool kStore8, bool kAt> __global__ __launch_bounds__(LEOAM_WAVE) void page_append_token_kernel(AppendArgs a) {
-    constexpr int EPL = T::kEpl, LPR = Row<T>::kLanesPerRow, ROWB = Row<T>::kRowBytes, STOREB = kStore8 ? LEOAM_D : ROWB, THREADS = LEOAM_WAVE;
+    constexpr int EPL = T::kEpl, LPR = Row<T>::kLanesPerRow, ROWB = Row<T>::kRowBytes, STOREB = kStore8 ? LEOAM_D : ROWB;
+    constexpr int THREADS = LEOAM_WAVE;
     const int hkv = a.n_kv_heads, ps = a.page_size, tid = threadIdx.x, col = (tid % LPR) * EPL;
     if ((int)blockIdx.x < a.batch) {
         report<T, kStore8, THREADS, kAt>(a, blockIdx.x, nullptr);
@@ -611,7 +616,8 @@ template <typename T, bool kStore8, int PASSES, bool kAt> static hipError_t laun
     const long long q_units = a.q ? (long long)a.n_new * ((a.n_q_heads + per - 1) / per) : 0, kv_units = (long long)a.n_slots * a.n_kv_heads;
     const long long units = a.batch + (kStore8 ? 2 * kv_units : kv_units + q_units);
     if (units > 0x7fffffffll || q_units > 0x7fffffffll) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((page_append_prompt_kernel<T, kStore8, kPromptThreads, PASSES, kAt>), dim3((unsigned)units), dim3(kPromptThreads), 0, stream, a);
+    hipLaunchKernelGGL((page_append_prompt_kernel<T, kStore8, kPromptThreads, PASSES, kAt>), dim3((unsigned)units), dim3(kPromptThreads), 0,
+                       stream, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || !kStore8 || q_units == 0) return e;
     hipLaunchKernelGGL((page_append_queries_kernel<T, kPromptThreads, kAt>), dim3((unsigned)q_units), dim3(kPromptThreads), 0, stream, a);

@@ -403,8 +403,8 @@ template <typename T, typename S, int G> static hipError_t launch_weight(PageWei
     a.total = (int)total;
     if (!many) {
         const long long groups = (total + kAttWaves - 1) / kAttWaves;
-        hipLaunchKernelGGL((page_weight_few_kernel<T, S, G>), dim3((unsigned)(groups < kFewGroups ? groups : kFewGroups)), dim3(kAttThreads), 0,
-                           stream, a);
+        const dim3 grid((unsigned)(groups < kFewGroups ? groups : kFewGroups));
+        hipLaunchKernelGGL((page_weight_few_kernel<T, S, G>), grid, dim3(kAttThreads), 0, stream, a);
         return hipGetLastError();
     }
     const dim3 grid((unsigned)(total < kManyGroups ? total : kManyGroups));

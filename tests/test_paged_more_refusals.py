@@ -6,7 +6,7 @@ import torch
 
 from tests.test_paged_refusals import INVALID, L, ODD, OK, P, SHAPES, UNSUPPORTED, WORKSPACE, pages  # noqa: F401
 
-MISALIGNED4 = ctypes.c_void_p(4096 + 4)
+MISALIGNED4, P2 = ctypes.c_void_p(4096 + 4), ctypes.c_void_p(8192)
 
 
 def ref(s):
@@ -37,7 +37,7 @@ def weigh(L, s, **kw):
 
 
 def select(L, s, **kw):
-    a = dict(weight=P, ids=P, seen=P, len=P, keep=P, first=None, recent=0, moves=P, m_max=4, count=P, new=P, status=None, ws=P, nbytes=1 << 40)
+    a = dict(weight=P, ids=P, seen=P, len=P, keep=P, first=None, recent=0, moves=P, m_max=4, count=P, new=P2, status=None, ws=P, nbytes=1 << 40)
     a.update(kw)
     return L.binding._lib.page_evict_select(ref(s), a["weight"], a["ids"], a["seen"], a["len"], a["keep"], a["first"], a["recent"], a["moves"],
                                             a["m_max"], a["count"], a["new"], a["status"], a["ws"], a["nbytes"], None)
@@ -103,6 +103,7 @@ def test_select(L):
     for name in ("weight", "len", "keep", "moves", "count", "new", "ids", "seen"):
         assert select(L, s, **{name: None}) == INVALID, name
     assert select(L, s, recent=-1) == INVALID and select(L, s, m_max=0) == INVALID and select(L, s, moves=MISALIGNED4) == INVALID
+    assert select(L, s, new=P) == INVALID and select(L, s, new=P, keep=P2) == INVALID and select(L, s, new=P, len=P2) == INVALID
     assert select(L, s, ws=None) == WORKSPACE and select(L, s, ws=ODD) == WORKSPACE
     assert select(L, s, nbytes=L.leoam_page_evict_workspace_bytes(s) - 1) == WORKSPACE
 
