@@ -8,9 +8,10 @@
 // way.  They come as whole rows, which the caches serve at four times the rate of an operand's 16 bytes of 16 rows, and become
 // operands in LDS.  Sixteen tokens of sequences to 33001 (617 MB): 128 us, 4.8 TB/s; with operands straight from the loads and no
 // equal shares 187; with weights written for 32 keys at a time 134.
-// Many rows: bound by the exponentials and the instructions around them.  The waves of a workgroup share 64 keys (fp32: 32) and go
-// through the blocks of columns in turn; their sums are added in order at the end.  Queries, too, come as whole rows.  A prompt of
-// 4096 with 32 heads: 115 us (268 M exponentials, 69 GFLOP); with operands straight from the loads 191.
+// Many rows: bound by the exponentials and the instructions around them.  The waves of a workgroup share 64 keys (fp32: 32; half as
+// many where keys are few) and go through the blocks of columns in turn; their sums are added in order at the end.  Queries, too,
+// come as whole rows.  A prompt of 4096 with 32 heads: 114 us (268 M exponentials, 69 GFLOP); with operands straight from the
+// loads 191.
 #include "page_common.h"
 
 namespace leoam {
@@ -30,8 +31,9 @@ struct PageWeightArgs {
     int total;      // (block of keys, sequence, kv head) triples of a full table
 };
 
-// tiles of 16 keys that a wave has in registers
-template <typename T, bool kSplitRows> constexpr int kWeightTiles = (T::kTag == LEOAM_F32 ? 1 : 2) * (kSplitRows ? 2 : 1);
+// tiles of 16 keys that a wave has in registers: few rows; many rows
+template <typename T> constexpr int kFewTiles = T::kTag == LEOAM_F32 ? 1 : 2;
+template <typename T> constexpr int kManyTiles = T::kTag == LEOAM_F32 ? 2 : 4;
 
 // A stretch of keys: (sequence, kv head), its first key, the sequence's length, its rows of the call and the place of the first
 // one's token.
@@ -45,9 +47,10 @@ template <typename T> struct WeightColumns {
     int pos;         // the row's place, -1: no column, or a row that attended to nothing
 };
 
-template <typename T, typename S, int G, bool kSplitRows> struct Weighing {
+// TILES: of 16 keys, that a wave has in registers
+template <typename T, typename S, int G, bool kSplitRows, int TILES> struct Weighing {
     static constexpr bool k8 = std::is_same<S, E4M3>::value, k32 = T::kTag == LEOAM_F32;
-    static constexpr int ROWB = LEOAM_D * S::kBytes, QROWB = Row<T>::kRowBytes, NT = kWeightTiles<T, kSplitRows>, KEYS = 16 * NT;
+    static constexpr int ROWB = LEOAM_D * S::kBytes, QROWB = Row<T>::kRowBytes, NT = TILES, KEYS = 16 * NT;
     static constexpr int NQ = WeightColumns<T>::NQ, NK = k32 ? 8 : k8 ? 2 : 4;
     // Tile j, token l16; a token that does not count re-reads the last one that does.  (Few rows: as they lie in the page, a row by
     // kPieces neighbouring lanes.)
@@ -195,7 +198,7 @@ template <typename T, typename S, int G, bool kSplitRows> struct Weighing {
             }
         }
     }
-    // The columns' sums of TILES tiles: lane l16 keeps that of register l16 % 4 of tile l16 / 4, token `slot` of the stretch.
+    // The columns' sums of N tiles: lane l16 keeps that of register l16 % 4 of tile l16 / 4, token `slot` of the stretch.
     static __device__ __forceinline__ int slot() { return 16 * ((lane_id() & 15) >> 2) + 4 * (lane_id() >> 4) + (lane_id() & 3); }
     static __device__ __forceinline__ bool keeps(const WeightUnit& u, int tiles) {
         return (lane_id() & 15) < 4 * tiles && u.t0 + slot() < u.len;
@@ -203,10 +206,10 @@ template <typename T, typename S, int G, bool kSplitRows> struct Weighing {
     static __device__ __forceinline__ size_t place(const PageWeightArgs& a, const WeightUnit& u) {
         return (size_t)u.bh * ((size_t)a.max_pages << a.page_shift) + min(u.t0 + slot(), u.len - 1);
     }
-    template <int TILES> static __device__ __forceinline__ float sums(uint32_t have, const float (*w)[4]) {
+    template <int N> static __device__ __forceinline__ float sums(uint32_t have, const float (*w)[4]) {
         float mine = 0.f;
 #pragma unroll
-        for (int j = 0; j < TILES; ++j)
+        for (int j = 0; j < N; ++j)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const float sum = row16_sum(w[j][r]);
@@ -224,7 +227,7 @@ template <typename T, typename S, int G, bool kSplitRows> struct Weighing {
 
 // ---- few rows for each sequence -------------------------------------------------------------------------------
 template <typename T, typename S, int G> __global__ __launch_bounds__(kAttThreads, 2) void page_weight_few_kernel(PageWeightArgs a) {
-    using W = Weighing<T, S, G, false>;
+    using W = Weighing<T, S, G, false, kFewTiles<T>>;
     __shared__ long long sh_sum[kAttWaves], sh_in[kAttWaves];
     __shared__ int sh_entry[kAttWaves];
     __shared__ __align__(16) char sh_keys[kAttWaves][W::KEYS * W::ROWB];
@@ -327,9 +330,9 @@ template <typename T, typename S, int G> __global__ __launch_bounds__(kAttThread
 }
 
 // ---- many rows ------------------------------------------------------------------------------------------------
-template <typename T, typename S, int G, int WAVES>
+template <typename T, typename S, int G, int TILES, int WAVES>
 __global__ __launch_bounds__(WAVES * LEOAM_WAVE, 2) void page_weight_many_kernel(PageWeightArgs a) {
-    using W = Weighing<T, S, G, true>;
+    using W = Weighing<T, S, G, true, TILES>;
     __shared__ float sh[WAVES][W::KEYS];
     __shared__ __align__(16) char sh_queries[WAVES][16 * W::QROWB];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / LEOAM_WAVE), rows_bh = a.batch * a.n_kv_heads;
@@ -388,16 +391,21 @@ constexpr int kManyGroups = 65536;
 // Waves that share a stretch of many rows: one, where the stretches by themselves fill the card (a workgroup of eight is alone on its
 // compute unit, and its loads are waited for at each stretch: 64 rows behind 32001 tokens 39 us, four waves 58, eight 110); more,
 // where few stretches would leave it idle (256 rows behind 2000 36, 14, 13; prompt of 4096 530, 168, 129).  Prompts without much
-// before them take more: the last stretches have few rows, the first ones all (8 prompts of 4096 1078, 865, 888).
-static int waves_of(long long stretches, long long columns, bool prompts) {
-    if (columns >= 512 && stretches <= (prompts ? 1024 : 256)) return 8;
-    return columns >= 256 && (prompts || stretches <= 1024) ? 4 : 1;
+// before them take more: the last stretches have few rows, the first ones all (8 prompts of 4096 1078, 865, 888).  Very few stretches
+// are halved as well (prompt of 1024 with 8 kv heads 134, 41, 31 and 24 us; two of 1250 with 4 163, 51, 38, 29; of 4096, which has
+// enough of them, 124 and 172).
+struct ManyShape { int waves; bool half; };
+static ManyShape many_shape(long long stretches, long long columns, bool prompts) {
+    if (columns < 256) return {1, false};
+    if (stretches <= 256) return {8, true};
+    if (columns >= 512 && prompts && stretches <= 1024) return {8, false};
+    return {prompts || stretches <= 1024 ? 4 : 1, false};
 }
 
 template <typename T, typename S, int G> static hipError_t launch_weight(PageWeightArgs a, hipStream_t stream) {
     const long long capacity = (long long)a.max_pages << a.page_shift, columns = (long long)a.n_new * G;
     const bool many = columns > (long long)kFewColumns * a.batch;
-    const int block = 16 * (many ? kWeightTiles<T, true> : 2 * kWeightTiles<T, false>);
+    const int block = 16 * (many ? kManyTiles<T> : 2 * kFewTiles<T>);
     const long long total = (capacity + block - 1) / block * a.batch * a.n_kv_heads;
     if (total > 0x7fffffffll - kManyGroups) return hipErrorInvalidValue;
     a.total = (int)total;
@@ -407,12 +415,20 @@ template <typename T, typename S, int G> static hipError_t launch_weight(PageWei
         hipLaunchKernelGGL((page_weight_few_kernel<T, S, G>), grid, dim3(kAttThreads), 0, stream, a);
         return hipGetLastError();
     }
-    const dim3 grid((unsigned)(total < kManyGroups ? total : kManyGroups));
-    switch (waves_of(total, columns / a.batch, 2ll * a.n_new >= a.batch * capacity)) {
-    case 8: hipLaunchKernelGGL((page_weight_many_kernel<T, S, G, 8>), grid, dim3(8 * LEOAM_WAVE), 0, stream, a); break;
-    case 4: hipLaunchKernelGGL((page_weight_many_kernel<T, S, G, 4>), grid, dim3(4 * LEOAM_WAVE), 0, stream, a); break;
-    default: hipLaunchKernelGGL((page_weight_many_kernel<T, S, G, 1>), grid, dim3(LEOAM_WAVE), 0, stream, a);
-    }
+    auto many_rows = [&](auto tiles, auto waves) {
+        constexpr int TILES = decltype(tiles)::value, WAVES = decltype(waves)::value;
+        const long long units = (capacity + 16 * TILES - 1) / (16 * TILES) * a.batch * a.n_kv_heads;
+        a.total = (int)units;
+        hipLaunchKernelGGL((page_weight_many_kernel<T, S, G, TILES, WAVES>), dim3((unsigned)(units < kManyGroups ? units : kManyGroups)),
+                           dim3(WAVES * LEOAM_WAVE), 0, stream, a);
+    };
+    constexpr std::integral_constant<int, kManyTiles<T>> wide{};
+    constexpr std::integral_constant<int, 8> eight{};
+    const ManyShape shape = many_shape(total, columns / a.batch, 2ll * a.n_new >= a.batch * capacity);
+    if (shape.half) many_rows(std::integral_constant<int, kManyTiles<T> / 2>{}, eight);
+    else if (shape.waves == 8) many_rows(wide, eight);
+    else if (shape.waves == 4) many_rows(wide, std::integral_constant<int, 4>{});
+    else many_rows(wide, std::integral_constant<int, 1>{});
     return hipGetLastError();
 }
 template <typename T, typename S> static hipError_t weight_of(const PageWeightArgs& a, int group, hipStream_t stream) {

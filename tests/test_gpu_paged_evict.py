@@ -100,8 +100,15 @@ def test_weigh_page_sizes(L, dtype, q8, page):
 @pytest.mark.parametrize("dtype,q8", KINDS, ids=KIND_IDS)
 @pytest.mark.parametrize("rows,history", [(4, 700), (5, 700), (33, 1200), (65, 900), (65, 0), (130, 800), (150, 10)])
 def test_weigh_rows_behind_a_history(L, dtype, q8, rows, history):
-    """One, four and eight waves to a stretch of keys, and the borders between them."""
     run_weigh(L, Made(dtype, q8, [rows + history, rows], 2, 32, seed=rows), 8, [rows, rows], seed=rows)
+
+
+@pytest.mark.parametrize("dtype,q8", KINDS, ids=KIND_IDS)
+@pytest.mark.parametrize("batch,rows,history", [(8, 300, 0), (20, 100, 0), (8, 70, 250), (4, 300, 20)])
+def test_weigh_rows_of_many_heads(L, dtype, q8, batch, rows, history):
+    """Every number of waves to a stretch of keys, and stretches of either size."""
+    lengths = [rows + history - b % 3 for b in range(batch)]
+    run_weigh(L, Made(dtype, q8, lengths, 8, 32, seed=rows), 32, [rows - b % 3 for b in range(batch)], seed=rows)
 
 
 def test_weigh_long_prompt(L):
