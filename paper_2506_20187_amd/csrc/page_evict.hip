@@ -7,7 +7,7 @@
 //
 // A weight becomes a 32-bit key of the same order, protected ones the highest, and the lowest key that stays is found by histograms of
 // 11, 11 and 10 of its bits.  What is read is 8 bytes a token; bound by latency, where there are many rows by the instructions for each
-// key.  A workgroup holds the keys of a row in registers (16 rows of 4200 tokens 9.6 us, of 32000 31, 512 rows of 20000 52).  Longer
+// key.  A workgroup holds the keys of a row in registers (16 rows of 4200 tokens 8.4 us, of 32000 31, 512 rows of 20000 52).  Longer
 // rows are cut into parts of 8192 places (at `keep`, too, so that what stays before it is a sum over parts): three launches make the
 // parts' histograms, each beginning with the sums of the last one's, a fourth one lists (16 rows of 64000 29 us; 35 when every
 // workgroup read all bins of its row's parts).
@@ -76,7 +76,7 @@ template <int THREADS, int HELD> struct HeldKeys {
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / LEOAM_WAVE), seg = (hi - lo + THREADS - 1) / THREADS * LEOAM_WAVE;
         begin = min(hi, lo + wave * seg);
         end = min(hi, begin + seg);
-        constexpr int TOGETHER = 16;      // on their way together; places past the last repeat it
+        constexpr int TOGETHER = HELD < 16 ? HELD : 16;      // on their way together; places past the last repeat it
 #pragma unroll
         for (int i0 = 0; i0 < HELD; i0 += TOGETHER) {
             if (begin + i0 * LEOAM_WAVE >= end) break;
@@ -173,9 +173,8 @@ __device__ __forceinline__ void list_moves(const HeldKeys<THREADS, HELD>& held, 
 }
 
 // ---- a row to a workgroup ---------------------------------------------------------------------------------
-// (Rows of up to 8192 places: 512 threads, so that four workgroups share a compute unit.)
 template <int THREADS, int HELD>
-__global__ __launch_bounds__(THREADS, THREADS == 512 ? 8 : 4) void page_evict_row_kernel(EvictArgs a) {
+__global__ __launch_bounds__(THREADS, HELD <= 16 ? 8 : 4) void page_evict_row_kernel(EvictArgs a) {
     constexpr int WAVES = THREADS / LEOAM_WAVE;
     __shared__ uint32_t hist[3][kEvictBins];
     __shared__ int sh_find[WAVES + 3], sh_above[WAVES], sh_equal[WAVES], sh_kept_low[2];
@@ -429,7 +428,11 @@ hipError_t page_evict_dispatch(const leoam_pages* s, const float* weight, const 
     a.n_kv_heads = s->n_kv_heads; a.capacity = s->max_pages * s->page_size;
     const int rows = s->batch * s->n_kv_heads, parts = evict_parts(s);
     if (parts == 0) {
-        if (a.capacity <= 16 * 512) hipLaunchKernelGGL((page_evict_row_kernel<512, 16>), dim3(rows), dim3(512), 0, stream, a);
+        // (two workgroups of 1024 threads share a compute unit, four of 512: 16 rows of 4200 8.4 against 9.7 us, 512 of those 13.8 / 14.7,
+        // 1024 25.9 / 22.0)
+        if (a.capacity <= 8 * 1024 && rows <= 512)
+            hipLaunchKernelGGL((page_evict_row_kernel<1024, 8>), dim3(rows), dim3(1024), 0, stream, a);
+        else if (a.capacity <= 16 * 512) hipLaunchKernelGGL((page_evict_row_kernel<512, 16>), dim3(rows), dim3(512), 0, stream, a);
         else if (a.capacity <= 16 * 1024) hipLaunchKernelGGL((page_evict_row_kernel<1024, 16>), dim3(rows), dim3(1024), 0, stream, a);
         else if (a.capacity <= 32 * 1024) hipLaunchKernelGGL((page_evict_row_kernel<1024, 32>), dim3(rows), dim3(1024), 0, stream, a);
         else hipLaunchKernelGGL((page_evict_row_kernel<1024, kRowHeld>), dim3(rows), dim3(1024), 0, stream, a);

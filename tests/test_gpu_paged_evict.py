@@ -288,6 +288,13 @@ def test_select_many_long_rows(L, n):
     run_select(L, lengths, [n // 2, 39, n - 300, 1] + 28 * [5], hkv=4, first=[4] * 3 + [0] * 29, recent=100, seed=n)
 
 
+@pytest.mark.parametrize("n", [50, 700])
+def test_select_many_short_rows(L, n):
+    """More rows than fit the card at a time."""
+    lengths = [n - b % 7 for b in range(140)]
+    run_select(L, lengths, [n // 2 + b % 3 for b in range(140)], hkv=4, first=[b % 5 for b in range(140)], recent=9, seed=n)
+
+
 def test_select_more_protected_than_stay(L):
     run_select(L, [500] * 4, [100] * 4, first=[100, 101, 500, 90], recent=30)
     run_select(L, [500] * 4, [100] * 4, first=[0, 99, 100, 1 << 30], recent=1 << 30, ids=False)
