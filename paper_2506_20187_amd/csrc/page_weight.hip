@@ -6,8 +6,9 @@
 // Few rows for each sequence: every key is read once, bound by that.  The stretches of 64 keys (fp32: 32) of all sequences and heads
 // are laid end to end and shared out equally to the waves; a wave works on half of one while the next half's keys are on their
 // way.  They come as whole rows, which the caches serve at four times the rate of an operand's 16 bytes of 16 rows, and become
-// operands in LDS.  Sixteen tokens of sequences to 33001 (617 MB): 128 us, 4.8 TB/s; with operands straight from the loads and no
-// equal shares 187; with weights written for 32 keys at a time 134.
+// operands in LDS.  Sixteen tokens of sequences to 33001 (617 MB): 125 us, 4.9 TB/s; with operands straight from the loads and no
+// equal shares 187; with weights written for 32 keys at a time 134, with lengths and
+// pages looked up when the keys are asked for 129.
 // Many rows: bound by the exponentials and the instructions around them.  The waves of a workgroup share 64 keys (fp32: 32; half as
 // many where keys are few) and go through the blocks of columns in turn; their sums are added in order at the end.  Queries, too,
 // come as whole rows.  A prompt of 4096 with 32 heads: 114 us (268 M exponentials, 69 GFLOP); with operands straight from the
@@ -84,16 +85,20 @@ template <typename T, typename S, int G, bool kSplitRows, int TILES> struct Weig
     static __device__ __forceinline__ int first_row(const WeightUnit& u) { return kSplitRows ? max(0, u.t0 - u.first) : 0; }
     static __device__ __forceinline__ int columns(const WeightUnit& u) { return (u.m - first_row(u)) * G; }
 
-    static __device__ __forceinline__ void fetch_keys(const PageWeightArgs& a, const WeightUnit& u, Keys& x) {
-        const int lane = lane_id(), grp = lane >> 4, l16 = lane & 15;
-        x.have = 0;
-        int id[NT];
+    struct PageIds { int id[NT]; };
+    static __device__ __forceinline__ PageIds pages_of(const PageWeightArgs& a, const WeightUnit& u) {
+        PageIds p;
 #pragma unroll
         for (int j = 0; j < NT; ++j)
-            id[j] = scalar_at(a.page_table, (size_t)u.b * a.max_pages + (min(u.t0 + 16 * j, u.len - 1) >> a.page_shift));
+            p.id[j] = scalar_at(a.page_table, (size_t)u.b * a.max_pages + (min(u.t0 + 16 * j, u.len - 1) >> a.page_shift));
+        return p;
+    }
+    static __device__ __forceinline__ void fetch_keys(const PageWeightArgs& a, const WeightUnit& u, const PageIds& p, Keys& x) {
+        const int lane = lane_id(), grp = lane >> 4, l16 = lane & 15;
+        x.have = 0;
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
-            const int t = min(u.t0 + 16 * j, u.len - 1), valid = min(u.len - (u.t0 + 16 * j), 16), page = id[j];
+            const int t = min(u.t0 + 16 * j, u.len - 1), valid = min(u.len - (u.t0 + 16 * j), 16), page = p.id[j];
             const bool ok = (uint32_t)page < (uint32_t)a.n_pages && valid > 0;
             x.have |= (ok ? 1u : 0u) << j;
             const size_t row = (size_t)(ok ? page : 0) * a.n_kv_heads + u.h;
@@ -102,8 +107,9 @@ template <typename T, typename S, int G, bool kSplitRows, int TILES> struct Weig
             if constexpr (k8) x.ks[j] = scalar_at(a.k_scale, row);
 #pragma unroll
             for (int s = 0; s < NK; ++s) {
-                const uint32_t r = kSplitRows ? l16 : s * kRowsOfLoad + lane / kPieces, p = kSplitRows ? 4 * s + grp : lane % kPieces;
-                x.k[NK * j + s] = load16(kp, (row0 + min(r, last)) * ROWB + 16 * p);
+                const uint32_t r = kSplitRows ? l16 : s * kRowsOfLoad + lane / kPieces;
+                const uint32_t piece = kSplitRows ? 4 * s + grp : lane % kPieces;
+                x.k[NK * j + s] = load16(kp, (row0 + min(r, last)) * ROWB + 16 * piece);
             }
         }
     }
@@ -286,15 +292,28 @@ template <typename T, typename S, int G> __global__ __launch_bounds__(kAttThread
     typename W::Keys even, odd;
     WeightColumns<T> cols;
     int cols_of = -1;      // which (sequence, kv head) they are of
-    W::fetch_keys(a, half_at(0), even);
+    // (what is looked up - lengths, pages - is looked up a half ahead of the keys that wait for it)
+    WeightUnit u = half_at(0), v = half_at(1);      // (the second may lie behind the last token)
+    W::fetch_keys(a, u, W::pages_of(a, u), even);
+    typename W::PageIds v_pages = W::pages_of(a, v);
     while (left > 0) {
-        const WeightUnit u = half_at(0), v = half_at(1);      // (the second may lie behind the last token)
         if (u.bh != cols_of) {
             cols_of = u.bh;
             W::fetch_columns(a, u, 0, cols);
         }
-        W::fetch_keys(a, v, odd);
+        W::fetch_keys(a, v, v_pages, odd);
         const float was = a.before ? a.before[W::place(a, u)] : 0.f;
+        // to the next stretch (behind the share's last: that one again, from the caches)
+        if (--left > 0 && ++block * STRETCH >= u.len) {
+            block = 0;
+            if (++h == hkv) {
+                h = 0;
+                do ++b;
+                while (blocks_of(scalar_at(a.seq_len, b)) == 0);      // (there is one: the share is not at its end)
+            }
+        }
+        const WeightUnit next = half_at(0);
+        const typename W::PageIds next_pages = W::pages_of(a, next);
         float w[2 * W::NT][4];
 #pragma unroll
         for (int j = 0; j < 2 * W::NT; ++j)
@@ -313,19 +332,14 @@ template <typename T, typename S, int G> __global__ __launch_bounds__(kAttThread
         };
         work(u, even, w);
         const uint32_t have = even.have;
-        // to the next stretch (behind the share's last: that one again, from the caches)
-        if (--left > 0 && ++block * STRETCH >= u.len) {
-            block = 0;
-            if (++h == hkv) {
-                h = 0;
-                do ++b;
-                while (blocks_of(scalar_at(a.seq_len, b)) == 0);      // (there is one: the share is not at its end)
-            }
-        }
-        W::fetch_keys(a, half_at(0), even);
+        W::fetch_keys(a, next, next_pages, even);
+        const WeightUnit next_v = half_at(1);
+        v_pages = W::pages_of(a, next_v);
         work(v, odd, w + W::NT);
         const float mine = W::template sums<2 * W::NT>(have | odd.have << W::NT, w);
         if (W::keeps(u, 2 * W::NT)) W::store(a, u, was, mine);
+        u = next;
+        v = next_v;
     }
 }
 
@@ -341,7 +355,7 @@ __global__ __launch_bounds__(WAVES * LEOAM_WAVE, 2) void page_weight_many_kernel
         const WeightUnit u = W::unit_at(a, unit - block * rows_bh, block * W::KEYS);
         if (u.t0 >= u.len) continue;
         typename W::Keys keys;
-        W::fetch_keys(a, u, keys);
+        W::fetch_keys(a, u, W::pages_of(a, u), keys);
         const float was = a.before ? a.before[W::place(a, u)] : 0.f;
         uint4 wide[W::NT * W::NQ];      // (8 bits: widened once)
 #pragma unroll
