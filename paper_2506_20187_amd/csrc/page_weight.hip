@@ -7,8 +7,7 @@
 // are laid end to end and shared out equally to the waves; a wave works on half of one while the next half's keys are on their
 // way.  They come as whole rows, which the caches serve at four times the rate of an operand's 16 bytes of 16 rows, and become
 // operands in LDS.  Sixteen tokens of sequences to 33001 (617 MB): 125 us, 4.9 TB/s; with operands straight from the loads and no
-// equal shares 187; with weights written for 32 keys at a time 134, with lengths and
-// pages looked up when the keys are asked for 129.
+// equal shares 187; with weights written for 32 keys at a time 134; with lengths and pages looked up when the keys are fetched 129.
 // Many rows: bound by the exponentials and the instructions around them.  The waves of a workgroup share 64 keys (fp32: 32; half as
 // many where keys are few) and go through the blocks of columns in turn; their sums are added in order at the end.  Queries, too,
 // come as whole rows.  A prompt of 4096 with 32 heads: 114 us (268 M exponentials, 69 GFLOP); with operands straight from the
@@ -232,7 +231,11 @@ template <typename T, typename S, int G, bool kSplitRows, int TILES> struct Weig
 };
 
 // ---- few rows for each sequence -------------------------------------------------------------------------------
-template <typename T, typename S, int G> __global__ __launch_bounds__(kAttThreads, 2) void page_weight_few_kernel(PageWeightArgs a) {
+// Workgroups of a compute unit: two (three, with fewer registers each: 150 against 136 us, 16 sequences to 33001), in 8 bits three (16
+// sequences of 33001 125 us, two 135).
+template <typename S> constexpr int kFewPerUnit = std::is_same<S, E4M3>::value ? 3 : 2;
+template <typename T, typename S, int G>
+__global__ __launch_bounds__(kAttThreads, kFewPerUnit<S>) void page_weight_few_kernel(PageWeightArgs a) {
     using W = Weighing<T, S, G, false, kFewTiles<T>>;
     __shared__ long long sh_sum[kAttWaves], sh_in[kAttWaves];
     __shared__ int sh_entry[kAttWaves];
@@ -398,8 +401,6 @@ __global__ __launch_bounds__(WAVES * LEOAM_WAVE, 2) void page_weight_many_kernel
 
 // More than a block of columns for each sequence on average: many rows.
 constexpr int kFewColumns = 16;
-// workgroups of few rows: two fill a compute unit (three, with fewer registers each: 150 against 136 us, 16 sequences to 33001)
-constexpr int kFewGroups = 512;
 constexpr int kManyGroups = 65536;
 
 // Waves that share a stretch of many rows: one, where the stretches by themselves fill the card (a workgroup of eight is alone on its
@@ -424,8 +425,9 @@ template <typename T, typename S, int G> static hipError_t launch_weight(PageWei
     if (total > 0x7fffffffll - kManyGroups) return hipErrorInvalidValue;
     a.total = (int)total;
     if (!many) {
+        constexpr int most = 256 * kFewPerUnit<S>;
         const long long groups = (total + kAttWaves - 1) / kAttWaves;
-        const dim3 grid((unsigned)(groups < kFewGroups ? groups : kFewGroups));
+        const dim3 grid((unsigned)(groups < most ? groups : most));
         hipLaunchKernelGGL((page_weight_few_kernel<T, S, G>), grid, dim3(kAttThreads), 0, stream, a);
         return hipGetLastError();
     }
