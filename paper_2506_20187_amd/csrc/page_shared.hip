@@ -78,6 +78,13 @@ template <typename T, typename S> struct SharedStep {
 __device__ __forceinline__ int tile_cost(int ways) { return ways == 1 ? 2 : ways == 2 ? 4 : kMostTileCost; }
 
 __device__ __forceinline__ int shared_tiles(int tokens) { return max(1, (tokens + kSharedTile - 1) / kSharedTile); }
+// A sequence's own tokens that are this few: where there are more (sequence, kv head) pairs than half the workgroups, a unit is four of
+// its heads, one to a wave, and is not cut.  (Us, a head to a unit : four: 126 sequences with a token of their own, 32 kv heads, in 8
+// bits 65 : 35, 128 behind 1000 with 100 to 120, 8 heads, bf16 30.2 : 29.9, 93 of up to 71, 4 heads, fp32 35 : 25; with 64 tokens at most
+// 31.5 and 31 of the latter two, with 256 nothing more.)
+constexpr int kBundleTokens = 128;
+__device__ __forceinline__ int bundle_cost(int tokens) { return 1 + 2 * ((tokens + 31) / 32); }
+
 // of the waves, over a unit's columns
 __device__ __forceinline__ int ways_of(int n_cols) { return n_cols <= kWaveColumns ? 1 : n_cols <= 2 * kWaveColumns ? 2 : 4; }
 
@@ -149,6 +156,8 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
         const int shared = prefix_of(lo - 1);
         return len >= shared ? shared : 0;      // (a sequence that is shorter has all of its tokens to itself)
     };
+    const bool bundles = hkv > 1 && (long long)a.batch * hkv > a.sharers / 2;
+    auto bundled = [&](int tokens) { return bundles && tokens <= kBundleTokens; };
     // entries: groups, then sequences
     auto entry_of = [&](int e) {
         if (e < a.n_groups) {
@@ -157,8 +166,9 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
             const int full = members / most_members, rest = members - full * most_members;
             return SharedEntry{full * hkv, rest ? hkv : 0, shared_tiles(tokens), tile_cost(4), tile_cost(ways_of(rest << a.group_shift))};
         }
-        const int b = e - a.n_groups, len = length_of(b);
-        return SharedEntry{0, hkv, shared_tiles(len - before_of(b, len)), 1, tile_cost(1)};
+        const int b = e - a.n_groups, len = length_of(b), tokens = len - before_of(b, len);
+        if (bundled(tokens)) return SharedEntry{0, (hkv + kAttWaves - 1) / kAttWaves, 1, 1, bundle_cost(tokens)};
+        return SharedEntry{0, hkv, shared_tiles(tokens), 1, tile_cost(1)};
     };
     const int n_entries = a.n_groups + a.batch;
     long long pos, end, share, first;      // its places on the line of all costs, [first, end), and where on it the work is
@@ -211,7 +221,8 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
         q = counts ? make_uint4(q.x ^ a.flip, q.y ^ a.flip, q.z ^ a.flip, q.w ^ a.flip) : make_uint4(0, 0, 0, 0);
     };
     // One stretch of a unit: tokens [t_begin, t_end) of row b_table, for this wave's columns, NB blocks of 16, WAYS of the four waves on
-    // columns of their own.  rows, counts: the lane's row of q in each block, and whether the column is one.
+    // columns of their own (four: each on those of a head, h).  rows, counts: the lane's row of q in each block, and whether the column
+    // is one.
     auto walk = [&](auto blocks, auto apart, int b_table, int h, int t_begin, int t_end, int n_cols, const size_t* rows, const bool* counts,
                     auto&& leave) {
         const int lane = here(lane_id()), tid = here(threadIdx.x), grp = lane >> 4, l16 = lane & 15;
@@ -480,8 +491,8 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
         }
         __syncthreads();
         for (int i = tid; i < n_cols * (LEOAM_D / 4); i += kAttThreads) {
-            const int c = i / (LEOAM_D / 4), d = 4 * (i % (LEOAM_D / 4)), in = c % kWaveColumns;
-            const int w0 = WAYS == 1 ? 0 : c / kWaveColumns;
+            const int c = i / (LEOAM_D / 4), d = 4 * (i % (LEOAM_D / 4)), in = WAYS == 4 ? c & (group - 1) : c % kWaveColumns;
+            const int w0 = WAYS == 1 ? 0 : WAYS == 4 ? c >> a.group_shift : c / kWaveColumns;
             float ms[STREAMS], ls[STREAMS], m = -INFINITY, l = 0.f;
             float4 x[STREAMS], v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
@@ -740,14 +751,14 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
         };
         const int tile0 = tiles_before(off), tile1 = min(tiles, tiles_before(off + take));
         if (tile0 < tile1) {
-            const int h = unit % hkv;
+            int h = unit % hkv;
             const bool prefix = entry < a.n_groups, whole = tile1 - tile0 == tiles;
             const int slot = 2 * (int)blockIdx.x + (first_piece ? 0 : 1);      // opens the share, or closes it
             // pieces of the unit, and where the first lies, if it begins here
             const long long last_at = pos - first - off + kSharedStart + (long long)(tiles - 1) * cost;
             const int count = whole ? kWhole : tile0 ? 1 : (int)quotient(last_at, share) + 1;
             int n_cols, b0, tokens, before = 0, b_table;
-            bool work = true;
+            bool work = true, bundle = false;
             if (prefix) {
                 b0 = off_of(entry) + unit / hkv * most_members;
                 const int members = min(off_of(entry + 1) - b0, most_members);
@@ -773,11 +784,16 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
                 const int len = uniform(length_of(b0));
                 before = uniform(before_of(b0, len));
                 tokens = len - before;
+                bundle = bundled(tokens);
+                if (bundle) {
+                    h = kAttWaves * unit;
+                    n_cols = min(kAttWaves, hkv - h) << a.group_shift;
+                }
             }
             tokens = uniform(tokens);
             const bool final_ = !prefix && before == 0 && whole;
-            if (!prefix && tile0 == 0 && tid == 0) {
-                SharedRow* r = a.rows + (size_t)b0 * hkv + h;
+            if (!prefix && tile0 == 0 && tid < (bundle ? n_cols >> a.group_shift : 1)) {
+                SharedRow* r = a.rows + (size_t)b0 * hkv + h + tid;
                 r->own_count = final_ ? kFinal : tokens == 0 ? 0 : count;
                 r->own_slot = slot;
                 if (before == 0) r->pre_count = 0;
@@ -786,10 +802,11 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
                 // (columns past the last repeat it; what is asked for does not wait for whether it counts)
                 auto row_of = [&](int c) {
                     c = min(c, n_cols - 1);
+                    if (bundle) return (((size_t)b0 * hkv + h) << a.group_shift) + c;
                     return (((size_t)(b0 + (c >> a.group_shift)) * hkv + h) << a.group_shift) + (c & (group - 1));
                 };
                 auto counts_of = [&](int c) { return c < n_cols && (!prefix || length_of(b0 + (c >> a.group_shift)) >= tokens); };
-                const int t_begin = before + tile0 * kSharedTile, t_end = before + min(tokens, tile1 * kSharedTile);
+                const int t_begin = before + tile0 * kSharedTile, t_end = before + (bundle ? tokens : min(tokens, tile1 * kSharedTile));
                 auto leave = [&](int c, int d, const float4& v, float m, float l) {
                     const size_t j = row_of(c);
                     if (final_) {
@@ -804,7 +821,13 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
                 };
                 constexpr std::integral_constant<int, 1> one{};
                 constexpr std::integral_constant<int, 2> two{};
-                if (n_cols <= 2 * kWaveColumns) {
+                constexpr std::integral_constant<int, 4> four{};
+                if (bundle) {
+                    const bool has = wave << a.group_shift < n_cols;
+                    const size_t rows[1] = {row_of((wave << a.group_shift) + min(l16, group - 1))};
+                    const bool counts[1] = {has && l16 < group};
+                    walk(one, four, b_table, min(h + wave, hkv - 1), t_begin, has ? t_end : t_begin, n_cols, rows, counts, leave);
+                } else if (n_cols <= 2 * kWaveColumns) {
                     const int c0 = (n_cols <= kWaveColumns ? 0 : kWaveColumns * (wave & 1)) + l16;
                     const size_t rows[2] = {row_of(c0), row_of(c0 + 16)};
                     const bool counts[2] = {counts_of(c0), counts_of(c0 + 16)};

@@ -132,6 +132,17 @@ def test_pages_that_are_missing_hold_no_tokens(L, dtype, q8):
     run_shared(L, made, 8)      # (of the third nothing is left)
 
 
+@pytest.mark.parametrize("dtype,q8", KINDS, ids=KIND_IDS)
+@pytest.mark.parametrize("hkv,group", [(5, 1), (8, 2), (6, 8)])
+def test_short_tails_of_many_sequences(L, dtype, q8, hkv, group):
+    # four heads to a workgroup: numbers of heads that four divides and does not, tails at the border, longer and none, pages missing
+    made = Grouped(dtype, q8, hkv, 16, [(2, [0, 1, 15, 16, 31, 32, 33, 64, 65, 127, 128, 129, None, -1, 200] * 2), (0, [1, 5, 130] * 5), (3, [7, 2, 90])],
+                   seed=hkv, alone_after=(0, 1, 128, 129, 40))
+    assert len(made.lengths) * hkv > 256
+    made.table[3, 2], made.table[9, 3], made.table[26, 2:] = -1, 1 << 20, -1
+    run_shared(L, made, hkv * group, rows=sorted({*range(16), 18, 25, 26, *range(29, 36), *range(len(made.lengths) - 8, len(made.lengths))}))
+
+
 @pytest.mark.parametrize("scale", [-0.3, 0.0, 1e-30, 3.0])
 def test_scales_of_any_sign(L, scale):
     run_shared(L, Grouped(F16, False, 1, 16, [(5, [3, 40, 0])], seed=5), 4, scale=scale)
