@@ -408,10 +408,12 @@ constexpr int kManyGroups = 65536;
 // where few stretches would leave it idle (256 rows behind 2000 36, 14, 13; prompt of 4096 530, 168, 129).  Prompts without much
 // before them take more: the last stretches have few rows, the first ones all (8 prompts of 4096 1078, 865, 888).  Very few stretches
 // are halved as well (prompt of 1024 with 8 kv heads 134, 41, 31 and 24 us; two of 1250 with 4 163, 51, 38, 29; of 4096, which has
-// enough of them, 124 and 172).
+// enough of them, 124 and 172), and with fewer columns four waves share those (50 rows behind 1000, one wave and four: 11.1, 6.2; of
+// two sequences 11.0, 7.6; fp32 24, 12.6).
 struct ManyShape { int waves; bool half; };
 static ManyShape many_shape(long long stretches, long long columns, bool prompts) {
-    if (columns < 256) return {1, false};
+    if (columns < 64) return {1, false};
+    if (columns < 256) return stretches <= 512 ? ManyShape{4, true} : ManyShape{1, false};
     if (stretches <= 256) return {8, true};
     if (columns >= 512 && prompts && stretches <= 1024) return {8, false};
     return {prompts || stretches <= 1024 ? 4 : 1, false};
@@ -439,11 +441,14 @@ template <typename T, typename S, int G> static hipError_t launch_weight(PageWei
                            dim3(WAVES * LEOAM_WAVE), 0, stream, a);
     };
     constexpr std::integral_constant<int, kManyTiles<T>> wide{};
+    constexpr std::integral_constant<int, kManyTiles<T> / 2> half{};
     constexpr std::integral_constant<int, 8> eight{};
+    constexpr std::integral_constant<int, 4> four{};
     const ManyShape shape = many_shape(total, columns / a.batch, 2ll * a.n_new >= a.batch * capacity);
-    if (shape.half) many_rows(std::integral_constant<int, kManyTiles<T> / 2>{}, eight);
+    if (shape.half && shape.waves == 8) many_rows(half, eight);
+    else if (shape.half) many_rows(half, four);
     else if (shape.waves == 8) many_rows(wide, eight);
-    else if (shape.waves == 4) many_rows(wide, std::integral_constant<int, 4>{});
+    else if (shape.waves == 4) many_rows(wide, four);
     else many_rows(wide, std::integral_constant<int, 1>{});
     return hipGetLastError();
 }
