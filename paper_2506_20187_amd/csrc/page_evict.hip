@@ -8,9 +8,8 @@
 // A weight becomes a 32-bit key of the same order, protected ones the highest, and the lowest key that stays is found by histograms of
 // 11, 11 and 10 of its bits.  What is read is 8 bytes a token; bound by latency, where there are many rows by the instructions for each
 // key.  A workgroup holds the keys of a row in registers (16 rows of 4200 tokens 8.4 us, of 32000 31, 512 rows of 20000 52).  Longer
-// rows are cut into parts of 8192 places (at `keep`, too, so that what stays before it is a sum over parts): three launches make the
-// parts' histograms, each beginning with the sums of the last one's, a fourth one lists (16 rows of 64000 29 us; 35 when every
-// workgroup read all bins of its row's parts).
+// rows are cut into parts of 4096 or 8192 places (at `keep`, too, so that what stays before it is a sum over parts): three launches make
+// the parts' histograms, each beginning with the sums of the last one's, a fourth one lists (16 rows of 64000 24 us).
 #include "page_common.h"
 
 namespace leoam {
@@ -25,7 +24,7 @@ struct EvictArgs {
     int n_kv_heads, capacity;
 };
 
-constexpr int kPartThreads = 512, kPartHeld = 16, kEvictPart = kPartThreads * kPartHeld;      // threads, keys of a thread
+constexpr int kPartThreads = 512;      // of a part
 constexpr int kEvictBins = 2048;
 constexpr uint32_t kProtected = 0xffffffffu;       // above every weight's key
 
@@ -245,14 +244,14 @@ struct EvictLong {
 };
 
 // the parts of a row: those below `keep`, then those from it on
-struct PartOf {
+template <int PART> struct PartOf {
     int n_low, n_parts, begin, end;
     __device__ __forceinline__ PartOf(const EvictRow& row, int p) {
-        n_low = (row.keep + kEvictPart - 1) / kEvictPart;
-        n_parts = n_low + (row.n - row.keep + kEvictPart - 1) / kEvictPart;
+        n_low = (row.keep + PART - 1) / PART;
+        n_parts = n_low + (row.n - row.keep + PART - 1) / PART;
         const int lo = p < n_low ? 0 : row.keep, hi = p < n_low ? row.keep : row.n;
-        begin = lo + (p < n_low ? p : p - n_low) * kEvictPart;
-        end = min(hi, begin + kEvictPart);
+        begin = lo + (p < n_low ? p : p - n_low) * PART;
+        end = min(hi, begin + PART);
     }
 };
 
@@ -315,16 +314,16 @@ template <int K> struct PartBin {
     }
 };
 
-template <int STAGE> __global__ __launch_bounds__(kPartThreads, 4) void page_evict_hist_kernel(EvictArgs a, EvictLong s) {
+template <int STAGE, int HELD> __global__ __launch_bounds__(kPartThreads, 4) void page_evict_hist_kernel(EvictArgs a, EvictLong s) {
     __shared__ __align__(16) uint32_t hist[kEvictBins];
     __shared__ PartSums<1> sh_find;
     const int tid = threadIdx.x, bh = blockIdx.x / s.parts, p = blockIdx.x % s.parts;
     const EvictRow row(a, bh);
     if (STAGE == 0 && tid == 0 && p == 0) row.report(a, bh);
     if (row.none) return;
-    const PartOf part(row, p);
+    const PartOf<HELD * kPartThreads> part(row, p);
     if (p >= part.n_parts) return;
-    const HeldKeys<kPartThreads, kPartHeld> held(row, part.begin, part.end);
+    const HeldKeys<kPartThreads, HELD> held(row, part.begin, part.end);
     const size_t here = ((size_t)(STAGE & 1) * s.rows + bh) * s.parts + p;
     for (int i = tid; i < kEvictBins; i += kPartThreads) hist[i] = 0;
     uint32_t prefix = 0;
@@ -346,7 +345,7 @@ template <int STAGE> __global__ __launch_bounds__(kPartThreads, 4) void page_evi
         if (tid == 0 && p == 0) s.found[(size_t)(STAGE - 1) * s.rows + bh] = EvictFound{prefix, need - found.above};
     }
     __syncthreads();
-    count_keys<STAGE, kPartThreads, kPartHeld>(held, prefix, hist);
+    count_keys<STAGE, kPartThreads, HELD>(held, prefix, hist);
     __syncthreads();
     static_assert(kEvictBins == 4 * kPartThreads && kFine == 32, "a thread writes four bins, eight threads a coarse one");
     const uint4 mine = *reinterpret_cast<const uint4*>(hist + 4 * tid);
@@ -358,7 +357,7 @@ template <int STAGE> __global__ __launch_bounds__(kPartThreads, 4) void page_evi
     if (tid == 0) s.above[here] = above;
 }
 
-__global__ __launch_bounds__(kPartThreads, 4) void page_evict_list_kernel(EvictArgs a, EvictLong s) {
+template <int HELD> __global__ __launch_bounds__(kPartThreads, 4) void page_evict_list_kernel(EvictArgs a, EvictLong s) {
     constexpr int WAVES = kPartThreads / LEOAM_WAVE;
     __shared__ PartSums<2> sh_find;
     __shared__ int sh_above[WAVES], sh_equal[WAVES];
@@ -366,9 +365,9 @@ __global__ __launch_bounds__(kPartThreads, 4) void page_evict_list_kernel(EvictA
     const int bh = blockIdx.x / s.parts, p = blockIdx.x % s.parts;
     const EvictRow row(a, bh);
     if (row.none) return;
-    const PartOf part(row, p);
+    const PartOf<HELD * kPartThreads> part(row, p);
     if (p >= part.n_parts) return;
-    const HeldKeys<kPartThreads, kPartHeld> held(row, part.begin, part.end);
+    const HeldKeys<kPartThreads, HELD> held(row, part.begin, part.end);
     // of the parts before this one, and of those below `keep`: keys above the bound and equal to it
     const size_t first = (size_t)bh * s.parts;      // (stage 2's)
     const EvictFound before = s.found[s.rows + bh];
@@ -399,16 +398,18 @@ __global__ __launch_bounds__(kPartThreads, 4) void page_evict_list_kernel(EvictA
     equal = found.equal_of[0] + before_wave<WAVES>(sh_equal, wave);
     const int kept_low = above_of[1] + min(found.equal_of[1], ties);
     if (tid == 0 && p == 0) a.move_count[bh] = row.keep - kept_low;
-    list_moves<kPartThreads, kPartHeld>(held, row.keep, bound, ties, above, equal, kept_low, a.moves + (size_t)bh * a.m_max * 2);
+    list_moves<kPartThreads, HELD>(held, row.keep, bound, ties, above, equal, kept_low, a.moves + (size_t)bh * a.m_max * 2);
 }
 
 // Into how many parts rows are cut at most; 0: a row to a workgroup.  That takes a microsecond for a thousand tokens, four launches take
-// 28 whatever the length if there are few rows (16 of 20000 24 against 28, of 32000 31 / 28, of 64000 60 / 29), but more work in all
-// (128 rows of 32000 33 / 57, of 60000 61 / 74, 512 of those 142 / 221).
+// 22 to 26 if there are few rows (four of 40000 22.5, 16 of 64000 24; a workgroup 16 of 20000 24, of 32000 31, of 64000 60), but more
+// work in all (128 rows of 32000, parts 57, a workgroup 33; of 60000 74 / 61, 512 of those 221 / 142).
+// Keys of a part's thread: few for few rows (16 rows of 64000, 8 and 16 keys: 24, 29; 64 of those 47, 51; 256 of 130000 307, 232).
 constexpr int kRowHeld = 64;      // keys of a thread, at most
+static int part_held(int rows) { return rows <= 64 ? 8 : 16; }
 static int evict_parts(const leoam_pages* s) {
     const int capacity = s->max_pages * s->page_size, rows = s->batch * s->n_kv_heads;
-    return capacity <= (rows < 128 ? 32 : kRowHeld) * 1024 ? 0 : capacity / kEvictPart + 2;
+    return capacity <= (rows < 64 ? 16 : rows < 128 ? 32 : kRowHeld) * 1024 ? 0 : capacity / (part_held(rows) * kPartThreads) + 2;
 }
 static size_t evict_hist_bytes(const leoam_pages* s) {
     return 2 * (size_t)s->batch * s->n_kv_heads * evict_parts(s) * kEvictBins * sizeof(uint32_t);
@@ -446,10 +447,15 @@ hipError_t page_evict_dispatch(const leoam_pages* s, const float* weight, const 
     l.found = (EvictFound*)((char*)l.above + evict_above_bytes(s));
     l.rows = rows; l.parts = parts;
     const dim3 grid((unsigned)(rows * parts)), block(kPartThreads);
-    hipLaunchKernelGGL(page_evict_hist_kernel<0>, grid, block, 0, stream, a, l);
-    hipLaunchKernelGGL(page_evict_hist_kernel<1>, grid, block, 0, stream, a, l);
-    hipLaunchKernelGGL(page_evict_hist_kernel<2>, grid, block, 0, stream, a, l);
-    hipLaunchKernelGGL(page_evict_list_kernel, grid, block, 0, stream, a, l);
+    auto launch = [&](auto held) {
+        constexpr int HELD = decltype(held)::value;
+        hipLaunchKernelGGL((page_evict_hist_kernel<0, HELD>), grid, block, 0, stream, a, l);
+        hipLaunchKernelGGL((page_evict_hist_kernel<1, HELD>), grid, block, 0, stream, a, l);
+        hipLaunchKernelGGL((page_evict_hist_kernel<2, HELD>), grid, block, 0, stream, a, l);
+        hipLaunchKernelGGL(page_evict_list_kernel<HELD>, grid, block, 0, stream, a, l);
+    };
+    if (part_held(rows) == 8) launch(std::integral_constant<int, 8>{});
+    else launch(std::integral_constant<int, 16>{});
     return hipGetLastError();
 }
 

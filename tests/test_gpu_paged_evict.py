@@ -286,6 +286,8 @@ def test_select_ties_and_special_weights(L, n):
 def test_select_many_long_rows(L, n):
     lengths = [n, 40, n - 1, 33000] + 28 * [700]
     run_select(L, lengths, [n // 2, 39, n - 300, 1] + 28 * [5], hkv=4, first=[4] * 3 + [0] * 29, recent=100, seed=n)
+    # fewer of them: by parts, long and short
+    run_select(L, lengths[:20], [n // 2, 39, n - 300, 1] + 16 * [5], hkv=4, first=[4] * 3 + [0] * 17, recent=100, seed=n)
 
 
 @pytest.mark.parametrize("n", [50, 700])
