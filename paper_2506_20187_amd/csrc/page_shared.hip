@@ -34,6 +34,10 @@ constexpr int kWaveColumns = 32;
 constexpr int kGroupsInLds = 512;
 
 constexpr int kSharedStart = 6, kMostTileCost = 6;
+// Most pieces of a unit: a head's are folded one batch after another, which lasts longer than what more workgroups save (us with 64,
+// 128, 192 and as many as there are workgroups: 8 heads of one kv head behind 65536 tokens, 8 sequences 46, 34, 31, 47, 4 of 4 heads 28,
+// 23, 25, 33).
+constexpr int kMostPieces = 128;
 
 struct PageSharedArgs {
     const char *q, *k_pages, *v_pages;
@@ -93,6 +97,11 @@ __device__ __forceinline__ long long quotient(long long a, long long b) {
     return (unsigned long long)(a | b) >> 32 ? a / b : (long long)((uint32_t)a / (uint32_t)b);
 }
 
+// a 64-bit value that is the same in all lanes, to scalar registers
+__device__ __forceinline__ long long uniform64(long long v) {
+    return (long long)((uint64_t)(uint32_t)uniform((int)(v >> 32)) << 32 | (uint32_t)uniform((int)v));
+}
+
 // A value that the compiler takes for a new one, so that what is computed from it stays where it is used: what depends on the lane
 // alone it would compute for all walks ahead of the loop over units, in more registers than there are (51 of them in scratch memory,
 // 27 MB a launch).
@@ -126,7 +135,7 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
     float (*xw)[kWaveColumns][kStride] = reinterpret_cast<float (*)[kWaveColumns][kStride]>(smem);
     __shared__ int sh_off[kGroupsInLds + 1], sh_pages[kGroupsInLds];
     __shared__ long long sh_sum[kAttWaves], sh_at;
-    __shared__ int sh_entry;
+    __shared__ int sh_entry, sh_longest[kAttWaves];
 
     const int tid = threadIdx.x, lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(tid / LEOAM_WAVE);
     const int hkv = a.n_kv_heads, group = 1 << a.group_shift, cap = a.max_pages << a.page_shift;
@@ -176,22 +185,36 @@ __global__ __launch_bounds__(kAttThreads) __attribute__((amdgpu_waves_per_eu(2))
     {
         const int per = (n_entries + kAttThreads - 1) / kAttThreads, e0 = min(tid * per, n_entries), e1 = min(e0 + per, n_entries);
         long long mine = 0;
-        for (int e = e0; e < e1; ++e) mine += entry_of(e).total();
+        int longest = 0;      // unit of them
+        for (int e = e0; e < e1; ++e) {
+            const SharedEntry x = entry_of(e);
+            mine += x.total();
+            longest = max(longest, x.full ? x.length(0) : x.length(x.full));
+        }
         long long incl = mine;
 #pragma unroll
         for (int d = 1; d < LEOAM_WAVE; d <<= 1) {
             const long long o = __shfl_up(incl, d, LEOAM_WAVE);
             if (lane >= d) incl += o;
         }
-        if (lane == LEOAM_WAVE - 1) sh_sum[wave] = incl;
+#pragma unroll
+        for (int d = 1; d < LEOAM_WAVE; d <<= 1) longest = max(longest, __shfl_xor(longest, d, LEOAM_WAVE));
+        if (lane == LEOAM_WAVE - 1) {
+            sh_sum[wave] = incl;
+            sh_longest[wave] = longest;
+        }
         __syncthreads();
         long long total = 0, before = incl - mine;
 #pragma unroll
         for (int w = 0; w < kAttWaves; ++w) {
             if (w < wave) before += sh_sum[w];
             total += sh_sum[w];
+            longest = max(longest, sh_longest[w]);
         }
-        share = max(quotient(total + a.sharers - 1, a.sharers), (long long)kMostTileCost);      // (so that a tile begins in each)
+        total = uniform64(total);
+        longest = uniform(longest);
+        // (a tile begins in each, and a unit is not cut into more pieces than pay)
+        share = max(quotient(total + a.sharers - 1, a.sharers), (long long)max(kMostTileCost, (longest + kMostPieces - 1) / kMostPieces));
         pos = first = share * blockIdx.x;
         end = min(total, pos + share);
         if (pos >= end) return;
