@@ -14,8 +14,8 @@
 // the first-level cache serves at a quarter of its rate, four times over.  Weights go in as two fp16 or three bf16 numbers that add up to
 // them (22 or 24 bits), so the float output keeps its precision, at twice the cost of rounded ones beyond 64 columns.
 //
-// 48 sequences behind 32768 tokens, 32 of 8 heads, bf16: 89 us (221 MB and 26 GFLOP; each by itself, as page_attention_decode has it,
-// would read 6.6 GB); 70 of 64 heads in nine groups behind 9000, 8 bits: 85; four of 8 heads behind 1024, fp32: 15, launches and
+// 48 sequences behind 32768 tokens, 32 of 8 heads, bf16: 91 us (221 MB and 26 GFLOP; each by itself, as page_attention_decode has it,
+// would read 6.6 GB); 70 of 64 heads in nine groups behind 9000, 8 bits: 88; four of 8 heads behind 1024, fp32: 16, launches and
 // dependent round trips.
 #include <cfloat>
 
