@@ -938,13 +938,13 @@ __global__ __launch_bounds__(kMergeThreads) void page_shared_merge_kernel(const 
     __syncthreads();
     if (part || done) return;
     for (int p = 1; p < kMergeParts; ++p) m = fmaxf(m, sh_m[mine][p]);
+    // (A part without pieces adds zeros.  One whose logits are all NaN has a maximum of -inf as well, and its NaN stays.)
     l = 0.f;
     o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
     for (int p = 0; p < kMergeParts; ++p) {
         const float w = exp2_or_zero(sh_m[mine][p], m);
         const float4 x = *reinterpret_cast<const float4*>(&sh_o[mine][p][d]);
-        if (sh_m[mine][p] == -INFINITY) continue;      // (a part without pieces)
         l += w * sh_l[mine][p];
         o.x += w * x.x; o.y += w * x.y; o.z += w * x.z; o.w += w * x.w;
     }
