@@ -588,7 +588,8 @@ size_t leoam_page_shared_workspace_min(const leoam_pages* pages);
 /*
  * How much of the attention of the call's rows each cached token got.  Row r of q [n_new, Hq, 128] (rotated, as the attention
  * call took it) has place p in its sequence (new_off as above: the last rows are the sequence's last tokens) and lse [n_new, Hq] is
- * what the attention call left.  For every sequence b with m rows, kv head h and place t < seq_len[b]:
+ * what the attention call left, one over all pages: with the lse of one over selected pages the other pages' tokens get as much as if
+ * they had been attended to.  For every sequence b with m rows, kv head h and place t < seq_len[b]:
  *   weight[b,h,t] = decay * (t < seq_len[b] - m ? weight_before[b,h,t] : 0)
  *                   + sum over rows r with p >= t, heads j of h's group, of exp(softmax_scale * (q[r,j] . K_t) - lse[r,j]).
  *   weight, weight_before  [batch, n_kv_heads, max_pages * page_size] float; they may be the same array; weight_before may be NULL

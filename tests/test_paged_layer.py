@@ -1,0 +1,65 @@
+"""What PagedLayer refuses and which buffers its calls get (no GPU needed: the library's calls are replaced by ones that note what they were
+given)."""
+import pytest
+import torch
+
+import paper_2506_20187_amd as L
+from paper_2506_20187_amd import paged
+
+CALLS = ("kv_page_append", "kv_page_append_at", "chunk_score", "chunk_topk_select", "page_attention_decode", "page_attention_prefill",
+         "page_attention_decode_shared", "page_weight_add", "page_evict_select", "kv_page_move")
+B, HQ, HKV, PAGE, MAX_PAGES = 3, 8, 2, 16, 5
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    """[(name, arguments)] of the library's calls"""
+    made = []
+    for name in CALLS:
+        monkeypatch.setattr(paged.B, name, lambda *a, _name=name: made.append((_name, a)))
+    return made
+
+
+def layer(**kw):
+    table, seq_len = torch.zeros(B, MAX_PAGES, dtype=torch.int32), torch.full((B,), 20, dtype=torch.int32)
+    return L.PagedLayer(table, seq_len, HQ, HKV, 9, PAGE, torch.bfloat16, **kw)
+
+
+Q = torch.zeros(B, HQ, 128, dtype=torch.bfloat16)
+N = torch.zeros(B, dtype=torch.int32)
+GROUPS = (torch.tensor([0, B], dtype=torch.int32), torch.tensor([1], dtype=torch.int32))
+
+
+def weighed_with(calls):
+    name, args = calls[-1]
+    assert name == "page_weight_add"
+    return args[8]      # lse
+
+
+@pytest.mark.parametrize("budget", [dict(max_chunks=2), dict(token_budget=20)], ids=str)
+def test_weigh_refuses_the_logarithms_of_an_attention_over_kept_pages(calls, budget):
+    x = layer(evicts=4, groups=1, **budget)
+    with pytest.raises(ValueError, match="lse"):      # (nothing was attended to yet)
+        x.weigh(Q, N)
+    x.attend(Q)
+    with pytest.raises(ValueError, match="lse"):
+        x.weigh(Q, N)
+    assert calls[-1][0] == "page_attention_decode"
+    given = torch.zeros(B, HQ)
+    x.weigh(Q, N, lse=given)                          # (what the caller gives is the caller's to know)
+    assert weighed_with(calls) is given
+    x.attend_shared(Q, *GROUPS)
+    x.weigh(Q, N)
+    assert weighed_with(calls) is x.lse
+    x.attend(Q)
+    with pytest.raises(ValueError, match="lse"):
+        x.weigh(Q, N)
+
+
+def test_weigh_takes_the_logarithms_of_an_attention_over_all_pages(calls):
+    x = layer(evicts=4)
+    with pytest.raises(ValueError, match="lse"):
+        x.weigh(Q, N)
+    x.attend(Q)
+    x.weigh(Q, N)
+    assert weighed_with(calls) is x.lse
