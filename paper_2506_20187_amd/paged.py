@@ -67,7 +67,7 @@ others set by the caller: to 0 and to their places.
         self.status = torch.zeros(batch, dtype=torch.int32, device=dev)
         self.out = torch.empty(batch, n_q_heads, head_dim, dtype=torch.float32, device=dev)
         self.lse = torch.empty(batch, n_q_heads, dtype=torch.float32, device=dev)
-        self.lse_of_all = False      # what stands there is of an attention over all pages
+        self.lse_of_all = False      # what stands there is the last attention's, over all pages
         self.max_chunks, self.token_budget = int(max_chunks), int(token_budget)
         self.selects = self.max_chunks > 0 or self.token_budget > 0
         self.abstract = self.chunk_off = self.n_chunks = self.sel_idx = self.sel_count = None
@@ -148,12 +148,13 @@ others set by the caller: to 0 and to their places.
         return self.out
 
     def weigh(self, q, n_seen, new_off=None, lse=None, decay: float = 1.0, stream=None) -> None:
-        """q (rotated) and lse of an attention call of this step, over all pages; lse None: what attend or attend_shared left.  Under a
-        budget attend's is over the kept pages, and the other pages' tokens would get weight that nobody gave them: refused."""
+        """q (rotated) and lse of an attention call of this step, over all pages.  lse None: what attend or attend_shared left; refused
+        after prompt, which leaves its logarithms in the lse that it is given, and after attend under a budget: that is over the kept
+        pages, and the other pages' tokens would get weight that nobody gave them."""
         if self.weight is None:
             raise ValueError("PagedLayer was made without evictions")
         if lse is None and not self.lse_of_all:
-            raise ValueError("lse: the layer's last attention was over kept pages, or there was none")
+            raise ValueError("lse: the layer's last attention was over kept pages or a prompt's, or there was none")
         B.page_weight_add(self.pages, q, new_off, self.k_pages, self.k_scale, self.page_table, self.seq_len, self.scale,
                           self.lse if lse is None else lse, decay, self.weight, self.weight, n_seen, self.token_id, stream)
 
@@ -181,4 +182,5 @@ others set by the caller: to 0 and to their places.
             self.prompt_workspaces.append(self._new(-(-need >> 20) << 20, torch.uint8, stream))
         B.page_attention_prefill(self.pages, q_out, new_off, self.k_pages, self.v_pages, self.k_scale, self.v_scale,
                                  self.page_table, self.seq_len, self.scale, out, lse, self.prompt_workspaces[-1], stream)
+        self.lse_of_all = False      # (self.lse is an earlier step's)
         return out

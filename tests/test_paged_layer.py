@@ -63,3 +63,18 @@ def test_weigh_takes_the_logarithms_of_an_attention_over_all_pages(calls):
     x.attend(Q)
     x.weigh(Q, N)
     assert weighed_with(calls) is x.lse
+
+
+def test_weigh_wants_the_logarithms_of_a_prompt(calls):
+    # (as many rows as sequences: those that the last step left would fit, and are of other rows)
+    x, lse = layer(evicts=4), torch.zeros(B, HQ)
+    for off in (torch.tensor([0, 2, 2, 3], dtype=torch.int32), torch.arange(B + 1, dtype=torch.int32)):
+        x.attend(Q)
+        x.weigh(Q, N, off)
+        assert weighed_with(calls) is x.lse
+        x.prompt(Q, Q[:, :HKV], Q[:, :HKV], off, lse=lse)
+        for o in (off, None):
+            with pytest.raises(ValueError, match="lse"):
+                x.weigh(Q, N, o)
+        x.weigh(Q, N, off, lse)
+        assert weighed_with(calls) is lse
