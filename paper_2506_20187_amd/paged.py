@@ -31,6 +31,7 @@ and, for caches that are shared and kept within bounds,
       weigh          what each cached token got of the attention of some rows, added to `weight`
       evict          the sequences brought down to `keep_len` tokens, by `weight` (`evicts`: the most rows of a sequence that
                      may move in a call); returns the new lengths, which become seq_len once all layers have evicted
+                     (tokens of pages that several sequences list have to be among the first ones, which stay: `n_first`)
 
 After an eviction a token's place is not its position: `append`, `step` and `prompt` then want `position` ([axes, rows]; with several
 axes `axis` [rot_dim / 2] says whose each pair is).  `n_seen` [B] int32 is how many tokens a sequence ever had, brought up to date by
@@ -159,9 +160,13 @@ others set by the caller: to 0 and to their places.
                           self.lse if lse is None else lse, decay, self.weight, self.weight, n_seen, self.token_id, stream)
 
     def evict(self, keep_len, n_seen, n_first=None, n_recent: int = 0, stream=None) -> torch.Tensor:
-        """keep_len, n_seen, n_first [B] int32; new lengths [B] int32 (evict_status says where nothing could be done)."""
+        """keep_len, n_seen, n_first [B] int32; new lengths [B] int32 (evict_status says where nothing could be done).  The first n_first
+        tokens stay where they are.  Pages that several sequences list must be among them, or one sequence's rows would be moved into
+        what the others read: n_first says at least how many tokens those hold, and a layer made with `groups` wants it given."""
         if self.weight is None:
             raise ValueError("PagedLayer was made without evictions")
+        if n_first is None and self.groups:
+            raise ValueError("n_first: tokens of shared pages must stay where they are")
         B.page_evict_select(self.pages, self.weight, self.token_id, n_seen, self.seq_len, keep_len, n_first, n_recent, self.moves,
                             self.move_count, self.new_len, self.evict_status, self.evict_workspace, stream)
         B.kv_page_move(self.pages, self.moves, self.move_count, self.seq_len, self.new_len, self.page_table, self.k_pages, self.v_pages,

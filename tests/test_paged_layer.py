@@ -78,3 +78,13 @@ def test_weigh_wants_the_logarithms_of_a_prompt(calls):
                 x.weigh(Q, N, o)
         x.weigh(Q, N, off, lse)
         assert weighed_with(calls) is lse
+
+
+def test_evict_of_a_layer_with_groups_wants_the_tokens_that_stay(calls):
+    x = layer(evicts=4, groups=1)
+    with pytest.raises(ValueError, match="n_first"):
+        x.evict(N, N)
+    assert not calls
+    x.evict(N, N, N)
+    assert [c[0] for c in calls] == ["page_evict_select", "kv_page_move"] and calls[0][1][6] is N
+    layer(evicts=4).evict(N, N)
