@@ -43,9 +43,11 @@ others set by the caller: to 0 and to their places.
     Under a budget a place in the batch that another sequence takes over must be idle (length 0) for a step in between, or
     have its `n_chunks` set to 0: the rows of abstracts are the place's, and are made anew from the pages then.
 
-    Calls of one layer must not overlap, on two streams or as two graphs: they share its buffers.  Workspaces (up to 66 MiB each)
-    hold nothing between calls: `workspaces_of` another layer makes this one use that one's, as the layers of a model can, whose
-    calls follow one another on one stream.
+    Calls of one layer must not overlap, on two streams or as two graphs: they share its buffers.  Workspaces hold nothing between
+    calls: `workspaces_of` another layer makes this one use that one's where they are large enough, as the layers of a model can, whose
+    calls follow one another on one stream.  The leoam_page_*workspace_bytes calls say how large they are: attend's a few MiB, prompt's
+    up to 66, attend_shared's 65 and a KiB for every query head of every sequence; evict's 16 KiB for every 4096 or 8192 places that the
+    table has for a (sequence, kv head), where these are too many for a workgroup (32 sequences of up to 131072 tokens, 8 heads: 74 MiB).
     """
 
     def __init__(self, page_table: torch.Tensor, seq_len: torch.Tensor, n_q_heads: int, n_kv_heads: int, n_pages: int,
@@ -90,7 +92,7 @@ others set by the caller: to 0 and to their places.
         self.prompt_workspaces = [] if workspaces_of is None else workspaces_of.prompt_workspaces
         self.scale = B.default_scale(head_dim)
         self.axis, self.groups, self.evicts = axis, int(groups), int(evicts)
-        self.weight = self.token_id = self.shared_workspace = None
+        self.weight = self.token_id = self.shared_workspace = self.evict_workspace = None
         if self.groups:
             need = B.leoam_page_shared_workspace_bytes(self.pages, self.groups)
             other = getattr(workspaces_of, "shared_workspace", None)
@@ -103,7 +105,9 @@ others set by the caller: to 0 and to their places.
             self.move_count = torch.empty(batch, n_kv_heads, dtype=torch.int32, device=dev)
             self.new_len = torch.zeros(batch, dtype=torch.int32, device=dev)
             self.evict_status = torch.zeros(batch, dtype=torch.int32, device=dev)
-            self.evict_workspace = self._new(B.leoam_page_evict_workspace_bytes(self.pages), torch.uint8, None)
+            need = B.leoam_page_evict_workspace_bytes(self.pages)
+            other = getattr(workspaces_of, "evict_workspace", None)
+            self.evict_workspace = other if other is not None and other.numel() >= need else self._new(need, torch.uint8, None)
 
     def _new(self, shape, dtype, stream) -> torch.Tensor:
         """Of the stream's own memory: freed before its kernels have run, it is given to later ones of that stream only."""

@@ -88,3 +88,22 @@ def test_evict_of_a_layer_with_groups_wants_the_tokens_that_stay(calls):
     x.evict(N, N, N)
     assert [c[0] for c in calls] == ["page_evict_select", "kv_page_move"] and calls[0][1][6] is N
     layer(evicts=4).evict(N, N)
+
+
+def test_layers_of_a_model_share_their_workspaces(calls):
+    kinds = ("workspace", "shared_workspace", "evict_workspace")
+    first = layer(evicts=4, groups=1)
+    second = layer(evicts=4, groups=1, workspaces_of=first)
+    third = layer(evicts=4, groups=1, workspaces_of=second)
+    for x in (second, third):
+        assert all(getattr(x, k) is getattr(first, k) for k in kinds)
+        x.evict(N, N, N)
+        assert calls[-2][1][-2] is first.evict_workspace
+        # what a layer's calls leave for the caller is its own
+        assert all(getattr(x, k) is not getattr(first, k) for k in ("new_len", "evict_status", "moves", "move_count", "weight", "token_id"))
+    # of one that has none, or a smaller one: its own
+    assert layer(evicts=4, workspaces_of=layer()).evict_workspace is not None
+    table = torch.zeros(B, 1 << 13, dtype=torch.int32)
+    long = L.PagedLayer(table, N, HQ, HKV, 9, PAGE, torch.bfloat16, evicts=4, workspaces_of=first)
+    assert long.evict_workspace.numel() >= L.leoam_page_evict_workspace_bytes(long.pages) > first.evict_workspace.numel()
+    assert layer(workspaces_of=first).evict_workspace is None
