@@ -614,7 +614,8 @@ int page_weight_add(const leoam_pages* pages, const void* q, int32_t n_new, cons
  *   moves       [batch, n_kv_heads, m_max, 2] int32: (place that becomes free, place of the token that moves there); entries from
  *               move_count[b,h] on are left as they are
  *   move_count  [batch, n_kv_heads] int32
- *   new_len     [batch] int32: keep_len[b], or seq_len[b] if the sequence is not longer than that; an array of its own
+ *   new_len     [batch] int32: keep_len[b], or seq_len[b] if the sequence is not longer than that.  new_len, status and move_count
+ *               must not lie over seq_len, keep_len, n_first, n_seen or one another (LEOAM_E_INVALID_ARG)
  *   token_id, n_seen  (both or neither) as page_weight_add keeps them: a token is recent if its number is n_seen[b] - n_recent or
  *               more.  NULL: places tell (nothing was ever moved).
  *   n_first     [batch] int32, nullable (0)

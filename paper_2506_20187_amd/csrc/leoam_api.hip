@@ -148,6 +148,11 @@ static inline int from_hip(hipError_t e) { return e == hipSuccess ? LEOAM_OK : L
 // K, V, q, the abstract and the blobs are read with 16-byte loads
 template <typename... P> static inline bool misaligned16(P... p) { return ((... | (uintptr_t)p) & 15u) != 0; }
 
+// whether two lists, of n and m words, share some (nullptr: there is none)
+static inline bool overlap(const int32_t* a, size_t n, const int32_t* b, size_t m) {
+    return a && b && (uintptr_t)a < (uintptr_t)b + 4 * m && (uintptr_t)b < (uintptr_t)a + 4 * n;
+}
+
 // ---- workspace of chunk_select_attention_decode_static ------------------------------------------
 // Device memory that belongs to the library image: every GPU the library runs on holds its own copy
 // until the process ends.  `static_scratch` names the array in DEVICE code only; on the host the
@@ -615,9 +620,15 @@ int page_evict_select(const leoam_pages* pages, const float* weight, const int32
     if (rc) return rc;
     if (n_recent < 0 || m_max < 1) return LEOAM_E_INVALID_ARG;
     if (!weight || !seq_len || !keep_len || !moves || !move_count || !new_len || !token_id != !n_seen) return LEOAM_E_INVALID_ARG;
-    // (other workgroups still read the lengths when new_len is written)
-    if (((uintptr_t)moves & 7u) || new_len == seq_len || new_len == keep_len) return LEOAM_E_INVALID_ARG;
+    if ((uintptr_t)moves & 7u) return LEOAM_E_INVALID_ARG;
     if (!workspace || workspace_bytes < page_evict_workspace_bytes(pages) || ((uintptr_t)workspace & 15u)) return LEOAM_E_WORKSPACE;
+    // other workgroups, and later launches, still read these lists when the outputs are written
+    const size_t batch = pages->batch, rows = batch * pages->n_kv_heads;
+    for (const int32_t* read : {seq_len, keep_len, n_first, n_seen})
+        if (overlap(read, batch, new_len, batch) || overlap(read, batch, status, batch) || overlap(read, batch, move_count, rows))
+            return LEOAM_E_INVALID_ARG;
+    if (overlap(new_len, batch, status, batch) || overlap(new_len, batch, move_count, rows) || overlap(status, batch, move_count, rows))
+        return LEOAM_E_INVALID_ARG;
     return from_hip(page_evict_dispatch(pages, weight, token_id, n_seen, seq_len, keep_len, n_first, n_recent, moves, m_max, move_count,
                                         new_len, status, workspace, (hipStream_t)stream));
 }
