@@ -597,6 +597,7 @@ size_t leoam_page_shared_workspace_min(const leoam_pages* pages);
  *   n_seen, token_id       (both or neither) token_id [batch, n_kv_heads, max_pages * page_size] int32 numbers the tokens
  *                          in the order in which the sequence got them; n_seen [batch] int32 is how many it ever had, these rows
  *                          counted in.  The rows' own places get n_seen[b] - (seq_len[b] - t); others are left as they are.
+ * n_new == 0: nothing is done (a sequence without rows in a call that has some is: its weights are multiplied by decay).
  * Rows with lse = -inf (nothing was attended to) add nothing, nor do rows whose place is negative; tokens of a page that is not in
  * the pool get nothing.  Of the queries of a long prompt the last ones alone may be given (their logarithms with them): weight_before
  * then stands for the tokens before them, and their numbers are the caller's to set.  Sums are in binary32, each token's in an order

@@ -404,6 +404,9 @@ template <int HELD> __global__ __launch_bounds__(kPartThreads, 4) void page_evic
 // Into how many parts rows are cut at most; 0: a row to a workgroup.  That takes a microsecond for a thousand tokens, four launches take
 // 22 to 26 if there are few rows (four of 40000 22.5, 16 of 64000 24; a workgroup 16 of 20000 24, of 32000 31, of 64000 60), but more
 // work in all (128 rows of 32000, parts 57, a workgroup 33; of 60000 74 / 61, 512 of those 221 / 142).
+// The width is the table's: short rows of a wide one get workgroups with registers for more keys, of which fewer share a compute unit, or
+// the four launches, most of whose workgroups find nothing to do (320 rows of 4200 in tables of 4288 tokens 13.8, of 16384 16.6, of 32768
+// 27.3; of 131072, four launches, 66.4).
 // Keys of a part's thread: few for few rows (16 rows of 64000, 8 and 16 keys: 24, 29; 64 of those 47, 51; 256 of 130000 307, 232).
 constexpr int kRowHeld = 64;      // keys of a thread, at most
 static int part_held(int rows) { return rows <= 64 ? 8 : 16; }

@@ -8,7 +8,8 @@
 // way.  They come as whole rows, which the caches serve at four times the rate of an operand's 16 bytes of 16 rows, and become
 // operands in LDS.  Sixteen tokens of sequences to 33001 (617 MB): 125 us, 4.9 TB/s; with operands straight from the loads and no
 // equal shares 187; with weights written for 32 keys at a time 134; with lengths and pages looked up when the keys are fetched 129.
-// Many rows: bound by the exponentials and the instructions around them.  The waves of a workgroup share 64 keys (fp32: 32; half as
+// Many rows: the vector ALU (an exponential, a multiply-add, a sum and the mask for each weight) is busy 57 % of the time, the rest goes to
+// uneven work: the first stretches have all rows, the last ones few.  The waves of a workgroup share 64 keys (fp32: 32; half as
 // many where keys are few) and go through the blocks of columns in turn; their sums are added in order at the end.  Queries, too,
 // come as whole rows.  A prompt of 4096 with 32 heads: 114 us (268 M exponentials, 69 GFLOP); with operands straight from the
 // loads 191.
@@ -399,7 +400,9 @@ __global__ __launch_bounds__(WAVES * LEOAM_WAVE, 2) void page_weight_many_kernel
     }
 }
 
-// More than a block of columns for each sequence on average: many rows.
+// More than a block of columns for each sequence on average: many rows.  (On average: the host does not know new_off.  A prompt's chunk
+// beside many single tokens is taken for few rows, and each stretch's wave goes through all of its columns: 700 rows and 255 tokens
+// behind 1000, 32 of 8 heads, bf16 2690 us, in calls of their own 18 and 105.)
 constexpr int kFewColumns = 16;
 constexpr int kManyGroups = 65536;
 
@@ -410,6 +413,9 @@ constexpr int kManyGroups = 65536;
 // are halved as well (prompt of 1024 with 8 kv heads 134, 41, 31 and 24 us; two of 1250 with 4 163, 51, 38, 29; of 4096, which has
 // enough of them, 124 and 172), and with fewer columns four waves share those (50 rows behind 1000, one wave and four: 11.1, 6.2; of
 // two sequences 11.0, 7.6; fp32 24, 12.6).
+// The stretches are those that the table has room for, since the host does not know the lengths: the figures are of tables a page wider
+// than the sequences.  In much wider ones prompts are taken for rows behind long histories and get a wave (prompt of 4096
+// in a table of 16384 tokens 528 us, of 131072 546; of 1024 in either 134; two of 1250 with 4 heads 164).
 struct ManyShape { int waves; bool half; };
 static ManyShape many_shape(long long stretches, long long columns, bool prompts) {
     if (columns < 64) return {1, false};
